@@ -2,7 +2,9 @@
  * astra_xc.h -- C ABI of the MI355X (gfx950) classifier-layer hot path of ASTRA
  * (arXiv 2409.20156): hard-negative mining by exact top-k inner product, the
  * hard+uniform negative mixture, and the sampled BCE training step with a sparse
- * SGD update of the classifier rows.
+ * SGD update of the classifier rows; dropout of the embeddings that enter a step,
+ * the scores of all labels from 8-bit integers, and the check of drafted labels
+ * against the classifier's probabilities.
  *
  * Conventions shared by every call
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library
@@ -50,6 +52,8 @@ typedef enum {
 #define XC_MAX_CANDIDATES 16384 /* k_p + n_neg accepted by xc_step                 */
 #define XC_MAX_KP 256          /* k_p accepted by xc_step                          */
 #define XC_STATIC_SCRATCH_BYTES (32u << 20)  /* temporaries xc_step_static can hold    */
+#define XC_MAX_D_QUANTIZED 131072 /* d accepted by the 8-bit calls: |sum| <= 127^2 d < 2^31 */
+#define XC_MAX_DRAFTS 1024     /* n accepted by xc_verify_drafts                   */
 
 const char* xc_strerror(int status);
 int xc_last_hip_error(void);
@@ -237,9 +241,82 @@ int xc_step_static(const void* Z /* [B*d] */, void* W /* [L*d], updated in place
                    void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Rows in 8 bits.  Row i of X (d elements of type t) becomes
+ *   scale[i] = m / 127 (fp32), m the row's largest magnitude;
+ *   Q[i*pitch + j] = 127 x_ij / m to the nearest integer, halves to the even one,
+ *   decided exactly; zeros for d <= j < pitch, pitch = d rounded up to 16.
+ * A row of zeros gets scale 0; a row with an element that is not a finite number
+ * gets zeros and a scale that is not a number.
+ * ids == NULL: all N rows.  Else only rows ids[0..m), or ids[0..min(m, count[0]))
+ * if count (device memory) is not NULL, for example the `touched` and `n_touched`
+ * of the step that changed them; ids outside [0,N) are ignored, an id may occur
+ * several times, the other rows of Q and scale keep their values.
+ * Requires N >= 1, m >= 0, d*sizeof(element) a multiple of 16, d <= XC_MAX_D_QUANTIZED.
+ * ------------------------------------------------------------------------- */
+int xc_quantize_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
+                     const int32_t* ids /* [m] or NULL */, int64_t m, const int32_t* count /* [1] or NULL */,
+                     int8_t* Q /* [N*pitch] out */, float* scale /* [N] out */, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The scores of all labels from 8-bit integers: the rows of Z (type t) are brought
+ * to integers p and scales a as above, and
+ *   out[i*L + l] = (<p_i, q_l> * a_i) * scale[l],
+ * <p, q> exact in 32-bit integers, then rounded to fp32, multiplied in fp32 and
+ * rounded to out_t at the end.  Q and scale are what xc_quantize_rows gives for the
+ * classifier (or for a contiguous range of its rows).  The workspace holds the
+ * integers of Z; it is written before it is read.
+ * Requires B >= 1, 1 <= L < 2^31, d as above.
+ * ------------------------------------------------------------------------- */
+int xc_scores_workspace(int64_t B, int d, size_t* bytes);
+int xc_scores_quantized(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,
+                        const int8_t* Q /* [L*pitch] */, const float* scale /* [L] */, int64_t L,
+                        xc_dtype out_t, void* out /* [B*L] out */, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Drafted labels checked against the classifier's probabilities, so that what is
+ * kept is distributed as if it had been drawn from these.  Sequence b has drafts
+ * x_0, x_1, ... (the first of drafts[b*n ..] that lies outside [0,V) ends them),
+ * drawn from the rows of draft_probs [B*n*V]; target is [B*(n+1)*V], one row per
+ * draft and one behind the last; u [B*(n+1)] are uniform random numbers in [0,1).
+ *   Draft i stands if u[b,i] * draft_probs[b,i,x_i] < target[b,i,x_i] (decided exactly).
+ *   accepted[b] = a, the drafts before the first that falls, or all of them;
+ *   tokens[b*(n+1) + i] = x_i for i < a; one more label at i = a; -1 behind it.
+ * That label is the first v at which the running sum of w passes u[b,n] times the
+ * sum of all w (the last v with w > 0 if none does), with
+ *   w_v = max(0, target[b,a,v] - draft_probs[b,a,v])  where a draft fell,
+ *   w_v = target[b,a,v]                               where all of them stand, or where the former are all zero;
+ * -1 if these are all zero too.  Entries (or differences) that are negative,
+ * infinite or not a number have w = 0.  Sums are held in 64 bits and added in an
+ * order that depends on V alone.
+ * draft_probs == NULL: drafts that were looked up, not drawn (probability 1 each):
+ * draft i stands if u[b,i] < target[b,i,x_i], and w_v of a fallen one is the
+ * target's without x_a.
+ * Requires B >= 1, 0 <= n <= XC_MAX_DRAFTS, 1 <= V < 2^31; drafts may be NULL if n = 0.
+ * ------------------------------------------------------------------------- */
+int xc_verify_workspace(int64_t B, int64_t V, size_t* bytes);
+int xc_verify_drafts(const int32_t* drafts /* [B*n] */, int64_t B, int n, int64_t V,
+                     const void* target /* [B*(n+1)*V] */, const void* draft_probs /* [B*n*V] or NULL */, xc_dtype t,
+                     const float* u /* [B*(n+1)] */, int32_t* tokens /* [B*(n+1)] out */,
+                     int32_t* accepted /* [B] out */, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Dropout without a stored mask: Y_ij = X_ij * 65536 / (65536 - T) or, if dropped, 0
+ * (whatever X_ij is), with T = floor(65536 rate + 1/2).  Element (i, j) is dropped if
+ * field j mod 4 (16 bits each, the lowest first) of word g = j / 4 (rounded down) is less than T,
+ *   word = fmix(fmix((seed ^ K3) ^ K1*(row0+i+1)) + K2*(g+1)),
+ * fmix, K1, K2 as in xc_sample_negatives, K3 = 0x64726F706F757431 (a step may use one
+ * seed for its samples and its dropout).  The gradient of dropout is the same map with
+ * the same rate, seed and row0, applied to the gradient.  The product is formed in
+ * fp32 and rounded once.  X and Y may be the same array if their types are.
+ * Requires B >= 1, 1 <= d < 2^31, rate >= 0, T <= 65535, row0 >= 0.
+ * ------------------------------------------------------------------------- */
+int xc_dropout(const void* X /* [B*d] */, xc_dtype t, int64_t B, int64_t d, float rate, uint64_t seed,
+               int64_t row0, void* Y /* [B*d] out */, xc_dtype out_t, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Measurement aid (no passage of the paper: used by the benchmark to time each
  * kernel with HIP events on the stream it is launched on).  While enabled, every
- * kernel launch of the three calls above is bracketed by a pair of events.
+ * kernel launch of the calls above is bracketed by a pair of events.
  * xc_profile_collect() waits for the recorded events (host-side wait), adds the
  * elapsed times to per-kernel totals and returns the number of kernel names;
  * xc_profile_get(i, ...) reads total milliseconds and launch count of name i;

@@ -44,6 +44,12 @@ _SIGNATURES = {
     "xc_mfma_probe": (_i32, [ctypes.c_void_p, _i32, _i32, ctypes.POINTER(ctypes.c_double), ctypes.c_void_p]),
     "xc_step": (_i32, [_ptr, _ptr, _i64, _i64, _i32, _ptr, _i32, _ptr, _ptr, _i32, _f32, _i32, _i32,
                        _ptr, _ptr, _ptr, _ptr, _ptr, _ptr, ctypes.c_size_t, _ptr]),
+    "xc_quantize_rows": (_i32, [_ptr, _i64, _i32, _i32, _ptr, _i64, _ptr, _ptr, _ptr, _ptr]),
+    "xc_scores_workspace": (_i32, [_i64, _i32, _szp]),
+    "xc_scores_quantized": (_i32, [_ptr, _i64, _i32, _i32, _ptr, _ptr, _i64, _i32, _ptr, _ptr, ctypes.c_size_t, _ptr]),
+    "xc_verify_workspace": (_i32, [_i64, _i64, _szp]),
+    "xc_verify_drafts": (_i32, [_ptr, _i64, _i32, _i64, _ptr, _ptr, _i32, _ptr, _ptr, _ptr, _ptr, ctypes.c_size_t, _ptr]),
+    "xc_dropout": (_i32, [_ptr, _i32, _i64, _i64, _f32, _u64, _i64, _ptr, _i32, _ptr]),
     "xc_step_static": (_i32, [_ptr, _ptr, _i64, _i64, _i32, _ptr, _i32, _ptr, _ptr, _i32, _f32, _i32, _i32,
                               _ptr, _ptr, _ptr, _ptr, _ptr, _ptr]),
 }
@@ -288,6 +294,168 @@ def xc_step(Z: torch.Tensor, W: torch.Tensor, pos: torch.Tensor, neg: torch.Tens
                        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()),
            "xc_step")
     return {"loss": loss, "dZ": dZ, "touched": touched, "n_touched": n_touched, "W_rows": rows}
+
+
+def _launch(fn, where: str, dev: torch.device, *args) -> None:
+    """Call an entry point on the current stream of the device that holds the tensors."""
+    stream = ctypes.c_void_p(torch.cuda.current_stream(dev).cuda_stream)
+    if torch.cuda.current_device() == dev.index:
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, stream)
+    _check(status, where)
+
+
+def _same_device(first: torch.Tensor, *others) -> torch.device:
+    for t in others:
+        if t is not None and t.device != first.device:
+            raise ValueError("all tensors of a call must be on one device, got %s and %s" % (first.device, t.device))
+    return first.device
+
+
+def _shaped(t: torch.Tensor, shape, name: str) -> None:
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+
+
+def quantized_pitch(d: int) -> int:
+    """Bytes of a row of d elements in 8 bits: d rounded up to 16."""
+    return (d + 15) // 16 * 16
+
+
+def quantize_rows(X: torch.Tensor, *, rows: torch.Tensor | None = None, count: torch.Tensor | None = None,
+                  out: tuple | None = None):
+    """(Q int8 [N, pitch], scale fp32 [N]): the rows of X [N, d] as integers 127 x / max|x| (nearest, halves to even; zeros
+    behind column d) and their scales max|x| / 127.
+
+    rows int32 [m]: only these rows of `out` are written, or the first count[0] of them (`touched` and `n_touched`
+    of a training step)."""
+    lib = load_library()
+    code = _dtype_code(X)
+    if X.dim() != 2:
+        raise ValueError("X must be [N, d]")
+    N, d = X.shape
+    if rows is not None and out is None:
+        raise ValueError("rows need the `out` of an earlier call: the other rows keep their values")
+    if rows is None and count is not None:
+        raise ValueError("count needs rows")
+    if out is None:
+        out = (torch.empty((N, quantized_pitch(d)), dtype=torch.int8, device=X.device),
+               torch.empty(N, dtype=torch.float32, device=X.device))
+    Q, scale = out
+    _shaped(Q, (N, quantized_pitch(d)), "Q")
+    _shaped(scale, (N,), "scale")
+    if rows is not None and rows.dim() != 1:
+        raise ValueError("rows must be [m]")
+    if count is not None and count.numel() < 1:
+        raise ValueError("count must hold a number")
+    dev = _same_device(X, Q, scale, rows, count)
+    args = (_dev(X, name="X"), N, d, code, _dev(rows, torch.int32, "rows") if rows is not None else None,
+            rows.numel() if rows is not None else 0, _dev(count, torch.int32, "count") if count is not None else None,
+            _dev(Q, torch.int8, "Q"), _dev(scale, torch.float32, "scale"))
+    if rows is None or rows.numel():                       # (no rows: an empty tensor has no address to pass)
+        _launch(lib.xc_quantize_rows, "xc_quantize_rows", dev, *args)
+    return out
+
+
+def scores_workspace(B: int, d: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.xc_scores_workspace(B, d, ctypes.byref(n)), "xc_scores_workspace")
+    return n.value
+
+
+def scores_quantized(Z: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor, *, dtype: torch.dtype = torch.float32,
+                     workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """[B, L] scores of all labels: the rows of Z [B, d] in 8 bits times the rows of Q, with the scales of both (Q and scale
+    from `quantize_rows` of the classifier).  fp32 or bf16, by `out` or `dtype`."""
+    lib = load_library()
+    code = _dtype_code(Z)
+    if Z.dim() != 2 or Q.dim() != 2 or Q.shape[1] != quantized_pitch(Z.shape[1]):
+        raise ValueError("Z must be [B, d] and Q [L, d rounded up to 16]")
+    B, d = Z.shape
+    L = Q.shape[0]
+    _shaped(scale, (L,), "scale")
+    if workspace is None:
+        workspace = torch.empty(scores_workspace(B, d), dtype=torch.uint8, device=Z.device)
+    if out is None:
+        out = torch.empty((B, L), dtype=dtype, device=Z.device)
+    _shaped(out, (B, L), "out")
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("out must be float32 or bfloat16, got %s" % out.dtype)
+    dev = _same_device(Z, Q, scale, workspace, out)
+    _launch(lib.xc_scores_quantized, "xc_scores_quantized", dev, _dev(Z, name="Z"), B, d, code, _dev(Q, torch.int8, "Q"),
+            _dev(scale, torch.float32, "scale"), L, _dtype_code(out), _dev(out, name="out"),
+            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    return out
+
+
+def verify_workspace(B: int, V: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.xc_verify_workspace(B, V, ctypes.byref(n)), "xc_verify_workspace")
+    return n.value
+
+
+def verify_drafts(drafts: torch.Tensor, target: torch.Tensor, draft_probs: torch.Tensor | None, u: torch.Tensor, *,
+                  workspace: torch.Tensor | None = None, out: tuple | None = None):
+    """(tokens int32 [B, n+1], accepted int32 [B]): how many of the drafted labels stand against the target's
+    probabilities, these labels, one more label drawn behind them, and -1 from there on.
+
+    drafts int32 [B, n] (the first outside [0, V) ends a row), target [B, n+1, V], draft_probs [B, n, V] or None (labels that
+    were looked up, not drawn), u fp32 [B, n+1] in [0, 1): one number per draft, the last one for the label behind them."""
+    lib = load_library()
+    code = _dtype_code(target)
+    if drafts.dim() != 2 or target.dim() != 3:
+        raise ValueError("drafts must be [B, n] and target [B, n+1, V]")
+    B, n = drafts.shape
+    V = target.shape[2]
+    _shaped(target, (B, n + 1, V), "target")
+    _shaped(u, (B, n + 1), "u")
+    if draft_probs is not None:
+        _shaped(draft_probs, (B, n, V), "draft_probs")
+        if draft_probs.dtype != target.dtype:
+            raise ValueError("draft_probs and target must share dtype")
+    if workspace is None:
+        workspace = torch.empty(verify_workspace(B, V), dtype=torch.uint8, device=target.device)
+    if out is None:
+        out = (torch.empty((B, n + 1), dtype=torch.int32, device=target.device),
+               torch.empty(B, dtype=torch.int32, device=target.device))
+    tokens, accepted = out
+    _shaped(tokens, (B, n + 1), "tokens")
+    _shaped(accepted, (B,), "accepted")
+    dev = _same_device(target, drafts, draft_probs, u, workspace, tokens, accepted)
+    _launch(lib.xc_verify_drafts, "xc_verify_drafts", dev, _dev(drafts, torch.int32, "drafts") if n else None, B, n, V,
+            _dev(target, name="target"), _dev(draft_probs, name="draft_probs") if draft_probs is not None and n else None, code,
+            _dev(u, torch.float32, "u"), _dev(tokens, torch.int32, "tokens"), _dev(accepted, torch.int32, "accepted"),
+            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    return out
+
+
+def dropout(X: torch.Tensor, rate: float, seed: int, *, row0: int = 0, dtype: torch.dtype | None = None,
+            out: torch.Tensor | None = None) -> torch.Tensor:
+    """X [B, d] with elements dropped (set to zero) at `rate`, to the nearest 1/65536, and the others scaled up so that the
+    mean stays; a function of (seed, row0 + row, column).  fp32 or bf16, by `out`, `dtype` or X; out may be X."""
+    lib = load_library()
+    code = _dtype_code(X)
+    if X.dim() != 2:
+        raise ValueError("X must be [B, d]")
+    if out is None:
+        out = torch.empty(X.shape, dtype=dtype or X.dtype, device=X.device)
+    _shaped(out, X.shape, "out")
+    out_code = _dtype_code(out)
+    dev = _same_device(X, out)
+    _launch(lib.xc_dropout, "xc_dropout", dev, _dev(X, name="X"), code, X.shape[0], X.shape[1], float(rate),
+            seed & ((1 << 64) - 1), row0, _dev(out, name="out"), out_code)
+    return out
+
+
+def dropout_grad(dY: torch.Tensor, rate: float, seed: int, *, row0: int = 0, dtype: torch.dtype | None = None,
+                 out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient for the input of `dropout` from that for its output (for example the dZ of a training step): the same map
+    with the same rate, seed and row0.  out may be dY."""
+    return dropout(dY, rate, seed, row0=row0, dtype=dtype, out=out)
 
 
 def profile_enable(on: bool) -> None:

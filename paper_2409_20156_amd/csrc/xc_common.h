@@ -26,7 +26,8 @@ void set_last_hip_error(hipError_t e);
 // ---- optional per-kernel event timing ----------------------------------------
 enum KernelId {
     K_MINE_TILE = 0, K_MINE_SELECT, K_SAMPLE, K_GATHER, K_RADIX_COUNT, K_RADIX_SCAN,
-    K_RADIX_SCATTER, K_BUCKET_SORT, K_HEADS_COUNT, K_HEADS_WRITE, K_UPDATE, K_NUM_KERNELS
+    K_RADIX_SCATTER, K_BUCKET_SORT, K_HEADS_COUNT, K_HEADS_WRITE, K_UPDATE, K_QUANTIZE, K_SCORES,
+    K_VERIFY, K_DROPOUT, K_NUM_KERNELS
 };
 bool profile_on();
 void profile_mark(int kernel_id, hipStream_t st, bool begin);
@@ -84,6 +85,17 @@ __device__ __forceinline__ float key_score(uint64_t k) {
 }
 __device__ __forceinline__ int32_t key_id(uint64_t k) { return static_cast<int32_t>(k & 0xffffffffu); }
 constexpr uint64_t kKeySentinel = ~0ull;   // score -NaN pattern never produced, id -1
+
+// ---- counter-based random words: fmix(fmix(seed ^ kQueryMul (row + 1)) + kDrawMul (word + 1)), the splitmix64 finaliser twice
+constexpr uint64_t kQueryMul = 0x9E3779B97F4A7C15ull;
+constexpr uint64_t kDrawMul = 0xD1B54A32D192ED03ull;
+
+__device__ __forceinline__ uint64_t fmix64(uint64_t x) {
+    x ^= x >> 30; x *= 0xBF58476D1CE4E5B9ull;
+    x ^= x >> 27; x *= 0x94D049BB133111EBull;
+    x ^= x >> 31;
+    return x;
+}
 
 // ---- wave helpers -----------------------------------------------------------
 __device__ __forceinline__ int lane_id() { return threadIdx.x & (kWave - 1); }

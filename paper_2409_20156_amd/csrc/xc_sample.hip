@@ -11,16 +11,6 @@
 namespace xc {
 
 constexpr int kSampleThreads = 256;
-constexpr uint64_t kQueryMul = 0x9E3779B97F4A7C15ull;
-constexpr uint64_t kDrawMul = 0xD1B54A32D192ED03ull;
-
-__device__ __forceinline__ uint64_t fmix64(uint64_t x) {
-    x ^= x >> 30; x *= 0xBF58476D1CE4E5B9ull;
-    x ^= x >> 27; x *= 0x94D049BB133111EBull;
-    x ^= x >> 31;
-    return x;
-}
-
 // One workgroup per query.  The distinct in-range ids of the shortlist row, in ascending order h_0 < h_1 < ..., are
 // stored as a_m = h_m - m, which is non-decreasing.  Draw r in [0, M) then maps to the r-th label of the complement:
 // r + #{m : a_m <= r}.
