@@ -10,6 +10,10 @@ current W is copied to a snapshot, the search runs on a second stream (default p
 that snapshot while the training steps go on with the older shortlists, and the new shortlists
 take over exactly `lag` steps later (the step stream waits for the search there), so the result
 does not depend on timing.
+
+With dropout > 0 a step trains on its batch of embeddings with elements dropped, as they come out of the encoder's last layer in
+training, and the dZ it returns is the gradient for the embeddings before that.  The searches see them whole.  The mask is a
+function of the step's seed, so nothing is stored and a resumed schedule drops the same elements.
 """
 from __future__ import annotations
 
@@ -21,12 +25,16 @@ from . import binding as xc
 class Schedule:
     def __init__(self, Z_pool: torch.Tensor, W: torch.Tensor, pos_pool: torch.Tensor, B: int, k_h: int,
                  k_r: int, tau_s: int, tau_r: int, lr: float, kind: int = xc.XC_LOSS_BCE, lag: int = 0,
-                 warm_margin: float | None = None):
+                 warm_margin: float | None = None, dropout: float = 0.0):
+        if not 0.0 <= dropout < 1.0:
+            raise ValueError("dropout must lie in [0, 1)")
         if lag < 0 or (lag > 0 and lag > tau_r):
             raise ValueError("lag must lie in [0, tau_r]")
         self.Z, self.W, self.pos = Z_pool, W, pos_pool
         self.B, self.k_h, self.k_r, self.tau_s, self.tau_r, self.lr, self.kind = B, k_h, k_r, tau_s, tau_r, lr, kind
         self.lag = lag
+        self.dropout = dropout
+        self.Z_dropped = torch.empty((B, Z_pool.shape[1]), dtype=Z_pool.dtype, device=Z_pool.device) if dropout > 0 else None
         self.warm_margin = warm_margin                 # refreshes after the first start from the last thresholds
         self.searched = False
         self.full_repeats = torch.zeros(1, dtype=torch.int32, device=W.device)   # warm searches that had to be repeated in full
@@ -145,7 +153,12 @@ class Schedule:
         rows = self.shortlist[self.cur][lo:hi] if self.cur >= 0 else None
         xc.sample_negatives(rows, self.k_h, self.k_r, self.L, seed, B=self.B, device=self.W.device,
                             neg=self.neg, logq=self.logq)
-        xc.xc_step(self.Z[lo:hi], self.W, self.pos[lo:hi], self.neg, self.logq, self.lr, kind=self.kind,
+        Z = self.Z[lo:hi]
+        if self.dropout > 0:
+            Z = xc.dropout(Z, self.dropout, seed, out=self.Z_dropped)
+        xc.xc_step(Z, self.W, self.pos[lo:hi], self.neg, self.logq, self.lr, kind=self.kind,
                    workspace=self.step_ws, out=self.out)
+        if self.dropout > 0:
+            xc.dropout_grad(self.out["dZ"], self.dropout, seed, out=self.out["dZ"])
         self.t += 1
         return self.out
