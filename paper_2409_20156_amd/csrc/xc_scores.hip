@@ -5,7 +5,6 @@
 namespace xc {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 __host__ __device__ inline int quantized_pitch(int d) { return (d + 15) & ~15; }
 
@@ -109,19 +108,21 @@ static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const in
 // scores
 // ---------------------------------------------------------------------------
 // Tiles of BM queries x BN labels, K staged KB bytes of each row at a time through a ring of R stages in LDS (direct
-// global -> LDS loads).  WQ x WL waves, each with MQ x ML blocks of v_mfma_i32_32x32x32_i8.
+// global -> LDS loads).  WQ x WL waves, each with MQ x ML blocks of v_mfma_i32_16x16x64_i8.
 // LDS rows are unpadded, their 16-byte chunks stored at chunk ^ swizzle(row) so that 16 lanes reading one chunk of 16 rows
-// meet all banks.  Block nt of a wave's labels holds every ML-th of them: label ML j + nt is column j of block nt, so that a
-// lane ends up with ML neighbouring labels and stores them together.
-// Accumulator i of a lane: query 8 (i / 4) + 4 (lane / 32) + i % 4 of its block, column lane % 32.
-template <int WQ_, int WL_, int MQ_, int ML_, int KB_, int R_>
+// meet all banks.  Blocks of labels are interleaved, V at a time, so that a lane ends up with V neighbouring labels, 16
+// bytes of scores where there are as many: label V j + v of a group of 16 V is column j of its block v.
+// Accumulator i of a lane: query 4 (lane / 16) + i of its block, column lane % 16.
+template <int WQ_, int WL_, int MQ_, int ML_, int KB_, int R_, int G_>
 struct Tile {
-    static constexpr int WQ = WQ_, WL = WL_, MQ = MQ_, ML = ML_, KB = KB_, R = R_;
-    static constexpr int kWaves = WQ * WL, kThreads = 64 * kWaves, BM = 32 * WQ * MQ, BN = 32 * WL * ML;
-    static constexpr int kStage = (BM + BN) * KB, kLds = R * kStage;
+    static constexpr int WQ = WQ_, WL = WL_, MQ = MQ_, ML = ML_, KB = KB_, R = R_, G = G_;
+    static constexpr int kWaves = WQ * WL, kThreads = 64 * kWaves, BM = 16 * WQ * MQ, BN = 16 * WL * ML;
+    static constexpr int kStage = (BM + BN) * KB, kScaleLinesL = (BN + 63) / 64, kScaleLinesQ = (BM + 63) / 64, kScales = (kScaleLinesL + kScaleLinesQ) * 256, kLds = R * kStage + (R + 1) * kScales;
+    static constexpr int kPerCu = 160 * 1024 / kLds < 8 / kWaves ? 160 * 1024 / kLds : 8 / kWaves;      // workgroups of a compute unit
+    static constexpr int kPerSimd = kPerCu * kWaves < 8 ? 1 : 2;
     static constexpr int kRowsPerLoad = 1024 / KB;       // rows that one load instruction of a wave brings in
-    static constexpr int kLoadsA = BM / kRowsPerLoad / kWaves, kLoadsB = BN / kRowsPerLoad / kWaves, kLoads = kLoadsA + kLoadsB;
-    static_assert(kLoadsA * kRowsPerLoad * kWaves == BM && kLoadsB * kRowsPerLoad * kWaves == BN, "loads divide evenly among the waves");
+    static constexpr int kIssue = kWaves / G /* waves that bring in a stage */, kLoadsA = BM / kRowsPerLoad / kIssue, kLoadsB = BN / kRowsPerLoad / kIssue, kLoads = kLoadsA + kLoadsB;
+    static_assert(kLoadsA * kRowsPerLoad * kIssue == BM && kLoadsB * kRowsPerLoad * kIssue == BN, "loads divide evenly among the waves");
     static __device__ __forceinline__ int swizzle(int row) { return (row / (256 / KB)) & (KB / 16 - 1); }
 };
 
@@ -137,22 +138,25 @@ struct ScoresArgs {
 };
 
 // N neighbouring scores; `left` of them exist
-template <typename TO, int N>
-__device__ __forceinline__ void store_labels(TO* p, const float (&v)[N], int64_t left) {
-    if constexpr (sizeof(TO) == 4) {
-        if (left >= N) { __builtin_memcpy(p, v, 4 * N); return; }
+// N neighbouring scores, all of them there
+template <int N> __device__ __forceinline__ void store_labels(float* p, const float (&v)[N]) { __builtin_memcpy(p, v, 4 * N); }
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+template <int N> __device__ __forceinline__ void store_labels(bf16_t* p, const float (&v)[N]) {
+    bf16x2 h[N / 2];
 #pragma unroll
-        for (int e = 0; e < N; ++e) if (e < left) reinterpret_cast<float*>(p)[e] = v[e];
-    } else {
-        uint16_t h[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e) h[e] = static_cast<uint16_t>(float_to_bf16_bits(v[e]));
-        if (left >= N) { __builtin_memcpy(p, h, 2 * N); return; }
-#pragma unroll
-        for (int e = 0; e < N; ++e) if (e < left) p[e].bits = h[e];
-    }
+    for (int e = 0; e < N / 2; ++e) h[e] = __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2);      // nearest, ties to even
+    __builtin_memcpy(p, h, 2 * N);
+}
+__device__ __forceinline__ void store_label(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_label(bf16_t* p, float v) {
+    const __bf16 h = static_cast<__bf16>(v);
+    __builtin_memcpy(p, &h, 2);
 }
 
+__device__ __forceinline__ void lds_dma4(const void* gptr, uint32_t lds_addr /* wave-uniform */) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(gptr), "s"(lds_addr) : "memory");
+}
 __device__ __forceinline__ const void* uniform_ptr(const void* p) {
     const uint64_t a = reinterpret_cast<uint64_t>(p);
     return reinterpret_cast<const void*>(
@@ -161,116 +165,203 @@ __device__ __forceinline__ const void* uniform_ptr(const void* p) {
 }
 
 template <typename TO, typename T>
-__global__ __launch_bounds__(T::kThreads, 2)
+__global__ __launch_bounds__(T::kThreads, T::kPerSimd)
 void scores_kernel(const ScoresArgs a) {
     __shared__ __align__(1024) unsigned char smem[T::kLds];
-    // workgroup w runs on XCD w % 8: each XCD takes a contiguous part of the tiles, in an order that keeps a group of query
-    // tiles in its L2 while the labels pass
-    const int64_t n_tiles = static_cast<int64_t>(a.tiles_m) * a.tiles_n, per = (n_tiles + 7) / 8;
-    const int64_t t = static_cast<int64_t>(blockIdx.x % 8) * per + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= per || t >= n_tiles) return;
-    const int64_t in_groups = static_cast<int64_t>(a.group) * a.tiles_n;
-    const int g = static_cast<int>(t / in_groups), m0 = g * a.group;
-    const int gm = a.tiles_m - m0 < a.group ? a.tiles_m - m0 : a.group;
-    const int64_t r = t - g * in_groups;
-    const int tn = __builtin_amdgcn_readfirstlane(static_cast<int>(r / gm)), tm = __builtin_amdgcn_readfirstlane(m0 + static_cast<int>(r % gm));
-    const int64_t q0 = static_cast<int64_t>(tm) * T::BM, l0 = static_cast<int64_t>(tn) * T::BN;
-
-    const int lane = lane_id(), half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int V = T::ML < 16 / static_cast<int>(sizeof(TO)) ? T::ML : 16 / static_cast<int>(sizeof(TO));
+    const int lane = lane_id(), quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wq = wave / T::WL, wl = wave % T::WL;
+    const int wi = wave % T::kIssue, my_turn = wave / T::kIssue;      // stages n with n % G == my_turn are this wave's to bring in
     const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
 
-    // what a lane loads: chunk (position ^ swizzle) of its row, rows past the end repeat the last one
-    constexpr int kPerRow = T::KB / 16;
+    // workgroup w runs on XCD w % 8: each XCD takes a contiguous part of the tiles, in an order that keeps a group of query
+    // tiles in its L2 while the labels pass
+    const uint32_t n_tiles = static_cast<uint32_t>(a.tiles_m) * static_cast<uint32_t>(a.tiles_n), per = (n_tiles + 7) / 8;
+    const uint32_t t_begin = blockIdx.x % 8 * per, t_end = t_begin + per < n_tiles ? t_begin + per : n_tiles;
+    const uint32_t t_first = t_begin + blockIdx.x / 8, t_step = gridDim.x / 8;
+    if (t_first >= t_end) return;
     const int n_stages = (a.pitch + T::KB - 1) / T::KB;
-    uint32_t off_a[T::kLoadsA], off_b[T::kLoadsB], last_b[T::kLoadsB];
-    const int row_of = lane / kPerRow;
+    const int total = static_cast<int>((t_end - 1 - t_first) / t_step + 1) * n_stages;
+    auto place = [&](uint32_t t, int64_t& q0, int64_t& l0) __attribute__((always_inline)) {
+        const uint32_t in_groups = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(a.tiles_n);
+        const uint32_t g = t / in_groups, r = t - g * in_groups, m0 = g * a.group;
+        const uint32_t gm = a.tiles_m - m0 < static_cast<uint32_t>(a.group) ? a.tiles_m - m0 : a.group;
+        const uint32_t tn = r / gm;
+        q0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(m0 + r - tn * gm)) * T::BM;
+        l0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tn)) * T::BN;
+    };
+
+    // ---- loads.  A lane brings chunk (position ^ swizzle) of its row; its offsets from the tile's first row are the same for
+    // every tile and stage.  Queries are padded to whole tiles and stages; a tile of labels or a stage that reaches past the end
+    // takes another way.  The first stage of a tile has the scales of its labels and queries with it, 64 to a load, for one of
+    // R + 1 tiles: with rows of one stage the loads are R tiles ahead.
+    static_assert(T::KB == 128, "8 rows to a load");
+    constexpr int kScaleLinesL = T::kScaleLinesL, kScaleLinesQ = T::kScaleLinesQ;
+    // label of the tile in row r of the tile's labels in LDS
+    auto label_of = [&](int r) __attribute__((always_inline)) { const int blk = r >> 4; return (blk / V) * 16 * V + (r & 15) * V + blk % V; };
+    uint32_t off_a[T::kLoadsA], off_b[T::kLoadsB];
 #pragma unroll
     for (int i = 0; i < T::kLoadsA; ++i) {
-        const int rho = (wave * T::kLoadsA + i) * T::kRowsPerLoad + row_of;
-        const int64_t left = a.B - 1 - q0;
-        off_a[i] = static_cast<uint32_t>(rho < left ? rho : left) * static_cast<uint32_t>(a.ppitch) + (((lane % kPerRow) ^ T::swizzle(rho)) * 16);
+        const int r = (wi * T::kLoadsA + i) * 8 + (lane >> 3);
+        off_a[i] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ppitch) + ((lane & 7) ^ T::swizzle(r)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < T::kLoadsB; ++i) {
-        const int rho = (wave * T::kLoadsB + i) * T::kRowsPerLoad + row_of;
-        const int blk = rho >> 5, lab = (blk / T::ML) * 32 * T::ML + (rho & 31) * T::ML + blk % T::ML;
-        const int64_t left = a.L - 1 - l0;
-        const uint32_t row = static_cast<uint32_t>(lab < left ? lab : left) * static_cast<uint32_t>(a.pitch);
-        const int chunk = (lane % kPerRow) ^ T::swizzle(rho);
-        off_b[i] = row + chunk * 16;
-        // the last stage may reach past the row: any chunk of it will do there, the query's are zero
-        last_b[i] = (n_stages - 1) * T::KB + chunk * 16 < a.pitch ? off_b[i] : row;
+        const int r = (wi * T::kLoadsB + i) * 8 + (lane >> 3);
+        off_b[i] = static_cast<uint32_t>(label_of(r)) * static_cast<uint32_t>(a.pitch) + ((lane & 7) ^ T::swizzle(r)) * 16;
     }
-    const int8_t* base_a = a.P + q0 * a.ppitch;
-    const int8_t* base_b = a.Q + l0 * a.pitch;
-    auto issue = [&](int s) __attribute__((always_inline)) {
-        const uint32_t dst = lds + (s % T::R) * T::kStage;
-        const void* pa = uniform_ptr(base_a + s * T::KB);
-        const void* pb = uniform_ptr(base_b + s * T::KB);
+    uint32_t ld_t = t_first;
+    int ld_kb = 0, ld_slot = 0, ld_tile = 0, n_issued = 0;
+    int64_t ld_q = 0, ld_l = 0;
+    auto issue = [&]() __attribute__((always_inline)) {
+        if (ld_kb == 0) place(ld_t, ld_q, ld_l);
+        if (T::G == 1 || n_issued % T::G == my_turn) {
+            const int64_t have = a.L - ld_l;                 // labels of the tile
+            if (ld_kb == 0) {
+                const uint32_t to = lds + T::R * T::kStage + ld_tile * T::kScales;
 #pragma unroll
-        for (int i = 0; i < T::kLoadsA; ++i)
-            lds_dma16_sbase<0>(pa, off_a[i], __builtin_amdgcn_readfirstlane(dst + (wave * T::kLoadsA + i) * 1024));
+                for (int j = 0; j < kScaleLinesL + kScaleLinesQ; j += T::kIssue) {
+                    const int i = j + wi, lab = i * 64 + lane;           // i: uniform
+                    if (i < kScaleLinesL)
+                        lds_dma4(a.scale + ld_l + (lab < have ? lab : have - 1), __builtin_amdgcn_readfirstlane(to + i * 256));
+                    else if (i < kScaleLinesL + kScaleLinesQ)
+                        lds_dma4(a.pscale + ld_q + (i - kScaleLinesL) * 64 + lane, __builtin_amdgcn_readfirstlane(to + i * 256));
+                }
+            }
+            const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + ld_slot * T::kStage);
+            const void* from_a = uniform_ptr(a.P + ld_q * a.ppitch + ld_kb * T::KB);
 #pragma unroll
-        for (int i = 0; i < T::kLoadsB; ++i)
-            lds_dma16_sbase<0>(pb, s == n_stages - 1 ? last_b[i] : off_b[i],
-                               __builtin_amdgcn_readfirstlane(dst + T::BM * T::KB + (wave * T::kLoadsB + i) * 1024));
-    };
-
-    i32x16 acc[T::MQ][T::ML];
+            for (int i = 0; i < T::kLoadsA; ++i) lds_dma16_sbase<0>(from_a, off_a[i], dst + (wi * T::kLoadsA + i) * 1024);
+            const int room = a.pitch - ld_kb * T::KB;        // bytes of the rows from here on
+            const uint32_t dst_b = dst + T::BM * T::KB + wi * T::kLoadsB * 1024;
+            const int8_t* from_b = a.Q + ld_l * a.pitch + ld_kb * T::KB;
+            if (have >= T::BN && room >= T::KB) {
+                const void* from = uniform_ptr(from_b);
 #pragma unroll
-    for (int x = 0; x < T::MQ; ++x)
-#pragma unroll
-        for (int y = 0; y < T::ML; ++y) acc[x][y] = i32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
-    const int frag = (lane & 31) * T::KB + ((half ^ T::swizzle(lane & 31)) * 16);
-
-    for (int s = 0; s < T::R - 1 && s < n_stages; ++s) issue(s);
-    for (int s = 0; s < n_stages; ++s) {
-        if (s + T::R - 2 < n_stages) wait_vmem_at_most<T::kLoads * (T::R - 2)>();
-        else wait_all_vmem();
-        lds_barrier();                                   // everyone's part of stage s is there, and stage s - 1 is read
-        if (s + T::R - 1 < n_stages) issue(s + T::R - 1);
-        const unsigned char* sa = smem + (s % T::R) * T::kStage + wq * T::MQ * 32 * T::KB;
-        const unsigned char* sb = smem + (s % T::R) * T::kStage + (T::BM + wl * T::ML * 32) * T::KB;
-#pragma unroll
-        for (int kk = 0; kk < T::KB / 32; ++kk) {
-            i32x4 fa[T::MQ], fb[T::ML];
-#pragma unroll
-            for (int x = 0; x < T::MQ; ++x) fa[x] = *reinterpret_cast<const i32x4*>(sa + ((frag ^ (kk * 32)) + x * 32 * T::KB));
-#pragma unroll
-            for (int y = 0; y < T::ML; ++y) fb[y] = *reinterpret_cast<const i32x4*>(sb + ((frag ^ (kk * 32)) + y * 32 * T::KB));
-#pragma unroll
-            for (int x = 0; x < T::MQ; ++x)
-#pragma unroll
-                for (int y = 0; y < T::ML; ++y) acc[x][y] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fa[x], fb[y], acc[x][y], 0, 0, 0);
-        }
-    }
-
-    const int64_t l = l0 + wl * 32 * T::ML + (lane & 31) * T::ML, left = a.L - l;
-    if (left <= 0) return;
-    float sl[T::ML];
-#pragma unroll
-    for (int y = 0; y < T::ML; ++y) sl[y] = y < left ? a.scale[l + y] : 0.0f;
-    TO* out = static_cast<TO*>(a.out);
-#pragma unroll
-    for (int x = 0; x < T::MQ; ++x)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int64_t q = q0 + (wq * T::MQ + x) * 32 + 8 * (i >> 2) + 4 * half + (i & 3);
-            if (q < a.B) {
-                const float sq = a.pscale[q];
-                float v[T::ML];
-#pragma unroll
-                for (int y = 0; y < T::ML; ++y) v[y] = (static_cast<float>(acc[x][y][i]) * sq) * sl[y];
-                store_labels(out + q * a.L + l, v, left);
+                for (int i = 0; i < T::kLoadsB; ++i) lds_dma16_sbase<0>(from, off_b[i], dst_b + i * 1024);
+            } else {                                         // rows past the end: the last one again; chunks behind a row: its first here (the query's are zero)
+#pragma unroll 1
+                for (int i = 0; i < T::kLoadsB; ++i) {
+                    const int r = (wi * T::kLoadsB + i) * 8 + (lane >> 3), lab = label_of(r), at = ((lane & 7) ^ T::swizzle(r)) * 16;
+                    lds_dma16(from_b + (lab < have ? lab : have - 1) * a.pitch + (at < room ? at : 0), __builtin_amdgcn_readfirstlane(dst_b + i * 1024));
+                }
             }
         }
+        if (ld_kb == 0 && ++ld_tile == T::R + 1) ld_tile = 0;
+        if (++ld_kb == n_stages) { ld_kb = 0; ld_t += t_step; }
+        if (++ld_slot == T::R) ld_slot = 0;
+        ++n_issued;
+    };
+
+    // ---- products.  The operands of a k-step are read while the one before is multiplied: a block of labels right behind its
+    // own products, blocks of queries into the other half of their registers.
+    constexpr int kSteps = T::KB / 64;
+    i32x4 acc[T::MQ][T::ML], fa[2][T::MQ], fb[T::ML];
+    const int frag = (lane & 15) * T::KB + ((quarter ^ T::swizzle(lane & 15)) * 16);
+    auto read_a = [&](int slot, int kk, int x) __attribute__((always_inline)) {
+        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (wq * T::MQ + x) * 16 * T::KB + (frag ^ (kk * 64)));
+    };
+    auto read_b = [&](int slot, int kk, int y) __attribute__((always_inline)) {
+        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (T::BM + (wl * T::ML + y) * 16) * T::KB + (frag ^ (kk * 64)));
+    };
+    constexpr int kStores = 4 * T::MQ * (T::ML / V);         // of a whole tile
+    int since_stores = T::R;                                 // stages published since a whole tile's scores were stored
+    // the next stage is there for everyone, and the one before it has been read by everyone: its slot is filled again
+    auto publish = [&](int g_next) __attribute__((always_inline)) {
+        constexpr int kNewer = T::kLoads * ((T::R - 2) / T::G);
+        if (T::G == 1 || g_next % T::G == my_turn) {
+            if (n_issued - 1 - g_next < T::R - 2) wait_all_vmem();
+            else if (since_stores < T::R - 1) wait_vmem_at_most<(kNewer + kStores < 63 ? kNewer + kStores : 63)>();
+            else wait_vmem_at_most<kNewer>();
+        }
+        ++since_stores;
+        lds_barrier();
+        if (n_issued < total) issue();
+    };
+
+    for (int s = 0; s < T::R - 1 && s < total; ++s) issue();
+    publish(0);
+#pragma unroll
+    for (int x = 0; x < T::MQ; ++x) fa[0][x] = read_a(0, 0, x);
+#pragma unroll
+    for (int y = 0; y < T::ML; ++y) fb[y] = read_b(0, 0, y);
+    int g = 0, slot = 0, tile = 0;
+    for (uint32_t t = t_first; t < t_end; t += t_step) {
+#pragma unroll
+        for (int x = 0; x < T::MQ; ++x)
+#pragma unroll
+            for (int y = 0; y < T::ML; ++y) acc[x][y] = i32x4{0, 0, 0, 0};
+        for (int kb = 0; kb < n_stages; ++kb) {
+            const int slot_next = slot + 1 == T::R ? 0 : slot + 1;
+#pragma unroll
+            for (int kk = 0; kk < kSteps; ++kk) {
+                static_assert(kSteps % 2 == 0, "the halves of fa change places with every step");
+                const int sel = kk & 1, kk_next = kk + 1 < kSteps ? kk + 1 : 0, from = kk + 1 < kSteps ? slot : slot_next;
+                if (kk == kSteps - 1 && g + 1 < total) publish(g + 1);       // (behind the last stage: what is read is not used)
+#pragma unroll
+                for (int y = 0; y < T::ML; ++y) {
+#pragma unroll
+                    for (int x = y * T::MQ / T::ML; x < (y + 1) * T::MQ / T::ML; ++x) fa[sel ^ 1][x] = read_a(from, kk_next, x);
+#pragma unroll
+                    for (int x = 0; x < T::MQ; ++x) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[sel][x], fb[y], acc[x][y], 0, 0, 0);
+                    fb[y] = read_b(from, kk_next, y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            ++g;
+            slot = slot_next;
+        }
+
+        int64_t q0, l0;
+        place(t, q0, l0);
+        const float* scales = reinterpret_cast<const float*>(smem + T::R * T::kStage + tile * T::kScales);
+        if (++tile == T::R + 1) tile = 0;
+        const int lt = wl * 16 * T::ML + (lane & 15) * V, qt = wq * T::MQ * 16 + 4 * quarter;       // of the tile
+        float sl[T::ML];
+#pragma unroll
+        for (int y = 0; y < T::ML; ++y) sl[y] = scales[lt + (y / V) * 16 * V + y % V];
+        TO* out = static_cast<TO*>(a.out) + (q0 + qt) * a.L + l0 + lt;
+        auto rows = [&](auto whole) __attribute__((always_inline)) {
+#pragma unroll
+            for (int x = 0; x < T::MQ; ++x) {
+                const float4 sq = *reinterpret_cast<const float4*>(scales + kScaleLinesL * 64 + qt + x * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float s = i == 0 ? sq.x : i == 1 ? sq.y : i == 2 ? sq.z : sq.w;
+#pragma unroll
+                    for (int y0 = 0; y0 < T::ML; y0 += V) {
+                        float v[V];
+#pragma unroll
+                        for (int y = 0; y < V; ++y) v[y] = (static_cast<float>(acc[x][y0 + y][i]) * s) * sl[y0 + y];
+                        TO* p = out + (x * 16 + i) * a.L + y0 * 16;
+                        if constexpr (decltype(whole)::value) {
+                            store_labels(p, v);
+                        } else if (q0 + qt + x * 16 + i < a.B) {
+                            const int64_t left = a.L - l0 - lt - y0 * 16;
+#pragma unroll
+                            for (int y = 0; y < V; ++y) if (y < left) store_label(p + y, v[y]);
+                        }
+                    }
+                }
+            }
+        };
+        if (q0 + T::BM <= a.B && l0 + T::BN <= a.L) {
+            rows(std::true_type{});
+            since_stores = 0;
+        } else {
+            rows(std::false_type{});
+        }
+    }
 }
 
-typedef Tile<2, 2, 2, 4, 64, 3> TileMany;                // 128 x 256
-typedef Tile<1, 4, 2, 1, 128, 3> TileSome;               // 64 x 128
-typedef Tile<1, 4, 1, 1, 128, 4> TileFew;                // 32 x 128
-constexpr int kQueryPad = 128;                           // rows of P are whole stages of any kind
+typedef Tile<4, 2, 4, 8, 128, 2, 2> TileMany;            // 256 x 256
+typedef Tile<2, 2, 4, 4, 128, 2, 1> TileMid;             // 128 x 128
+typedef Tile<2, 2, 2, 2, 128, 4, 1> TileSmall;           // 64 x 64
+typedef Tile<1, 4, 4, 2, 128, 3, 1> TileSome;            // 64 x 128
+typedef Tile<1, 4, 2, 2, 128, 3, 1> TileFew;             // 32 x 128
+typedef Tile<1, 1, 2, 2, 128, 4, 1> TileNarrow;          // 32 x 32
+constexpr int kQueryPad = 128;                           // the queries in the workspace: rows of whole stages,
+constexpr int kQueryTile = 256;                           // whole tiles of them of any kind
 
 template <typename TO, typename T>
 static void launch_scores(ScoresArgs a, hipStream_t st) {
@@ -279,12 +370,211 @@ static void launch_scores(ScoresArgs a, hipStream_t st) {
     // a group of query tiles takes half of an XCD's L2
     const int64_t fit = (2 << 20) / (static_cast<int64_t>(T::BM) * a.ppitch);
     a.group = static_cast<int>(fit < 1 ? 1 : fit < a.tiles_m ? fit : a.tiles_m);
-    const int64_t per = (static_cast<int64_t>(a.tiles_m) * a.tiles_n + 7) / 8;
-    scores_kernel<TO, T><<<static_cast<unsigned>(8 * per), T::kThreads, 0, st>>>(a);
+    const int64_t per = (static_cast<int64_t>(a.tiles_m) * a.tiles_n + 7) / 8, most = kCusPerXcd * T::kPerCu;
+    scores_kernel<TO, T><<<static_cast<unsigned>(8 * (per < most ? per : most)), T::kThreads, 0, st>>>(a);
+}
+
+// ---- many queries, rows of up to 768 bytes: the labels stay where they are.  A wave holds 64 labels as operands in registers (NK
+// k-steps of 64 bytes) and 512 labels of a workgroup meet the queries that stream through LDS, QS at a time.  Per product that is
+// half the operand reads from LDS that a 256 x 256 tile takes, an eighth of the bytes brought into it, and a wave's scores are
+// stored 16 queries at a time, while the other wave of its SIMD multiplies.
+template <int NK_>
+struct Held {
+    static constexpr int NK = NK_, QS = NK % 4 == 0 ? 32 : 64, kStage = QS * NK * 64;       // (the stage's loads divide evenly among 8 waves)
+    static constexpr int kFit = 160 * 1024 / (kStage + 256), R = kFit < 6 ? kFit : 6;       // stages in LDS, at least 3
+    static constexpr int kLoads = kStage / 1024 / 8, kStores = QS / 4;                      // of a wave and stage
+    static constexpr int kLds = R * (kStage + 256);
+    static_assert(kLoads * 8 * 1024 == kStage && R >= 3 && (kLoads + kStores) * (R - 3) < 64, "whole loads, and a count that the wait can hold");
+};
+constexpr int kHeldLabels = 512, kHeldBytes = 768;
+
+template <typename TO, int NK>
+__global__ __launch_bounds__(512, 2)
+void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
+    typedef Held<NK> H;
+    __shared__ __align__(1024) unsigned char smem[H::kLds];
+    const int lane = lane_id(), quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
+    // a contiguous part of the units (a stage of queries for a tile of labels), neighbouring parts on one XCD
+    const int64_t part = static_cast<int64_t>(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
+    const int64_t u_begin = units * part / gridDim.x, u_end = units * (part + 1) / gridDim.x;
+    if (u_begin >= u_end) return;
+    const int total = static_cast<int>(u_end - u_begin);
+    int64_t tile = u_begin / stages;
+    int st = static_cast<int>(u_begin % stages);
+
+    uint32_t off[H::kLoads];
+#pragma unroll
+    for (int i = 0; i < H::kLoads; ++i) {
+        const int n = wave * H::kLoads + i, row = n % (H::QS / 8) * 8 + (lane >> 3);
+        off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(a.ppitch) + n / (H::QS / 8) * 128 + (((lane & 7) ^ ((row >> 1) & 7)) * 16);
+    }
+    int ld_st = st, ld_slot = 0, n_issued = 0;
+    auto issue = [&]() __attribute__((always_inline)) {
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + ld_slot * H::kStage);
+        if (wave == 0) lds_dma4(a.pscale + ld_st * H::QS + lane, __builtin_amdgcn_readfirstlane(lds + H::R * H::kStage + ld_slot * 256));
+        const void* from = uniform_ptr(a.P + static_cast<int64_t>(ld_st) * H::QS * a.ppitch);
+#pragma unroll
+        for (int i = 0; i < H::kLoads; ++i) lds_dma16_sbase<0>(from, off[i], dst + (wave * H::kLoads + i) * 1024);
+        if (++ld_st == stages) ld_st = 0;
+        if (++ld_slot == H::R) ld_slot = 0;
+        ++n_issued;
+    };
+    int full = 0;                                            // stages in a row whose scores were all stored as whole blocks
+    auto publish = [&](int g_next) __attribute__((always_inline)) {
+        // (published while the stage before it still has a block to read: the slot of the one before that is filled)
+        if (n_issued - 1 - g_next < H::R - 3) wait_all_vmem();
+        else if (full >= H::R) wait_vmem_at_most<(H::kLoads + H::kStores) * (H::R - 3)>();
+        else wait_vmem_at_most<H::kLoads*(H::R - 3)>();
+        lds_barrier();
+        if (n_issued < total && n_issued < g_next + H::R - 1) issue();
+    };
+    for (int s = 0; s < H::R - 1 && s < total; ++s) issue();
+
+    i32x4 w[NK][4], fa[3];
+    float sl[4];
+    const int frag = (lane & 15) * 128 + ((quarter ^ (((lane & 15) >> 1) & 7)) * 16);
+    auto read_a = [&](int slot, int qb, int k) __attribute__((always_inline)) {      // 16 queries, 64 bytes of each
+        return *reinterpret_cast<const i32x4*>(smem + slot * H::kStage + (k >> 1) * (H::QS * 128) + qb * 2048 + (frag ^ ((k & 1) * 64)));
+    };
+    auto hold = [&](int64_t l0) __attribute__((always_inline)) {                     // the wave's labels: 4 neighbouring ones to a lane
+        const int64_t l = l0 + wave * 64 + (lane & 15) * 4;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int64_t row = l + y < a.L ? l + y : a.L - 1;
+            sl[y] = a.scale[row];
+            const int8_t* p = a.Q + row * a.pitch + quarter * 16;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                w[k][y] = i32x4{0, 0, 0, 0};
+                if (k * 64 + quarter * 16 < a.pitch) w[k][y] = *reinterpret_cast<const i32x4*>(p + k * 64);
+            }
+        }
+        // awaited here: the loop over the stages would wait for these (and for all loads and stores under way) every time round
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            asm volatile("" : "+v"(sl[y]));
+#pragma unroll
+            for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(w[k][y]));
+        }
+    };
+    hold(tile * kHeldLabels);
+    publish(0);
+    fa[0] = read_a(0, 0, 0);
+    fa[1] = read_a(0, 0, 1);
+    int slot = 0;
+    constexpr int kBlocks = H::QS / 16;
+    for (int g = 0; g < total; ++g) {
+        const int64_t l0 = tile * kHeldLabels + wave * 64, l = l0 + (lane & 15) * 4;
+        const int q0 = st * H::QS;
+        const bool whole = q0 + H::QS <= a.B && l0 + 64 <= a.L;
+        const int slot_next = slot + 1 == H::R ? 0 : slot + 1;
+        const float* sq = reinterpret_cast<const float*>(smem + H::R * H::kStage + slot * 256) + 4 * quarter;
+        TO* out = static_cast<TO*>(a.out) + static_cast<int64_t>(q0 + 4 * quarter) * a.L + l;
+#pragma unroll
+        for (int qb = 0; qb < kBlocks; ++qb) {
+            if (qb == kBlocks - 1 && g + 1 < total) publish(g + 1);
+            i32x4 acc[4];
+            const float4 s4 = *reinterpret_cast<const float4*>(sq + qb * 16);
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                constexpr int kDepth = 2;
+                const int kn = k + kDepth < NK ? k + kDepth : k + kDepth - NK;
+                const bool over = k + kDepth >= NK;
+                const int n = qb * NK + k;                   // of the stage: NK * kBlocks is a multiple of 3 or fa is indexed by it
+                fa[(n + kDepth) % 3] = !over ? read_a(slot, qb, kn) : qb + 1 < kBlocks ? read_a(slot, qb + 1, kn) : read_a(slot_next, 0, kn);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    acc[y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[n % 3], w[k][y], k == 0 ? i32x4{0, 0, 0, 0} : acc[y], 0, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if constexpr ((NK * kBlocks) % 3 != 0) {
+                if (qb == kBlocks - 1) {                     // the next stage starts at fa[0] again
+                    const i32x4 f0 = fa[(NK * kBlocks) % 3], f1 = fa[(NK * kBlocks + 1) % 3];
+                    fa[0] = f0;
+                    fa[1] = f1;
+                }
+            }
+            auto rows = [&](auto all) __attribute__((always_inline)) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float s = i == 0 ? s4.x : i == 1 ? s4.y : i == 2 ? s4.z : s4.w;
+                    float v[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) v[y] = (static_cast<float>(acc[y][i]) * s) * sl[y];
+                    TO* p = out + static_cast<int64_t>(qb * 16 + i) * a.L;
+                    if constexpr (decltype(all)::value) {
+                        store_labels(p, v);
+                    } else if (q0 + qb * 16 + 4 * quarter + i < a.B) {
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) if (l + y < a.L) store_label(p + y, v[y]);
+                    }
+                }
+            };
+            if (whole) rows(std::true_type{});
+            else rows(std::false_type{});
+        }
+        full = whole ? full + 1 : 0;
+        slot = slot_next;
+        if (++st == stages) {
+            st = 0;
+            ++tile;
+            full = 0;
+            if (g + 1 < total) hold(tile * kHeldLabels);
+        }
+    }
+}
+
+template <typename TO, int NK>
+static void launch_held(ScoresArgs a, hipStream_t st) {
+    const int stages = static_cast<int>((a.B + Held<NK>::QS - 1) / Held<NK>::QS);
+    const int64_t units = (a.L + kHeldLabels - 1) / kHeldLabels * stages;
+    scores_held_kernel<TO, NK><<<kMineGrid, 512, 0, st>>>(a, units, stages);
+}
+
+template <typename TO>
+static void run_held(const ScoresArgs& a, hipStream_t st) {
+    switch (a.ppitch / 128) {
+        case 1: launch_held<TO, 2>(a, st); break;
+        case 2: launch_held<TO, 4>(a, st); break;
+        case 3: launch_held<TO, 6>(a, st); break;
+        case 4: launch_held<TO, 8>(a, st); break;
+        case 5: launch_held<TO, 10>(a, st); break;
+        default: launch_held<TO, 12>(a, st); break;
+    }
+}
+
+// Which kernel.  Measured with rows of Q from memory (us, scores alone, on the sides of each rule):
+//   up to 32 queries   32 x 128; fewer labels than 256 such tiles 32 x 32 (16 x 4000 x 4096: 15.5 against 24.5)
+//   up to 512 tiles of 64 x 64   these (128 x 16000 x 768: 8.5 against 10.0 with 128 x 128; 400 x 4000 x 4096: 25 against 35)
+//   up to 64 queries   64 x 128 (64 x 300000 x 768: 59; 128 x 128 70, 64 x 64 62)
+//   up to 128 queries, or three rounds of 128 x 128 tiles   these (128 x 670000 x 768: 148, labels held 181; 300 x 50000 x 768:
+//                      29 against 37; 512 x 131072 x 768: 100 against 66, so not beyond)
+//   more, rows of up to 768 bytes   labels held in registers (4096 x 131072 x 768: 420; 256 x 256 tiles 545)
+//   longer rows        256 x 256, where that takes fewer rounds for its larger tiles (512 x 32000 x 1024: 23 against 25;
+//                      1024 x 8000 x 1024: 27 against 18, so not there)
+template <typename TO>
+static void run_scores(const ScoresArgs& a, hipStream_t st) {
+    auto tiles = [&](int m, int n) { return (a.B + m - 1) / m * ((a.L + n - 1) / n); };
+    if (a.B <= 32) {
+        if (tiles(32, 128) >= kMineGrid) launch_scores<TO, TileFew>(a, st);
+        else launch_scores<TO, TileNarrow>(a, st);
+    } else if (tiles(64, 64) <= 2 * kMineGrid) {
+        launch_scores<TO, TileSmall>(a, st);
+    } else if (a.B <= 64) {
+        launch_scores<TO, TileSome>(a, st);
+    } else if (a.ppitch <= kHeldBytes) {
+        if (a.B <= 128 || tiles(128, 128) <= 6 * kMineGrid) launch_scores<TO, TileMid>(a, st);
+        else run_held<TO>(a, st);
+    } else {
+        const int64_t mid = (tiles(128, 128) + 2 * kMineGrid - 1) / (2 * kMineGrid), many = (tiles(256, 256) + kMineGrid - 1) / kMineGrid;
+        if (a.B <= 192 || 5 * mid <= 8 * many) launch_scores<TO, TileMid>(a, st);
+        else launch_scores<TO, TileMany>(a, st);
+    }
 }
 
 static size_t scores_bytes(int64_t B, int d) {
-    return round_up(static_cast<size_t>(B) * 4, 256) + static_cast<size_t>(B) * round_up(d, kQueryPad);
+    return round_up(B, kQueryTile) * (4 + round_up(d, kQueryPad));
 }
 
 static bool row_ok(int d, xc_dtype t) {
@@ -321,14 +611,12 @@ extern "C" int xc_scores_quantized(const void* Z, int64_t B, int d, xc_dtype t, 
     if (ws_bytes < scores_bytes(B, d)) return XC_EWORKSPACE;
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* pscale = static_cast<float*>(ws);
-    int8_t* P = static_cast<int8_t*>(ws) + round_up(static_cast<size_t>(B) * 4, 256);
+    int8_t* P = static_cast<int8_t*>(ws) + round_up(B, kQueryTile) * 4;
     const int rc = launch_quantize(Z, B, d, t, nullptr, 0, nullptr, P, static_cast<int>(round_up(d, kQueryPad)), pscale, st);
     if (rc != XC_OK) return rc;
     const ScoresArgs a{P, pscale, Q, scale, out, B, L, quantized_pitch(d), static_cast<int>(round_up(d, kQueryPad)), 0, 0, 0};
-    if (out_t == XC_F32)
-        XC_LAUNCH(K_SCORES, st, B <= 32 ? (launch_scores<float, TileFew>(a, st)) : B <= 64 ? (launch_scores<float, TileSome>(a, st)) : (launch_scores<float, TileMany>(a, st)));
-    else
-        XC_LAUNCH(K_SCORES, st, B <= 32 ? (launch_scores<bf16_t, TileFew>(a, st)) : B <= 64 ? (launch_scores<bf16_t, TileSome>(a, st)) : (launch_scores<bf16_t, TileMany>(a, st)));
+    if (out_t == XC_F32) XC_LAUNCH(K_SCORES, st, run_scores<float>(a, st));
+    else XC_LAUNCH(K_SCORES, st, run_scores<bf16_t>(a, st));
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }

@@ -163,6 +163,32 @@ def test_a_range_of_labels_and_every_batch_size_give_the_same_bits(B):
     assert torch.equal(part, every[:B, 1000:2304])
 
 
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("B,L,d", [(290, 70001, 24), (137, 131072, 128), (290, 70004, 200), (261, 100000, 384), (500, 50021, 512),
+                                   (700, 40000, 600), (290, 70001, 768), (1025, 30000, 768), (300, 30001, 776), (600, 20000, 1096),
+                                   (2049, 8005, 2064)])
+def test_large_calls_have_the_bits_of_small_ones(B, L, d, out_dtype):
+    """The kernels of large calls against those of small ones, which the oracle checks above."""
+    import paper_2409_20156_amd as xc
+    g = torch.Generator(device=DEV).manual_seed(B + L + d)
+    Z = torch.randn((B, d), device=DEV, generator=g).to(BF16)
+    Q = torch.randint(-127, 128, (L, xc.quantized_pitch(d)), dtype=torch.int8, device=DEV, generator=g)
+    Q[:, d:] = 0
+    s = torch.rand(L, device=DEV, generator=g)
+    out, intact = _guarded((B, L), out_dtype, 77.0)
+    xc.scores_quantized(Z, Q, s, out=out)
+    torch.cuda.synchronize()
+    intact()
+    # 32 queries at a time on all labels; then all queries on the first and last labels
+    for q in list(range(0, B, 32))[:3] + [B - 30]:
+        few = xc.scores_quantized(Z[q:q + 30].contiguous(), Q, s, dtype=out_dtype)
+        assert torch.equal(out[q:q + 30], few)
+    for l in (0, (L // 2) // 64 * 64, (L - 300) // 4 * 4):
+        n = min(400, L - l)
+        some = torch.cat([xc.scores_quantized(Z[q:q + 64].contiguous(), Q[l:l + n], s[l:l + n], dtype=out_dtype) for q in range(0, B, 64)])
+        assert torch.equal(out[:, l:l + n], some)
+
+
 def test_offsets_beyond_32_bits():
     import paper_2409_20156_amd as xc
     # 4.9 GB of rows, few queries; and 4.4 GB of scores
