@@ -38,68 +38,169 @@ __device__ __forceinline__ RowScale row_scale(uint32_t bits) {
     return r;
 }
 
-template <typename T> struct Row;
-template <> struct Row<float> {
-    static constexpr int kPer = 4;       // elements of 16 bytes
-    static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[4]) {
-        f[0] = __uint_as_float(v.x); f[1] = __uint_as_float(v.y); f[2] = __uint_as_float(v.z); f[3] = __uint_as_float(v.w);
+// 8 neighbouring elements of a row.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    uint4 v[2];
+    __device__ __forceinline__ void zero() { v[0] = v[1] = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const unsigned char* row, int e, int d) {
+        v[0] = *reinterpret_cast<const uint4*>(row + e * 4);
+        if (e + 4 < d) v[1] = *reinterpret_cast<const uint4*>(row + e * 4 + 16);         // (d is a multiple of 4)
+    }
+    __device__ __forceinline__ uint32_t largest() const {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t x[4] = {v[i].x & 0x7fffffffu, v[i].y & 0x7fffffffu, v[i].z & 0x7fffffffu, v[i].w & 0x7fffffffu};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = x[e] > m ? x[e] : m;
+        }
+        return m;
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f[4 * i] = __uint_as_float(v[i].x); f[4 * i + 1] = __uint_as_float(v[i].y);
+            f[4 * i + 2] = __uint_as_float(v[i].z); f[4 * i + 3] = __uint_as_float(v[i].w);
+        }
     }
 };
-template <> struct Row<bf16_t> {
-    static constexpr int kPer = 8;
-    static __device__ __forceinline__ void unpack(const uint4& v, float (&f)[8]) { unpack8(v, f); }
+template <> struct Eight<bf16_t> {
+    uint4 v;
+    __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
+    __device__ __forceinline__ void load(const unsigned char* row, int e, int) { v = *reinterpret_cast<const uint4*>(row + e * 2); }
+    __device__ __forceinline__ uint32_t largest() const {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        const uint32_t u[4] = {v.x & 0x7fff7fffu, v.y & 0x7fff7fffu, v.z & 0x7fff7fffu, v.w & 0x7fff7fffu};
+        u16x2 x[4];
+        __builtin_memcpy(x, u, 16);
+        const u16x2 m = __builtin_elementwise_max(__builtin_elementwise_max(x[0], x[1]), __builtin_elementwise_max(x[2], x[3]));
+        return static_cast<uint32_t>(m.x > m.y ? m.x : m.y) << 16;
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const { unpack8(v, f); }
 };
 
-// One wave per row, which is read twice.
-template <typename T>
+// 8 elements -> 8 integers.  Adding 1.5 * 2^23 leaves the nearest integer in the low bits; where any of the 8 comes near a
+// half, all are decided exactly.
+__device__ __forceinline__ uint2 to_integers(float (&f)[8], const RowScale& s) {
+    constexpr float kMagic = 12582912.0f;
+    if (s.up != 1.0f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] *= s.up;
+    }
+    uint32_t b[8];
+    float off = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float r = fmaf(f[e], s.inv, kMagic);
+        off = fmaxf(off, fabsf(fmaf(f[e], s.inv, kMagic - r)));
+        b[e] = __float_as_uint(r);
+    }
+    if (__builtin_expect(off > 0.5f - 1e-4f, 0)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = static_cast<uint32_t>(to_integer(f[e], s.m, s.inv));
+    }
+    uint2 o;
+    o.x = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u), __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
+    o.y = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[7], b[6], 0x0c0c0400u), __builtin_amdgcn_perm(b[5], b[4], 0x0c0c0400u), 0x05040100u);
+    return o;
+}
+
+// 2^lg lanes per row, which they hold in registers: C groups of 8 elements each, read once.  C = 0: longer rows, one wave per
+// row, read twice.
+template <typename T, int C>
 __global__ __launch_bounds__(256)
 void quantize_kernel(const unsigned char* __restrict__ X, int64_t N, int d, const int32_t* __restrict__ ids, int64_t m,
-                     const int32_t* __restrict__ count, int8_t* __restrict__ Q, int pitch, float* __restrict__ scale) {
-    constexpr int kPer = Row<T>::kPer;
-    const int chunks = d / kPer, lane = lane_id();
+                     const int32_t* __restrict__ count, int8_t* __restrict__ Q, int pitch, float* __restrict__ scale, int lg) {
+    const int lane = lane_id(), per = 1 << lg, sub = lane & (per - 1);
+    const int64_t row_bytes = static_cast<int64_t>(d) * (sizeof(T) == 4 ? 4 : 2);
     int64_t rows = ids != nullptr ? m : N;
     if (ids != nullptr && count != nullptr) {
         const int64_t c = count[0];
         rows = c < rows ? c : rows;
     }
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); i < rows; i += static_cast<int64_t>(gridDim.x) * 4) {
+    const int64_t step = static_cast<int64_t>(gridDim.x) * 4 << (6 - lg);
+    for (int64_t i = ((static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6)) << (6 - lg)) + (lane >> lg); i < rows; i += step) {
         const int64_t row = ids != nullptr ? ids[i] : i;
-        if (row < 0 || row >= N) continue;
-        const uint4* src = reinterpret_cast<const uint4*>(X) + row * chunks;
-        uint32_t big = 0;
-        for (int c = lane; c < chunks; c += kWave) {
-            float f[kPer];
-            Row<T>::unpack(src[c], f);
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) { const uint32_t b = __float_as_uint(f[e]) & 0x7fffffffu; big = b > big ? b : big; }
-        }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) { const uint32_t o = __shfl_xor(big, off, kWave); big = o > big ? o : big; }
-        const RowScale s = row_scale(big);
+        if (row < 0 || row >= N) continue;               // (lanes of a row leave together)
+        const unsigned char* src = X + row * row_bytes;
         int8_t* dst = Q + row * pitch;
-        for (int c = lane; c * kPer < pitch; c += kWave) {
-            float f[kPer];
+        uint32_t big = 0;
+        Eight<T> v[C > 0 ? C : 1];
+        if constexpr (C > 0) {
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) f[e] = 0.0f;
-            if (c < chunks) Row<T>::unpack(src[c], f);
+            for (int c = 0; c < C; ++c) {
+                v[c].zero();
+                const int e = ((c << lg) + sub) * 8;
+                if (e < d) v[c].load(src, e, d);
+            }
 #pragma unroll
-            for (int e = 0; e < kPer; ++e) dst[c * kPer + e] = s.inv == 0.0f ? 0 : static_cast<int8_t>(to_integer(f[e] * s.up, s.m, s.inv));
+            for (int c = 0; c < C; ++c) { const uint32_t b = v[c].largest(); big = b > big ? b : big; }
+        } else {
+            for (int e = sub * 8; e < d; e += 8 << lg) {
+                v[0].zero();
+                v[0].load(src, e, d);
+                const uint32_t b = v[0].largest();
+                big = b > big ? b : big;
+            }
         }
-        if (lane == 0) scale[row] = s.scale;
+        for (int off = per >> 1; off > 0; off >>= 1) { const uint32_t o = __shfl_xor(big, off, kWave); big = o > big ? o : big; }
+        const RowScale s = row_scale(big);
+        auto put = [&](const Eight<T>& x, int e) __attribute__((always_inline)) {
+            float f[8];
+            x.values(f);
+            const uint2 o = to_integers(f, s);
+            *reinterpret_cast<uint2*>(dst + e) = s.inv == 0.0f ? make_uint2(0, 0) : o;
+        };
+        if constexpr (C > 0) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int e = ((c << lg) + sub) * 8;
+                if (e < pitch) put(v[c], e);
+            }
+        } else {
+            for (int e = sub * 8; e < pitch; e += 8 << lg) {
+                v[0].zero();
+                if (e < d) v[0].load(src, e, d);
+                put(v[0], e);
+            }
+        }
+        if (sub == 0) scale[row] = s.scale;
+    }
+}
+
+template <typename T>
+static void launch_quantize_kernel(const unsigned char* X, int64_t N, int d, const int32_t* ids, int64_t m, const int32_t* count,
+                                   int8_t* Q, int pitch, float* scale, hipStream_t st) {
+    const int64_t rows = ids != nullptr ? m : N;
+    // lanes per row and groups of 8 per lane: as few lanes as hold the row, unless that leaves more of them idle
+    const int groups = (pitch + 7) / 8;
+    int lg = 6, C = 0, best = 1 << 30;
+    for (int c : {1, 2, 3, 4, 6, 8}) {
+        int g = 2;
+        while (g < 6 && (c << g) < groups) ++g;
+        if ((c << g) >= groups && (c << g) < best) { best = c << g; lg = g; C = c; }
+    }
+    const int64_t want = (rows + (4 << (6 - lg)) - 1) / (4 << (6 - lg));
+    const unsigned grid = static_cast<unsigned>(want < 32768 ? want : 32768);
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(X, N, d, ids, m, count, Q, pitch, scale, lg); };
+    switch (C) {
+        case 1: go(quantize_kernel<T, 1>); break;
+        case 2: go(quantize_kernel<T, 2>); break;
+        case 3: go(quantize_kernel<T, 3>); break;
+        case 4: go(quantize_kernel<T, 4>); break;
+        case 6: go(quantize_kernel<T, 6>); break;
+        case 8: go(quantize_kernel<T, 8>); break;
+        default: go(quantize_kernel<T, 0>); break;
     }
 }
 
 static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const int32_t* ids, int64_t m, const int32_t* count,
                            int8_t* Q, int pitch, float* scale, hipStream_t st) {
-    const int64_t rows = ids != nullptr ? m : N;
-    if (rows == 0) return XC_OK;
-    const int64_t want = (rows + 3) / 4;
-    const unsigned grid = static_cast<unsigned>(want < 16384 ? want : 16384);
+    if (ids != nullptr && m == 0) return XC_OK;
     const unsigned char* x = static_cast<const unsigned char*>(X);
-    if (t == XC_F32)
-        XC_LAUNCH(K_QUANTIZE, st, (quantize_kernel<float><<<grid, 256, 0, st>>>(x, N, d, ids, m, count, Q, pitch, scale)));
-    else
-        XC_LAUNCH(K_QUANTIZE, st, (quantize_kernel<bf16_t><<<grid, 256, 0, st>>>(x, N, d, ids, m, count, Q, pitch, scale)));
+    if (t == XC_F32) XC_LAUNCH(K_QUANTIZE, st, launch_quantize_kernel<float>(x, N, d, ids, m, count, Q, pitch, scale, st));
+    else XC_LAUNCH(K_QUANTIZE, st, launch_quantize_kernel<bf16_t>(x, N, d, ids, m, count, Q, pitch, scale, st));
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }
