@@ -4,9 +4,12 @@
 
 namespace xc {
 
-constexpr int kVerifyThreads = 256;
 constexpr int kPiece = 512;              // elements of a wave's step: 8 neighbouring ones per lane
-constexpr int kChunk = 4096;             // elements of a partial sum, whatever the launch
+constexpr int kPieces = 4;               // of a chunk, whose loads are under way together
+constexpr int kChunk = kPieces * kPiece; // elements of a partial sum, formed by one wave whatever the launch
+constexpr int kVerifyThreads = 256, kDrawWaves = kVerifyThreads / kWave;
+constexpr int kOneChunks = 8;            // of a sequence that one workgroup does alone
+constexpr int64_t kSumGrid = 2048;       // workgroups that fill the device
 
 struct VerifyArgs {
     const int32_t* drafts;
@@ -15,6 +18,7 @@ struct VerifyArgs {
     const float* u;
     int32_t* tokens;
     int32_t* accepted;
+    int4* verdicts;                      // [B]
     double* sums;                        // [B][n_chunks]
     int64_t V;
     int n, n_chunks;
@@ -51,140 +55,344 @@ __device__ __forceinline__ Verdict judge(const VerifyArgs& v, int64_t b) {
     return Verdict{v.n, false, -1};
 }
 
-// The weights of elements e .. e + 7 of a row.
-template <typename T>
-__device__ __forceinline__ void weights8(const T* p, const T* q, Weights kind, int32_t without, int64_t e, int64_t V, double (&w)[8]) {
+// Elements e .. e + 7 of a row (zeros behind its end), whose address may be any.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    uint4 v[2];
+    __device__ __forceinline__ void load(const float* p, int64_t e, int64_t V) {
+        if (e + 8 <= V) {
+            __builtin_memcpy(v, p + e, 32);
+        } else {
+            v[0] = v[1] = make_uint4(0, 0, 0, 0);
+            if (e < V) {
+                float f[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        w[i] = 0.0;
-        if (e + i < V) {
-            double x = prob(p + e + i);
-            if (kind == kDifference) x -= static_cast<double>(prob(q + e + i));
-            if (kind == kWithout && e + i == without) x = 0.0;
-            w[i] = x > 0.0 && x < static_cast<double>(INFINITY) ? x : 0.0;
+                for (int i = 0; i < 8; ++i) f[i] = e + i < V ? p[e + i] : 0.0f;
+                __builtin_memcpy(v, f, 32);
+            }
         }
     }
-}
-__device__ __forceinline__ double wave_sum(double s) {
+    __device__ __forceinline__ void values(float (&f)[8]) const { __builtin_memcpy(f, v, 32); }
+};
+template <> struct Eight<bf16_t> {
+    uint4 v;
+    __device__ __forceinline__ void load(const bf16_t* p, int64_t e, int64_t V) {
+        if (e + 8 <= V) {
+            __builtin_memcpy(&v, p + e, 16);
+        } else {
+            v = make_uint4(0, 0, 0, 0);
+            if (e < V) {
+                uint32_t h[8];
 #pragma unroll
-    for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, kWave);
-    return s;
+                for (int i = 0; i < 8; ++i) h[i] = e + i < V ? p[e + i].bits : 0u;
+                v = make_uint4(h[0] | (h[1] << 16), h[2] | (h[3] << 16), h[4] | (h[5] << 16), h[6] | (h[7] << 16));
+            }
+        }
+    }
+    __device__ __forceinline__ void values(float (&f)[8]) const { unpack8(v, f); }
+};
+
+// ---- sums over a wave's lanes, in lane order (the neighbours' values come by DPP, not through LDS)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double from_lanes(double s) {     // 0 where there is no such lane
+    const uint64_t u = static_cast<uint64_t>(__double_as_longlong(s));
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, ROWS, 0xf, false);
+    return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo));
 }
 __device__ __forceinline__ double wave_incl_scan(double s) {
-    const int lane = lane_id();
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const double t = __shfl_up(s, off, kWave);
-        if (lane >= off) s += t;
-    }
+    s += from_lanes<0x111, 0xf>(s);          // row_shr 1, 2, 4, 8
+    s += from_lanes<0x112, 0xf>(s);
+    s += from_lanes<0x114, 0xf>(s);
+    s += from_lanes<0x118, 0xf>(s);
+    s += from_lanes<0x142, 0xa>(s);          // row_bcast 15 into rows 1 and 3
+    s += from_lanes<0x143, 0xc>(s);          // row_bcast 31 into rows 2 and 3
     return s;
 }
+__device__ __forceinline__ double of_lane(double s, int lane /* uniform */) {
+    const uint64_t u = static_cast<uint64_t>(__double_as_longlong(s));
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(u), lane), hi = __builtin_amdgcn_readlane(static_cast<int>(u >> 32), lane);
+    return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo));
+}
+__device__ __forceinline__ int first_lane(uint64_t m) { return __ffsll(static_cast<long long>(m)) - 1; }
+__device__ __forceinline__ int last_lane(uint64_t m) { return 63 - __clzll(static_cast<long long>(m)); }
 
-// Sum of chunk c, the same in all lanes: 8 pieces per lane, then the lanes.
+// ---- a row's weights
 template <typename T>
-__device__ __forceinline__ double chunk_sum(const T* p, const T* q, Weights kind, int32_t without, int c, int64_t V) {
-    double s = 0.0;
-    for (int k = 0; k < kChunk; k += kPiece) {
-        double w[8];
-        weights8(p, q, kind, without, static_cast<int64_t>(c) * kChunk + k + lane_id() * 8, V, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) s += w[i];
+struct Row {
+    const T *p, *q;
+    Weights kind;
+    int32_t without;
+    int64_t V;
+    // the lane's elements of piece k of chunk c: 8 from here on
+    static __device__ __forceinline__ int64_t first(int c, int k) { return static_cast<int64_t>(c) * kChunk + k * kPiece + lane_id() * 8; }
+    __device__ __forceinline__ void load(int c, int k, Eight<T>& x, Eight<T>& y) const {
+        x.load(p, first(c, k), V);
+        if (kind == kDifference) y.load(q, first(c, k), V);          // uniform
     }
-    return wave_sum(s);
+    __device__ __forceinline__ void values(int c, int k, const Eight<T>& x, const Eight<T>& y, float (&f)[8], float (&g)[8]) const {
+        x.values(f);
+        if (kind == kDifference) {
+            y.values(g);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                g[i] = 0.0f;
+                if (kind == kWithout && first(c, k) + i == without) f[i] = 0.0f;
+            }
+        }
+    }
+    static __device__ __forceinline__ double weight(float x, float y) {
+        const double w = static_cast<double>(x) - static_cast<double>(y);
+        return w > 0.0 && w < static_cast<double>(INFINITY) ? w : 0.0;
+    }
+};
+
+// Sum of a lane's 8 elements: pairs, then pairs of these.
+__device__ __forceinline__ double sum8(const double (&w)[8]) {
+    return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
 }
 
-// First element of chunk c at which the running sum, `before` ahead of the chunk, passes t; else the last one with a weight.
+// Sum of chunk c, the same in all lanes.
 template <typename T>
-__device__ __forceinline__ int32_t find_in_chunk(const T* p, const T* q, Weights kind, int32_t without, int c, int64_t V, double before, double t) {
-    int32_t last = -1;
-    for (int k = 0; k < kChunk; k += kPiece) {
-        const int64_t e = static_cast<int64_t>(c) * kChunk + k + lane_id() * 8;
-        double w[8], s = 0.0;
-        weights8(p, q, kind, without, e, V, w);
+__device__ __forceinline__ double chunk_sum(const Row<T>& r, int c) {
+    Eight<T> x[kPieces], y[kPieces];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s += w[i];
-        const double incl = wave_incl_scan(s);
+    for (int k = 0; k < kPieces; ++k) r.load(c, k, x[k], y[k]);
+    double s = 0.0;
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+        float f[8], g[8];
+        double w[8];
+        r.values(c, k, x[k], y[k], f, g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = fmax(static_cast<double>(f[i]) - static_cast<double>(g[i]), 0.0);         // (no number: 0)
+        s += sum8(w);
+    }
+    if (__builtin_expect(!(s < static_cast<double>(INFINITY)), 0)) {                   // an infinity among them counts as 0
+        s = 0.0;
+#pragma unroll 1
+        for (int k = 0; k < kPieces; ++k) {
+            float f[8], g[8];
+            double w[8];
+            r.load(c, k, x[0], y[0]);
+            r.values(c, k, x[0], y[0], f, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = Row<T>::weight(f[i], g[i]);
+            s += sum8(w);
+        }
+    }
+    return of_lane(wave_incl_scan(s), kWave - 1);
+}
+
+// ---- the label drawn, by a workgroup of 4 waves from the chunks' sums: -1 if all weights are zero.
+struct DrawShared { double group[kDrawWaves]; uint64_t pass[kDrawWaves], some[kDrawWaves]; double before[kDrawWaves]; int32_t label; };
+
+template <typename T>
+__device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sums, int n_chunks, float u, DrawShared& sh) {
+    const int lane = lane_id(), wave = threadIdx.x >> 6;
+    constexpr int kRound = kDrawWaves * kWave;
+    // the chunk: 256 at a time, 64 to a wave
+    double total = 0.0, incl = 0.0, s = 0.0;
+    for (int c0 = 0; c0 < n_chunks; c0 += kRound) {
+        const int c = c0 + static_cast<int>(threadIdx.x);
+        s = c < n_chunks ? sums[c] : 0.0;
+        incl = wave_incl_scan(s);
+        if (lane == kWave - 1) sh.group[wave] = incl;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kDrawWaves; ++w) total += sh.group[w];
+        __syncthreads();
+    }
+    if (!(total > 0.0)) return -1;                           // uniform
+    const double t = static_cast<double>(u) * total;
+    double before = 0.0, chunk_before = 0.0;
+    int chunk = 0;
+    for (int c0 = 0; c0 < n_chunks; c0 += kRound) {
+        if (n_chunks > kRound) {                             // (else these are the ones at hand)
+            const int c = c0 + static_cast<int>(threadIdx.x);
+            s = c < n_chunks ? sums[c] : 0.0;
+            incl = wave_incl_scan(s);
+            if (lane == kWave - 1) sh.group[wave] = incl;
+            __syncthreads();
+        }
+        double mine = before;
+        for (int w = 0; w < wave; ++w) mine += sh.group[w];
+        const uint64_t some = __ballot(s > 0.0), pass = __ballot(s > 0.0 && mine + incl > t);
+        const uint64_t take = pass != 0ull ? pass & (~pass + 1ull) : some;
+        if (take != 0ull && lane == last_lane(take)) sh.before[wave] = mine + (incl - s);
+        if (lane == 0) { sh.pass[wave] = pass; sh.some[wave] = some; }
+        __syncthreads();
+        int hit = -1, last = -1;                             // (no chunk passes: the last with a weight)
+#pragma unroll
+        for (int w = 0; w < kDrawWaves; ++w) {
+            if (hit < 0 && sh.pass[w] != 0ull) hit = w;
+            if (sh.some[w] != 0ull) last = w;
+        }
+        const int w = hit >= 0 ? hit : last;
+        if (w >= 0) {
+            chunk = c0 + w * kWave + (hit >= 0 ? first_lane(sh.pass[w]) : last_lane(sh.some[w]));
+            chunk_before = sh.before[w];
+        }
+#pragma unroll
+        for (int v = 0; v < kDrawWaves; ++v) before += sh.group[v];
+        __syncthreads();
+        if (hit >= 0) break;                                 // uniform
+    }
+    // the label: a piece of the chunk to a wave.  The first lane whose own sum passes t decides; its elements' running sum may
+    // stay below by a rounding: its last one then.  So may all lanes' sums: the last element with a weight.
+    static_assert(kPieces == kDrawWaves, "");
+    Eight<T> x, y;
+    float f[8], g[8];
+    double wt[8];
+    r.load(chunk, wave, x, y);
+    r.values(chunk, wave, x, y, f, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) wt[i] = Row<T>::weight(f[i], g[i]);
+    s = sum8(wt);
+    incl = wave_incl_scan(s);
+    if (lane == kWave - 1) sh.group[wave] = incl;
+    __syncthreads();
+    before = chunk_before;
+    for (int w = 0; w < wave; ++w) before += sh.group[w];
+    const uint64_t some = __ballot(s > 0.0), pass = __ballot(s > 0.0 && before + incl > t);
+    if (lane == 0) { sh.pass[wave] = pass; sh.some[wave] = some; }
+    __syncthreads();
+    int hit = -1, last = -1;
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; ++w) {
+        if (hit < 0 && sh.pass[w] != 0ull) hit = w;
+        if (sh.some[w] != 0ull) last = w;
+    }
+    if (wave == (hit >= 0 ? hit : last) && lane == (hit >= 0 ? first_lane(pass) : last_lane(some))) {
         double run = before + (incl - s);
         int32_t here = -1, mine = -1;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            run += w[i];
-            if (w[i] > 0.0) {
-                mine = static_cast<int32_t>(e + i);
+            run += wt[i];
+            if (wt[i] > 0.0) {
+                mine = static_cast<int32_t>(Row<T>::first(chunk, wave) + i);
                 if (here < 0 && run > t) here = mine;
             }
         }
-        // the first lane whose own sum passes t decides; its elements' running sum may stay below by a rounding: its last one then
-        const uint64_t pass = __ballot(s > 0.0 && before + incl > t);
-        if (pass != 0ull) return __shfl(here >= 0 ? here : mine, __ffsll(static_cast<long long>(pass)) - 1, kWave);
-        const uint64_t some = __ballot(mine >= 0);
-        if (some != 0ull) last = __shfl(mine, 63 - __clzll(static_cast<long long>(some)), kWave);
-        before += __shfl(incl, kWave - 1, kWave);
+        sh.label = hit >= 0 && here >= 0 ? here : mine;
     }
-    return last;
+    __syncthreads();
+    return sh.label;
 }
 
-// The label drawn, by one wave from the chunks' sums.  -1 if all weights are zero.
 template <typename T>
-__device__ __forceinline__ int32_t draw_label(const VerifyArgs& v, const double* sums, const T* p, const T* q, Weights kind, int32_t without, float u) {
-    const int lane = lane_id();
-    double total = 0.0;
-    for (int c0 = 0; c0 < v.n_chunks; c0 += kWave) {
-        const double s = c0 + lane < v.n_chunks ? sums[c0 + lane] : 0.0;
-        total += __shfl(wave_incl_scan(s), kWave - 1, kWave);
-    }
-    if (!(total > 0.0)) return -1;
-    const double t = static_cast<double>(u) * total;
-    double before = 0.0, last_before = 0.0;
-    int chunk = -1;
-    for (int c0 = 0; c0 < v.n_chunks; c0 += kWave) {
-        const double s = c0 + lane < v.n_chunks ? sums[c0 + lane] : 0.0;
-        const double incl = wave_incl_scan(s);
-        const uint64_t some = __ballot(s > 0.0), pass = __ballot(s > 0.0 && before + incl > t);
-        const uint64_t take = pass != 0ull ? pass & (~pass + 1ull) : some;
-        if (take != 0ull) {              // (no chunk passes: the last with a weight)
-            const int f = 63 - __clzll(static_cast<long long>(take));
-            chunk = c0 + f;
-            last_before = before + __shfl(incl - s, f, kWave);
-        }
-        if (pass != 0ull) break;
-        before += __shfl(incl, kWave - 1, kWave);
-    }
-    return find_in_chunk(p, q, kind, without, chunk, v.V, last_before, t);
+__device__ __forceinline__ Row<T> deciding_row(const VerifyArgs& v, int64_t b, const Verdict& j) {
+    Row<T> r;
+    r.p = static_cast<const T*>(v.target) + (b * (v.n + 1) + j.a) * v.V;
+    r.q = v.draft != nullptr && j.fell ? static_cast<const T*>(v.draft) + (b * v.n + j.a) * v.V : nullptr;
+    r.kind = !j.fell ? kTarget : v.draft != nullptr ? kDifference : kWithout;
+    r.without = j.x;
+    r.V = v.V;
+    return r;
+}
+__device__ __forceinline__ void write_tokens(const VerifyArgs& v, int64_t b, int a, int32_t drawn) {
+    for (int i = threadIdx.x; i <= v.n; i += kVerifyThreads)
+        v.tokens[b * (v.n + 1) + i] = i < a ? v.drafts[b * v.n + i] : i == a ? drawn : -1;
+    if (threadIdx.x == 0) v.accepted[b] = a;
 }
 
+// One workgroup does a sequence with few chunks.
 template <typename T>
 __global__ __launch_bounds__(kVerifyThreads)
-void verify_kernel(const VerifyArgs v) {
+void verify_one_kernel(const VerifyArgs v) {
     const int64_t b = blockIdx.x;
     const int wave = threadIdx.x >> 6;
-    __shared__ int32_t drawn;
+    __shared__ double sums[kOneChunks];
+    __shared__ DrawShared sh;
+    const float u = v.u[b * (v.n + 1) + v.n];
     const Verdict j = judge<T>(v, b);
-    const T* p = static_cast<const T*>(v.target) + (b * (v.n + 1) + j.a) * v.V;
-    const T* q = v.draft != nullptr ? static_cast<const T*>(v.draft) + (b * v.n + j.a) * v.V : nullptr;
-    double* sums = v.sums + b * v.n_chunks;
-    Weights kind = !j.fell ? kTarget : v.draft != nullptr ? kDifference : kWithout;
+    Row<T> r = deciding_row<T>(v, b, j);
+    int32_t drawn;
     for (;;) {
-        for (int c = wave; c < v.n_chunks; c += kVerifyThreads / kWave) {
-            const double s = chunk_sum(p, q, kind, j.x, c, v.V);
+        for (int c = wave; c < v.n_chunks; c += kDrawWaves) {
+            const double s = chunk_sum(r, c);
             if (lane_id() == 0) sums[c] = s;
         }
         __syncthreads();
-        if (wave == 0) {
-            const int32_t l = draw_label(v, sums, p, q, kind, j.x, v.u[b * (v.n + 1) + v.n]);
-            if (lane_id() == 0) drawn = l;
-        }
-        __syncthreads();
-        if (drawn >= 0 || kind == kTarget) break;
-        kind = kTarget;                  // nothing is left of the target above the draft: the target itself
+        drawn = draw_label(r, sums, v.n_chunks, u, sh);
+        if (drawn >= 0 || r.kind == kTarget) break;          // uniform
+        r.kind = kTarget;                // nothing is left of the target above the draft: the target itself
         __syncthreads();
     }
-    for (int i = threadIdx.x; i <= v.n; i += kVerifyThreads)
-        v.tokens[b * (v.n + 1) + i] = i < j.a ? v.drafts[b * v.n + i] : i == j.a ? drawn : -1;
-    if (threadIdx.x == 0) v.accepted[b] = j.a;
+    write_tokens(v, b, j.a, drawn);
+}
+
+// Longer rows: the partial sums by many workgroups, a chunk to a wave; then a workgroup per sequence.
+template <typename T>
+__global__ __launch_bounds__(kVerifyThreads)
+void verify_sums_kernel(const VerifyArgs v) {
+    const int64_t b = blockIdx.y;
+    const int c0 = blockIdx.x * kDrawWaves + (threadIdx.x >> 6), step = gridDim.x * kDrawWaves;
+    if (c0 >= v.n_chunks) return;
+    const Verdict j = judge<T>(v, b);
+    const Row<T> r = deciding_row<T>(v, b, j);
+    for (int c = c0; c < v.n_chunks; c += step) {
+        const double s = chunk_sum(r, c);
+        if (lane_id() == 0) v.sums[b * v.n_chunks + c] = s;
+    }
+    if (c0 == 0 && lane_id() == 0) v.verdicts[b] = make_int4(j.a, j.fell ? 1 : 0, j.x, 0);
+}
+template <typename T>
+__global__ __launch_bounds__(kVerifyThreads)
+void verify_draw_kernel(const VerifyArgs v) {
+    const int64_t b = blockIdx.x;
+    __shared__ DrawShared sh;
+    double* sums = v.sums + b * v.n_chunks;
+    const int4 w = v.verdicts[b];
+    const float u = v.u[b * (v.n + 1) + v.n];
+    const Verdict j{w.x, w.y != 0, w.z};
+    Row<T> r = deciding_row<T>(v, b, j);
+    int32_t drawn = draw_label(r, sums, v.n_chunks, u, sh);
+    if (drawn < 0 && r.kind != kTarget) {                    // as above; so rare that one workgroup adds the row up
+        r.kind = kTarget;
+        __syncthreads();
+        for (int c = threadIdx.x >> 6; c < v.n_chunks; c += kDrawWaves) {
+            const double s = chunk_sum(r, c);
+            if (lane_id() == 0) sums[c] = s;
+        }
+        __syncthreads();
+        drawn = draw_label(r, sums, v.n_chunks, u, sh);
+    }
+    write_tokens(v, b, j.a, drawn);
+}
+
+template <typename T>
+static void launch_verify(const VerifyArgs& v, int64_t B, hipStream_t st) {
+    // (1 x 16384: 6.4 us in one launch, 6.9 in two; 1 x 24000: 8.8 and 8.1; 256 x 16384 fp32: 7.8 and 10.2)
+    if (v.n_chunks <= kOneChunks) {
+        verify_one_kernel<T><<<static_cast<unsigned>(B), kVerifyThreads, 0, st>>>(v);
+        return;
+    }
+    for (int64_t b0 = 0; b0 < B; b0 += 65535) {              // (sequences of a launch)
+        VerifyArgs p = v;
+        const int64_t nb = B - b0 < 65535 ? B - b0 : 65535;
+        p.drafts = v.drafts + b0 * v.n;
+        p.target = static_cast<const T*>(v.target) + b0 * (v.n + 1) * v.V;
+        if (v.draft != nullptr) p.draft = static_cast<const T*>(v.draft) + b0 * v.n * v.V;
+        p.u += b0 * (v.n + 1);
+        p.tokens += b0 * (v.n + 1);
+        p.accepted += b0;
+        p.verdicts += b0;
+        p.sums += b0 * v.n_chunks;
+        // as many chunks to a wave as leave the device full
+        const int64_t wide = (v.n_chunks + kDrawWaves - 1) / kDrawWaves, most = kSumGrid / nb > 0 ? kSumGrid / nb : 1;
+        const int64_t rounds = (wide + most - 1) / most, gx = (wide + rounds - 1) / rounds;
+        verify_sums_kernel<T><<<dim3(static_cast<unsigned>(gx), static_cast<unsigned>(nb)), kVerifyThreads, 0, st>>>(p);
+        verify_draw_kernel<T><<<static_cast<unsigned>(nb), kVerifyThreads, 0, st>>>(p);
+    }
 }
 
 static int verify_chunks(int64_t V) { return static_cast<int>((V + kChunk - 1) / kChunk); }
+
+static size_t verify_bytes(int64_t B, int64_t V) {
+    return static_cast<size_t>(B) * (sizeof(int4) + static_cast<size_t>(verify_chunks(V)) * sizeof(double));
+}
 
 }  // namespace xc
 
@@ -192,7 +400,7 @@ extern "C" int xc_verify_workspace(int64_t B, int64_t V, size_t* bytes) {
     using namespace xc;
     if (!bytes) return XC_EINVAL;
     if (B < 1 || B > 0x7fffffffLL || V < 1 || V > 0x7fffffffLL) return XC_ESHAPE;
-    *bytes = static_cast<size_t>(B) * verify_chunks(V) * sizeof(double);
+    *bytes = verify_bytes(B, V);
     return XC_OK;
 }
 
@@ -206,13 +414,12 @@ extern "C" int xc_verify_drafts(const int32_t* drafts, int64_t B, int n, int64_t
     if (!aligned16(drafts) || !aligned16(target) || !aligned16(draft_probs) || !aligned16(u) || !aligned16(tokens) ||
         !aligned16(accepted) || !aligned16(ws))
         return XC_EINVAL;
-    VerifyArgs v{drafts, target, draft_probs, u, tokens, accepted, static_cast<double*>(ws), V, n, verify_chunks(V)};
-    if (ws_bytes < static_cast<size_t>(B) * v.n_chunks * sizeof(double)) return XC_EWORKSPACE;
+    if (ws_bytes < verify_bytes(B, V)) return XC_EWORKSPACE;
+    int4* verdicts = static_cast<int4*>(ws);
+    const VerifyArgs v{drafts, target, draft_probs, u, tokens, accepted, verdicts, reinterpret_cast<double*>(verdicts + B), V, n, verify_chunks(V)};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (t == XC_F32)
-        XC_LAUNCH(K_VERIFY, st, (verify_kernel<float><<<static_cast<unsigned>(B), kVerifyThreads, 0, st>>>(v)));
-    else
-        XC_LAUNCH(K_VERIFY, st, (verify_kernel<bf16_t><<<static_cast<unsigned>(B), kVerifyThreads, 0, st>>>(v)));
+    if (t == XC_F32) XC_LAUNCH(K_VERIFY, st, launch_verify<float>(v, B, st));
+    else XC_LAUNCH(K_VERIFY, st, launch_verify<bf16_t>(v, B, st));
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }
