@@ -214,20 +214,23 @@ static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const in
 // meet all banks.  Blocks of labels are interleaved, V at a time, so that a lane ends up with V neighbouring labels, 16
 // bytes of scores where there are as many: label V j + v of a group of 16 V is column j of its block v.
 // Accumulator i of a lane: query 4 (lane / 16) + i of its block, column lane % 16.
-template <int WQ_, int WL_, int MQ_, int ML_, int KB_, int R_, int G_>
+template <int WQ_, int WL_, int MQ_, int ML_, int KB_, int R_, int G_, int RES_ = 0>
 struct Tile {
     static constexpr int WQ = WQ_, WL = WL_, MQ = MQ_, ML = ML_, KB = KB_, R = R_, G = G_;
+    static constexpr int RES = RES_;     // bytes of a query's row in LDS for good, brought to integers by the workgroup itself (0: staged like the labels)
     static constexpr int kWaves = WQ * WL, kThreads = 64 * kWaves, BM = 16 * WQ * MQ, BN = 16 * WL * ML;
-    static constexpr int kStage = (BM + BN) * KB, kScaleLinesL = (BN + 63) / 64, kScaleLinesQ = (BM + 63) / 64, kScales = (kScaleLinesL + kScaleLinesQ) * 256, kLds = R * kStage + (R + 1) * kScales;
+    static constexpr int kStageRows = (RES > 0 ? 0 : BM) + BN, kStage = kStageRows * KB, kScaleLinesL = (BN + 63) / 64, kScaleLinesQ = RES > 0 ? 0 : (BM + 63) / 64, kScales = (kScaleLinesL + kScaleLinesQ) * 256, kLds = R * kStage + (R + 1) * kScales + (RES > 0 ? BM * RES + BM * 4 : 0);
     static constexpr int kPerCu = 160 * 1024 / kLds < 8 / kWaves ? 160 * 1024 / kLds : 8 / kWaves;      // workgroups of a compute unit
     static constexpr int kPerSimd = kPerCu * kWaves < 8 ? 1 : 2;
     static constexpr int kRowsPerLoad = 1024 / KB;       // rows that one load instruction of a wave brings in
-    static constexpr int kIssue = kWaves / G /* waves that bring in a stage */, kLoadsA = BM / kRowsPerLoad / kIssue, kLoadsB = BN / kRowsPerLoad / kIssue, kLoads = kLoadsA + kLoadsB;
-    static_assert(kLoadsA * kRowsPerLoad * kIssue == BM && kLoadsB * kRowsPerLoad * kIssue == BN, "loads divide evenly among the waves");
+    static constexpr int kIssue = kWaves / G /* waves that bring in a stage */, kLoadsA = RES > 0 ? 0 : BM / kRowsPerLoad / kIssue, kLoadsB = BN / kRowsPerLoad / kIssue, kLoads = kLoadsA + kLoadsB;
+    static_assert((RES > 0 || kLoadsA * kRowsPerLoad * kIssue == BM) && kLoadsB * kRowsPerLoad * kIssue == BN, "loads divide evenly among the waves");
     static __device__ __forceinline__ int swizzle(int row) { return (row / (256 / KB)) & (KB / 16 - 1); }
 };
 
 struct ScoresArgs {
+    const unsigned char* Z;              // queries as they came, rows of d elements (tiles that bring them to integers themselves)
+    int d;
     const int8_t* P;                     // queries in 8 bits, rows of ppitch bytes (zeros from column d on)
     const float* pscale;
     const int8_t* Q;
@@ -265,7 +268,7 @@ __device__ __forceinline__ const void* uniform_ptr(const void* p) {
         static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a)))));
 }
 
-template <typename TO, typename T>
+template <typename TO, typename T, typename TZ = float>
 __global__ __launch_bounds__(T::kThreads, T::kPerSimd)
 void scores_kernel(const ScoresArgs a) {
     __shared__ __align__(1024) unsigned char smem[T::kLds];
@@ -300,7 +303,7 @@ void scores_kernel(const ScoresArgs a) {
     constexpr int kScaleLinesL = T::kScaleLinesL, kScaleLinesQ = T::kScaleLinesQ;
     // label of the tile in row r of the tile's labels in LDS
     auto label_of = [&](int r) __attribute__((always_inline)) { const int blk = r >> 4; return (blk / V) * 16 * V + (r & 15) * V + blk % V; };
-    uint32_t off_a[T::kLoadsA], off_b[T::kLoadsB];
+    uint32_t off_a[T::kLoadsA > 0 ? T::kLoadsA : 1], off_b[T::kLoadsB];
 #pragma unroll
     for (int i = 0; i < T::kLoadsA; ++i) {
         const int r = (wi * T::kLoadsA + i) * 8 + (lane >> 3);
@@ -334,7 +337,7 @@ void scores_kernel(const ScoresArgs a) {
 #pragma unroll
             for (int i = 0; i < T::kLoadsA; ++i) lds_dma16_sbase<0>(from_a, off_a[i], dst + (wi * T::kLoadsA + i) * 1024);
             const int room = a.pitch - ld_kb * T::KB;        // bytes of the rows from here on
-            const uint32_t dst_b = dst + T::BM * T::KB + wi * T::kLoadsB * 1024;
+            const uint32_t dst_b = dst + (T::kStageRows - T::BN) * T::KB + wi * T::kLoadsB * 1024;
             const int8_t* from_b = a.Q + ld_l * a.pitch + ld_kb * T::KB;
             if (have >= T::BN && room >= T::KB) {
                 const void* from = uniform_ptr(from_b);
@@ -359,11 +362,14 @@ void scores_kernel(const ScoresArgs a) {
     constexpr int kSteps = T::KB / 64;
     i32x4 acc[T::MQ][T::ML], fa[2][T::MQ], fb[T::ML];
     const int frag = (lane & 15) * T::KB + ((quarter ^ T::swizzle(lane & 15)) * 16);
-    auto read_a = [&](int slot, int kk, int x) __attribute__((always_inline)) {
+    constexpr int kResAt = T::R * T::kStage + (T::R + 1) * T::kScales;     // resident queries: 128 bytes of every row, the next 128, ..; their scales
+    auto read_a = [&](int slot, int kb, int kk, int x) __attribute__((always_inline)) {
+        if constexpr (T::RES > 0)
+            return *reinterpret_cast<const i32x4*>(smem + kResAt + kb * (T::BM * T::KB) + (wq * T::MQ + x) * 16 * T::KB + (frag ^ (kk * 64)));
         return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (wq * T::MQ + x) * 16 * T::KB + (frag ^ (kk * 64)));
     };
     auto read_b = [&](int slot, int kk, int y) __attribute__((always_inline)) {
-        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (T::BM + (wl * T::ML + y) * 16) * T::KB + (frag ^ (kk * 64)));
+        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (T::kStageRows - T::BN + (wl * T::ML + y) * 16) * T::KB + (frag ^ (kk * 64)));
     };
     constexpr int kStores = 4 * T::MQ * (T::ML / V);         // of a whole tile
     int since_stores = T::R;                                 // stages published since a whole tile's scores were stored
@@ -380,10 +386,59 @@ void scores_kernel(const ScoresArgs a) {
         if (n_issued < total) issue();
     };
 
+    if constexpr (T::RES > 0) {
+        // The queries (one tile of them) to integers, before the wave's own loads of labels, which it would have to wait for as
+        // well.  Rows past the end are zeros.
+        constexpr int kGroups = (T::RES + 511) / 512, kRows = 4;                 // groups of 8 elements to a lane; rows under way at a time
+        float* qs = reinterpret_cast<float*>(smem + kResAt + T::BM * T::RES);
+        const int64_t row_bytes = static_cast<int64_t>(a.d) * (sizeof(TZ) == 4 ? 4 : 2);
+        for (int i = threadIdx.x; i < a.ppitch / 16 * T::BM; i += T::kThreads)
+            if ((i >> 3) % T::BM >= a.B) *reinterpret_cast<uint4*>(smem + kResAt + i * 16) = make_uint4(0, 0, 0, 0);
+        for (int r0 = wave; r0 < a.B; r0 += kRows * T::kWaves) {
+            Eight<TZ> v[kRows][kGroups];
+            uint32_t big[kRows];
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                for (int c = 0; c < kGroups; ++c) {
+                    const int r = r0 + i * T::kWaves, e = (c * kWave + lane) * 8;
+                    v[i][c].zero();
+                    if (r < a.B && e < a.d) v[i][c].load(a.Z + r * row_bytes, e, a.d);
+                }
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                big[i] = 0;
+#pragma unroll
+                for (int c = 0; c < kGroups; ++c) { const uint32_t b = v[i][c].largest(); big[i] = b > big[i] ? b : big[i]; }
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) { const uint32_t b = __shfl_xor(big[i], o, kWave); big[i] = b > big[i] ? b : big[i]; }
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) {
+                const int r = r0 + i * T::kWaves;
+                if (r >= a.B) break;                         // uniform
+                const RowScale s = row_scale(big[i]);
+#pragma unroll
+                for (int c = 0; c < kGroups; ++c) {
+                    const int e = (c * kWave + lane) * 8;
+                    if (e < a.ppitch) {
+                        float f[8];
+                        v[i][c].values(f);
+                        const uint2 o = to_integers(f, s);
+                        *reinterpret_cast<uint2*>(smem + kResAt + (e >> 7) * (T::BM * T::KB) + r * T::KB + ((((e & 127) >> 4) ^ T::swizzle(r)) * 16) + (e & 15)) =
+                            s.inv == 0.0f ? make_uint2(0, 0) : o;
+                    }
+                }
+                if (lane == 0) qs[r] = s.scale;
+            }
+        }
+    }
     for (int s = 0; s < T::R - 1 && s < total; ++s) issue();
     publish(0);
 #pragma unroll
-    for (int x = 0; x < T::MQ; ++x) fa[0][x] = read_a(0, 0, x);
+    for (int x = 0; x < T::MQ; ++x) fa[0][x] = read_a(0, 0, 0, x);
 #pragma unroll
     for (int y = 0; y < T::ML; ++y) fb[y] = read_b(0, 0, y);
     int g = 0, slot = 0, tile = 0;
@@ -402,7 +457,7 @@ void scores_kernel(const ScoresArgs a) {
 #pragma unroll
                 for (int y = 0; y < T::ML; ++y) {
 #pragma unroll
-                    for (int x = y * T::MQ / T::ML; x < (y + 1) * T::MQ / T::ML; ++x) fa[sel ^ 1][x] = read_a(from, kk_next, x);
+                    for (int x = y * T::MQ / T::ML; x < (y + 1) * T::MQ / T::ML; ++x) fa[sel ^ 1][x] = read_a(from, kk + 1 < kSteps ? kb : kb + 1 == n_stages ? 0 : kb + 1, kk_next, x);
 #pragma unroll
                     for (int x = 0; x < T::MQ; ++x) acc[x][y] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fa[sel][x], fb[y], acc[x][y], 0, 0, 0);
                     fb[y] = read_b(from, kk_next, y);
@@ -425,7 +480,8 @@ void scores_kernel(const ScoresArgs a) {
         auto rows = [&](auto whole) __attribute__((always_inline)) {
 #pragma unroll
             for (int x = 0; x < T::MQ; ++x) {
-                const float4 sq = *reinterpret_cast<const float4*>(scales + kScaleLinesL * 64 + qt + x * 16);
+                const float4 sq = *reinterpret_cast<const float4*>(
+                    (T::RES > 0 ? reinterpret_cast<const float*>(smem + kResAt + T::BM * T::RES) : scales + kScaleLinesL * 64) + qt + x * 16);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float s = i == 0 ? sq.x : i == 1 ? sq.y : i == 2 ? sq.z : sq.w;
@@ -461,10 +517,11 @@ typedef Tile<2, 2, 2, 2, 128, 4, 1> TileSmall;           // 64 x 64
 typedef Tile<1, 4, 4, 2, 128, 3, 1> TileSome;            // 64 x 128
 typedef Tile<1, 4, 2, 2, 128, 3, 1> TileFew;             // 32 x 128
 typedef Tile<1, 1, 2, 2, 128, 4, 1> TileNarrow;          // 32 x 32
+typedef Tile<1, 4, 1, 2, 128, 4, 1, 768> TileOnline;     // 16 x 128, queries of up to 768 bytes resident
 constexpr int kQueryPad = 128;                           // the queries in the workspace: rows of whole stages,
 constexpr int kQueryTile = 256;                           // whole tiles of them of any kind
 
-template <typename TO, typename T>
+template <typename TO, typename T, typename TZ = float>
 static void launch_scores(ScoresArgs a, hipStream_t st) {
     a.tiles_m = static_cast<int>((a.B + T::BM - 1) / T::BM);
     a.tiles_n = static_cast<int>((a.L + T::BN - 1) / T::BN);
@@ -472,7 +529,7 @@ static void launch_scores(ScoresArgs a, hipStream_t st) {
     const int64_t fit = (2 << 20) / (static_cast<int64_t>(T::BM) * a.ppitch);
     a.group = static_cast<int>(fit < 1 ? 1 : fit < a.tiles_m ? fit : a.tiles_m);
     const int64_t per = (static_cast<int64_t>(a.tiles_m) * a.tiles_n + 7) / 8, most = kCusPerXcd * T::kPerCu;
-    scores_kernel<TO, T><<<static_cast<unsigned>(8 * (per < most ? per : most)), T::kThreads, 0, st>>>(a);
+    scores_kernel<TO, T, TZ><<<static_cast<unsigned>(8 * (per < most ? per : most)), T::kThreads, 0, st>>>(a);
 }
 
 // ---- many queries, rows of up to 768 bytes: the labels stay where they are.  A wave holds 64 labels as operands in registers (NK
@@ -674,6 +731,15 @@ static void run_scores(const ScoresArgs& a, hipStream_t st) {
     }
 }
 
+// Up to 16 queries on rows of up to 768 bytes: one launch, every workgroup brings the queries to integers for itself (1 x 131072 x
+// 768: 18.3 us a call, 21.0 with a launch of their own; 1 x 4000 x 768: 8.0 and 10.8; 16 x 131072 x 768: 23.5 and 24.2; with
+// tiles of 32, 32 x 131072 x 768: 29.9 and 26.3, so not beyond 16).
+template <typename TZ>
+static void run_few(const ScoresArgs& a, xc_dtype out_t, hipStream_t st) {
+    if (out_t == XC_F32) launch_scores<float, TileOnline, TZ>(a, st);
+    else launch_scores<bf16_t, TileOnline, TZ>(a, st);
+}
+
 static size_t scores_bytes(int64_t B, int d) {
     return round_up(B, kQueryTile) * (4 + round_up(d, kQueryPad));
 }
@@ -713,11 +779,17 @@ extern "C" int xc_scores_quantized(const void* Z, int64_t B, int d, xc_dtype t, 
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* pscale = static_cast<float*>(ws);
     int8_t* P = static_cast<int8_t*>(ws) + round_up(B, kQueryTile) * 4;
-    const int rc = launch_quantize(Z, B, d, t, nullptr, 0, nullptr, P, static_cast<int>(round_up(d, kQueryPad)), pscale, st);
-    if (rc != XC_OK) return rc;
-    const ScoresArgs a{P, pscale, Q, scale, out, B, L, quantized_pitch(d), static_cast<int>(round_up(d, kQueryPad)), 0, 0, 0};
-    if (out_t == XC_F32) XC_LAUNCH(K_SCORES, st, run_scores<float>(a, st));
-    else XC_LAUNCH(K_SCORES, st, run_scores<bf16_t>(a, st));
+    const int ppitch = static_cast<int>(round_up(d, kQueryPad));
+    const ScoresArgs a{static_cast<const unsigned char*>(Z), d, P, pscale, Q, scale, out, B, L, quantized_pitch(d), ppitch, 0, 0, 0};
+    if (B <= TileOnline::BM && ppitch <= TileOnline::RES) {
+        if (t == XC_F32) XC_LAUNCH(K_SCORES, st, run_few<float>(a, out_t, st));
+        else XC_LAUNCH(K_SCORES, st, run_few<bf16_t>(a, out_t, st));
+    } else {
+        const int rc = launch_quantize(Z, B, d, t, nullptr, 0, nullptr, P, ppitch, pscale, st);
+        if (rc != XC_OK) return rc;
+        if (out_t == XC_F32) XC_LAUNCH(K_SCORES, st, run_scores<float>(a, st));
+        else XC_LAUNCH(K_SCORES, st, run_scores<bf16_t>(a, st));
+    }
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }
