@@ -302,7 +302,7 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i:
 def _launch(fn, where: str, dev: torch.device, *args) -> None:
     """Call an entry point on the current stream of the device that holds the tensors."""
     # (the stream's handle alone: making a Stream object of it takes a fifth of a small call's time)
-    stream = ctypes.c_void_p(_raw_stream(dev.index))
+    stream = _raw_stream(dev.index)
     if torch.cuda.current_device() == dev.index:
         status = fn(*args, stream)
     else:
@@ -312,14 +312,22 @@ def _launch(fn, where: str, dev: torch.device, *args) -> None:
 
 
 def _same_device(first: torch.Tensor, *others) -> torch.device:
+    dev = first.device
     for t in others:
-        if t is not None and t.device != first.device:
-            raise ValueError("all tensors of a call must be on one device, got %s and %s" % (first.device, t.device))
-    return first.device
+        if t is not None and t.device != dev:
+            raise ValueError("all tensors of a call must be on one device, got %s and %s" % (dev, t.device))
+    return dev
 
 
-def _shaped(t: torch.Tensor, shape, name: str) -> None:
-    if tuple(t.shape) != tuple(shape):
+def _at(t: torch.Tensor, dtype, name: str) -> int:
+    """Address of a tensor that a call may read or write (as `_dev`, without an object around it)."""
+    if t.is_cuda and t.dtype == dtype and t.is_contiguous():
+        return t.data_ptr()
+    return _dev(t, dtype, name).value or 0
+
+
+def _shaped(t: torch.Tensor, shape: tuple, name: str) -> None:
+    if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
 
 
@@ -355,9 +363,9 @@ def quantize_rows(X: torch.Tensor, *, rows: torch.Tensor | None = None, count: t
     if count is not None and count.numel() < 1:
         raise ValueError("count must hold a number")
     dev = _same_device(X, Q, scale, rows, count)
-    args = (_dev(X, name="X"), N, d, code, _dev(rows, torch.int32, "rows") if rows is not None else None,
-            rows.numel() if rows is not None else 0, _dev(count, torch.int32, "count") if count is not None else None,
-            _dev(Q, torch.int8, "Q"), _dev(scale, torch.float32, "scale"))
+    args = (_at(X, X.dtype, "X"), N, d, code, _at(rows, torch.int32, "rows") if rows is not None else None,
+            rows.numel() if rows is not None else 0, _at(count, torch.int32, "count") if count is not None else None,
+            _at(Q, torch.int8, "Q"), _at(scale, torch.float32, "scale"))
     if rows is None or rows.numel():                       # (no rows: an empty tensor has no address to pass)
         _launch(lib.xc_quantize_rows, "xc_quantize_rows", dev, *args)
     return out
@@ -389,9 +397,9 @@ def scores_quantized(Z: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor, *, d
     if out.dtype not in (torch.float32, torch.bfloat16):
         raise TypeError("out must be float32 or bfloat16, got %s" % out.dtype)
     dev = _same_device(Z, Q, scale, workspace, out)
-    _launch(lib.xc_scores_quantized, "xc_scores_quantized", dev, _dev(Z, name="Z"), B, d, code, _dev(Q, torch.int8, "Q"),
-            _dev(scale, torch.float32, "scale"), L, _dtype_code(out), _dev(out, name="out"),
-            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    _launch(lib.xc_scores_quantized, "xc_scores_quantized", dev, _at(Z, Z.dtype, "Z"), B, d, code, _at(Q, torch.int8, "Q"),
+            _at(scale, torch.float32, "scale"), L, _dtype_code(out), _at(out, out.dtype, "out"),
+            _at(workspace, torch.uint8, "workspace"), workspace.numel())
     return out
 
 
@@ -430,10 +438,10 @@ def verify_drafts(drafts: torch.Tensor, target: torch.Tensor, draft_probs: torch
     _shaped(tokens, (B, n + 1), "tokens")
     _shaped(accepted, (B,), "accepted")
     dev = _same_device(target, drafts, draft_probs, u, workspace, tokens, accepted)
-    _launch(lib.xc_verify_drafts, "xc_verify_drafts", dev, _dev(drafts, torch.int32, "drafts") if n else None, B, n, V,
-            _dev(target, name="target"), _dev(draft_probs, name="draft_probs") if draft_probs is not None and n else None, code,
-            _dev(u, torch.float32, "u"), _dev(tokens, torch.int32, "tokens"), _dev(accepted, torch.int32, "accepted"),
-            _dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    _launch(lib.xc_verify_drafts, "xc_verify_drafts", dev, _at(drafts, torch.int32, "drafts") if n else None, B, n, V,
+            _at(target, target.dtype, "target"), _at(draft_probs, target.dtype, "draft_probs") if draft_probs is not None and n else None, code,
+            _at(u, torch.float32, "u"), _at(tokens, torch.int32, "tokens"), _at(accepted, torch.int32, "accepted"),
+            _at(workspace, torch.uint8, "workspace"), workspace.numel())
     return out
 
 
@@ -450,8 +458,8 @@ def dropout(X: torch.Tensor, rate: float, seed: int, *, row0: int = 0, dtype: to
     _shaped(out, X.shape, "out")
     out_code = _dtype_code(out)
     dev = _same_device(X, out)
-    _launch(lib.xc_dropout, "xc_dropout", dev, _dev(X, name="X"), code, X.shape[0], X.shape[1], float(rate),
-            seed & ((1 << 64) - 1), row0, _dev(out, name="out"), out_code)
+    _launch(lib.xc_dropout, "xc_dropout", dev, _at(X, X.dtype, "X"), code, X.shape[0], X.shape[1], float(rate),
+            seed & ((1 << 64) - 1), row0, _at(out, out.dtype, "out"), out_code)
     return out
 
 
