@@ -265,7 +265,8 @@ int xc_quantize_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
  * rounded to out_t at the end.  Q and scale are what xc_quantize_rows gives for the
  * classifier (or for a contiguous range of its rows).  The workspace holds the
  * integers of Z; it is written before it is read.
- * Requires B >= 1, 1 <= L < 2^31, d as above.
+ * A score does not depend on how many queries or labels are scored with it, bit for bit.
+ * Requires B >= 1, 1 <= L < 2^31, B*L <= 2^40, d as above.
  * ------------------------------------------------------------------------- */
 int xc_scores_workspace(int64_t B, int d, size_t* bytes);
 int xc_scores_quantized(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,

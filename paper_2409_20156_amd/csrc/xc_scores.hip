@@ -106,8 +106,9 @@ __device__ __forceinline__ uint2 to_integers(float (&f)[8], const RowScale& s) {
     return o;
 }
 
-// 2^lg lanes per row, which they hold in registers: C groups of 8 elements each, read once.  C = 0: longer rows, one wave per
-// row, read twice.
+// 2^lg lanes per row, which they hold in registers: C groups of 8 elements each, read once.  C = 0: rows of more than 4096
+// elements, one wave per row, read twice.  Bound: memory, one read and half a write per bf16 element.  670000 x 768 bf16: 274 us,
+// 5.6 TB/s (a form that read rows twice, rounded by rint and stored bytes: 501).
 template <typename T, int C>
 __global__ __launch_bounds__(256)
 void quantize_kernel(const unsigned char* __restrict__ X, int64_t N, int d, const int32_t* __restrict__ ids, int64_t m,
@@ -208,25 +209,37 @@ static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const in
 // ---------------------------------------------------------------------------
 // scores
 // ---------------------------------------------------------------------------
-// Tiles of BM queries x BN labels, K staged KB bytes of each row at a time through a ring of R stages in LDS (direct
+// Tiles of BM queries x BN labels, K staged 128 bytes of each row at a time through a ring of R stages in LDS (direct
 // global -> LDS loads).  WQ x WL waves, each with MQ x ML blocks of v_mfma_i32_16x16x64_i8.
 // LDS rows are unpadded, their 16-byte chunks stored at chunk ^ swizzle(row) so that 16 lanes reading one chunk of 16 rows
 // meet all banks.  Blocks of labels are interleaved, V at a time, so that a lane ends up with V neighbouring labels, 16
 // bytes of scores where there are as many: label V j + v of a group of 16 V is column j of its block v.
 // Accumulator i of a lane: query 4 (lane / 16) + i of its block, column lane % 16.
-template <int WQ_, int WL_, int MQ_, int ML_, int KB_, int R_, int G_, int RES_ = 0>
+// A persistent workgroup takes its tiles one after the other with the loads running ahead into the next, so a tile's scores are
+// stored while the next one's operands arrive; the waits count loads and stores, which retire in the order of their issue.
+// Bound: few queries, the rows of Q from memory (1 x 131072 x 768: 17.6 us in the kernel, 5.7 TB/s; 64 x 670000 x 768, which
+// also stores 86 MB: 127 us, 4.7 TB/s); many, the matrix pipe at the chip's power limit and what brings both operands through
+// LDS (4096 x 100000 x 4096: 1.33 ms, 2.5 POP/s; the library's product of 8192^3 integers runs at 2.1).  Measured on 4096 x 131072 x
+// 768 to bf16 (us): tiles of 128 x 256, one a workgroup, 813; epilogue on packed conversions and scales held ready 670; 256 x 256
+// 602; persistent 570; stages brought in by half of the waves in turn, the others at their products already, 550; 16 x 16
+// products, whose lanes end up with 16 bytes of scores, 540.  Of that the stores took 140, the loads 100.
+template <int WQ_, int WL_, int MQ_, int ML_, int R_, int G_, int RES_ = 0>
 struct Tile {
-    static constexpr int WQ = WQ_, WL = WL_, MQ = MQ_, ML = ML_, KB = KB_, R = R_, G = G_;
+    static constexpr int WQ = WQ_, WL = WL_, MQ = MQ_, ML = ML_, R = R_;
+    static constexpr int G = G_;         // groups of waves that bring in the stages in turn
     static constexpr int RES = RES_;     // bytes of a query's row in LDS for good, brought to integers by the workgroup itself (0: staged like the labels)
     static constexpr int kWaves = WQ * WL, kThreads = 64 * kWaves, BM = 16 * WQ * MQ, BN = 16 * WL * ML;
-    static constexpr int kStageRows = (RES > 0 ? 0 : BM) + BN, kStage = kStageRows * KB, kScaleLinesL = (BN + 63) / 64, kScaleLinesQ = RES > 0 ? 0 : (BM + 63) / 64, kScales = (kScaleLinesL + kScaleLinesQ) * 256, kLds = R * kStage + (R + 1) * kScales + (RES > 0 ? BM * RES + BM * 4 : 0);
-    static constexpr int kPerCu = 160 * 1024 / kLds < 8 / kWaves ? 160 * 1024 / kLds : 8 / kWaves;      // workgroups of a compute unit
+    static constexpr int kStageRows = (RES > 0 ? 0 : BM) + BN, kStage = kStageRows * kStageBytes;
+    static constexpr int kScaleLinesL = (BN + 63) / 64, kScaleLinesQ = RES > 0 ? 0 : (BM + 63) / 64;        // of 64 scales
+    static constexpr int kScales = (kScaleLinesL + kScaleLinesQ) * 256;
+    static constexpr int kLds = R * kStage + (R + 1) * kScales + (RES > 0 ? BM * (RES + 4) : 0);
+    static constexpr int kPerCu = 160 * 1024 / kLds < 8 / kWaves ? 160 * 1024 / kLds : 8 / kWaves;           // workgroups of a compute unit
     static constexpr int kPerSimd = kPerCu * kWaves < 8 ? 1 : 2;
-    static constexpr int kRowsPerLoad = 1024 / KB;       // rows that one load instruction of a wave brings in
-    static constexpr int kIssue = kWaves / G /* waves that bring in a stage */, kLoadsA = RES > 0 ? 0 : BM / kRowsPerLoad / kIssue, kLoadsB = BN / kRowsPerLoad / kIssue, kLoads = kLoadsA + kLoadsB;
-    static_assert((RES > 0 || kLoadsA * kRowsPerLoad * kIssue == BM) && kLoadsB * kRowsPerLoad * kIssue == BN, "loads divide evenly among the waves");
-    static __device__ __forceinline__ int swizzle(int row) { return (row / (256 / KB)) & (KB / 16 - 1); }
+    // a wave's loads of a stage: 8 rows each
+    static constexpr int kIssue = kWaves / G, kLoadsA = RES > 0 ? 0 : BM / 8 / kIssue, kLoadsB = BN / 8 / kIssue, kLoads = kLoadsA + kLoadsB;
+    static_assert((RES > 0 || kLoadsA * 8 * kIssue == BM) && kLoadsB * 8 * kIssue == BN, "loads divide evenly among the waves");
 };
+__device__ __forceinline__ int row_swizzle(int row) { return (row >> 1) & 7; }
 
 struct ScoresArgs {
     const unsigned char* Z;              // queries as they came, rows of d elements (tiles that bring them to integers themselves)
@@ -241,7 +254,6 @@ struct ScoresArgs {
     int tiles_m, tiles_n, group;         // tiles of queries that are taken together, label tile by label tile
 };
 
-// N neighbouring scores; `left` of them exist
 // N neighbouring scores, all of them there
 template <int N> __device__ __forceinline__ void store_labels(float* p, const float (&v)[N]) { __builtin_memcpy(p, v, 4 * N); }
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -284,7 +296,7 @@ void scores_kernel(const ScoresArgs a) {
     const uint32_t t_begin = blockIdx.x % 8 * per, t_end = t_begin + per < n_tiles ? t_begin + per : n_tiles;
     const uint32_t t_first = t_begin + blockIdx.x / 8, t_step = gridDim.x / 8;
     if (t_first >= t_end) return;
-    const int n_stages = (a.pitch + T::KB - 1) / T::KB;
+    const int n_stages = (a.pitch + kStageBytes - 1) / kStageBytes;
     const int total = static_cast<int>((t_end - 1 - t_first) / t_step + 1) * n_stages;
     auto place = [&](uint32_t t, int64_t& q0, int64_t& l0) __attribute__((always_inline)) {
         const uint32_t in_groups = static_cast<uint32_t>(a.group) * static_cast<uint32_t>(a.tiles_n);
@@ -299,7 +311,6 @@ void scores_kernel(const ScoresArgs a) {
     // every tile and stage.  Queries are padded to whole tiles and stages; a tile of labels or a stage that reaches past the end
     // takes another way.  The first stage of a tile has the scales of its labels and queries with it, 64 to a load, for one of
     // R + 1 tiles: with rows of one stage the loads are R tiles ahead.
-    static_assert(T::KB == 128, "8 rows to a load");
     constexpr int kScaleLinesL = T::kScaleLinesL, kScaleLinesQ = T::kScaleLinesQ;
     // label of the tile in row r of the tile's labels in LDS
     auto label_of = [&](int r) __attribute__((always_inline)) { const int blk = r >> 4; return (blk / V) * 16 * V + (r & 15) * V + blk % V; };
@@ -307,12 +318,12 @@ void scores_kernel(const ScoresArgs a) {
 #pragma unroll
     for (int i = 0; i < T::kLoadsA; ++i) {
         const int r = (wi * T::kLoadsA + i) * 8 + (lane >> 3);
-        off_a[i] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ppitch) + ((lane & 7) ^ T::swizzle(r)) * 16;
+        off_a[i] = static_cast<uint32_t>(r) * static_cast<uint32_t>(a.ppitch) + ((lane & 7) ^ row_swizzle(r)) * 16;
     }
 #pragma unroll
     for (int i = 0; i < T::kLoadsB; ++i) {
         const int r = (wi * T::kLoadsB + i) * 8 + (lane >> 3);
-        off_b[i] = static_cast<uint32_t>(label_of(r)) * static_cast<uint32_t>(a.pitch) + ((lane & 7) ^ T::swizzle(r)) * 16;
+        off_b[i] = static_cast<uint32_t>(label_of(r)) * static_cast<uint32_t>(a.pitch) + ((lane & 7) ^ row_swizzle(r)) * 16;
     }
     uint32_t ld_t = t_first;
     int ld_kb = 0, ld_slot = 0, ld_tile = 0, n_issued = 0;
@@ -333,20 +344,20 @@ void scores_kernel(const ScoresArgs a) {
                 }
             }
             const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + ld_slot * T::kStage);
-            const void* from_a = uniform_ptr(a.P + ld_q * a.ppitch + ld_kb * T::KB);
+            const void* from_a = uniform_ptr(a.P + ld_q * a.ppitch + ld_kb * kStageBytes);
 #pragma unroll
             for (int i = 0; i < T::kLoadsA; ++i) lds_dma16_sbase<0>(from_a, off_a[i], dst + (wi * T::kLoadsA + i) * 1024);
-            const int room = a.pitch - ld_kb * T::KB;        // bytes of the rows from here on
-            const uint32_t dst_b = dst + (T::kStageRows - T::BN) * T::KB + wi * T::kLoadsB * 1024;
-            const int8_t* from_b = a.Q + ld_l * a.pitch + ld_kb * T::KB;
-            if (have >= T::BN && room >= T::KB) {
+            const int room = a.pitch - ld_kb * kStageBytes;        // bytes of the rows from here on
+            const uint32_t dst_b = dst + (T::kStageRows - T::BN) * kStageBytes + wi * T::kLoadsB * 1024;
+            const int8_t* from_b = a.Q + ld_l * a.pitch + ld_kb * kStageBytes;
+            if (have >= T::BN && room >= kStageBytes) {
                 const void* from = uniform_ptr(from_b);
 #pragma unroll
                 for (int i = 0; i < T::kLoadsB; ++i) lds_dma16_sbase<0>(from, off_b[i], dst_b + i * 1024);
             } else {                                         // rows past the end: the last one again; chunks behind a row: its first here (the query's are zero)
 #pragma unroll 1
                 for (int i = 0; i < T::kLoadsB; ++i) {
-                    const int r = (wi * T::kLoadsB + i) * 8 + (lane >> 3), lab = label_of(r), at = ((lane & 7) ^ T::swizzle(r)) * 16;
+                    const int r = (wi * T::kLoadsB + i) * 8 + (lane >> 3), lab = label_of(r), at = ((lane & 7) ^ row_swizzle(r)) * 16;
                     lds_dma16(from_b + (lab < have ? lab : have - 1) * a.pitch + (at < room ? at : 0), __builtin_amdgcn_readfirstlane(dst_b + i * 1024));
                 }
             }
@@ -359,17 +370,17 @@ void scores_kernel(const ScoresArgs a) {
 
     // ---- products.  The operands of a k-step are read while the one before is multiplied: a block of labels right behind its
     // own products, blocks of queries into the other half of their registers.
-    constexpr int kSteps = T::KB / 64;
+    constexpr int kSteps = kStageBytes / 64;
     i32x4 acc[T::MQ][T::ML], fa[2][T::MQ], fb[T::ML];
-    const int frag = (lane & 15) * T::KB + ((quarter ^ T::swizzle(lane & 15)) * 16);
+    const int frag = (lane & 15) * kStageBytes + ((quarter ^ row_swizzle(lane & 15)) * 16);
     constexpr int kResAt = T::R * T::kStage + (T::R + 1) * T::kScales;     // resident queries: 128 bytes of every row, the next 128, ..; their scales
     auto read_a = [&](int slot, int kb, int kk, int x) __attribute__((always_inline)) {
         if constexpr (T::RES > 0)
-            return *reinterpret_cast<const i32x4*>(smem + kResAt + kb * (T::BM * T::KB) + (wq * T::MQ + x) * 16 * T::KB + (frag ^ (kk * 64)));
-        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (wq * T::MQ + x) * 16 * T::KB + (frag ^ (kk * 64)));
+            return *reinterpret_cast<const i32x4*>(smem + kResAt + kb * (T::BM * kStageBytes) + (wq * T::MQ + x) * 16 * kStageBytes + (frag ^ (kk * 64)));
+        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (wq * T::MQ + x) * 16 * kStageBytes + (frag ^ (kk * 64)));
     };
     auto read_b = [&](int slot, int kk, int y) __attribute__((always_inline)) {
-        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (T::kStageRows - T::BN + (wl * T::ML + y) * 16) * T::KB + (frag ^ (kk * 64)));
+        return *reinterpret_cast<const i32x4*>(smem + slot * T::kStage + (T::kStageRows - T::BN + (wl * T::ML + y) * 16) * kStageBytes + (frag ^ (kk * 64)));
     };
     constexpr int kStores = 4 * T::MQ * (T::ML / V);         // of a whole tile
     int since_stores = T::R;                                 // stages published since a whole tile's scores were stored
@@ -427,7 +438,7 @@ void scores_kernel(const ScoresArgs a) {
                         float f[8];
                         v[i][c].values(f);
                         const uint2 o = to_integers(f, s);
-                        *reinterpret_cast<uint2*>(smem + kResAt + (e >> 7) * (T::BM * T::KB) + r * T::KB + ((((e & 127) >> 4) ^ T::swizzle(r)) * 16) + (e & 15)) =
+                        *reinterpret_cast<uint2*>(smem + kResAt + (e >> 7) * (T::BM * kStageBytes) + r * kStageBytes + ((((e & 127) >> 4) ^ row_swizzle(r)) * 16) + (e & 15)) =
                             s.inv == 0.0f ? make_uint2(0, 0) : o;
                     }
                 }
@@ -511,15 +522,15 @@ void scores_kernel(const ScoresArgs a) {
     }
 }
 
-typedef Tile<4, 2, 4, 8, 128, 2, 2> TileMany;            // 256 x 256
-typedef Tile<2, 2, 4, 4, 128, 2, 1> TileMid;             // 128 x 128
-typedef Tile<2, 2, 2, 2, 128, 4, 1> TileSmall;           // 64 x 64
-typedef Tile<1, 4, 4, 2, 128, 3, 1> TileSome;            // 64 x 128
-typedef Tile<1, 4, 2, 2, 128, 3, 1> TileFew;             // 32 x 128
-typedef Tile<1, 1, 2, 2, 128, 4, 1> TileNarrow;          // 32 x 32
-typedef Tile<1, 4, 1, 2, 128, 4, 1, 768> TileOnline;     // 16 x 128, queries of up to 768 bytes resident
+typedef Tile<4, 2, 4, 8, 2, 2> TileMany;            // 256 x 256
+typedef Tile<2, 2, 4, 4, 2, 1> TileMid;             // 128 x 128
+typedef Tile<2, 2, 2, 2, 4, 1> TileSmall;           // 64 x 64
+typedef Tile<1, 4, 4, 2, 3, 1> TileSome;            // 64 x 128
+typedef Tile<1, 4, 2, 2, 3, 1> TileFew;             // 32 x 128
+typedef Tile<1, 1, 2, 2, 4, 1> TileNarrow;          // 32 x 32
+typedef Tile<1, 4, 1, 2, 4, 1, 768> TileOnline;     // 16 x 128, queries of up to 768 bytes resident
 constexpr int kQueryPad = 128;                           // the queries in the workspace: rows of whole stages,
-constexpr int kQueryTile = 256;                           // whole tiles of them of any kind
+constexpr int kQueryTile = 256;                          // whole tiles of them of any kind
 
 template <typename TO, typename T, typename TZ = float>
 static void launch_scores(ScoresArgs a, hipStream_t st) {
@@ -534,8 +545,12 @@ static void launch_scores(ScoresArgs a, hipStream_t st) {
 
 // ---- many queries, rows of up to 768 bytes: the labels stay where they are.  A wave holds 64 labels as operands in registers (NK
 // k-steps of 64 bytes) and 512 labels of a workgroup meet the queries that stream through LDS, QS at a time.  Per product that is
-// half the operand reads from LDS that a 256 x 256 tile takes, an eighth of the bytes brought into it, and a wave's scores are
+// two thirds of the operand reads from LDS that a 256 x 256 tile takes, a quarter of the bytes brought into it, and a wave's scores are
 // stored 16 queries at a time, while the other wave of its SIMD multiplies.
+// Bound: the matrix pipe at the chip's power limit and the stores beside it.  4096 x 131072 x 768 to bf16: 360 us under sustained load
+// (2.3 POP/s; 320 from a cool chip), without the stores 281, without the loads the same as with them.  Neither 16-byte stores (rows
+// exchanged between neighbouring lanes: 379 against 368 us a call) nor wave priorities changed it.  Rows of an odd number of
+// bf16 scores are stored at addresses that are no multiple of 8: 131071 labels take 474 us.
 template <int NK_>
 struct Held {
     static constexpr int NK = NK_, QS = NK % 4 == 0 ? 32 : 64, kStage = QS * NK * 64;       // (the stage's loads divide evenly among 8 waves)
@@ -565,7 +580,7 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
 #pragma unroll
     for (int i = 0; i < H::kLoads; ++i) {
         const int n = wave * H::kLoads + i, row = n % (H::QS / 8) * 8 + (lane >> 3);
-        off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(a.ppitch) + n / (H::QS / 8) * 128 + (((lane & 7) ^ ((row >> 1) & 7)) * 16);
+        off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(a.ppitch) + n / (H::QS / 8) * 128 + (((lane & 7) ^ row_swizzle(row)) * 16);
     }
     int ld_st = st, ld_slot = 0, n_issued = 0;
     auto issue = [&]() __attribute__((always_inline)) {
@@ -591,7 +606,7 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
 
     i32x4 w[NK][4], fa[3];
     float sl[4];
-    const int frag = (lane & 15) * 128 + ((quarter ^ (((lane & 15) >> 1) & 7)) * 16);
+    const int frag = (lane & 15) * 128 + ((quarter ^ row_swizzle(lane & 15)) * 16);
     auto read_a = [&](int slot, int qb, int k) __attribute__((always_inline)) {      // 16 queries, 64 bytes of each
         return *reinterpret_cast<const i32x4*>(smem + slot * H::kStage + (k >> 1) * (H::QS * 128) + qb * 2048 + (frag ^ ((k & 1) * 64)));
     };
@@ -639,7 +654,7 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
                 constexpr int kDepth = 2;
                 const int kn = k + kDepth < NK ? k + kDepth : k + kDepth - NK;
                 const bool over = k + kDepth >= NK;
-                const int n = qb * NK + k;                   // of the stage: NK * kBlocks is a multiple of 3 or fa is indexed by it
+                const int n = qb * NK + k;                   // of the stage: NK * kBlocks is a multiple of 3 or fa is put right behind it
                 fa[(n + kDepth) % 3] = !over ? read_a(slot, qb, kn) : qb + 1 < kBlocks ? read_a(slot, qb + 1, kn) : read_a(slot_next, 0, kn);
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
@@ -772,7 +787,7 @@ extern "C" int xc_scores_quantized(const void* Z, int64_t B, int d, xc_dtype t, 
                                    xc_dtype out_t, void* out, void* ws, size_t ws_bytes, void* stream) {
     using namespace xc;
     if ((t != XC_F32 && t != XC_BF16) || (out_t != XC_F32 && out_t != XC_BF16)) return XC_EDTYPE;
-    if (B < 1 || B > 0x7fffffffLL || L < 1 || L > 0x7fffffffLL || !row_ok(d, t)) return XC_ESHAPE;
+    if (B < 1 || B > 0x7fffffffLL || L < 1 || L > 0x7fffffffLL || B > (1LL << 40) / L || !row_ok(d, t)) return XC_ESHAPE;
     if (!Z || !Q || !scale || !out || !ws) return XC_EINVAL;
     if (!aligned16(Z) || !aligned16(Q) || !aligned16(scale) || !aligned16(out) || !aligned16(ws)) return XC_EINVAL;
     if (ws_bytes < scores_bytes(B, d)) return XC_EWORKSPACE;
