@@ -534,6 +534,7 @@ constexpr int kQueryTile = 256;                          // whole tiles of them 
 
 template <typename TO, typename T, typename TZ = float>
 static void launch_scores(ScoresArgs a, hipStream_t st) {
+    static_assert(kQueryTile % T::BM == 0, "the last tile of queries ends within the padded rows");
     a.tiles_m = static_cast<int>((a.B + T::BM - 1) / T::BM);
     a.tiles_n = static_cast<int>((a.L + T::BN - 1) / T::BN);
     // a group of query tiles takes half of an XCD's L2
