@@ -4,8 +4,8 @@
 // depends on V alone (a wave's lanes by 8 neighbouring elements, pieces of a chunk one after the other, then the lanes, then the
 // chunks), so a sequence's label depends neither on the others in the batch nor on the launch.
 // Bound: few sequences, dependent memory accesses (draft -> its two probabilities -> the row -> the chunk again) and launches:
-// 1 x 4 x 4096 fp32 5.0 us on the device, 8 x 5 x 131072 8.6 (two launches of about 4); a batch, the rows from memory: 256 x 4 x 131072
-// bf16 23.6 us for the sums (110 MB, 4.7 TB/s) + 5.3 for the draws.  First form, one workgroup per sequence: 27, 140 and 181 us.
+// 1 x 4 x 4096 fp32 5.0 us on the device, 8 x 5 x 131072 7.4 (two launches); a batch, the rows from memory: 256 x 4 x 131072 bf16 23 us
+// (110 MB, 4.8 TB/s).  First form, 8 elements of a chunk at a time and all of it by one workgroup of 4 waves: 27, 140 and 181 us.
 #include "xc_common.h"
 
 namespace xc {
@@ -14,7 +14,8 @@ constexpr int kPiece = 512;              // elements of a wave's step: 8 neighbo
 constexpr int kPieces = 4;               // of a chunk, whose loads are under way together
 constexpr int kChunk = kPieces * kPiece; // elements of a partial sum, formed by one wave whatever the launch
 constexpr int kVerifyThreads = 256, kDrawWaves = kVerifyThreads / kWave;
-constexpr int kOneChunks = 8;            // of a sequence that one workgroup does alone
+constexpr int kOneChunks = 1024;         // of a sequence that one workgroup does alone
+constexpr int64_t kManySequences = 192;  // that keep most compute units busy
 constexpr int64_t kSumGrid = 2048;       // workgroups that fill the device
 
 struct VerifyArgs {
@@ -191,14 +192,14 @@ __device__ __forceinline__ double chunk_sum(const Row<T>& r, int c) {
     return of_lane(wave_incl_scan(s), kWave - 1);
 }
 
-// ---- the label drawn, by a workgroup of 4 waves from the chunks' sums: -1 if all weights are zero.
-struct DrawShared { double group[kDrawWaves]; uint64_t pass[kDrawWaves], some[kDrawWaves]; double before[kDrawWaves]; int32_t label; };
+// ---- the label drawn, by a workgroup of W waves from the chunks' sums: -1 if all weights are zero.
+template <int W> struct DrawShared { double group[W]; uint64_t pass[W], some[W]; double before[W]; int32_t label; };
 
-template <typename T>
-__device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sums, int n_chunks, float u, DrawShared& sh) {
+template <typename T, int W>
+__device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sums, int n_chunks, float u, DrawShared<W>& sh) {
     const int lane = lane_id(), wave = threadIdx.x >> 6;
-    constexpr int kRound = kDrawWaves * kWave;
-    // the chunk: 256 at a time, 64 to a wave
+    constexpr int kRound = W * kWave;
+    // the chunk: 64 at a time to a wave
     double total = 0.0, incl = 0.0, s = 0.0;
     for (int c0 = 0; c0 < n_chunks; c0 += kRound) {
         const int c = c0 + static_cast<int>(threadIdx.x);
@@ -207,7 +208,7 @@ __device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sum
         if (lane == kWave - 1) sh.group[wave] = incl;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kDrawWaves; ++w) total += sh.group[w];
+        for (int w = 0; w < W; ++w) total += sh.group[w];
         __syncthreads();
     }
     if (!(total > 0.0)) return -1;                           // uniform
@@ -231,7 +232,7 @@ __device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sum
         __syncthreads();
         int hit = -1, last = -1;                             // (no chunk passes: the last with a weight)
 #pragma unroll
-        for (int w = 0; w < kDrawWaves; ++w) {
+        for (int w = 0; w < W; ++w) {
             if (hit < 0 && sh.pass[w] != 0ull) hit = w;
             if (sh.some[w] != 0ull) last = w;
         }
@@ -241,32 +242,35 @@ __device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sum
             chunk_before = sh.before[w];
         }
 #pragma unroll
-        for (int v = 0; v < kDrawWaves; ++v) before += sh.group[v];
+        for (int v = 0; v < W; ++v) before += sh.group[v];
         __syncthreads();
         if (hit >= 0) break;                                 // uniform
     }
-    // the label: a piece of the chunk to a wave.  The first lane whose own sum passes t decides; its elements' running sum may
-    // stay below by a rounding: its last one then.  So may all lanes' sums: the last element with a weight.
-    static_assert(kPieces == kDrawWaves, "");
-    Eight<T> x, y;
-    float f[8], g[8];
+    // the label: a piece of the chunk to each of the first waves.  The first lane whose own sum passes t decides; its elements'
+    // running sum may stay below by a rounding: its last one then.  So may all lanes' sums: the last element with a weight.
+    static_assert(kPieces <= W, "");
     double wt[8];
-    r.load(chunk, wave, x, y);
-    r.values(chunk, wave, x, y, f, g);
+    s = 0.0;
+    if (wave < kPieces) {
+        Eight<T> x, y;
+        float f[8], g[8];
+        r.load(chunk, wave, x, y);
+        r.values(chunk, wave, x, y, f, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) wt[i] = Row<T>::weight(f[i], g[i]);
-    s = sum8(wt);
+        for (int i = 0; i < 8; ++i) wt[i] = Row<T>::weight(f[i], g[i]);
+        s = sum8(wt);
+    }
     incl = wave_incl_scan(s);
     if (lane == kWave - 1) sh.group[wave] = incl;
     __syncthreads();
     before = chunk_before;
-    for (int w = 0; w < wave; ++w) before += sh.group[w];
+    for (int w = 0; w < wave && w < kPieces; ++w) before += sh.group[w];
     const uint64_t some = __ballot(s > 0.0), pass = __ballot(s > 0.0 && before + incl > t);
     if (lane == 0) { sh.pass[wave] = pass; sh.some[wave] = some; }
     __syncthreads();
     int hit = -1, last = -1;
 #pragma unroll
-    for (int w = 0; w < kDrawWaves; ++w) {
+    for (int w = 0; w < kPieces; ++w) {
         if (hit < 0 && sh.pass[w] != 0ull) hit = w;
         if (sh.some[w] != 0ull) last = w;
     }
@@ -298,30 +302,30 @@ __device__ __forceinline__ Row<T> deciding_row(const VerifyArgs& v, int64_t b, c
     return r;
 }
 __device__ __forceinline__ void write_tokens(const VerifyArgs& v, int64_t b, int a, int32_t drawn) {
-    for (int i = threadIdx.x; i <= v.n; i += kVerifyThreads)
+    for (int i = threadIdx.x; i <= v.n; i += static_cast<int>(blockDim.x))
         v.tokens[b * (v.n + 1) + i] = i < a ? v.drafts[b * v.n + i] : i == a ? drawn : -1;
     if (threadIdx.x == 0) v.accepted[b] = a;
 }
 
 // One workgroup does a sequence with few chunks.
-template <typename T>
-__global__ __launch_bounds__(kVerifyThreads)
+template <typename T, int W>
+__global__ __launch_bounds__(W * kWave)
 void verify_one_kernel(const VerifyArgs v) {
     const int64_t b = blockIdx.x;
     const int wave = threadIdx.x >> 6;
     __shared__ double sums[kOneChunks];
-    __shared__ DrawShared sh;
+    __shared__ DrawShared<W> sh;
     const float u = v.u[b * (v.n + 1) + v.n];
     const Verdict j = judge<T>(v, b);
     Row<T> r = deciding_row<T>(v, b, j);
     int32_t drawn;
     for (;;) {
-        for (int c = wave; c < v.n_chunks; c += kDrawWaves) {
+        for (int c = wave; c < v.n_chunks; c += W) {
             const double s = chunk_sum(r, c);
             if (lane_id() == 0) sums[c] = s;
         }
         __syncthreads();
-        drawn = draw_label(r, sums, v.n_chunks, u, sh);
+        drawn = draw_label<T, W>(r, sums, v.n_chunks, u, sh);
         if (drawn >= 0 || r.kind == kTarget) break;          // uniform
         r.kind = kTarget;                // nothing is left of the target above the draft: the target itself
         __syncthreads();
@@ -348,13 +352,13 @@ template <typename T>
 __global__ __launch_bounds__(kVerifyThreads)
 void verify_draw_kernel(const VerifyArgs v) {
     const int64_t b = blockIdx.x;
-    __shared__ DrawShared sh;
+    __shared__ DrawShared<kDrawWaves> sh;
     double* sums = v.sums + b * v.n_chunks;
     const int4 w = v.verdicts[b];
     const float u = v.u[b * (v.n + 1) + v.n];
     const Verdict j{w.x, w.y != 0, w.z};
     Row<T> r = deciding_row<T>(v, b, j);
-    int32_t drawn = draw_label(r, sums, v.n_chunks, u, sh);
+    int32_t drawn = draw_label<T, kDrawWaves>(r, sums, v.n_chunks, u, sh);
     if (drawn < 0 && r.kind != kTarget) {                    // as above; so rare that one workgroup adds the row up
         r.kind = kTarget;
         __syncthreads();
@@ -363,16 +367,23 @@ void verify_draw_kernel(const VerifyArgs v) {
             if (lane_id() == 0) sums[c] = s;
         }
         __syncthreads();
-        drawn = draw_label(r, sums, v.n_chunks, u, sh);
+        drawn = draw_label<T, kDrawWaves>(r, sums, v.n_chunks, u, sh);
     }
     write_tokens(v, b, j.a, drawn);
 }
 
 template <typename T>
 static void launch_verify(const VerifyArgs& v, int64_t B, hipStream_t st) {
-    // (1 x 16384: 6.4 us in one launch, 6.9 in two; 1 x 24000: 8.8 and 8.1; 256 x 16384 fp32: 7.8 and 10.2)
-    if (v.n_chunks <= kOneChunks) {
-        verify_one_kernel<T><<<static_cast<unsigned>(B), kVerifyThreads, 0, st>>>(v);
+    // A workgroup per sequence saves a launch; many workgroups per sequence bring a long row in faster, where the sequences alone
+    // leave compute units idle.  Device time, us, by 4 waves, by 8, by many: 1 x 8192 fp32 5.3, 5.9, 6.5; 1 x 32768 8.7, 7.8, 7.1 (a call of
+    // which the caller takes 8 with one launch and 10.5 with two); 1 x 65536 12.9, 10.9, 7.1; 64 x 131072 27.9, 19.6, 17.0; 256 x
+    // 131072 41.3, 39.7, 41.3, in bf16 29.9, 23.2, 26.2.
+    if (v.n_chunks <= 8) {
+        verify_one_kernel<T, 4><<<static_cast<unsigned>(B), 4 * kWave, 0, st>>>(v);
+        return;
+    }
+    if (v.n_chunks <= 16 || (B >= kManySequences && v.n_chunks <= kOneChunks)) {
+        verify_one_kernel<T, 8><<<static_cast<unsigned>(B), 8 * kWave, 0, st>>>(v);
         return;
     }
     for (int64_t b0 = 0; b0 < B; b0 += 65535) {              // (sequences of a launch)
