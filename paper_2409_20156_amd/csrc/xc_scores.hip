@@ -43,9 +43,9 @@ template <typename T> struct Eight;
 template <> struct Eight<float> {
     uint4 v[2];
     __device__ __forceinline__ void zero() { v[0] = v[1] = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void load(const unsigned char* row, int e, int d) {
-        v[0] = *reinterpret_cast<const uint4*>(row + e * 4);
-        if (e + 4 < d) v[1] = *reinterpret_cast<const uint4*>(row + e * 4 + 16);         // (d is a multiple of 4)
+    template <bool STREAM> __device__ __forceinline__ void load(const unsigned char* row, int e, int d) {
+        v[0] = load16<STREAM>(row + e * 4);
+        if (e + 4 < d) v[1] = load16<STREAM>(row + e * 4 + 16);                          // (d is a multiple of 4)
     }
     __device__ __forceinline__ uint32_t largest() const {
         uint32_t m = 0;
@@ -68,7 +68,7 @@ template <> struct Eight<float> {
 template <> struct Eight<bf16_t> {
     uint4 v;
     __device__ __forceinline__ void zero() { v = make_uint4(0, 0, 0, 0); }
-    __device__ __forceinline__ void load(const unsigned char* row, int e, int) { v = *reinterpret_cast<const uint4*>(row + e * 2); }
+    template <bool STREAM> __device__ __forceinline__ void load(const unsigned char* row, int e, int) { v = load16<STREAM>(row + e * 2); }
     __device__ __forceinline__ uint32_t largest() const {
         typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
         const uint32_t u[4] = {v.x & 0x7fff7fffu, v.y & 0x7fff7fffu, v.z & 0x7fff7fffu, v.w & 0x7fff7fffu};
@@ -107,12 +107,14 @@ __device__ __forceinline__ uint2 to_integers(float (&f)[8], const RowScale& s) {
 }
 
 // 2^lg lanes per row, which they hold in registers: C groups of 8 elements each, read once.  C = 0: rows of more than 4096
-// elements, one wave per row, read twice.  Bound: memory, one read and half a write per bf16 element.  670000 x 768 bf16: 274 us,
-// 5.6 TB/s (a form that read rows twice, rounded by rint and stored bytes: 501).
+// elements, one wave per row, read twice.  Bound: memory, one read and half a write per bf16 element.  670000 x 768 bf16: 254 us,
+// 6.1 TB/s; without the non-temporal hint, which rows beyond the last-level cache are loaded with, 276; a form that read rows twice,
+// rounded by rint and stored bytes 501.
+constexpr int64_t kCachedBytes = 256ll << 20;
 template <typename T, int C>
 __global__ __launch_bounds__(256)
 void quantize_kernel(const unsigned char* __restrict__ X, int64_t N, int d, const int32_t* __restrict__ ids, int64_t m,
-                     const int32_t* __restrict__ count, int8_t* __restrict__ Q, int pitch, float* __restrict__ scale, int lg) {
+                     const int32_t* __restrict__ count, int8_t* __restrict__ Q, int pitch, float* __restrict__ scale, int lg, bool stream) {
     const int lane = lane_id(), per = 1 << lg, sub = lane & (per - 1);
     const int64_t row_bytes = static_cast<int64_t>(d) * (sizeof(T) == 4 ? 4 : 2);
     int64_t rows = ids != nullptr ? m : N;
@@ -133,14 +135,17 @@ void quantize_kernel(const unsigned char* __restrict__ X, int64_t N, int d, cons
             for (int c = 0; c < C; ++c) {
                 v[c].zero();
                 const int e = ((c << lg) + sub) * 8;
-                if (e < d) v[c].load(src, e, d);
+                if (e < d) {
+                    if (stream) v[c].template load<true>(src, e, d);                   // uniform
+                    else v[c].template load<false>(src, e, d);
+                }
             }
 #pragma unroll
             for (int c = 0; c < C; ++c) { const uint32_t b = v[c].largest(); big = b > big ? b : big; }
         } else {
             for (int e = sub * 8; e < d; e += 8 << lg) {
                 v[0].zero();
-                v[0].load(src, e, d);
+                v[0].template load<false>(src, e, d);
                 const uint32_t b = v[0].largest();
                 big = b > big ? b : big;
             }
@@ -162,7 +167,7 @@ void quantize_kernel(const unsigned char* __restrict__ X, int64_t N, int d, cons
         } else {
             for (int e = sub * 8; e < pitch; e += 8 << lg) {
                 v[0].zero();
-                if (e < d) v[0].load(src, e, d);
+                if (e < d) v[0].template load<false>(src, e, d);
                 put(v[0], e);
             }
         }
@@ -184,7 +189,8 @@ static void launch_quantize_kernel(const unsigned char* X, int64_t N, int d, con
     }
     const int64_t want = (rows + (4 << (6 - lg)) - 1) / (4 << (6 - lg));
     const unsigned grid = static_cast<unsigned>(want < 32768 ? want : 32768);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(X, N, d, ids, m, count, Q, pitch, scale, lg); };
+    const bool stream = rows * d * static_cast<int64_t>(sizeof(T) == 4 ? 4 : 2) > kCachedBytes;
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(X, N, d, ids, m, count, Q, pitch, scale, lg, stream); };
     switch (C) {
         case 1: go(quantize_kernel<T, 1>); break;
         case 2: go(quantize_kernel<T, 2>); break;
@@ -423,7 +429,7 @@ void scores_kernel(const ScoresArgs a) {
                 for (int c = 0; c < kGroups; ++c) {
                     const int r = r0 + i * T::kWaves, e = (c * kWave + lane) * 8;
                     v[i][c].zero();
-                    if (r < a.B && e < a.d) v[i][c].load(a.Z + r * row_bytes, e, a.d);
+                    if (r < a.B && e < a.d) v[i][c].template load<false>(a.Z + r * row_bytes, e, a.d);
                 }
 #pragma unroll
             for (int i = 0; i < kRows; ++i) {
