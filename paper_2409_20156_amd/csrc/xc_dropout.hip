@@ -8,6 +8,7 @@ namespace xc {
 
 constexpr int kDropThreads = 256;
 constexpr int64_t kDropMany = 1024;         // workgroups from which on a thread takes four units
+constexpr int64_t kDropUnits = 1ll << 31;    // of a launch, at most
 constexpr uint64_t kDropoutKey = 0x64726F706F757431ull;
 
 // N neighbouring elements at any address, `have` of them there.
@@ -52,7 +53,8 @@ template <int N> struct Unit {
 };
 
 struct DropArgs {
-    int64_t d, n_units, row0;
+    int64_t d, n_units;
+    uint64_t row0;
     uint32_t units;                      // of a row
     uint32_t magic;                      // ceil(2^32 / units) for units < 1024
     uint32_t least;
@@ -98,7 +100,7 @@ void dropout_kernel(const TI* X, TO* Y, const DropArgs a) {
     uint32_t last_r, last_c;
     place(here - 1, last_r, last_c);
     for (uint32_t r = threadIdx.x; r <= last_r; r += kDropThreads)
-        rows[r] = fmix64(a.key ^ (kQueryMul * static_cast<uint64_t>(a.row0 + r0 + r + 1)));
+        rows[r] = fmix64(a.key ^ (kQueryMul * (a.row0 + static_cast<uint64_t>(r0) + r + 1)));
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -122,19 +124,23 @@ static int launch(const void* X, void* Y, int64_t B, int64_t d, uint32_t least, 
     DropArgs a;
     a.d = d;
     a.units = static_cast<uint32_t>((d + N - 1) / N);
-    a.n_units = B * a.units;
-    a.row0 = row0;
     a.magic = a.units > 1 ? static_cast<uint32_t>(((1ull << 32) + a.units - 1) / a.units) : 0u;
     a.least = least;
     a.scale = static_cast<float>(65536.0 / (65536 - static_cast<int>(least)));
     a.key = seed ^ kDropoutKey;
     const TI* x = static_cast<const TI*>(X);
     TO* y = static_cast<TO*>(Y);
-    // four units to a thread where that leaves every compute unit several workgroups
-    if (a.n_units >= kDropMany * 4 * kDropThreads)
-        XC_LAUNCH(K_DROPOUT, st, (dropout_kernel<TI, TO, N, 4><<<static_cast<unsigned>((a.n_units + 4 * kDropThreads - 1) / (4 * kDropThreads)), kDropThreads, 0, st>>>(x, y, a)));
-    else
-        XC_LAUNCH(K_DROPOUT, st, (dropout_kernel<TI, TO, N, 1><<<static_cast<unsigned>((a.n_units + kDropThreads - 1) / kDropThreads), kDropThreads, 0, st>>>(x, y, a)));
+    const int64_t most = kDropUnits / a.units;
+    for (int64_t b0 = 0; b0 < B; b0 += most) {
+        const int64_t nb = B - b0 < most ? B - b0 : most;
+        a.n_units = nb * a.units;
+        a.row0 = static_cast<uint64_t>(row0) + static_cast<uint64_t>(b0);
+        // four units to a thread where that leaves every compute unit several workgroups
+        if (a.n_units >= kDropMany * 4 * kDropThreads)
+            XC_LAUNCH(K_DROPOUT, st, (dropout_kernel<TI, TO, N, 4><<<static_cast<unsigned>((a.n_units + 4 * kDropThreads - 1) / (4 * kDropThreads)), kDropThreads, 0, st>>>(x + b0 * d, y + b0 * d, a)));
+        else
+            XC_LAUNCH(K_DROPOUT, st, (dropout_kernel<TI, TO, N, 1><<<static_cast<unsigned>((a.n_units + kDropThreads - 1) / kDropThreads), kDropThreads, 0, st>>>(x + b0 * d, y + b0 * d, a)));
+    }
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }

@@ -17,6 +17,7 @@ constexpr int kVerifyThreads = 256, kDrawWaves = kVerifyThreads / kWave;
 constexpr int kOneChunks = 1024;         // of a sequence that one workgroup does alone
 constexpr int64_t kManySequences = 192;  // that keep most compute units busy
 constexpr int64_t kSumGrid = 2048;       // workgroups that fill the device
+constexpr int64_t kSequences = 65535;    // of a launch
 
 struct VerifyArgs {
     const int32_t* drafts;
@@ -63,8 +64,8 @@ __device__ __forceinline__ Verdict judge(const VerifyArgs& v, int64_t b) {
 }
 
 // Elements e .. e + 7 of a row (zeros behind its end), whose address may be any.
-template <typename T> struct Eight;
-template <> struct Eight<float> {
+template <typename T> struct Octet;
+template <> struct Octet<float> {
     uint4 v[2];
     __device__ __forceinline__ void load(const float* p, int64_t e, int64_t V) {
         if (e + 8 <= V) {
@@ -81,7 +82,7 @@ template <> struct Eight<float> {
     }
     __device__ __forceinline__ void values(float (&f)[8]) const { __builtin_memcpy(f, v, 32); }
 };
-template <> struct Eight<bf16_t> {
+template <> struct Octet<bf16_t> {
     uint4 v;
     __device__ __forceinline__ void load(const bf16_t* p, int64_t e, int64_t V) {
         if (e + 8 <= V) {
@@ -133,11 +134,11 @@ struct Row {
     int64_t V;
     // the lane's elements of piece k of chunk c: 8 from here on
     static __device__ __forceinline__ int64_t first(int c, int k) { return static_cast<int64_t>(c) * kChunk + k * kPiece + lane_id() * 8; }
-    __device__ __forceinline__ void load(int c, int k, Eight<T>& x, Eight<T>& y) const {
+    __device__ __forceinline__ void load(int c, int k, Octet<T>& x, Octet<T>& y) const {
         x.load(p, first(c, k), V);
         if (kind == kDifference) y.load(q, first(c, k), V);          // uniform
     }
-    __device__ __forceinline__ void values(int c, int k, const Eight<T>& x, const Eight<T>& y, float (&f)[8], float (&g)[8]) const {
+    __device__ __forceinline__ void values(int c, int k, const Octet<T>& x, const Octet<T>& y, float (&f)[8], float (&g)[8]) const {
         x.values(f);
         if (kind == kDifference) {
             y.values(g);
@@ -163,7 +164,7 @@ __device__ __forceinline__ double sum8(const double (&w)[8]) {
 // Sum of chunk c, the same in all lanes.
 template <typename T>
 __device__ __forceinline__ double chunk_sum(const Row<T>& r, int c) {
-    Eight<T> x[kPieces], y[kPieces];
+    Octet<T> x[kPieces], y[kPieces];
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) r.load(c, k, x[k], y[k]);
     double s = 0.0;
@@ -252,7 +253,7 @@ __device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sum
     double wt[8];
     s = 0.0;
     if (wave < kPieces) {
-        Eight<T> x, y;
+        Octet<T> x, y;
         float f[8], g[8];
         r.load(chunk, wave, x, y);
         r.values(chunk, wave, x, y, f, g);
@@ -378,17 +379,10 @@ static void launch_verify(const VerifyArgs& v, int64_t B, hipStream_t st) {
     // leave compute units idle.  Device time, us, by 4 waves, by 8, by many: 1 x 8192 fp32 5.3, 5.9, 6.5; 1 x 32768 8.7, 7.8, 7.1 (a call of
     // which the caller takes 8 with one launch and 10.5 with two); 1 x 65536 12.9, 10.9, 7.1; 64 x 131072 27.9, 19.6, 17.0; 256 x
     // 131072 41.3, 39.7, 41.3, in bf16 29.9, 23.2, 26.2.
-    if (v.n_chunks <= 8) {
-        verify_one_kernel<T, 4><<<static_cast<unsigned>(B), 4 * kWave, 0, st>>>(v);
-        return;
-    }
-    if (v.n_chunks <= 16 || (B >= kManySequences && v.n_chunks <= kOneChunks)) {
-        verify_one_kernel<T, 8><<<static_cast<unsigned>(B), 8 * kWave, 0, st>>>(v);
-        return;
-    }
-    for (int64_t b0 = 0; b0 < B; b0 += 65535) {              // (sequences of a launch)
+    const int alone = v.n_chunks <= 8 ? 4 : v.n_chunks <= 16 || (B >= kManySequences && v.n_chunks <= kOneChunks) ? 8 : 0;
+    for (int64_t b0 = 0; b0 < B; b0 += kSequences) {
         VerifyArgs p = v;
-        const int64_t nb = B - b0 < 65535 ? B - b0 : 65535;
+        const int64_t nb = B - b0 < kSequences ? B - b0 : kSequences;
         p.drafts = v.drafts + b0 * v.n;
         p.target = static_cast<const T*>(v.target) + b0 * (v.n + 1) * v.V;
         if (v.draft != nullptr) p.draft = static_cast<const T*>(v.draft) + b0 * v.n * v.V;
@@ -397,6 +391,14 @@ static void launch_verify(const VerifyArgs& v, int64_t B, hipStream_t st) {
         p.accepted += b0;
         p.verdicts += b0;
         p.sums += b0 * v.n_chunks;
+        if (alone == 4) {
+            verify_one_kernel<T, 4><<<static_cast<unsigned>(nb), 4 * kWave, 0, st>>>(p);
+            continue;
+        }
+        if (alone == 8) {
+            verify_one_kernel<T, 8><<<static_cast<unsigned>(nb), 8 * kWave, 0, st>>>(p);
+            continue;
+        }
         // as many chunks to a wave as leave the device full
         const int64_t wide = (v.n_chunks + kDrawWaves - 1) / kDrawWaves, most = kSumGrid / nb > 0 ? kSumGrid / nb : 1;
         const int64_t rounds = (wide + most - 1) / most, gx = (wide + rounds - 1) / rounds;

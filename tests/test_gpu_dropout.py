@@ -109,6 +109,18 @@ def test_offsets_beyond_32_bits():
         assert (X[r].float().cpu().numpy() == 2.0 * so.dropout_kept(1, d, 0.5, 17, row0=r)[0]).all()
 
 
+def test_more_rows_than_one_launch_takes():
+    import paper_2409_20156_amd as xc
+    B = (1 << 31) + 300                                    # of one element
+    X = torch.ones((B, 1), dtype=BF16, device=DEV)
+    xc.dropout(X, 0.5, 19, row0=7, out=X)
+    for r in (0, (1 << 31) - 150, (1 << 31), B - 100):
+        n = min(B - r, 200)
+        want = xc.dropout(torch.ones((n, 1), dtype=BF16, device=DEV), 0.5, 19, row0=7 + r)
+        assert torch.equal(X[r:r + n], want)
+        assert (want.cpu().float().numpy() == 2.0 * so.dropout_kept(n, 1, 0.5, 19, row0=7 + r)).all()
+
+
 def test_another_stream_and_a_replayed_graph():
     import paper_2409_20156_amd as xc
     X = torch.randn((100, 768), device=DEV).to(BF16)

@@ -135,6 +135,28 @@ def test_a_sequence_does_not_depend_on_the_others(dtype, B, V):
         assert (one[0][0] == every[0][b]).all() and one[1][0] == every[1][b]
 
 
+@pytest.mark.parametrize("B,n,V", [(131071, 1, 3), (65536, 2, 8), (66000, 1, 17000)])
+def test_more_sequences_than_one_launch_takes(B, n, V):
+    import paper_2409_20156_amd as xc
+    g = torch.Generator(device=DEV).manual_seed(B)
+    p = torch.rand((B, n + 1, V), generator=g, device=DEV, dtype=F32).to(BF16)
+    x = torch.randint(0, V, (B, n), generator=g, device=DEV, dtype=torch.int32)
+    u = torch.rand((B, n + 1), generator=g, device=DEV)
+    tokens, accepted = xc.verify_drafts(x, p, None, u)
+    for b0, b1 in ((0, 5), (65533, 65536), (65534, min(B, 65540)), (B - 3, B)):
+        some = xc.verify_drafts(x[b0:b1].clone(), p[b0:b1].clone(), None, u[b0:b1].clone())
+        assert torch.equal(some[0], tokens[b0:b1]) and torch.equal(some[1], accepted[b0:b1])
+
+
+def test_as_many_sequences_as_have_more_threads_than_32_bits_count():
+    import paper_2409_20156_amd as xc
+    B = (1 << 24) + 9
+    p = torch.ones((B, 1, 1), dtype=BF16, device=DEV)
+    p[B - 2] = 0
+    tokens, accepted = xc.verify_drafts(torch.zeros((B, 0), dtype=torch.int32, device=DEV), p, None, torch.zeros((B, 1), device=DEV))
+    assert int(tokens[B - 2]) == -1 and int(tokens.sum()) == -1 and int(accepted.sum()) == 0
+
+
 def test_nothing_behind_the_outputs_is_written_and_the_workspace_may_hold_anything():
     import paper_2409_20156_amd as xc
     x, p, q, u = _case(8, 33, 3, 10007, F32)
