@@ -521,8 +521,12 @@ void scores_kernel(const ScoresArgs a) {
                             store_labels(p, v);
                         } else if (q0 + qt + x * 16 + i < a.B) {
                             const int64_t left = a.L - l0 - lt - y0 * 16;
+                            if (left >= V) {
+                                store_labels(p, v);
+                            } else {
 #pragma unroll
-                            for (int y = 0; y < V; ++y) if (y < left) store_label(p + y, v[y]);
+                                for (int y = 0; y < V; ++y) if (y < left) store_label(p + y, v[y]);
+                            }
                         }
                     }
                 }
@@ -697,8 +701,12 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
                     if constexpr (decltype(all)::value) {
                         store_labels(p, v);
                     } else if (q0 + qb * 16 + 4 * quarter + i < a.B) {
+                        if (l + 4 <= a.L) {
+                            store_labels(p, v);
+                        } else {
 #pragma unroll
-                        for (int y = 0; y < 4; ++y) if (l + y < a.L) store_label(p + y, v[y]);
+                            for (int y = 0; y < 4; ++y) if (l + y < a.L) store_label(p + y, v[y]);
+                        }
                     }
                 }
             };
@@ -739,11 +747,13 @@ static void run_held(const ScoresArgs& a, hipStream_t st) {
 //   up to 32 queries   32 x 128; fewer labels than 256 such tiles 32 x 32 (16 x 4000 x 4096: 15.5 against 24.5)
 //   up to 512 tiles of 64 x 64   these (128 x 16000 x 768: 8.5 against 10.0 with 128 x 128; 400 x 4000 x 4096: 25 against 35)
 //   up to 64 queries   64 x 128 (64 x 300000 x 768: 59; 128 x 128 70, 64 x 64 62)
-//   up to 128 queries, or three rounds of 128 x 128 tiles   these (128 x 670000 x 768: 148, labels held 181; 300 x 50000 x 768:
-//                      29 against 37; 512 x 131072 x 768: 100 against 66, so not beyond)
-//   more, rows of up to 768 bytes   labels held in registers (4096 x 131072 x 768: 420; 256 x 256 tiles 545)
-//   longer rows        256 x 256, where that takes fewer rounds for its larger tiles (512 x 32000 x 1024: 23 against 25;
-//                      1024 x 8000 x 1024: 27 against 18, so not there)
+//   more than 384 queries and 1792 tiles of 128 x 128, rows of up to 768 bytes   labels held in registers (4096 x 131072 x 768 to
+//                      bf16: 360; 256 x 256 tiles 545; 700 x 74141 x 768: 67, 128 x 128 tiles 74; 700 x 34200 x 768, 1608 tiles: 43 and
+//                      36; 300 x 167592 x 512: 67 and 60)
+//   else 128 x 128 tiles or, beyond 192 queries, 256 x 256 where that takes fewer rounds for its larger tiles (to bf16 512 x 209651 x
+//                      1024: 137 against 185; 1000 x 93139 x 4096: 338 against 428; 256 x 188816 x 512: 44 against 56; 800 x
+//                      17762 x 1536: 51 against 34, so not there; 130 x 141461 x 800: 71 against 55).  Short rows beyond 256 queries
+//                      are no longer worth it (300 x 87520 x 384: 37 against 29).
 template <typename TO>
 static void run_scores(const ScoresArgs& a, hipStream_t st) {
     auto tiles = [&](int m, int n) { return (a.B + m - 1) / m * ((a.L + n - 1) / n); };
@@ -754,12 +764,11 @@ static void run_scores(const ScoresArgs& a, hipStream_t st) {
         launch_scores<TO, TileSmall>(a, st);
     } else if (a.B <= 64) {
         launch_scores<TO, TileSome>(a, st);
-    } else if (a.ppitch <= kHeldBytes) {
-        if (a.B <= 128 || tiles(128, 128) <= 6 * kMineGrid) launch_scores<TO, TileMid>(a, st);
-        else run_held<TO>(a, st);
+    } else if (a.ppitch <= kHeldBytes && a.B > 384 && tiles(128, 128) > 7 * kMineGrid) {
+        run_held<TO>(a, st);
     } else {
         const int64_t mid = (tiles(128, 128) + 2 * kMineGrid - 1) / (2 * kMineGrid), many = (tiles(256, 256) + kMineGrid - 1) / kMineGrid;
-        if (a.B <= 192 || 5 * mid <= 8 * many) launch_scores<TO, TileMid>(a, st);
+        if (a.B <= 192 || (a.ppitch <= kHeldBytes && a.B > 256) || 5 * mid <= 8 * many) launch_scores<TO, TileMid>(a, st);
         else launch_scores<TO, TileMany>(a, st);
     }
 }
