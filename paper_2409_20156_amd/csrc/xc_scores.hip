@@ -265,9 +265,9 @@ template <int N> __device__ __forceinline__ void store_labels(float* p, const fl
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <int N> __device__ __forceinline__ void store_labels(bf16_t* p, const float (&v)[N]) {
-    bf16x2 h[N / 2];
+    bf16x2 h[(N + 1) / 2];
 #pragma unroll
-    for (int e = 0; e < N / 2; ++e) h[e] = __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, bf16x2);      // nearest, ties to even
+    for (int e = 0; e < (N + 1) / 2; ++e) h[e] = __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1 < N ? 2 * e + 1 : 2 * e]}, bf16x2);      // nearest, ties to even
     __builtin_memcpy(p, h, 2 * N);
 }
 __device__ __forceinline__ void store_label(float* p, float v) { *p = v; }
@@ -279,8 +279,10 @@ __device__ __forceinline__ void store_label(bf16_t* p, float v) {
 __device__ __forceinline__ void lds_dma4(const void* gptr, uint32_t lds_addr /* wave-uniform */) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(gptr), "s"(lds_addr) : "memory");
 }
-// Rows that a call reads once: marked for early replacement.  1 x 670000 x 768 89 -> 77 us, 32 x 131072 x 768 26.3 -> 24.3, where one call
-// after the other reads the same 100 MB, which the last-level cache holds, 17.4 -> 16.4; 64 x 670000 x 768 132 -> 121; 64 x 3 M x 256 233 -> 239.
+// Rows of whole lines that a call reads once: marked for early replacement.  1 x 670000 x 768 89 -> 77 us, 32 x 131072 x 768 26.3 ->
+// 24.3, where one call after the other reads the same 100 MB, which the last-level cache holds, 17.4 -> 16.4; 64 x 670000 x 768 132 ->
+// 121; 64 x 3 M x 256 233 -> 239.  Not where two loads share a line, of which the second would find nothing left: 126 x 441376 x 776
+// 185 us with the hint, 146 without; 32 x 600000 x 304 77 and 59.
 template <bool STREAM>
 __device__ __forceinline__ void load_labels(const void* sbase, uint32_t voff, uint32_t lds_addr) {
     if constexpr (STREAM)
@@ -365,7 +367,7 @@ void scores_kernel(const ScoresArgs a) {
             const int room = a.pitch - ld_kb * kStageBytes;        // bytes of the rows from here on
             const uint32_t dst_b = dst + (T::kStageRows - T::BN) * kStageBytes + wi * T::kLoadsB * 1024;
             const int8_t* from_b = a.Q + ld_l * a.pitch + ld_kb * kStageBytes;
-            if (have >= T::BN && room >= kStageBytes) {
+            if (have >= T::BN && (room >= kStageBytes || have >= T::BN + 7)) {     // (what is read behind a row, at most 112 bytes, meets zeros of the queries)
                 const void* from = uniform_ptr(from_b);
 #pragma unroll
                 for (int i = 0; i < T::kLoadsB; ++i) load_labels<STREAM>(from, off_b[i], dst_b + i * 1024);
@@ -544,9 +546,11 @@ void scores_kernel(const ScoresArgs a) {
 typedef Tile<4, 2, 4, 8, 2, 2> TileMany;            // 256 x 256
 typedef Tile<2, 2, 4, 4, 2, 1> TileMid;             // 128 x 128
 typedef Tile<2, 2, 2, 2, 4, 1> TileSmall;           // 64 x 64
+typedef Tile<2, 2, 2, 1, 4, 1> TileLow;             // 64 x 32
 typedef Tile<1, 4, 4, 2, 3, 1> TileSome;            // 64 x 128
 typedef Tile<1, 4, 2, 2, 3, 1> TileFew;             // 32 x 128
 typedef Tile<1, 1, 2, 2, 4, 1> TileNarrow;          // 32 x 32
+typedef Tile<1, 1, 1, 1, 4, 1> TileThin;            // 16 x 16
 typedef Tile<1, 4, 1, 2, 4, 1, 768> TileOnline;     // 16 x 128, queries of up to 768 bytes resident
 constexpr int kQueryPad = 128;                           // the queries in the workspace: rows of whole stages,
 constexpr int kQueryTile = 256;                          // whole tiles of them of any kind
@@ -561,8 +565,8 @@ static void launch_scores(ScoresArgs a, hipStream_t st) {
     a.group = static_cast<int>(fit < 1 ? 1 : fit < a.tiles_m ? fit : a.tiles_m);
     const int64_t per = (static_cast<int64_t>(a.tiles_m) * a.tiles_n + 7) / 8, most = kCusPerXcd * T::kPerCu;
     const unsigned grid = static_cast<unsigned>(8 * (per < most ? per : most));
-    if (T::BM <= 32 || a.tiles_m == 1) scores_kernel<TO, T, true, TZ><<<grid, T::kThreads, 0, st>>>(a);      // every row of Q is read once
-    else if constexpr (T::BM > 32) scores_kernel<TO, T, false, TZ><<<grid, T::kThreads, 0, st>>>(a);         // (32 queries and fewer are one tile)
+    if (a.tiles_m == 1 && a.pitch % kStageBytes == 0) scores_kernel<TO, T, true, TZ><<<grid, T::kThreads, 0, st>>>(a);      // every line of Q is read once
+    else scores_kernel<TO, T, false, TZ><<<grid, T::kThreads, 0, st>>>(a);
 }
 
 // ---- many queries, rows of up to 768 bytes: the labels stay where they are.  A wave holds 64 labels as operands in registers (NK
@@ -744,8 +748,11 @@ static void run_held(const ScoresArgs& a, hipStream_t st) {
 }
 
 // Which kernel.  Measured with rows of Q from memory (us, scores alone, on the sides of each rule):
-//   up to 32 queries   32 x 128; fewer labels than 256 such tiles 32 x 32 (16 x 4000 x 4096: 15.5 against 24.5)
-//   up to 512 tiles of 64 x 64   these (128 x 16000 x 768: 8.5 against 10.0 with 128 x 128; 400 x 4000 x 4096: 25 against 35)
+//   up to 32 queries   32 x 128; fewer labels than 256 such tiles 32 x 32, and up to 16 queries or 256 of those 16 x 16: a compute unit
+//                      keeps only so many lines of memory under way, so a short call wants many of them at it (32 x 30000 x 4096: 31,
+//                      38 with 16 x 16; 32 x 6000 x 4096: 24 and 14; 12 x 10000 x 4096: 23 and 15, with 32 x 128 24)
+//   up to 512 tiles of 64 x 64   these; up to 256 of 64 x 32 those (128 x 16000 x 768: 8.5 against 10.0 with 128 x 128 and 12 with 64 x 32;
+//                      400 x 4000 x 4096: 25, 35 and 34; 128 x 4000 x 4096: 21, with 64 x 32 16)
 //   up to 64 queries   64 x 128 (64 x 300000 x 768: 59; 128 x 128 70, 64 x 64 62)
 //   more than 384 queries and 1792 tiles of 128 x 128, rows of up to 768 bytes   labels held in registers (4096 x 131072 x 768 to
 //                      bf16: 360; 256 x 256 tiles 545; 700 x 74141 x 768: 67, 128 x 128 tiles 74; 700 x 34200 x 768, 1608 tiles: 43 and
@@ -759,7 +766,10 @@ static void run_scores(const ScoresArgs& a, hipStream_t st) {
     auto tiles = [&](int m, int n) { return (a.B + m - 1) / m * ((a.L + n - 1) / n); };
     if (a.B <= 32) {
         if (tiles(32, 128) >= kMineGrid) launch_scores<TO, TileFew>(a, st);
+        else if (a.B <= 16 || tiles(32, 32) <= kMineGrid) launch_scores<TO, TileThin>(a, st);
         else launch_scores<TO, TileNarrow>(a, st);
+    } else if (tiles(64, 32) <= kMineGrid) {
+        launch_scores<TO, TileLow>(a, st);
     } else if (tiles(64, 64) <= 2 * kMineGrid) {
         launch_scores<TO, TileSmall>(a, st);
     } else if (a.B <= 64) {

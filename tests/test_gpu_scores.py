@@ -105,7 +105,8 @@ SHAPES = [  # B, L, d
     (15, 129, 64), (16, 128, 128), (17, 127, 256), (31, 500, 200), (32, 512, 768), (33, 511, 768), (40, 1030, 1000), (63, 333, 72),
     (64, 700, 512), (65, 255, 384), (96, 2049, 88), (127, 256, 320), (128, 1000, 768), (129, 257, 264), (200, 1537, 104),
     (255, 600, 192), (256, 256, 768), (257, 1023, 776), (300, 5003, 304), (513, 515, 1544), (1000, 777, 64), (5, 2000, 8208),
-    (130, 300, 16400), (2, 70, 131072), (700, 3000, 8)]
+    (130, 300, 16400), (2, 70, 131072), (700, 3000, 8), (20, 9001, 72), (32, 16000, 200), (17, 12289, 776), (16, 33001, 1000),
+    (9, 10001, 800), (100, 9001, 136), (33, 7900, 16), (1, 40000, 16), (3, 33000, 1032)]
 
 
 @pytest.mark.parametrize("B,L,d", SHAPES)
