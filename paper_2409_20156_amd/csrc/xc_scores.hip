@@ -589,18 +589,22 @@ constexpr int kHeldLabels = 512, kHeldBytes = 768;
 
 template <typename TO, int NK>
 __global__ __launch_bounds__(512, 2)
-void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
+void scores_held_kernel(const ScoresArgs a, int64_t tiles, int stages) {
     typedef Held<NK> H;
     __shared__ __align__(1024) unsigned char smem[H::kLds];
     const int lane = lane_id(), quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
-    // a contiguous part of the units (a stage of queries for a tile of labels), neighbouring parts on one XCD
-    const int64_t part = static_cast<int64_t>(blockIdx.x % 8) * (gridDim.x / 8) + blockIdx.x / 8;
-    const int64_t u_begin = units * part / gridDim.x, u_end = units * (part + 1) / gridDim.x;
-    if (u_begin >= u_end) return;
-    const int total = static_cast<int>(u_end - u_begin);
-    int64_t tile = u_begin / stages;
-    int st = static_cast<int>(u_begin % stages);
+    // each XCD takes neighbouring tiles of labels, a workgroup one of every 32 for as long as there are 32, so that the lines that
+    // two tiles share are written at about the same time; then an equal part of what is left, counted in stages of queries of a tile
+    const int64_t xcd = blockIdx.x % 8, nth = blockIdx.x / 8, wgs = gridDim.x / 8;
+    const int64_t t_begin = tiles * xcd / 8, t_count = tiles * (xcd + 1) / 8 - t_begin, rounds = t_count / wgs;
+    const int64_t left = (t_count - rounds * wgs) * stages, left_begin = left * nth / wgs, left_end = left * (nth + 1) / wgs;
+    const int whole_units = static_cast<int>(rounds * stages), total = whole_units + static_cast<int>(left_end - left_begin);
+    if (total == 0) return;
+    const int64_t left_tile = t_begin + rounds * wgs + left_begin / stages;
+    const int left_st = static_cast<int>(left_begin % stages);
+    int64_t tile = rounds > 0 ? t_begin + nth : left_tile;
+    int st = rounds > 0 ? 0 : left_st;
 
     uint32_t off[H::kLoads];
 #pragma unroll
@@ -617,7 +621,7 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
         for (int i = 0; i < H::kLoads; ++i) lds_dma16_sbase<0>(from, off[i], dst + (wave * H::kLoads + i) * 1024);
         if (++ld_st == stages) ld_st = 0;
         if (++ld_slot == H::R) ld_slot = 0;
-        ++n_issued;
+        if (++n_issued == whole_units) ld_st = left_st;
     };
     int full = 0;                                            // stages in a row whose scores were all stored as whole blocks
     auto publish = [&](int g_next) __attribute__((always_inline)) {
@@ -720,8 +724,8 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
         full = whole ? full + 1 : 0;
         slot = slot_next;
         if (++st == stages) {
-            st = 0;
-            ++tile;
+            st = g + 1 == whole_units ? left_st : 0;
+            tile = g + 1 == whole_units ? left_tile : g + 1 < whole_units ? tile + wgs : tile + 1;
             full = 0;
             if (g + 1 < total) hold(tile * kHeldLabels);
         }
@@ -731,8 +735,7 @@ void scores_held_kernel(const ScoresArgs a, int64_t units, int stages) {
 template <typename TO, int NK>
 static void launch_held(ScoresArgs a, hipStream_t st) {
     const int stages = static_cast<int>((a.B + Held<NK>::QS - 1) / Held<NK>::QS);
-    const int64_t units = (a.L + kHeldLabels - 1) / kHeldLabels * stages;
-    scores_held_kernel<TO, NK><<<kMineGrid, 512, 0, st>>>(a, units, stages);
+    scores_held_kernel<TO, NK><<<kMineGrid, 512, 0, st>>>(a, (a.L + kHeldLabels - 1) / kHeldLabels, stages);
 }
 
 template <typename TO>
