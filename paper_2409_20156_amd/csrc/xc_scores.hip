@@ -574,9 +574,11 @@ static void launch_scores(ScoresArgs a, hipStream_t st) {
 // two thirds of the operand reads from LDS that a 256 x 256 tile takes, a quarter of the bytes brought into it, and a wave's scores are
 // stored 16 queries at a time, while the other wave of its SIMD multiplies.
 // Bound: the matrix pipe at the chip's power limit and the stores beside it.  4096 x 131072 x 768 to bf16: 360 us under sustained load
-// (2.3 POP/s; 320 from a cool chip), without the stores 281, without the loads the same as with them.  Neither 16-byte stores (rows
-// exchanged between neighbouring lanes: 379 against 368 us a call) nor wave priorities changed it.  Rows of an odd number of
-// bf16 scores are stored at addresses that are no multiple of 8: 131071 labels take 474 us.
+// (2.3 POP/s; 320 from a cool chip), without the stores 281, without the loads the same as with them; 846 x 570112 x 192, which the stores
+// bound, 223 (4.3 TB/s).  Rows that begin within a line cost 5 to 20 percent: 4096 x 131071 x 768 431, 846 x 569976 x 192 247; and did
+// 45 when a workgroup took neighbouring tiles one after the other, whose shared lines left the cache half written (351).  Neither
+// 16-byte stores (rows exchanged between neighbouring lanes: 379 against 368 us a call), nor rows put together in LDS and stored by
+// whole lines (4096 x 131080 x 768 610 against 355), nor wave priorities made it faster.
 template <int NK_>
 struct Held {
     static constexpr int NK = NK_, QS = NK % 4 == 0 ? 32 : 64, kStage = QS * NK * 64;       // (the stage's loads divide evenly among 8 waves)
@@ -757,9 +759,9 @@ static void run_held(const ScoresArgs& a, hipStream_t st) {
 //   up to 512 tiles of 64 x 64   these; up to 256 of 64 x 32 those (128 x 16000 x 768: 8.5 against 10.0 with 128 x 128 and 12 with 64 x 32;
 //                      400 x 4000 x 4096: 25, 35 and 34; 128 x 4000 x 4096: 21, with 64 x 32 16)
 //   up to 64 queries   64 x 128 (64 x 300000 x 768: 59; 128 x 128 70, 64 x 64 62)
-//   more than 384 queries and 1792 tiles of 128 x 128, rows of up to 768 bytes   labels held in registers (4096 x 131072 x 768 to
-//                      bf16: 360; 256 x 256 tiles 545; 700 x 74141 x 768: 67, 128 x 128 tiles 74; 700 x 34200 x 768, 1608 tiles: 43 and
-//                      36; 300 x 167592 x 512: 67 and 60)
+//   more than 1792 tiles of 128 x 128, rows of up to 768 bytes and more than 384 queries, or up to 384 and 128   labels held in registers
+//                      (4096 x 131072 x 768 to bf16: 360; 256 x 256 tiles 545; 700 x 74141 x 768: 67, 128 x 128 tiles 74; 340 x 526924 x
+//                      320: 143 and 168; 700 x 34200 x 768, 1608 tiles: 43 and 36; 340 x 188544 x 512: 83 and 72)
 //   else 128 x 128 tiles or, beyond 192 queries, 256 x 256 where that takes fewer rounds for its larger tiles (to bf16 512 x 209651 x
 //                      1024: 137 against 185; 1000 x 93139 x 4096: 338 against 428; 256 x 188816 x 512: 44 against 56; 800 x
 //                      17762 x 1536: 51 against 34, so not there; 130 x 141461 x 800: 71 against 55).  Short rows beyond 256 queries
@@ -777,7 +779,7 @@ static void run_scores(const ScoresArgs& a, hipStream_t st) {
         launch_scores<TO, TileSmall>(a, st);
     } else if (a.B <= 64) {
         launch_scores<TO, TileSome>(a, st);
-    } else if (a.ppitch <= kHeldBytes && a.B > 384 && tiles(128, 128) > 7 * kMineGrid) {
+    } else if (a.B > 128 && a.ppitch <= (a.B > 384 ? kHeldBytes : kHeldBytes / 2) && tiles(128, 128) > 7 * kMineGrid) {
         run_held<TO>(a, st);
     } else {
         const int64_t mid = (tiles(128, 128) + 2 * kMineGrid - 1) / (2 * kMineGrid), many = (tiles(256, 256) + kMineGrid - 1) / kMineGrid;
