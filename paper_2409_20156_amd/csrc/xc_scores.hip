@@ -588,25 +588,59 @@ struct Held {
     static_assert(kLoads * 8 * 1024 == kStage && R >= 3 && (kLoads + kStores) * (R - 3) < 64, "whole loads, and a count that the wait can hold");
 };
 constexpr int kHeldLabels = 512, kHeldBytes = 768;
+constexpr int kHeldPieces = 4;                           // of the tiles behind the last whole round, to a workgroup
 
 template <typename TO, int NK>
 __global__ __launch_bounds__(512, 2)
-void scores_held_kernel(const ScoresArgs a, int64_t tiles, int stages) {
+void scores_held_kernel(const ScoresArgs a, int tiles, int stages, int rest_tiles, int rest_parts, int rest_parts_more) {
     typedef Held<NK> H;
     __shared__ __align__(1024) unsigned char smem[H::kLds];
+    __shared__ int4 last[kHeldPieces + 1];
     const int lane = lane_id(), quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
-    // each XCD takes neighbouring tiles of labels, a workgroup one of every 32 for as long as there are 32, so that the lines that
-    // two tiles share are written at about the same time; then an equal part of what is left, counted in stages of queries of a tile
-    const int64_t xcd = blockIdx.x % 8, nth = blockIdx.x / 8, wgs = gridDim.x / 8;
-    const int64_t t_begin = tiles * xcd / 8, t_count = tiles * (xcd + 1) / 8 - t_begin, rounds = t_count / wgs;
-    const int64_t left = (t_count - rounds * wgs) * stages, left_begin = left * nth / wgs, left_end = left * (nth + 1) / wgs;
-    const int whole_units = static_cast<int>(rounds * stages), total = whole_units + static_cast<int>(left_end - left_begin);
+    // Each XCD takes neighbouring tiles of labels, a workgroup one of every 32, so that the lines that two tiles share are written at
+    // about the same time.  Of the last tiles, fewer than 32, a workgroup has parts of the queries: as many for each tile (`parts`), for
+    // the same reason, or (0) an equal number of stages.
+    const int xcd = blockIdx.x % 8, nth = blockIdx.x / 8;
+    const int t_begin = static_cast<int>(static_cast<int64_t>(tiles) * xcd / 8) + nth;
+    const int t_count = static_cast<int>(static_cast<int64_t>(tiles) * (xcd + 1) / 8) + nth - t_begin, rounds = t_count / kCusPerXcd;
+    if (threadIdx.x == 0) {
+        const int rest = t_count % kCusPerXcd, first = t_begin - nth + rounds * kCusPerXcd, parts = rest == rest_tiles ? rest_parts : rest_parts_more;
+        int n = 0;
+        if (parts > 0) {
+            for (int i = nth; i < rest * parts; i += kCusPerXcd)
+                last[n++] = make_int4(first + i % rest, static_cast<int>(static_cast<int64_t>(stages) * (i / rest) / parts),
+                                      static_cast<int>(static_cast<int64_t>(stages) * (i / rest + 1) / parts), 0);
+        } else {
+            const int64_t all = static_cast<int64_t>(rest) * stages, u1 = all * (nth + 1) / kCusPerXcd;
+            for (int64_t u = all * nth / kCusPerXcd; u < u1;) {
+                const int t = static_cast<int>(u / stages), s = static_cast<int>(u - static_cast<int64_t>(t) * stages);
+                const int e = stages - s < u1 - u ? stages : s + static_cast<int>(u1 - u);
+                last[n++] = make_int4(first + t, s, e, 0);
+                u += e - s;
+            }
+        }
+        int sum = 0;
+        for (int i = 0; i < n; ++i) sum += last[i].z - last[i].y;
+        last[0].w = rounds * stages + sum;
+    }
+    __syncthreads();
+    // the workgroup's n-th piece of work: a tile and stages of queries
+    auto piece = [&](int n, int& tile, int& begin, int& end) __attribute__((always_inline)) {
+        tile = t_begin + n * kCusPerXcd;
+        begin = 0;
+        end = stages;
+        if (n >= rounds) {
+            const int4 l = last[n - rounds];
+            tile = __builtin_amdgcn_readfirstlane(l.x);
+            begin = __builtin_amdgcn_readfirstlane(l.y);
+            end = __builtin_amdgcn_readfirstlane(l.z);
+        }
+    };
+    const int total = __builtin_amdgcn_readfirstlane(last[0].w);
     if (total == 0) return;
-    const int64_t left_tile = t_begin + rounds * wgs + left_begin / stages;
-    const int left_st = static_cast<int>(left_begin % stages);
-    int64_t tile = rounds > 0 ? t_begin + nth : left_tile;
-    int st = rounds > 0 ? 0 : left_st;
+    int tile, ld_tile, st, st_end;
+    piece(0, tile, st, st_end);
 
     uint32_t off[H::kLoads];
 #pragma unroll
@@ -614,16 +648,19 @@ void scores_held_kernel(const ScoresArgs a, int64_t tiles, int stages) {
         const int n = wave * H::kLoads + i, row = n % (H::QS / 8) * 8 + (lane >> 3);
         off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(a.ppitch) + n / (H::QS / 8) * 128 + (((lane & 7) ^ row_swizzle(row)) * 16);
     }
-    int ld_st = st, ld_slot = 0, n_issued = 0;
+    int n_piece = 0, ld_piece = 0;
+    int ld_st = st, ld_end = st_end, ld_slot = 0, n_issued = 0;
     auto issue = [&]() __attribute__((always_inline)) {
         const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + ld_slot * H::kStage);
-        if (wave == 0) lds_dma4(a.pscale + ld_st * H::QS + lane, __builtin_amdgcn_readfirstlane(lds + H::R * H::kStage + ld_slot * 256));
+        if (wave == 0) lds_dma4(a.pscale + static_cast<int64_t>(ld_st) * H::QS + lane, __builtin_amdgcn_readfirstlane(lds + H::R * H::kStage + ld_slot * 256));
         const void* from = uniform_ptr(a.P + static_cast<int64_t>(ld_st) * H::QS * a.ppitch);
 #pragma unroll
         for (int i = 0; i < H::kLoads; ++i) lds_dma16_sbase<0>(from, off[i], dst + (wave * H::kLoads + i) * 1024);
-        if (++ld_st == stages) ld_st = 0;
+        if (++ld_st == ld_end) {
+            piece(++ld_piece, ld_tile, ld_st, ld_end);
+        }
         if (++ld_slot == H::R) ld_slot = 0;
-        if (++n_issued == whole_units) ld_st = left_st;
+        ++n_issued;
     };
     int full = 0;                                            // stages in a row whose scores were all stored as whole blocks
     auto publish = [&](int g_next) __attribute__((always_inline)) {
@@ -663,16 +700,16 @@ void scores_held_kernel(const ScoresArgs a, int64_t tiles, int stages) {
             for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(w[k][y]));
         }
     };
-    hold(tile * kHeldLabels);
+    hold(static_cast<int64_t>(tile) * kHeldLabels);
     publish(0);
     fa[0] = read_a(0, 0, 0);
     fa[1] = read_a(0, 0, 1);
     int slot = 0;
     constexpr int kBlocks = H::QS / 16;
     for (int g = 0; g < total; ++g) {
-        const int64_t l0 = tile * kHeldLabels + wave * 64, l = l0 + (lane & 15) * 4;
+        const int64_t l0 = static_cast<int64_t>(tile) * kHeldLabels + wave * 64, l = l0 + (lane & 15) * 4;
         const int q0 = st * H::QS;
-        const bool whole = q0 + H::QS <= a.B && l0 + 64 <= a.L;
+        const bool whole = static_cast<int64_t>(q0) + H::QS <= a.B && l0 + 64 <= a.L;
         const int slot_next = slot + 1 == H::R ? 0 : slot + 1;
         const float* sq = reinterpret_cast<const float*>(smem + H::R * H::kStage + slot * 256) + 4 * quarter;
         TO* out = static_cast<TO*>(a.out) + static_cast<int64_t>(q0 + 4 * quarter) * a.L + l;
@@ -725,11 +762,10 @@ void scores_held_kernel(const ScoresArgs a, int64_t tiles, int stages) {
         }
         full = whole ? full + 1 : 0;
         slot = slot_next;
-        if (++st == stages) {
-            st = g + 1 == whole_units ? left_st : 0;
-            tile = g + 1 == whole_units ? left_tile : g + 1 < whole_units ? tile + wgs : tile + 1;
+        if (++st == st_end) {
+            piece(++n_piece, tile, st, st_end);
             full = 0;
-            if (g + 1 < total) hold(tile * kHeldLabels);
+            if (g + 1 < total) hold(static_cast<int64_t>(tile) * kHeldLabels);
         }
     }
 }
@@ -737,7 +773,21 @@ void scores_held_kernel(const ScoresArgs a, int64_t tiles, int stages) {
 template <typename TO, int NK>
 static void launch_held(ScoresArgs a, hipStream_t st) {
     const int stages = static_cast<int>((a.B + Held<NK>::QS - 1) / Held<NK>::QS);
-    scores_held_kernel<TO, NK><<<kMineGrid, 512, 0, st>>>(a, (a.L + kHeldLabels - 1) / kHeldLabels, stages);
+    const int tiles = static_cast<int>((a.L + kHeldLabels - 1) / kHeldLabels), rest = tiles / 8 % kCusPerXcd;      // of an XCD; some have one more
+    // As few rounds of the parts as may be: to hold a tile's labels takes the time of about 5 stages (2809 x 106363 x 232 to fp32 391 ->
+    // 285 us, 700 x 74141 x 640 89 -> 75).  Equal numbers of stages where rows of whole half lines leave next to nothing to share
+    // (106368 labels to bf16: 143, in parts 160), and where the products take longer than the stores (700 x 74141 x 640 to bf16: 63 and 72).
+    const bool equal = (sizeof(TO) == 2 && NK > 8) || ((reinterpret_cast<uintptr_t>(a.out) | static_cast<uintptr_t>(a.L) * sizeof(TO)) & 63) == 0;
+    auto parts_of = [&](int rest) {
+        int parts = 0, best = 0;
+        for (int p = 1; !equal && p <= stages && rest * p <= kHeldPieces * kCusPerXcd; ++p) {
+            const int cost = (rest * p + kCusPerXcd - 1) / kCusPerXcd * ((stages + p - 1) / p + 5);
+            if (parts == 0 || cost < best) { best = cost; parts = p; }
+            if (rest == 0) break;
+        }
+        return parts;
+    };
+    scores_held_kernel<TO, NK><<<kMineGrid, 512, 0, st>>>(a, tiles, stages, rest, parts_of(rest), parts_of((rest + 1) % kCusPerXcd));
 }
 
 template <typename TO>

@@ -168,7 +168,8 @@ def test_a_range_of_labels_and_every_batch_size_give_the_same_bits(B):
 @pytest.mark.parametrize("B,L,d", [(290, 70001, 24), (137, 131072, 128), (290, 70004, 200), (261, 100000, 384), (500, 50021, 512),
                                    (700, 40000, 600), (290, 70001, 768), (1025, 30000, 768), (300, 30001, 776), (600, 20000, 1096),
                                    (2049, 8005, 2064), (430, 60001, 24), (400, 57856, 128), (450, 60004, 200), (500, 58000, 384),
-                                   (390, 58001, 512), (256, 131072, 128), (255, 140001, 768), (253, 133000, 24), (140, 150001, 104), (300, 100010, 384), (385, 270000, 64)])
+                                   (390, 58001, 512), (256, 131072, 128), (255, 140001, 768), (253, 133000, 24), (140, 150001, 104), (300, 100010, 384), (385, 270000, 64),
+                                   (2809, 20011, 232), (1000, 131071, 64), (600, 170000, 128)])
 def test_large_calls_have_the_bits_of_small_ones(B, L, d, out_dtype):
     """The kernels of large calls against those of small ones, which the oracle checks above."""
     import paper_2409_20156_amd as xc
