@@ -223,8 +223,8 @@ static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const in
 // Accumulator i of a lane: query 4 (lane / 16) + i of its block, column lane % 16.
 // A persistent workgroup takes its tiles one after the other with the loads running ahead into the next, so a tile's scores are
 // stored while the next one's operands arrive; the waits count loads and stores, which retire in the order of their issue.
-// Bound: few queries, the rows of Q from memory (1 x 131072 x 768: 17.6 us in the kernel, 5.7 TB/s; 64 x 670000 x 768, which
-// also stores 86 MB: 127 us, 4.7 TB/s); many, the matrix pipe at the chip's power limit and what brings both operands through
+// Bound: few queries, the rows of Q from memory (1 x 131072 x 768: 16.4 us in the kernel, 6.1 TB/s; 64 x 670000 x 768, which
+// also stores 86 MB: 121 us, 5.0 TB/s); many, the matrix pipe at the chip's power limit and what brings both operands through
 // LDS (4096 x 100000 x 4096: 1.33 ms, 2.5 POP/s; the library's product of 8192^3 integers runs at 2.1).  Measured on 4096 x 131072 x
 // 768 to bf16 (us): tiles of 128 x 256, one a workgroup, 813; epilogue on packed conversions and scales held ready 670; 256 x 256
 // 602; persistent 570; stages brought in by half of the waves in turn, the others at their products already, 550; 16 x 16
