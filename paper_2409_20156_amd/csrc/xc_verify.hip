@@ -6,6 +6,8 @@
 // Bound: few sequences, dependent memory accesses (draft -> its two probabilities -> the row -> the chunk again) and launches:
 // 1 x 4 x 4096 fp32 5.0 us on the device, 8 x 5 x 131072 7.4 (two launches); a batch, the rows from memory: 256 x 4 x 131072 bf16 23 us
 // (110 MB, 4.8 TB/s).  First form, 8 elements of a chunk at a time and all of it by one workgroup of 4 waves: 27, 140 and 181 us.
+#include <type_traits>
+
 #include "xc_common.h"
 
 namespace xc {
@@ -134,19 +136,20 @@ struct Row {
     int64_t V;
     // the lane's elements of piece k of chunk c: 8 from here on
     static __device__ __forceinline__ int64_t first(int c, int k) { return static_cast<int64_t>(c) * kChunk + k * kPiece + lane_id() * 8; }
-    __device__ __forceinline__ void load(int c, int k, Octet<T>& x, Octet<T>& y) const {
+    template <bool DIFF> __device__ __forceinline__ void load(int c, int k, Octet<T>& x, Octet<T>& y) const {
         x.load(p, first(c, k), V);
-        if (kind == kDifference) y.load(q, first(c, k), V);          // uniform
+        if constexpr (DIFF) y.load(q, first(c, k), V);
     }
-    __device__ __forceinline__ void values(int c, int k, const Octet<T>& x, const Octet<T>& y, float (&f)[8], float (&g)[8]) const {
+    template <bool DIFF> __device__ __forceinline__ void values(int c, int k, const Octet<T>& x, const Octet<T>& y, float (&f)[8], float (&g)[8]) const {
         x.values(f);
-        if (kind == kDifference) {
+        if constexpr (DIFF) {
             y.values(g);
         } else {
+            const int64_t at = kind == kWithout ? without - first(c, k) : -1;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 g[i] = 0.0f;
-                if (kind == kWithout && first(c, k) + i == without) f[i] = 0.0f;
+                if (at == i) f[i] = 0.0f;
             }
         }
     }
@@ -162,17 +165,17 @@ __device__ __forceinline__ double sum8(const double (&w)[8]) {
 }
 
 // Sum of chunk c, the same in all lanes.
-template <typename T>
+template <bool DIFF, typename T>
 __device__ __forceinline__ double chunk_sum(const Row<T>& r, int c) {
     Octet<T> x[kPieces], y[kPieces];
 #pragma unroll
-    for (int k = 0; k < kPieces; ++k) r.load(c, k, x[k], y[k]);
+    for (int k = 0; k < kPieces; ++k) r.template load<DIFF>(c, k, x[k], y[k]);
     double s = 0.0;
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) {
         float f[8], g[8];
         double w[8];
-        r.values(c, k, x[k], y[k], f, g);
+        r.template values<DIFF>(c, k, x[k], y[k], f, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = fmax(static_cast<double>(f[i]) - static_cast<double>(g[i]), 0.0);         // (no number: 0)
         s += sum8(w);
@@ -183,14 +186,28 @@ __device__ __forceinline__ double chunk_sum(const Row<T>& r, int c) {
         for (int k = 0; k < kPieces; ++k) {
             float f[8], g[8];
             double w[8];
-            r.load(c, k, x[0], y[0]);
-            r.values(c, k, x[0], y[0], f, g);
+            r.template load<DIFF>(c, k, x[0], y[0]);
+            r.template values<DIFF>(c, k, x[0], y[0], f, g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = Row<T>::weight(f[i], g[i]);
             s += sum8(w);
         }
     }
     return of_lane(wave_incl_scan(s), kWave - 1);
+}
+
+// Sums of the chunks first, first + step, ..  The kind of weights is decided once: decided at every element it took 154 registers in place
+// of 108 (1000 x 20000 fp32 41 us, now 32).  More waves hide the memory's latency better than a chunk loaded ahead (254 registers: 46 us).
+template <typename T>
+__device__ __forceinline__ void chunk_sums(const Row<T>& r, double* sums, int first, int step, int n_chunks) {
+    auto go = [&](auto diff) __attribute__((always_inline)) {
+        for (int c = first; c < n_chunks; c += step) {
+            const double s = chunk_sum<decltype(diff)::value>(r, c);
+            if (lane_id() == 0) sums[c] = s;
+        }
+    };
+    if (r.kind == kDifference) go(std::true_type{});         // uniform
+    else go(std::false_type{});
 }
 
 // ---- the label drawn, by a workgroup of W waves from the chunks' sums: -1 if all weights are zero.
@@ -255,8 +272,13 @@ __device__ __forceinline__ int32_t draw_label(const Row<T>& r, const double* sum
     if (wave < kPieces) {
         Octet<T> x, y;
         float f[8], g[8];
-        r.load(chunk, wave, x, y);
-        r.values(chunk, wave, x, y, f, g);
+        if (r.kind == kDifference) {                         // uniform
+            r.template load<true>(chunk, wave, x, y);
+            r.template values<true>(chunk, wave, x, y, f, g);
+        } else {
+            r.template load<false>(chunk, wave, x, y);
+            r.template values<false>(chunk, wave, x, y, f, g);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) wt[i] = Row<T>::weight(f[i], g[i]);
         s = sum8(wt);
@@ -321,10 +343,7 @@ void verify_one_kernel(const VerifyArgs v) {
     Row<T> r = deciding_row<T>(v, b, j);
     int32_t drawn;
     for (;;) {
-        for (int c = wave; c < v.n_chunks; c += W) {
-            const double s = chunk_sum(r, c);
-            if (lane_id() == 0) sums[c] = s;
-        }
+        chunk_sums(r, sums, wave, W, v.n_chunks);
         __syncthreads();
         drawn = draw_label<T, W>(r, sums, v.n_chunks, u, sh);
         if (drawn >= 0 || r.kind == kTarget) break;          // uniform
@@ -343,10 +362,7 @@ void verify_sums_kernel(const VerifyArgs v) {
     if (c0 >= v.n_chunks) return;
     const Verdict j = judge<T>(v, b);
     const Row<T> r = deciding_row<T>(v, b, j);
-    for (int c = c0; c < v.n_chunks; c += step) {
-        const double s = chunk_sum(r, c);
-        if (lane_id() == 0) v.sums[b * v.n_chunks + c] = s;
-    }
+    chunk_sums(r, v.sums + b * v.n_chunks, c0, step, v.n_chunks);
     if (c0 == 0 && lane_id() == 0) v.verdicts[b] = make_int4(j.a, j.fell ? 1 : 0, j.x, 0);
 }
 template <typename T>
@@ -363,10 +379,7 @@ void verify_draw_kernel(const VerifyArgs v) {
     if (drawn < 0 && r.kind != kTarget) {                    // as above; so rare that one workgroup adds the row up
         r.kind = kTarget;
         __syncthreads();
-        for (int c = threadIdx.x >> 6; c < v.n_chunks; c += kDrawWaves) {
-            const double s = chunk_sum(r, c);
-            if (lane_id() == 0) sums[c] = s;
-        }
+        chunk_sums(r, sums, threadIdx.x >> 6, kDrawWaves, v.n_chunks);
         __syncthreads();
         drawn = draw_label<T, kDrawWaves>(r, sums, v.n_chunks, u, sh);
     }
