@@ -308,7 +308,8 @@ int xc_verify_drafts(const int32_t* drafts /* [B*n] */, int64_t B, int n, int64_
  * fmix, K1, K2 as in xc_sample_negatives, K3 = 0x64726F706F757431 (a step may use one
  * seed for its samples and its dropout).  The gradient of dropout is the same map with
  * the same rate, seed and row0, applied to the gradient.  The product is formed in
- * fp32 and rounded once.  X and Y may be the same array if their types are.
+ * fp32 and rounded once.  X and Y may be the same array if their types are; arrays
+ * that overlap otherwise are refused.
  * Requires B >= 1, 1 <= d < 2^31, B*d <= 2^40, rate >= 0, T <= 65535, row0 >= 0.
  * ------------------------------------------------------------------------- */
 int xc_dropout(const void* X /* [B*d] */, xc_dtype t, int64_t B, int64_t d, float rate, uint64_t seed,

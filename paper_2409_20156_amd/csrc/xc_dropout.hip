@@ -156,6 +156,8 @@ extern "C" int xc_dropout(const void* X, xc_dtype t, int64_t B, int64_t d, float
     const double least = std::floor(static_cast<double>(rate) * 65536.0 + 0.5);
     if (least > 65535.0) return XC_EINVAL;
     if (!X || !Y || !aligned16(X) || !aligned16(Y) || (X == Y && t != out_t)) return XC_EINVAL;
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(X), y0 = reinterpret_cast<uintptr_t>(Y), n = static_cast<uintptr_t>(B) * static_cast<uintptr_t>(d);
+    if (X != Y && x0 < y0 + n * (out_t == XC_F32 ? 4 : 2) && y0 < x0 + n * (t == XC_F32 ? 4 : 2)) return XC_EINVAL;      // they overlap
     hipStream_t st = static_cast<hipStream_t>(stream);
     const uint32_t m = static_cast<uint32_t>(least);
     if (t == XC_F32)

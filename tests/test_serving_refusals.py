@@ -75,6 +75,8 @@ def test_dropout(lib):
     assert call(row0=-1) == EINVAL
     assert call(X=None) == EINVAL and call(Y=None) == EINVAL and call(X=ODD) == EINVAL and call(Y=ODD) == EINVAL
     assert call(Y=P, out_t=1) == EINVAL                    # in place, but the types differ
+    assert call(X=ctypes.c_void_p(8192 - 128)) == EINVAL and call(X=ctypes.c_void_p(8192 + 128)) == EINVAL       # 144 bytes each: they overlap
+    assert call(X=ctypes.c_void_p(8192 + 64), out_t=1) == EINVAL and call(X=ctypes.c_void_p(8192 - 64), t=1) == EINVAL     # 72 bytes of bf16
 
 
 def test_binding_refuses_before_it_calls():
