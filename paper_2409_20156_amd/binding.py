@@ -7,6 +7,7 @@ of the same name.  Outputs and workspaces are allocated with torch.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -443,6 +444,16 @@ def verify_drafts(drafts: torch.Tensor, target: torch.Tensor, draft_probs: torch
             _at(u, torch.float32, "u"), _at(tokens, torch.int32, "tokens"), _at(accepted, torch.int32, "accepted"),
             _at(workspace, torch.uint8, "workspace"), workspace.numel())
     return out
+
+
+def dropout_least(rate: float) -> int:
+    """Of the 65536 values of an element's random bits, how many drop it: the rate (as fp32) to the nearest 1/65536."""
+    if not 0.0 <= rate < 1.0:
+        raise ValueError("a dropout rate must lie in [0, 1)")
+    least = math.floor(_f32(rate).value * 65536 + 0.5)
+    if least > 65535:
+        raise ValueError("a dropout rate may be at most 65535/65536 when rounded to the nearest 1/65536, got %r" % rate)
+    return least
 
 
 def dropout(X: torch.Tensor, rate: float, seed: int, *, row0: int = 0, dtype: torch.dtype | None = None,

@@ -13,7 +13,8 @@ does not depend on timing.
 
 With dropout > 0 a step trains on its batch of embeddings with elements dropped, as they come out of the encoder's last layer in
 training, and the dZ it returns is the gradient for the embeddings before that.  The searches see them whole.  The mask is a
-function of the step's seed, so nothing is stored and a resumed schedule drops the same elements.
+function of the step's seed, so nothing is stored and a resumed schedule drops the same elements.  Rates that round to 1 at
+the kernel's 1/65536 are refused when the schedule is made.
 """
 from __future__ import annotations
 
@@ -26,8 +27,7 @@ class Schedule:
     def __init__(self, Z_pool: torch.Tensor, W: torch.Tensor, pos_pool: torch.Tensor, B: int, k_h: int,
                  k_r: int, tau_s: int, tau_r: int, lr: float, kind: int = xc.XC_LOSS_BCE, lag: int = 0,
                  warm_margin: float | None = None, dropout: float = 0.0):
-        if not 0.0 <= dropout < 1.0:
-            raise ValueError("dropout must lie in [0, 1)")
+        xc.dropout_least(dropout)                      # refuses what a step would refuse, before anything is allocated
         if lag < 0 or (lag > 0 and lag > tau_r):
             raise ValueError("lag must lie in [0, tau_r]")
         self.Z, self.W, self.pos = Z_pool, W, pos_pool
