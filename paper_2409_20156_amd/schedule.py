@@ -78,7 +78,7 @@ class Schedule:
     def state_dict(self):
         """Everything a later `load_state_dict` needs to go on from here with the same results: the step
         counter, both shortlist buffers and which of them is active, built or waiting to take over, and a
-        copy of W.  A search still running on the second stream is waited for first (its takeover step is kept),
+        copy of W, and the dropout rate.  A search still running on the second stream is waited for first (its takeover step is kept),
         so the call synchronises.  The search thresholds are not part of it: the first refresh after a resume
         starts from scratch, which returns the same shortlists as one started from earlier thresholds."""
         if self.pending is not None:
@@ -86,11 +86,16 @@ class Schedule:
         torch.cuda.synchronize(self.W.device)
         return {"t": self.t, "cur": self.cur, "built": self.built, "had_previous": self.had_previous,
                 "pending": None if self.pending is None else (self.pending[0], self.pending[1]),
+                "dropout": self.dropout,
                 "full_repeats": int(self.full_repeats.item()),
                 "shortlist": [s.cpu().clone() for s in self.shortlist], "W": self.W.cpu().clone()}
 
     def load_state_dict(self, sd):
-        """Back to the state `state_dict` saved (same pool, shapes and schedule parameters); W is overwritten."""
+        """Back to the state `state_dict` saved (same pool, shapes and schedule parameters); W is overwritten.
+        Another dropout rate would go on with another mask and scale: refused, as are shapes that do not fit (a state
+        without a rate was saved by a schedule without dropout)."""
+        if xc.dropout_least(sd.get("dropout", 0.0)) != xc.dropout_least(self.dropout):
+            raise ValueError("the saved state has dropout %r, this schedule %r" % (sd.get("dropout", 0.0), self.dropout))
         if tuple(sd["W"].shape) != tuple(self.W.shape) or sd["W"].dtype != self.W.dtype:
             raise ValueError("the saved W does not fit this schedule")
         if any(tuple(a.shape) != tuple(b.shape) for a, b in zip(sd["shortlist"], self.shortlist)):

@@ -76,3 +76,24 @@ def test_dropout_outside_its_range_is_refused():
     for rate in (-0.1, 1.0, float("nan")):
         with pytest.raises(ValueError):
             Schedule(Z, W, torch.tensor(pos, device=DEV), B, k_h, k_r, TAU_S, TAU_R, LR, dropout=rate)
+
+
+@pytest.mark.parametrize("rate", [0.0, RATE])
+def test_the_rate_is_saved_and_states_without_one_are_those_of_schedules_without_dropout(rate):
+    from paper_2409_20156_amd.schedule import Schedule
+    W, Z, pos = _inputs()
+    make = lambda r: Schedule(Z, W, torch.tensor(pos, device=DEV), B, k_h, k_r, TAU_S, TAU_R, LR, dropout=r)  # noqa: E731
+    sch = make(rate)
+    sch.step(5)
+    saved = sch.state_dict()
+    assert saved["dropout"] == rate
+    sch.load_state_dict(saved)
+    assert sch.t == 1
+    with pytest.raises(ValueError, match="dropout"):
+        make(0.5).load_state_dict(saved)
+    del saved["dropout"]
+    if rate == 0.0:
+        sch.load_state_dict(saved)                         # as saved before there was a rate
+    else:
+        with pytest.raises(ValueError, match="dropout"):
+            sch.load_state_dict(saved)
