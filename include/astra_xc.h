@@ -293,6 +293,8 @@ int xc_scores_quantized(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,
  * draft i stands if u[b,i] < target[b,i,x_i], and w_v of a fallen one is the
  * target's without x_a.
  * Requires B >= 1, 0 <= n <= XC_MAX_DRAFTS, 1 <= V < 2^31; drafts may be NULL if n = 0.
+ * tokens, accepted and the workspace may overlap neither each other nor an input
+ * (XC_EINVAL).
  * ------------------------------------------------------------------------- */
 int xc_verify_workspace(int64_t B, int64_t V, size_t* bytes);
 int xc_verify_drafts(const int32_t* drafts /* [B*n] */, int64_t B, int n, int64_t V,

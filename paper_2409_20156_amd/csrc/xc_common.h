@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <initializer_list>
+
 #include "astra_xc.h"
 
 namespace xc {
@@ -43,6 +45,22 @@ void profile_mark(int kernel_id, hipStream_t st, bool begin);
     } while (0)
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Arrays of a call by address and size: those it writes may overlap neither each other nor what it reads.
+struct Span {
+    uintptr_t begin, end;
+    Span(const void* p, unsigned __int128 bytes) : begin(reinterpret_cast<uintptr_t>(p)), end(begin) {
+        if (p != nullptr) end = bytes < UINTPTR_MAX - begin ? begin + static_cast<uintptr_t>(bytes) : UINTPTR_MAX;
+    }
+    bool meets(const Span& o) const { return begin < end && o.begin < o.end && begin < o.end && o.begin < end; }
+};
+inline bool overlap(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+    for (const Span* w = written.begin(); w != written.end(); ++w) {
+        for (const Span* o = w + 1; o != written.end(); ++o) if (w->meets(*o)) return true;
+        for (const Span& r : read) if (w->meets(r)) return true;
+    }
+    return false;
+}
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // ---- element types ----------------------------------------------------------

@@ -447,6 +447,12 @@ extern "C" int xc_verify_drafts(const int32_t* drafts, int64_t B, int n, int64_t
         !aligned16(accepted) || !aligned16(ws))
         return XC_EINVAL;
     if (ws_bytes < verify_bytes(B, V)) return XC_EWORKSPACE;
+    // (a workgroup writes a sequence's labels while others have yet to read theirs)
+    const unsigned __int128 rows = static_cast<unsigned __int128>(B) * V * (t == XC_F32 ? 4 : 2);
+    const size_t ids = static_cast<size_t>(B) * 4;
+    if (overlap({Span(tokens, ids * (n + 1)), Span(accepted, ids), Span(ws, verify_bytes(B, V))},
+                {Span(drafts, ids * n), Span(u, ids * (n + 1)), Span(target, rows * (n + 1)), Span(draft_probs, rows * n)}))
+        return XC_EINVAL;
     int4* verdicts = static_cast<int4*>(ws);
     const VerifyArgs v{drafts, target, draft_probs, u, tokens, accepted, verdicts, reinterpret_cast<double*>(verdicts + B), V, n, verify_chunks(V)};
     hipStream_t st = static_cast<hipStream_t>(stream);

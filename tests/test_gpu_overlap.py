@@ -1,0 +1,35 @@
+"""Arrays that lie one behind the other in one allocation do not overlap: the calls take them and give what they give elsewhere."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _pack(*tensors):
+    """Copies of the tensors back to back (each from a multiple of 16 bytes on) in one allocation."""
+    size = [(t.numel() * t.element_size() + 15) // 16 * 16 for t in tensors]
+    flat, at, out = torch.zeros(sum(size), dtype=torch.uint8, device=DEV), 0, []
+    for t, n in zip(tensors, size):
+        v = flat[at:at + t.numel() * t.element_size()].view(t.dtype).view(t.shape)
+        v.copy_(t)
+        out.append(v)
+        at += n
+    return out
+
+
+@pytest.mark.parametrize("B,n,V", [(4, 3, 16), (8, 3, 40000), (2, 0, 64)])
+def test_verify(B, n, V):
+    import paper_2409_20156_amd as xc
+    g = torch.Generator(device=DEV).manual_seed(B + V)
+    p, q = (torch.rand((B, n + 1, V), device=DEV, generator=g), torch.rand((B, n, V), device=DEV, generator=g))
+    x, u = torch.randint(0, V, (B, n), device=DEV, generator=g, dtype=torch.int32), torch.rand((B, n + 1), device=DEV, generator=g)
+    want = xc.verify_drafts(x, p, q, u)
+    ws = torch.zeros(xc.verify_workspace(B, V), dtype=torch.uint8, device=DEV)
+    x2, tokens, p2, accepted, q2, ws2, u2 = _pack(x, torch.zeros_like(want[0]), p, torch.zeros_like(want[1]), q, ws, u)
+    got = xc.verify_drafts(x2, p2, q2, u2, workspace=ws2, out=(tokens, accepted))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    if n:
+        with pytest.raises(xc.XcError):
+            flat = torch.zeros((B * (n + 1),), dtype=torch.int32, device=DEV)
+            xc.verify_drafts(flat[:B * n].view(B, n), p, q, u, out=(flat.view(B, n + 1), want[1]))
