@@ -251,7 +251,8 @@ int xc_step_static(const void* Z /* [B*d] */, void* W /* [L*d], updated in place
  * if count (device memory) is not NULL, for example the `touched` and `n_touched`
  * of the step that changed them; ids outside [0,N) are ignored, an id may occur
  * several times, the other rows of Q and scale keep their values.
- * Requires N >= 1, m >= 0, d*sizeof(element) a multiple of 16, d <= XC_MAX_D_QUANTIZED.
+ * Requires N >= 1, m >= 0, d*sizeof(element) a multiple of 16, d <= XC_MAX_D_QUANTIZED;
+ * Q and scale may overlap neither each other nor an input (XC_EINVAL).
  * ------------------------------------------------------------------------- */
 int xc_quantize_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
                      const int32_t* ids /* [m] or NULL */, int64_t m, const int32_t* count /* [1] or NULL */,
@@ -266,7 +267,8 @@ int xc_quantize_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
  * classifier (or for a contiguous range of its rows).  The workspace holds the
  * integers of Z; it is written before it is read.
  * A score does not depend on how many queries or labels are scored with it, bit for bit.
- * Requires B >= 1, 1 <= L < 2^31, B*L <= 2^40, d as above.
+ * Requires B >= 1, 1 <= L < 2^31, B*L <= 2^40, d as above; out and the workspace may
+ * overlap neither each other nor an input (XC_EINVAL).
  * ------------------------------------------------------------------------- */
 int xc_scores_workspace(int64_t B, int d, size_t* bytes);
 int xc_scores_quantized(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,

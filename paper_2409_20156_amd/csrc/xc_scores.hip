@@ -204,7 +204,6 @@ static void launch_quantize_kernel(const unsigned char* X, int64_t N, int d, con
 
 static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const int32_t* ids, int64_t m, const int32_t* count,
                            int8_t* Q, int pitch, float* scale, hipStream_t st) {
-    if (ids != nullptr && m == 0) return XC_OK;
     const unsigned char* x = static_cast<const unsigned char*>(X);
     if (t == XC_F32) XC_LAUNCH(K_QUANTIZE, st, launch_quantize_kernel<float>(x, N, d, ids, m, count, Q, pitch, scale, st));
     else XC_LAUNCH(K_QUANTIZE, st, launch_quantize_kernel<bf16_t>(x, N, d, ids, m, count, Q, pitch, scale, st));
@@ -864,6 +863,11 @@ extern "C" int xc_quantize_rows(const void* X, int64_t N, int d, xc_dtype t, con
     if (N < 1 || N > (1LL << 40) || !row_ok(d, t) || m < 0 || m > (1LL << 40)) return XC_ESHAPE;
     if (!X || !Q || !scale || !aligned16(X) || !aligned16(Q) || !aligned16(scale) || !aligned16(ids) || !aligned16(count)) return XC_EINVAL;
     if (ids == nullptr && count != nullptr) return XC_EINVAL;
+    if (ids != nullptr && m == 0) return XC_OK;
+    const unsigned __int128 rows = N;
+    if (overlap({Span(Q, rows * quantized_pitch(d)), Span(scale, rows * 4)},
+                {Span(X, rows * d * (t == XC_F32 ? 4 : 2)), Span(ids, static_cast<unsigned __int128>(m) * 4), Span(count, 4)}))
+        return XC_EINVAL;
     return launch_quantize(X, N, d, t, ids, m, count, Q, quantized_pitch(d), scale, static_cast<hipStream_t>(stream));
 }
 
@@ -883,6 +887,10 @@ extern "C" int xc_scores_quantized(const void* Z, int64_t B, int d, xc_dtype t, 
     if (!Z || !Q || !scale || !out || !ws) return XC_EINVAL;
     if (!aligned16(Z) || !aligned16(Q) || !aligned16(scale) || !aligned16(out) || !aligned16(ws)) return XC_EINVAL;
     if (ws_bytes < scores_bytes(B, d)) return XC_EWORKSPACE;
+    const size_t queries = static_cast<size_t>(B), labels = static_cast<size_t>(L);
+    if (overlap({Span(out, queries * labels * (out_t == XC_F32 ? 4 : 2)), Span(ws, scores_bytes(B, d))},
+                {Span(Z, queries * d * (t == XC_F32 ? 4 : 2)), Span(Q, labels * quantized_pitch(d)), Span(scale, labels * 4)}))
+        return XC_EINVAL;
     hipStream_t st = static_cast<hipStream_t>(stream);
     float* pscale = static_cast<float*>(ws);
     int8_t* P = static_cast<int8_t*>(ws) + round_up(B, kQueryTile) * 4;

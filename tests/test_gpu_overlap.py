@@ -33,3 +33,19 @@ def test_verify(B, n, V):
         with pytest.raises(xc.XcError):
             flat = torch.zeros((B * (n + 1),), dtype=torch.int32, device=DEV)
             xc.verify_drafts(flat[:B * n].view(B, n), p, q, u, out=(flat.view(B, n + 1), want[1]))
+
+
+@pytest.mark.parametrize("B,L,d", [(3, 100, 64), (40, 3000, 72)])
+def test_rows_in_8_bits_and_their_scores(B, L, d):
+    import paper_2409_20156_amd as xc
+    g = torch.Generator(device=DEV).manual_seed(B + L)
+    Z, W = (torch.randn((n, d), device=DEV, generator=g).bfloat16() for n in (B, L))
+    Q, s = xc.quantize_rows(W)
+    want = xc.scores_quantized(Z, Q, s)
+    ws = torch.zeros(xc.scores_workspace(B, d), dtype=torch.uint8, device=DEV)
+    s2, W2, Q2, out, Z2, ws2 = _pack(torch.zeros_like(s), W, torch.zeros_like(Q), torch.zeros_like(want), Z, ws)
+    xc.quantize_rows(W2, out=(Q2, s2))
+    xc.scores_quantized(Z2, Q2, s2, workspace=ws2, out=out)
+    assert torch.equal(Q2, Q) and torch.equal(s2, s) and torch.equal(out, want)
+    with pytest.raises(xc.XcError):
+        xc.quantize_rows(W2, out=(W2.view(torch.int8).view(-1)[:Q.numel()].view(Q.shape), s2))

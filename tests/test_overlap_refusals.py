@@ -53,3 +53,23 @@ def test_verify(lib, t, B, n, V, with_draft):
         rc = lib.xc_verify_drafts(at["drafts"] if n else None, B, n, V, at["target"], at["draft"] if with_draft else None, t, at["u"],
                                   at["tokens"], at["accepted"], at["ws"], need, None)
         assert rc == EINVAL, (w, o)
+
+
+@pytest.mark.parametrize("t,N,d", [(0, 100, 60), (1, 100, 72), (1, 1, 8), (1, 5, 20000)])
+@pytest.mark.parametrize("m,counted", [(0, False), (7, False), (50, True)])
+def test_quantize_rows(lib, t, N, d, m, counted):
+    pitch = (d + 15) // 16 * 16
+    sizes = {"Q": N * pitch, "scale": N * 4, "X": N * d * (2 if t else 4), "ids": m * 4, "count": 4 if counted else 0}
+    for w, o, at in _overlaps(sizes, ("Q", "scale")):
+        rc = lib.xc_quantize_rows(at["X"], N, d, t, at["ids"] if m else None, m, at["count"] if counted else None, at["Q"], at["scale"], None)
+        assert rc == EINVAL, (w, o)
+
+
+@pytest.mark.parametrize("t,out_t", [(0, 0), (0, 1), (1, 0), (1, 1)])
+@pytest.mark.parametrize("B,d,L", [(3, 72, 1000), (40, 72, 1000), (300, 4096, 7), (1, 8, 1)])
+def test_scores(lib, t, out_t, B, d, L):
+    need = _need(lib.xc_scores_workspace, B, d)
+    sizes = {"out": B * L * (2 if out_t else 4), "ws": need, "Z": B * d * (2 if t else 4), "Q": L * ((d + 15) // 16 * 16), "scale": L * 4}
+    for w, o, at in _overlaps(sizes, ("out", "ws")):
+        rc = lib.xc_scores_quantized(at["Z"], B, d, t, at["Q"], at["scale"], L, out_t, at["out"], at["ws"], need, None)
+        assert rc == EINVAL, (w, o)
