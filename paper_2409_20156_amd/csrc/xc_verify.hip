@@ -405,18 +405,18 @@ static void launch_verify(const VerifyArgs& v, int64_t B, hipStream_t st) {
         p.verdicts += b0;
         p.sums += b0 * v.n_chunks;
         if (alone == 4) {
-            verify_one_kernel<T, 4><<<static_cast<unsigned>(nb), 4 * kWave, 0, st>>>(p);
+            XC_LAUNCH(K_VERIFY, st, (verify_one_kernel<T, 4><<<static_cast<unsigned>(nb), 4 * kWave, 0, st>>>(p)));
             continue;
         }
         if (alone == 8) {
-            verify_one_kernel<T, 8><<<static_cast<unsigned>(nb), 8 * kWave, 0, st>>>(p);
+            XC_LAUNCH(K_VERIFY, st, (verify_one_kernel<T, 8><<<static_cast<unsigned>(nb), 8 * kWave, 0, st>>>(p)));
             continue;
         }
         // as many chunks to a wave as leave the device full
         const int64_t wide = (v.n_chunks + kDrawWaves - 1) / kDrawWaves, most = kSumGrid / nb > 0 ? kSumGrid / nb : 1;
         const int64_t rounds = (wide + most - 1) / most, gx = (wide + rounds - 1) / rounds;
-        verify_sums_kernel<T><<<dim3(static_cast<unsigned>(gx), static_cast<unsigned>(nb)), kVerifyThreads, 0, st>>>(p);
-        verify_draw_kernel<T><<<static_cast<unsigned>(nb), kVerifyThreads, 0, st>>>(p);
+        XC_LAUNCH(K_VERIFY_SUMS, st, (verify_sums_kernel<T><<<dim3(static_cast<unsigned>(gx), static_cast<unsigned>(nb)), kVerifyThreads, 0, st>>>(p)));
+        XC_LAUNCH(K_VERIFY, st, (verify_draw_kernel<T><<<static_cast<unsigned>(nb), kVerifyThreads, 0, st>>>(p)));
     }
 }
 
@@ -456,8 +456,8 @@ extern "C" int xc_verify_drafts(const int32_t* drafts, int64_t B, int n, int64_t
     int4* verdicts = static_cast<int4*>(ws);
     const VerifyArgs v{drafts, target, draft_probs, u, tokens, accepted, verdicts, reinterpret_cast<double*>(verdicts + B), V, n, verify_chunks(V)};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (t == XC_F32) XC_LAUNCH(K_VERIFY, st, launch_verify<float>(v, B, st));
-    else XC_LAUNCH(K_VERIFY, st, launch_verify<bf16_t>(v, B, st));
+    if (t == XC_F32) launch_verify<float>(v, B, st);
+    else launch_verify<bf16_t>(v, B, st);
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }

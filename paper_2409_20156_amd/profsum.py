@@ -37,7 +37,7 @@ KERNELS = {"mine_tile_kernel": "mine_tile", "mine_rows_kernel": "mine_tile", "mi
            "bucket_sort_kernel": "bucket_sort",
            "heads_count_kernel": "heads_count", "heads_write_kernel": "heads_write",
            "update_kernel": "update", "quantize_kernel": "quantize", "scores_kernel": "scores", "scores_held_kernel": "scores",
-           "verify_one_kernel": "verify", "verify_sums_kernel": "verify", "verify_draw_kernel": "verify", "dropout_kernel": "dropout",
+           "verify_one_kernel": "verify", "verify_sums_kernel": "verify_sums", "verify_draw_kernel": "verify", "dropout_kernel": "dropout",
            "copy_probe_kernel": "copy_probe", "mfma_probe_kernel": "mfma_probe"}
 
 kXcds, kSimds = 8, 1024          # MI355X: one GRBM per XCD; 256 CUs x 4 SIMDs

@@ -229,3 +229,20 @@ def test_refusals_on_the_device():
         xc.verify_drafts(x, p, q, u, workspace=torch.empty(0, dtype=torch.uint8, device=DEV))
     with pytest.raises(xc.XcError):
         xc.verify_drafts(x[1:], p[1:], q[1:], u[1:])       # rows from addresses that are no multiples of 16
+
+
+@pytest.mark.parametrize("B,V,verify,sums", [(5, 3000, 1, 0), (3, 20000, 1, 0), (200, 40000, 1, 0), (3, 40000, 1, 1), (70000, 2, 2, 0)])
+def test_event_timing_counts_every_launch(B, V, verify, sums):
+    import paper_2409_20156_amd as xc
+    from paper_2409_20156_amd import binding
+    p, u = torch.rand((B, 2, V), device=DEV).to(BF16), torch.rand((B, 2), device=DEV)
+    x = torch.zeros((B, 1), dtype=torch.int32, device=DEV)
+    binding.profile_reset()
+    binding.profile_enable(True)
+    try:
+        xc.verify_drafts(x, p, None, u)
+    finally:
+        binding.profile_enable(False)
+    prof = binding.profile_collect()
+    binding.profile_reset()
+    assert {k: n for k, (_, n) in prof.items() if n} == {k: n for k, n in (("verify", verify), ("verify_sums", sums)) if n}
