@@ -459,7 +459,11 @@ def dropout_least(rate: float) -> int:
 def dropout(X: torch.Tensor, rate: float, seed: int, *, row0: int = 0, dtype: torch.dtype | None = None,
             out: torch.Tensor | None = None) -> torch.Tensor:
     """X [B, d] with elements dropped (set to zero) at `rate`, to the nearest 1/65536, and the others scaled up so that the
-    mean stays; a function of (seed, row0 + row, column).  fp32 or bf16, by `out`, `dtype` or X; out may be X."""
+    mean stays; a function of (seed, row0 + row, column).  fp32 or bf16, by `out`, `dtype` or X; out may be X.
+
+    As all calls here it leaves no trace in autograd, also where X requires a gradient: the result has no graph.  The gradient
+    goes back by hand, `X.backward(dropout_grad(dY, ...))` into the encoder that made X; out=X only if no backward pass to come
+    reads X (autograd does not see that it changed)."""
     lib = load_library()
     code = _dtype_code(X)
     if X.dim() != 2:

@@ -142,3 +142,21 @@ def test_another_stream_and_a_replayed_graph():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_an_encoder_gets_its_gradient_by_hand():
+    """No call records anything for autograd; the gradient of a loss that is linear in the dropped embeddings, put into the encoder by
+    hand, is what autograd gives through a mask written out.  Entries are small integers and the kept are doubled: sums are exact."""
+    import paper_2409_20156_amd as xc
+    g = torch.Generator().manual_seed(6)
+    x, A, C = (torch.randint(-8, 9, s, generator=g).float() for s in ((12, 20), (20, 24), (12, 24)))
+    keep = torch.tensor(so.dropout_kept(12, 24, 0.5, 9))
+    ref = A.clone().requires_grad_()
+    (C * ((x @ ref) * 2.0 * keep)).sum().backward()
+    enc = A.to(DEV).requires_grad_()
+    Z = x.to(DEV) @ enc
+    Zd = xc.dropout(Z, 0.5, 9)
+    assert Z.requires_grad and not Zd.requires_grad and Zd.grad_fn is None
+    assert torch.equal(Zd.cpu(), (x @ A) * 2.0 * keep)
+    Z.backward(xc.dropout_grad(C.to(DEV), 0.5, 9))
+    assert torch.equal(enc.grad.cpu(), ref.grad)
