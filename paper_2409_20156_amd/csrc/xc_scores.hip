@@ -1,6 +1,7 @@
 // Rows in 8 bits, and the scores of all labels from them: out = (<p, q> a) b with integers p, q and a scale per row on
 // either side.  The integer sums are exact, so their order (and how the work is cut) cannot change a score.
 #include "xc_mine.h"
+#include "xc_scores_choice.h"
 
 namespace xc {
 
@@ -551,6 +552,11 @@ typedef Tile<1, 4, 2, 2, 3, 1> TileFew;             // 32 x 128
 typedef Tile<1, 1, 2, 2, 4, 1> TileNarrow;          // 32 x 32
 typedef Tile<1, 1, 1, 1, 4, 1> TileThin;            // 16 x 16
 typedef Tile<1, 4, 1, 2, 4, 1, 768> TileOnline;     // 16 x 128, queries of up to 768 bytes resident
+template <typename T, int BM, int BN> constexpr bool tile_is() { return T::BM == BM && T::BN == BN; }
+static_assert(tile_is<TileMany, 256, 256>() && tile_is<TileMid, 128, 128>() && tile_is<TileSmall, 64, 64>() && tile_is<TileLow, 64, 32>() &&
+              tile_is<TileSome, 64, 128>() && tile_is<TileFew, 32, 128>() && tile_is<TileNarrow, 32, 32>() && tile_is<TileThin, 16, 16>() &&
+              tile_is<TileOnline, kOnlineQueries, 128>() && TileOnline::RES == kOnlineBytes && kScoresUnits == kMineGrid && kScoresXcds == kXcds,
+              "what choose_scores counts");
 constexpr int kQueryPad = 128;                           // the queries in the workspace: rows of whole stages,
 constexpr int kQueryTile = 256;                          // whole tiles of them of any kind
 
@@ -586,7 +592,6 @@ struct Held {
     static constexpr int kLds = R * (kStage + 256);
     static_assert(kLoads * 8 * 1024 == kStage && R >= 3 && (kLoads + kStores) * (R - 3) < 64, "whole loads, and a count that the wait can hold");
 };
-constexpr int kHeldLabels = 512, kHeldBytes = 768;
 constexpr int kHeldPieces = 4;                           // of the tiles behind the last whole round, to a workgroup
 
 template <typename TO, int NK>
@@ -801,45 +806,21 @@ static void run_held(const ScoresArgs& a, hipStream_t st) {
     }
 }
 
-// Which kernel.  Measured with rows of Q from memory (us, scores alone, on the sides of each rule):
-//   up to 32 queries   32 x 128; fewer labels than 256 such tiles 32 x 32, and up to 16 queries or 256 of those 16 x 16: a compute unit
-//                      keeps only so many lines of memory under way, so a short call wants many of them at it (32 x 30000 x 4096: 31,
-//                      38 with 16 x 16; 32 x 6000 x 4096: 24 and 14; 12 x 10000 x 4096: 23 and 15, with 32 x 128 24)
-//   up to 512 tiles of 64 x 64   these; up to 256 of 64 x 32 those (128 x 16000 x 768: 8.5 against 10.0 with 128 x 128 and 12 with 64 x 32;
-//                      400 x 4000 x 4096: 25, 35 and 34; 128 x 4000 x 4096: 21, with 64 x 32 16)
-//   up to 64 queries   64 x 128 (64 x 300000 x 768: 59; 128 x 128 70, 64 x 64 62)
-//   more than 1792 tiles of 128 x 128, rows of up to 768 bytes and more than 384 queries, or up to 384 and 128   labels held in registers
-//                      (4096 x 131072 x 768 to bf16: 360; 256 x 256 tiles 545; 700 x 74141 x 768: 67, 128 x 128 tiles 74; 340 x 526924 x
-//                      320: 143 and 168; 700 x 34200 x 768, 1608 tiles: 43 and 36; 340 x 188544 x 512: 83 and 72)
-//   else 128 x 128 tiles or, beyond 192 queries, 256 x 256 where that takes fewer rounds for its larger tiles (to bf16 512 x 209651 x
-//                      1024: 137 against 185; 1000 x 93139 x 4096: 338 against 428; 256 x 188816 x 512: 44 against 56; 800 x
-//                      17762 x 1536: 51 against 34, so not there; 130 x 141461 x 800: 71 against 55).  Short rows beyond 256 queries
-//                      are no longer worth it (300 x 87520 x 384: 37 against 29).
 template <typename TO>
-static void run_scores(const ScoresArgs& a, hipStream_t st) {
-    auto tiles = [&](int m, int n) { return (a.B + m - 1) / m * ((a.L + n - 1) / n); };
-    if (a.B <= 32) {
-        if (tiles(32, 128) >= kMineGrid) launch_scores<TO, TileFew>(a, st);
-        else if (a.B <= 16 || tiles(32, 32) <= kMineGrid) launch_scores<TO, TileThin>(a, st);
-        else launch_scores<TO, TileNarrow>(a, st);
-    } else if (tiles(64, 32) <= kMineGrid) {
-        launch_scores<TO, TileLow>(a, st);
-    } else if (tiles(64, 64) <= 2 * kMineGrid) {
-        launch_scores<TO, TileSmall>(a, st);
-    } else if (a.B <= 64) {
-        launch_scores<TO, TileSome>(a, st);
-    } else if (a.B > 128 && a.ppitch <= (a.B > 384 ? kHeldBytes : kHeldBytes / 2) && tiles(128, 128) > 7 * kMineGrid) {
-        run_held<TO>(a, st);
-    } else {
-        const int64_t mid = (tiles(128, 128) + 2 * kMineGrid - 1) / (2 * kMineGrid), many = (tiles(256, 256) + kMineGrid - 1) / kMineGrid;
-        if (a.B <= 192 || (a.ppitch <= kHeldBytes && a.B > 256) || 5 * mid <= 8 * many) launch_scores<TO, TileMid>(a, st);
-        else launch_scores<TO, TileMany>(a, st);
+static void run_scores(const ScoresArgs& a, ScoresKernel kernel, hipStream_t st) {
+    switch (kernel) {
+        case kScoresThin: launch_scores<TO, TileThin>(a, st); break;
+        case kScoresNarrow: launch_scores<TO, TileNarrow>(a, st); break;
+        case kScoresFew: launch_scores<TO, TileFew>(a, st); break;
+        case kScoresLow: launch_scores<TO, TileLow>(a, st); break;
+        case kScoresSmall: launch_scores<TO, TileSmall>(a, st); break;
+        case kScoresSome: launch_scores<TO, TileSome>(a, st); break;
+        case kScoresMid: launch_scores<TO, TileMid>(a, st); break;
+        case kScoresMany: launch_scores<TO, TileMany>(a, st); break;
+        default: run_held<TO>(a, st); break;
     }
 }
 
-// Up to 16 queries on rows of up to 768 bytes: one launch, every workgroup brings the queries to integers for itself (1 x 131072 x
-// 768: 18.3 us a call, 21.0 with a launch of their own; 1 x 4000 x 768: 8.0 and 10.8; 16 x 131072 x 768: 23.5 and 24.2; with
-// tiles of 32, 32 x 131072 x 768: 29.9 and 26.3, so not beyond 16).
 template <typename TZ>
 static void run_few(const ScoresArgs& a, xc_dtype out_t, hipStream_t st) {
     if (out_t == XC_F32) launch_scores<float, TileOnline, TZ>(a, st);
@@ -896,14 +877,15 @@ extern "C" int xc_scores_quantized(const void* Z, int64_t B, int d, xc_dtype t, 
     int8_t* P = static_cast<int8_t*>(ws) + round_up(B, kQueryTile) * 4;
     const int ppitch = static_cast<int>(round_up(d, kQueryPad));
     const ScoresArgs a{static_cast<const unsigned char*>(Z), d, P, pscale, Q, scale, out, B, L, quantized_pitch(d), ppitch, 0, 0, 0};
-    if (B <= TileOnline::BM && ppitch <= TileOnline::RES) {
+    const ScoresKernel kernel = choose_scores(B, L, ppitch);
+    if (kernel == kScoresOnline) {
         if (t == XC_F32) XC_LAUNCH(K_SCORES, st, run_few<float>(a, out_t, st));
         else XC_LAUNCH(K_SCORES, st, run_few<bf16_t>(a, out_t, st));
     } else {
         const int rc = launch_quantize(Z, B, d, t, nullptr, 0, nullptr, P, ppitch, pscale, st);
         if (rc != XC_OK) return rc;
-        if (out_t == XC_F32) XC_LAUNCH(K_SCORES, st, run_scores<float>(a, st));
-        else XC_LAUNCH(K_SCORES, st, run_scores<bf16_t>(a, st));
+        if (out_t == XC_F32) XC_LAUNCH(K_SCORES, st, run_scores<float>(a, kernel, st));
+        else XC_LAUNCH(K_SCORES, st, run_scores<bf16_t>(a, kernel, st));
     }
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
