@@ -877,7 +877,7 @@ extern "C" int xc_scores_quantized(const void* Z, int64_t B, int d, xc_dtype t, 
     int8_t* P = static_cast<int8_t*>(ws) + round_up(B, kQueryTile) * 4;
     const int ppitch = static_cast<int>(round_up(d, kQueryPad));
     const ScoresArgs a{static_cast<const unsigned char*>(Z), d, P, pscale, Q, scale, out, B, L, quantized_pitch(d), ppitch, 0, 0, 0};
-    const ScoresKernel kernel = choose_scores(B, L, ppitch);
+    const ScoresKernel kernel = choose_scores(B, L, ppitch, out_t == XC_F32 ? 4 : 2);
     if (kernel == kScoresOnline) {
         if (t == XC_F32) XC_LAUNCH(K_SCORES, st, run_few<float>(a, out_t, st));
         else XC_LAUNCH(K_SCORES, st, run_few<bf16_t>(a, out_t, st));

@@ -15,7 +15,7 @@ CASES = {  # kernel -> (queries, labels, elements of a row)
     "low": [(33, 8000, 200), (128, 4000, 2048), (300, 1601, 72)],
     "small": [(40, 20001, 136), (128, 16000, 768), (500, 4001, 1032), (64, 32768, 64)],
     "some": [(64, 40000, 768), (33, 40001, 72), (47, 33001, 776), (64, 70000, 128), (60, 33001, 128)],
-    "held": [(137, 131072, 128), (9600, 3549, 64), (10000, 3549, 768), (8400, 4100, 384), (4137, 8155, 136), (385, 90001, 600)],
+    "held": [(137, 131072, 128), (9600, 3549, 64), (10000, 3549, 768), (8400, 4095, 384), (4137, 8155, 136), (385, 90001, 600)],
     "mid": [(100, 40000, 768), (128, 33000, 128), (65, 33001, 24), (100, 33001, 200), (300, 60000, 200), (128, 70001, 1032)],
     "many": [(256, 40000, 64), (200, 60001, 24), (256, 40003, 128), (193, 64001, 800), (600, 17000, 800)],
 }
@@ -42,3 +42,10 @@ def test_bits_are_those_of_the_definition(kernel, B, L, d, out_dtype):
         sums = P @ Q[l:l + step].double().t()             # whole numbers below 2^53
         want = ((sums.to(F32) * a[:, None]) * s[None, l:l + step]).to(out_dtype)
         assert torch.equal(out[:, l:l + step], want), "labels from %d on" % l
+
+
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+@pytest.mark.parametrize("B,L,d", [(100000, 384, 64), (65600, 512, 128), (34205, 987, 200), (22521, 1499, 72), (13381, 2523, 384), (7385, 4571, 768),
+                                   (3880, 8704, 136), (9517, 3547, 72), (24829, 3547, 24), (9800, 3572, 128), (10161, 8667, 64)])
+def test_many_queries_on_few_labels(B, L, d, out_dtype):
+    test_bits_are_those_of_the_definition("", B, L, d, out_dtype)
