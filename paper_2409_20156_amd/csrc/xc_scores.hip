@@ -223,15 +223,16 @@ static int launch_quantize(const void* X, int64_t N, int d, xc_dtype t, const in
 // Accumulator i of a lane: query 4 (lane / 16) + i of its block, column lane % 16.
 // A persistent workgroup takes its tiles one after the other with the loads running ahead into the next, so a tile's scores are
 // stored while the next one's operands arrive; the waits count loads and stores, which retire in the order of their issue.
-// Bound: few queries, the rows of Q (1 x 131072 x 768: 18.0 us in the kernel where they come from memory, 5.6 TB/s, 15.9 to 17.1 where
-// one call after the other reads the same 100 MB, part of which the last-level cache still holds; 64 x 670000 x 768, which also stores
-// 86 MB: 121 us, 5.0 TB/s); many, what brings both operands through LDS and the clock that the chip's power limit allows (4096 x
-// 100000 x 4096: 1.33 ms, 2.5 POP/s; the library's product of 8192^3 integers runs at 2.1); rows beyond 768 bytes to fp32, the stores of a
-// 256 x 256 tile, which the loads of the next tile wait for (1440 x 164990 x 1472: 595 us, matrix pipe busy 27 % of the time, 905 MB
-// read and 985 written).  256 x 256 tiles spill 14 registers; their reloads lie in the way of tiles that reach past the end.  Measured on 4096 x 131072 x
-// 768 to bf16 (us): tiles of 128 x 256, one a workgroup, 813; epilogue on packed conversions and scales held ready 670; 256 x 256
-// 602; persistent 570; stages brought in by half of the waves in turn, the others at their products already, 550; 16 x 16
-// products, whose lanes end up with 16 bytes of scores, 540.  Of that the stores took 140, the loads 100.
+// Bound: few queries, the rows of Q (1 x 131072 x 768: 18.0 us in the kernel where they come from memory, 5.6 TB/s, 15.9 to 17.1
+// where one call after the other reads the same 100 MB, part of which the last-level cache still holds; 64 x 670000 x 768, which
+// also stores 86 MB: 121 us, 5.0 TB/s); many, what brings both operands through LDS and the clock that the chip's power limit
+// allows (4096 x 100000 x 4096: 1.33 ms, 2.5 POP/s; the library's product of 8192^3 integers runs at 2.1); rows beyond 768 bytes to
+// fp32, the stores of a 256 x 256 tile, which the loads of the next tile wait for (1440 x 164990 x 1472: 595 us, matrix pipe busy
+// 27 % of the time, 905 MB read and 985 written).  256 x 256 tiles spill 14 registers; their reloads lie in the way of tiles that
+// reach past the end.  Measured on 4096 x 131072 x 768 to bf16 (us): tiles of 128 x 256, one a workgroup, 813; epilogue on packed
+// conversions and scales held ready 670; 256 x 256 602; persistent 570; stages brought in by half of the waves in turn, the others
+// at their products already, 550; 16 x 16 products, whose lanes end up with 16 bytes of scores, 540.  Of that the stores took 140,
+// the loads 100.
 template <int WQ_, int WL_, int MQ_, int ML_, int R_, int G_, int RES_ = 0>
 struct Tile {
     static constexpr int WQ = WQ_, WL = WL_, MQ = MQ_, ML = ML_, R = R_;
@@ -282,10 +283,11 @@ __device__ __forceinline__ void store_label(bf16_t* p, float v) {
 __device__ __forceinline__ void lds_dma4(const void* gptr, uint32_t lds_addr /* wave-uniform */) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" :: "v"(gptr), "s"(lds_addr) : "memory");
 }
-// Rows of whole lines that a call reads once: marked for early replacement.  In the kernel, from memory: 1 x 131072 x 768 20.1 -> 18.0 us,
-// 32 x 131072 x 768 22.7 -> 20.8, 1 x 670000 x 768 91 -> 78, 64 x 670000 x 768 126 -> 117, 64 x 3 M x 256 228 -> 236; where one call after
-// the other reads the same 100 MB, part of which the last-level cache holds, 1 query 16.4 -> 15.9, 32 queries 18.4 -> 19.8.  Not where two loads share a line, of which the second would find nothing left: 126 x 441376 x 776
-// 185 us with the hint, 146 without; 32 x 600000 x 304 77 and 59.
+// Rows of whole lines that a call reads once: marked for early replacement.  In the kernel, from memory: 1 x 131072 x 768 20.1 ->
+// 18.0 us, 32 x 131072 x 768 22.7 -> 20.8, 1 x 670000 x 768 91 -> 78, 64 x 670000 x 768 126 -> 117, 64 x 3 M x 256 228 -> 236;
+// where one call after the other reads the same 100 MB, part of which the last-level cache holds, 1 query 16.4 -> 15.9, 32 queries
+// 18.4 -> 19.8.  Not where two loads share a line, of which the second would find nothing left: 126 x 441376 x 776 185 us with the
+// hint, 146 without; 32 x 600000 x 304 77 and 59.
 template <bool STREAM>
 __device__ __forceinline__ void load_labels(const void* sbase, uint32_t voff, uint32_t lds_addr) {
     if constexpr (STREAM)
@@ -581,14 +583,15 @@ static void launch_scores(ScoresArgs a, hipStream_t st) {
 // k-steps of 64 bytes) and 512 labels of a workgroup meet the queries that stream through LDS, QS at a time.  Per product that is
 // two thirds of the operand reads from LDS that a 256 x 256 tile takes, a quarter of the bytes brought into it, and a wave's scores are
 // stored 16 queries at a time, while the other wave of its SIMD multiplies.
-// Bound: the products at the clock that the chip's power limit allows, and the stores beside them.  4096 x 131072 x 768 to bf16, one
-// output written again and again: 360 to 365 us under sustained load (2.3 POP/s), 407 while the clock settles, 321 to 345 in the first
-// four calls; an output that no call has written before costs more (397 over 100 of them).  Counted: 1.8 GHz, the matrix pipe busy 64 % of the
-// time in which compute units are, 127 MB read and 1075 written.  Without the stores 281, without the loads the same as with them; 846 x 570112 x 192, which the stores
-// bound, 223 (4.3 TB/s).  Rows that begin within a line cost 5 to 20 percent: 4096 x 131071 x 768 431, 846 x 569976 x 192 247; and did
-// 45 when a workgroup took neighbouring tiles one after the other, whose shared lines left the cache half written (351).  Neither
-// 16-byte stores (rows exchanged between neighbouring lanes: 379 against 368 us a call), nor rows put together in LDS and stored by
-// whole lines (4096 x 131080 x 768 610 against 355), nor wave priorities made it faster.
+// Bound: the products at the clock that the chip's power limit allows, and the stores beside them.  4096 x 131072 x 768 to bf16,
+// one output written again and again: 360 to 365 us under sustained load (2.3 POP/s), 407 while the clock settles, 321 to 345 in
+// the first four calls; an output that no call has written before costs more (397 over 100 of them).  Counted: 1.8 GHz, the matrix
+// pipe busy 64 % of the time in which compute units are, 127 MB read and 1075 written.  Without the stores 281, without the loads
+// the same as with them; 846 x 570112 x 192, which the stores bound, 223 (4.3 TB/s).  Rows that begin within a line cost 5 to 20
+// percent: 4096 x 131071 x 768 431, 846 x 569976 x 192 247; and did 45 when a workgroup took neighbouring tiles one after the
+// other, whose shared lines left the cache half written (351).  Neither 16-byte stores (rows exchanged between neighbouring lanes:
+// 379 against 368 us a call), nor rows put together in LDS and stored by whole lines (4096 x 131080 x 768 610 against 355), nor
+// wave priorities made it faster.
 template <int NK_>
 struct Held {
     static constexpr int NK = NK_, QS = NK % 4 == 0 ? 32 : 64, kStage = QS * NK * 64;       // (the stage's loads divide evenly among 8 waves)

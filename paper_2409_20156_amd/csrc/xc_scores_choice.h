@@ -35,12 +35,13 @@ constexpr int kHeldLabels = 512, kHeldBytes = 768;
 //   more than 1792 tiles of 128 x 128, rows of up to 768 bytes and more than 384 queries, or up to 384 and 128   labels held in registers
 //                      (4096 x 131072 x 768 to bf16: 360; 256 x 256 tiles 545; 700 x 74141 x 768: 67, 128 x 128 tiles 74; 340 x 526924 x
 //                      320: 143 and 168; 700 x 34200 x 768, 1608 tiles: 43 and 36; 340 x 188544 x 512: 83 and 72)
-//                      Whole tiles of 512 labels go to an XCD: not where the busiest has more than half as many again as the mean (1
-//                      to 5, 9 and 10 tiles), which left up to seven XCDs without work (to fp32, bf16, held and 128 x 128:
-//                      65948 x 512 x 768: 167, 145 and 50, 43; 22521 x 1499 x 768: 85, 78 and 62, 43; 7385 x 4571 x 768: 67, 61 and 61, 44;
-//                      lost by it, to fp32: 34909 x 2523 x 768 143 and 152, 19000 x 5115 x 768 150 and 171).  To bf16, where 128 x 128 tiles store at less cost, the 1792 are
-//                      counted with what the busiest XCD has eight times (4096 x 8700 x 768: 60 and 42; 2645 x 12763 x 192: 32 and 26;
-//                      on the other side 10161 x 8667 x 768: 113 and 114), to fp32 not (4096 x 9000 x 384: 45 and 54; 2001 x 16859 x 768: 54 and 73)
+//                      Whole tiles of 512 labels go to an XCD: not where the busiest has more than half as many again as the mean (1 to 5,
+//                      9 and 10 tiles), which left up to seven XCDs without work (to fp32, bf16, held and 128 x 128: 65948 x 512 x 768:
+//                      167, 145 and 50, 43; 22521 x 1499 x 768: 85, 78 and 62, 43; 7385 x 4571 x 768: 67, 61 and 61, 44; lost by it, to
+//                      fp32: 34909 x 2523 x 768 143 and 152, 19000 x 5115 x 768 150 and 171).  To bf16, where 128 x 128 tiles store at less
+//                      cost, the 1792 are counted with what the busiest XCD has eight times (4096 x 8700 x 768: 60 and 42; 2645 x 12763 x
+//                      192: 32 and 26; on the other side 6901 x 12763 x 768: 94 and 97), to fp32 not (4096 x 9000 x 384: 45 and 54; 2001
+//                      x 16859 x 768: 54 and 73)
 //   else 128 x 128 tiles or, beyond 192 queries, 256 x 256 where that takes fewer rounds for its larger tiles (to bf16 512 x 209651 x
 //                      1024: 137 against 185; 1000 x 93139 x 4096: 338 against 428; 256 x 188816 x 512: 44 against 56; 800 x
 //                      17762 x 1536: 51 against 34, so not there; 130 x 141461 x 800: 71 against 55).  Short rows beyond 256 queries

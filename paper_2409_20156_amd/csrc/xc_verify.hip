@@ -3,9 +3,10 @@
 // Sums are held in 64 bits: with V = 10^5 equal weights a running sum in fp32 would be off by whole labels.  The order of the sums
 // depends on V alone (a wave's lanes by 8 neighbouring elements, pieces of a chunk one after the other, then the lanes, then the
 // chunks), so a sequence's label depends neither on the others in the batch nor on the launch.
-// Bound: few sequences, dependent memory accesses (draft -> its two probabilities -> the row -> the chunk again) and launches:
-// 1 x 4 x 4096 fp32 5.0 us on the device, 8 x 5 x 131072 7.4 (two launches); a batch, the rows from memory: 256 x 4 x 131072 bf16, drafts
-// that the target mostly takes, 23 us (110 MB, 4.8 TB/s), drafts that mostly fall 24 (127 MB read, 5.2 TB/s).  First form, 8 elements of a chunk at a time and all of it by one workgroup of 4 waves: 27, 140 and 181 us.
+// Bound: few sequences, dependent memory accesses (draft -> its two probabilities -> the row -> the chunk again) and launches: 1 x 4 x
+// 4096 fp32 5.0 us on the device, 8 x 5 x 131072 7.4 (two launches); a batch, the rows from memory: 256 x 4 x 131072 bf16, drafts that
+// the target mostly takes, 23 us (110 MB, 4.8 TB/s), drafts that mostly fall 24 (127 MB read, 5.2 TB/s).  First form, 8 elements of a
+// chunk at a time and all of it by one workgroup of 4 waves: 27, 140 and 181 us.
 #include <type_traits>
 
 #include "xc_common.h"
