@@ -3,8 +3,9 @@
  * (arXiv 2409.20156): hard-negative mining by exact top-k inner product, the
  * hard+uniform negative mixture, and the sampled BCE training step with a sparse
  * SGD update of the classifier rows; dropout of the embeddings that enter a step,
- * the scores of all labels from 8-bit integers, and the check of drafted labels
- * against the classifier's probabilities.
+ * the scores of all labels from 8-bit integers or 4-bit floating point, the check of
+ * drafted labels against the classifier's probabilities, log probabilities of labels
+ * under the soft-max of the scores, and the loss against a teacher's top labels.
  *
  * Conventions shared by every call
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library
@@ -54,6 +55,9 @@ typedef enum {
 #define XC_STATIC_SCRATCH_BYTES (32u << 20)  /* temporaries xc_step_static can hold    */
 #define XC_MAX_D_QUANTIZED 131072 /* d accepted by the 8-bit calls: |sum| <= 127^2 d < 2^31 */
 #define XC_MAX_DRAFTS 1024     /* n accepted by xc_verify_drafts                   */
+#define XC_MAX_GIVEN 256       /* n accepted by xc_label_logprobs                  */
+#define XC_MAX_TOP 128         /* k accepted by xc_label_logprobs                  */
+#define XC_MAX_TEACHER 256     /* K accepted by xc_distill                         */
 
 const char* xc_strerror(int status);
 int xc_last_hip_error(void);
@@ -274,6 +278,100 @@ int xc_scores_workspace(int64_t B, int d, size_t* bytes);
 int xc_scores_quantized(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,
                         const int8_t* Q /* [L*pitch] */, const float* scale /* [L] */, int64_t L,
                         xc_dtype out_t, void* out /* [B*L] out */, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Rows in 4-bit floating point with shared scales (the OCP microscaling format MXFP4).  32
+ * neighbouring elements of a row are a block; with m its largest magnitude,
+ *   scale byte s = floor(log2 m) - 2 + 127 (0 where that is less, and for a block of zeros);
+ *   element    x / 2^(s - 127) to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6, halves to the
+ *              neighbour whose code is even; what lies beyond 6 is 6.
+ * A code is a sign, two bits of exponent and one of mantissa; element j of a row is in the low
+ * (j even) or high half of byte j / 2.  Q[N * pitch / 2], scale[N * pitch / 32], pitch = d
+ * rounded up to 128; zeros behind column d.  A block with an element that is not a finite number
+ * gets zeros and scale 255, which makes every score with its row not a number.
+ * ids, m, count as in xc_quantize_rows.  Requires 1 <= N < 2^31, m >= 0, d*sizeof(element) a
+ * multiple of 16, d <= XC_MAX_D_QUANTIZED; Q and scale may overlap neither each other nor an
+ * input (XC_EINVAL).
+ * ------------------------------------------------------------------------- */
+int xc_microscale_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
+                       const int32_t* ids /* [m] or NULL */, int64_t m, const int32_t* count /* [1] or NULL */,
+                       uint8_t* Q /* [N*pitch/2] out */, uint8_t* scale /* [N*pitch/32] out */, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The scores of all labels from 4-bit floating point: the rows of Z (type t) are brought to 4 bits
+ * as above, and
+ *   out[i*L + l] = sum over blocks of 2^(s_i + s_l - 254) * (sum over the block of p_i q_l),
+ * sums in fp32 in an order that depends on d alone, rounded to out_t at the end: a score does not
+ * depend on how many queries or labels are scored with it, bit for bit.  Q and scale are what
+ * xc_microscale_rows gives for the classifier (or for a contiguous range of its rows).  The
+ * workspace holds the 4-bit rows of Z; it is written before it is read.
+ * Requires B >= 1, 1 <= L < 2^31, B*L <= 2^40, d as above; out and the workspace may
+ * overlap neither each other nor an input (XC_EINVAL).
+ * ------------------------------------------------------------------------- */
+int xc_scores_microscaled_workspace(int64_t B, int d, size_t* bytes);
+int xc_scores_microscaled(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,
+                          const uint8_t* Q /* [L*pitch/2] */, const uint8_t* scale /* [L*pitch/32] */, int64_t L,
+                          xc_dtype out_t, void* out /* [B*L] out */, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Log probabilities of labels under the soft-max of their scores.  X is B rows of V scores, ld >= V
+ * elements apart; a score of -infinity is a label that is not there.  With T the temperature,
+ * per row: m the largest score, S = sum_v exp((x_v - m) / T),
+ *   logp[b*n + j]     (x_v - m) / T - log S of label v = labels[b*n + j]; 0 for padding;
+ *   entropy[b]        of the soft-max, in nats;
+ *   norm[2*b], [2*b+1]  m and log S (their log-sum-exp is m / T + log S);
+ *   top[b*k + r]      the label with the r-th largest score, the lower one of equal ones first;
+ *   top_logp[b*k + r] its log probability.  Where the row has fewer than k labels: -1 and -infinity.
+ * A row without any label: m, log S and every logp are -infinity, its entropy is 0.  A row with a
+ * score that is not a number, or +infinity: log S, entropy and logp are not numbers; a score that
+ * is not a number is never among the top ones.
+ * Sums are fp32, in an order that depends on (B, V, t) and on where a row lies relative to 16 bytes.
+ * Requires B >= 1, 1 <= V < 2^31, B*ld <= 2^44, 0 <= n <= XC_MAX_GIVEN, 0 <= k <= min(V, XC_MAX_TOP),
+ * 1e-6 <= T <= 1e6.  labels and logp may be NULL if n = 0, top and top_logp if k = 0.  What is written
+ * may overlap nothing else of the call (XC_EINVAL).
+ * ------------------------------------------------------------------------- */
+int xc_label_logprobs_workspace(int64_t B, int64_t V, int k, xc_dtype t, size_t* bytes);
+int xc_label_logprobs(const void* X /* [B*ld] */, int64_t ld, int64_t B, int64_t V, xc_dtype t, float temperature,
+                      const int32_t* labels /* [B*n] */, int n, int k, float* logp /* [B*n] out */,
+                      float* entropy /* [B] out */, float* norm /* [B*2] out */, int32_t* top /* [B*k] out */,
+                      float* top_logp /* [B*k] out */, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradient for the scores, from those for logp and (dentropy, or NULL) for the entropy:
+ *   dX_v = (sum of dlogp over v's places in the list - p_v (G + dentropy (log p_v + entropy))) / T,
+ * G the row's sum of dlogp over labels that are no padding; norm and entropy (NULL without dentropy) as
+ * xc_label_logprobs gave them.  dX has rows ldd elements apart and type out_t; formed in fp32, rounded
+ * once.  A row without any label gets zeros.  dX may be X if types and row distances are the same;
+ * otherwise it may overlap nothing else of the call (XC_EINVAL).  Limits as above. */
+int xc_label_logprobs_grad(const void* X /* [B*ld] */, int64_t ld, int64_t B, int64_t V, xc_dtype t, float temperature,
+                           const int32_t* labels /* [B*n] */, int n, const float* dlogp /* [B*n] */,
+                           const float* norm /* [B*2] */, const float* entropy /* [B] or NULL */,
+                           const float* dentropy /* [B] or NULL */, void* dX /* [B*ldd] out */, int64_t ldd,
+                           xc_dtype out_t, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The loss of scores X (as above) against a teacher of which the top labels are given, and its gradient.
+ * labels[b*K ..] and teacher[b*K ..] are K labels (padding is ignored) and their logits at the temperature
+ * T, that is already divided by it.  p is the soft-max of x / T over all V labels.
+ *   tail = 0: q_k is the soft-max of the teacher's values over the list;
+ *   tail = 1: they are log probabilities, q_k = exp(teacher_k), and the labels that are not listed are one more
+ *             outcome: q_r = max(0, 1 - sum_k q_k), p_r the sum of p over them (q_r = 0 if none of them is there).
+ *   loss[b] = w_b T^2 (sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r)),
+ *   dX      = its derivative: w_b T (Q p_v - q_v) for a listed label, w_b T (Q p_r - q_r) p_v / p_r for any
+ *             other one, Q = sum_k q_k + q_r.
+ * Terms with q = 0 are 0.  A label that occurs several times in a list has the sum of its q.  weight is
+ * [B] or NULL (all 1); a row of weight 0 counts for nothing, whatever it holds: loss and gradient 0; so does a row
+ * without a label in its list, or (tail = 0) with teacher values of -infinity alone.  A row of scores without any
+ * label has loss infinity where q > 0, and p counts as 0 in its gradient.  Where scores or teacher values are not
+ * numbers, the loss is not a number.  Sums over a row are fp32, what is formed from them 64 bits.
+ * dX (or NULL: the loss alone) has rows ldd elements apart and type out_t; it may be X if types and row distances
+ * are the same.  Otherwise what is written may overlap nothing else of the call (XC_EINVAL).
+ * Requires B, V, ld, T as above, 1 <= K <= XC_MAX_TEACHER.
+ * ------------------------------------------------------------------------- */
+int xc_distill_workspace(int64_t B, int64_t V, xc_dtype t, size_t* bytes);
+int xc_distill(const void* X /* [B*ld] */, int64_t ld, int64_t B, int64_t V, xc_dtype t, float temperature,
+               const int32_t* labels /* [B*K] */, const float* teacher /* [B*K] */, int K, int tail,
+               const float* weight /* [B] or NULL */, float* loss /* [B] out */, void* dX /* [B*ldd] out, or NULL */,
+               int64_t ldd, xc_dtype out_t, void* ws, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
  * Drafted labels checked against the classifier's probabilities, so that what is

@@ -51,6 +51,16 @@ _SIGNATURES = {
     "xc_verify_workspace": (_i32, [_i64, _i64, _szp]),
     "xc_verify_drafts": (_i32, [_ptr, _i64, _i32, _i64, _ptr, _ptr, _i32, _ptr, _ptr, _ptr, _ptr, ctypes.c_size_t, _ptr]),
     "xc_dropout": (_i32, [_ptr, _i32, _i64, _i64, _f32, _u64, _i64, _ptr, _i32, _ptr]),
+    "xc_microscale_rows": (_i32, [_ptr, _i64, _i32, _i32, _ptr, _i64, _ptr, _ptr, _ptr, _ptr]),
+    "xc_scores_microscaled_workspace": (_i32, [_i64, _i32, _szp]),
+    "xc_scores_microscaled": (_i32, [_ptr, _i64, _i32, _i32, _ptr, _ptr, _i64, _i32, _ptr, _ptr, ctypes.c_size_t, _ptr]),
+    "xc_label_logprobs_workspace": (_i32, [_i64, _i64, _i32, _i32, _szp]),
+    "xc_label_logprobs": (_i32, [_ptr, _i64, _i64, _i64, _i32, _f32, _ptr, _i32, _i32, _ptr, _ptr, _ptr, _ptr, _ptr, _ptr,
+                                 ctypes.c_size_t, _ptr]),
+    "xc_label_logprobs_grad": (_i32, [_ptr, _i64, _i64, _i64, _i32, _f32, _ptr, _i32, _ptr, _ptr, _ptr, _ptr, _ptr, _i64, _i32, _ptr]),
+    "xc_distill_workspace": (_i32, [_i64, _i64, _i32, _szp]),
+    "xc_distill": (_i32, [_ptr, _i64, _i64, _i64, _i32, _f32, _ptr, _ptr, _i32, _i32, _ptr, _ptr, _ptr, _i64, _i32, _ptr,
+                          ctypes.c_size_t, _ptr]),
     "xc_step_static": (_i32, [_ptr, _ptr, _i64, _i64, _i32, _ptr, _i32, _ptr, _ptr, _i32, _f32, _i32, _i32,
                               _ptr, _ptr, _ptr, _ptr, _ptr, _ptr]),
 }
@@ -402,6 +412,219 @@ def scores_quantized(Z: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor, *, d
             _at(scale, torch.float32, "scale"), L, _dtype_code(out), _at(out, out.dtype, "out"),
             _at(workspace, torch.uint8, "workspace"), workspace.numel())
     return out
+
+
+def microscaled_pitch(d: int) -> int:
+    """Elements that a row of d is padded to in 4 bits: d rounded up to 128."""
+    return (d + 127) // 128 * 128
+
+
+def microscale_rows(X: torch.Tensor, *, rows: torch.Tensor | None = None, count: torch.Tensor | None = None,
+                    out: tuple | None = None):
+    """(Q uint8 [N, pitch / 2], scale uint8 [N, pitch / 32]): the rows of X [N, d] in 4-bit floating point (sign, two bits of
+    exponent, one of mantissa; two to a byte, the lower half first) with a scale 2^(byte - 127) for every 32 elements (MXFP4).
+
+    rows int32 [m]: only these rows of `out` are written, or the first count[0] of them (`touched` and `n_touched`
+    of a training step)."""
+    lib = load_library()
+    code = _dtype_code(X)
+    if X.dim() != 2:
+        raise ValueError("X must be [N, d]")
+    N, d = X.shape
+    if rows is not None and out is None:
+        raise ValueError("rows need the `out` of an earlier call: the other rows keep their values")
+    if rows is None and count is not None:
+        raise ValueError("count needs rows")
+    pitch = microscaled_pitch(d)
+    if out is None:
+        out = (torch.empty((N, pitch // 2), dtype=torch.uint8, device=X.device),
+               torch.empty((N, pitch // 32), dtype=torch.uint8, device=X.device))
+    Q, scale = out
+    _shaped(Q, (N, pitch // 2), "Q")
+    _shaped(scale, (N, pitch // 32), "scale")
+    if rows is not None and rows.dim() != 1:
+        raise ValueError("rows must be [m]")
+    if count is not None and count.numel() < 1:
+        raise ValueError("count must hold a number")
+    dev = _same_device(X, Q, scale, rows, count)
+    args = (_at(X, X.dtype, "X"), N, d, code, _at(rows, torch.int32, "rows") if rows is not None else None,
+            rows.numel() if rows is not None else 0, _at(count, torch.int32, "count") if count is not None else None,
+            _at(Q, torch.uint8, "Q"), _at(scale, torch.uint8, "scale"))
+    if rows is None or rows.numel():                       # (no rows: an empty tensor has no address to pass)
+        _launch(lib.xc_microscale_rows, "xc_microscale_rows", dev, *args)
+    return out
+
+
+def scores_microscaled_workspace(B: int, d: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.xc_scores_microscaled_workspace(B, d, ctypes.byref(n)), "xc_scores_microscaled_workspace")
+    return n.value
+
+
+def scores_microscaled(Z: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor, *, dtype: torch.dtype = torch.float32,
+                       workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """[B, L] scores of all labels: the rows of Z [B, d] in 4 bits times the rows of Q, block by block with the scales of both
+    (Q and scale from `microscale_rows` of the classifier).  fp32 or bf16, by `out` or `dtype`."""
+    lib = load_library()
+    code = _dtype_code(Z)
+    if Z.dim() != 2 or Q.dim() != 2 or Q.shape[1] * 2 != microscaled_pitch(Z.shape[1]):
+        raise ValueError("Z must be [B, d] and Q [L, half of d rounded up to 128]")
+    B, d = Z.shape
+    L = Q.shape[0]
+    _shaped(scale, (L, Q.shape[1] // 16), "scale")
+    if workspace is None:
+        workspace = torch.empty(scores_microscaled_workspace(B, d), dtype=torch.uint8, device=Z.device)
+    if out is None:
+        out = torch.empty((B, L), dtype=dtype, device=Z.device)
+    _shaped(out, (B, L), "out")
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("out must be float32 or bfloat16, got %s" % out.dtype)
+    dev = _same_device(Z, Q, scale, workspace, out)
+    _launch(lib.xc_scores_microscaled, "xc_scores_microscaled", dev, _at(Z, Z.dtype, "Z"), B, d, code, _at(Q, torch.uint8, "Q"),
+            _at(scale, torch.uint8, "scale"), L, _dtype_code(out), _at(out, out.dtype, "out"),
+            _at(workspace, torch.uint8, "workspace"), workspace.numel())
+    return out
+
+
+def _rows_at(t: torch.Tensor, name: str):
+    """Address and row distance of a matrix whose rows are contiguous, but may lie further apart than they are long."""
+    if t.dim() != 2:
+        raise ValueError("%s must be [B, V]" % name)
+    if not t.is_cuda:
+        raise RuntimeError("%s must live on the GPU: this library has no CPU path" % name)
+    B, V = t.shape
+    if (V > 1 and t.stride(1) != 1) or (B > 1 and t.stride(0) < V):
+        raise ValueError("the rows of %s must be contiguous and may not overlap" % name)
+    return t.data_ptr(), t.stride(0) if B > 1 else V
+
+
+def label_logprobs_workspace(B: int, V: int, top: int, dtype_code: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.xc_label_logprobs_workspace(B, V, top, dtype_code, ctypes.byref(n)), "xc_label_logprobs_workspace")
+    return n.value
+
+
+def label_logprobs(scores: torch.Tensor, labels: torch.Tensor, *, top: int = 0, temperature: float = 1.0,
+                   workspace: torch.Tensor | None = None, out: dict | None = None) -> dict:
+    """Log probabilities under the soft-max of scores [B, V] / temperature: dict(logp fp32 [B, n] of labels int32 [B, n] (0 for
+    padding, that is labels outside [0, V)), entropy fp32 [B], norm fp32 [B, 2] (largest score; log of the sum of exp((score -
+    largest) / temperature)), top int32 [B, top] and top_logp fp32 [B, top]: the labels with the largest scores, the lower of equal
+    ones first, or None).  A score of -infinity is a label that is not there; rows of scores may lie further apart than V."""
+    lib = load_library()
+    code = _dtype_code(scores)
+    if scores.dim() != 2 or labels.dim() != 2 or labels.shape[0] != scores.shape[0]:
+        raise ValueError("scores must be [B, V] and labels [B, n]")
+    B, V = scores.shape
+    n = labels.shape[1]
+    dev = scores.device
+    out = {} if out is None else out
+    shapes = {"logp": (B, n), "entropy": (B,), "norm": (B, 2), "top": (B, top), "top_logp": (B, top)}
+    r = {}
+    for name, shape in shapes.items():
+        t = out.get(name)
+        if top == 0 and name in ("top", "top_logp"):
+            t = None
+        elif t is None:
+            t = torch.empty(shape, dtype=torch.int32 if name == "top" else torch.float32, device=dev)
+        else:
+            _shaped(t, shape, name)
+        r[name] = t
+    if workspace is None:
+        workspace = torch.empty(label_logprobs_workspace(B, V, top, code), dtype=torch.uint8, device=dev)
+    _same_device(scores, labels, workspace, *r.values())
+    at, ld = _rows_at(scores, "scores")
+    _launch(lib.xc_label_logprobs, "xc_label_logprobs", dev, at, ld, B, V, code, float(temperature),
+            _at(labels, torch.int32, "labels") if n else None, n, top, _at(r["logp"], torch.float32, "logp") if n else None,
+            _at(r["entropy"], torch.float32, "entropy"), _at(r["norm"], torch.float32, "norm"),
+            _at(r["top"], torch.int32, "top") if top else None, _at(r["top_logp"], torch.float32, "top_logp") if top else None,
+            _at(workspace, torch.uint8, "workspace"), workspace.numel())
+    return r
+
+
+def label_logprobs_grad(scores: torch.Tensor, labels: torch.Tensor, dlogp: torch.Tensor, norm: torch.Tensor, *,
+                        temperature: float = 1.0, entropy: torch.Tensor | None = None, dentropy: torch.Tensor | None = None,
+                        dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The gradient for the scores [B, V] of a `label_logprobs` call from those for its logp (dlogp [B, n]) and its entropy
+    (dentropy [B], or None); norm and entropy as that call gave them.  fp32 or bf16, by `out`, `dtype` or scores; out may be
+    scores.  A dense soft-max loss is the case dlogp = -weight.  Nothing is recorded for autograd."""
+    lib = load_library()
+    code = _dtype_code(scores)
+    if scores.dim() != 2 or labels.dim() != 2 or labels.shape[0] != scores.shape[0]:
+        raise ValueError("scores must be [B, V] and labels [B, n]")
+    B, V = scores.shape
+    n = labels.shape[1]
+    _shaped(dlogp, (B, n), "dlogp")
+    _shaped(norm, (B, 2), "norm")
+    if dentropy is not None:
+        if entropy is None:
+            raise ValueError("dentropy needs the entropy")
+        _shaped(entropy, (B,), "entropy")
+        _shaped(dentropy, (B,), "dentropy")
+    if out is None:
+        out = torch.empty((B, V), dtype=dtype or scores.dtype, device=scores.device)
+    _shaped(out, (B, V), "out")
+    out_code = _dtype_code(out)
+    dev = _same_device(scores, labels, dlogp, norm, out, dentropy, entropy if dentropy is not None else None)
+    at, ld = _rows_at(scores, "scores")
+    out_at, ldd = _rows_at(out, "out")
+    _launch(lib.xc_label_logprobs_grad, "xc_label_logprobs_grad", dev, at, ld, B, V, code, float(temperature),
+            _at(labels, torch.int32, "labels") if n else None, n, _at(dlogp, torch.float32, "dlogp") if n else None,
+            _at(norm, torch.float32, "norm"), _at(entropy, torch.float32, "entropy") if dentropy is not None else None,
+            _at(dentropy, torch.float32, "dentropy") if dentropy is not None else None, out_at, ldd, out_code)
+    return out
+
+
+def distill_workspace(B: int, V: int, dtype_code: int) -> int:
+    lib = load_library()
+    n = ctypes.c_size_t(0)
+    _check(lib.xc_distill_workspace(B, V, dtype_code, ctypes.byref(n)), "xc_distill_workspace")
+    return n.value
+
+
+def distill(scores: torch.Tensor, labels: torch.Tensor, teacher: torch.Tensor, *, temperature: float = 1.0, tail: bool = False,
+            weight: torch.Tensor | None = None, grad: bool = True, dtype: torch.dtype | None = None,
+            workspace: torch.Tensor | None = None, out: tuple | None = None):
+    """(loss fp32 [B], gradient for the scores [B, V] or None): weight * temperature^2 * the divergence of the soft-max of scores /
+    temperature from a teacher's distribution, of which labels int32 [B, K] (padding is ignored) and teacher fp32 [B, K] are given.
+
+    teacher holds logits that are already divided by the temperature (for example `mine_negatives`' scores), whose soft-max over the
+    list is taken; with tail log probabilities (for example `label_logprobs`' top_logp), and the labels that are not listed are one
+    more outcome with the rest of the probability.  weight fp32 [B] or None: the gradient for each row's loss; rows of
+    weight 0 count for nothing, whatever they hold.  The gradient is fp32 or bf16, by `out`, `dtype` or scores; it may be scores
+    itself.  grad=False: the loss alone.  Nothing is recorded for autograd."""
+    lib = load_library()
+    code = _dtype_code(scores)
+    if scores.dim() != 2 or labels.dim() != 2 or labels.shape[0] != scores.shape[0]:
+        raise ValueError("scores must be [B, V] and labels [B, K]")
+    B, V = scores.shape
+    K = labels.shape[1]
+    _shaped(teacher, (B, K), "teacher")
+    if weight is not None:
+        _shaped(weight, (B,), "weight")
+    if out is None:
+        out = (torch.empty(B, dtype=torch.float32, device=scores.device),
+               torch.empty((B, V), dtype=dtype or scores.dtype, device=scores.device) if grad else None)
+    loss, dX = out
+    _shaped(loss, (B,), "loss")
+    if grad and dX is None:
+        raise ValueError("out holds no tensor for the gradient")
+    if not grad:
+        dX = None
+    if dX is not None:
+        _shaped(dX, (B, V), "the gradient")
+    out_code = _dtype_code(dX) if dX is not None else code
+    if workspace is None:
+        workspace = torch.empty(distill_workspace(B, V, code), dtype=torch.uint8, device=scores.device)
+    dev = _same_device(scores, labels, teacher, weight, loss, dX, workspace)
+    at, ld = _rows_at(scores, "scores")
+    out_at, ldd = _rows_at(dX, "the gradient") if dX is not None else (None, V)
+    _launch(lib.xc_distill, "xc_distill", dev, at, ld, B, V, code, float(temperature), _at(labels, torch.int32, "labels") if K else None,
+            _at(teacher, torch.float32, "teacher") if K else None, K, 1 if tail else 0,
+            _at(weight, torch.float32, "weight") if weight is not None else None, _at(loss, torch.float32, "loss"), out_at, ldd, out_code,
+            _at(workspace, torch.uint8, "workspace"), workspace.numel())
+    return loss, dX
 
 
 def verify_workspace(B: int, V: int) -> int:

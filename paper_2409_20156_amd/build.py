@@ -8,8 +8,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libastra_xc.so")
-SOURCES = ["xc_api.hip", "xc_dropout.hip", "xc_mine.hip", "xc_mine_few.hip", "xc_mine_q8.hip", "xc_sample.hip", "xc_scores.hip",
-           "xc_step.hip", "xc_verify.hip"]
+SOURCES = ["xc_api.hip", "xc_distill.hip", "xc_dropout.hip", "xc_logprobs.hip", "xc_microscaled.hip", "xc_mine.hip", "xc_mine_few.hip",
+           "xc_mine_q8.hip", "xc_sample.hip", "xc_scores.hip", "xc_step.hip", "xc_verify.hip"]
 
 
 def build(verbose: bool = False) -> str:

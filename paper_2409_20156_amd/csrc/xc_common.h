@@ -29,7 +29,8 @@ void set_last_hip_error(hipError_t e);
 enum KernelId {
     K_MINE_TILE = 0, K_MINE_SELECT, K_SAMPLE, K_GATHER, K_RADIX_COUNT, K_RADIX_SCAN,
     K_RADIX_SCATTER, K_BUCKET_SORT, K_HEADS_COUNT, K_HEADS_WRITE, K_UPDATE, K_QUANTIZE, K_SCORES,
-    K_VERIFY, K_VERIFY_SUMS, K_DROPOUT, K_NUM_KERNELS
+    K_VERIFY, K_VERIFY_SUMS, K_DROPOUT, K_LOGPROBS, K_LOGPROBS_JOIN, K_LOGPROBS_GRAD, K_DISTILL_SUMS, K_DISTILL_TERMS,
+    K_DISTILL_GRAD, K_MICROSCALE, K_SCORES_MICRO, K_NUM_KERNELS
 };
 bool profile_on();
 void profile_mark(int kernel_id, hipStream_t st, bool begin);

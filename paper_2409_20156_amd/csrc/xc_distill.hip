@@ -1,0 +1,383 @@
+// The loss against a teacher's distribution, of which its top labels are given, and its gradient.  Per row, with y = x / T:
+//   p = soft-max(y), q_k the teacher's probability of its k-th label, with a tail q_r = 1 - sum q_k for the labels that are not listed
+//   loss = w T^2 (sum q_k (log q_k - log p_k) + q_r (log q_r - log p_r)),  p_r the sum of p over these
+//   dX_v = w T (Q p_v - q_v) for a listed label, w T (Q p_r - q_r) r_v for any other one; Q = sum q_k + q_r, r the soft-max over the others.
+// With a tail the row's sums leave the listed labels out, and the sum over all labels is put together from these and the listed ones in
+// 64 bits: what the others' sum errs by leaves log p_r and log p_k - log p_r nearly alone, and p_r may be as small as it likes.
+#include "xc_softmax.h"
+
+namespace xc {
+
+struct DistillArgs {
+    const void* X;
+    const int32_t* labels;
+    const float *teacher, *weight;
+    float* loss;
+    void* dX;                            // or null
+    float4* parts;                       // [B][segments]: sums of a segment (with a tail: of the labels that are not listed)
+    struct RowTerms* terms;              // [B]
+    int64_t B, V, ld, ldd, segments, length;
+    float T, c;
+    int K;
+    bool tail;
+};
+
+// What a row's gradient is formed from.
+struct RowTerms {
+    float other;                         // factor of 2^((x - m) c - l): w T (Q p_r - q_r), without a tail w T
+    float m, l;                          // largest score of these labels, log2 of their sum
+    float factor, mass;                  // w T; Q
+    float m_all, l_all;                  // listed labels: p = 2^((x - m_all) c - l_all)
+    float t, t_log;                      // q = exp(teacher - t - t_log)
+    float live;                          // 0: the row counts for nothing
+    float pad[2];
+};
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double lanes_from(double x) {     // 0 where there is no such lane
+    const uint64_t u = static_cast<uint64_t>(__double_as_longlong(x));
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, ROWS, 0xf, false);
+    return __longlong_as_double(static_cast<long long>((static_cast<uint64_t>(hi) << 32) | lo));
+}
+__device__ __forceinline__ double wave_sum(double x) {
+    x += lanes_from<0x111, 0xf>(x);
+    x += lanes_from<0x112, 0xf>(x);
+    x += lanes_from<0x114, 0xf>(x);
+    x += lanes_from<0x118, 0xf>(x);
+    x += lanes_from<0x142, 0xa>(x);
+    x += lanes_from<0x143, 0xc>(x);
+    return __shfl(x, kWave - 1, kWave);
+}
+__device__ __forceinline__ bool is_label(int32_t v, int64_t V) { return v >= 0 && v < V; }
+
+// Loss and terms of a row from its sums, by one wave: a lane has every 64th place of the list.  In 64 bits, which cost nothing beside
+// the row.  An entry of the list whose label occurs before it does not count to the student's sum again.
+constexpr int kPlaces = XC_MAX_TEACHER / kWave;
+template <typename T>
+__device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, const Sums& s, float weight) {
+    const T* x = static_cast<const T*>(a.X) + b * a.ld;
+    const int32_t* labels = a.labels + b * a.K;
+    const double invT = 1.0 / static_cast<double>(a.T);
+    int32_t id[kPlaces];
+    double t[kPlaces], y[kPlaces];                           // (the student's relative to the row's largest score: that may be huge)
+    bool once[kPlaces];
+    float t_max = kNone, x_max = kNone;
+    int places = 0;
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+        const int k = i * kWave + lane_id();
+        id[i] = -1;
+        t[i] = y[i] = 0.0;
+        once[i] = false;
+        if (k < a.K) {
+            id[i] = labels[k];
+            if (is_label(id[i], a.V)) {
+                const float tk = a.teacher[b * a.K + k], xk = Elem<T>::get(x + id[i]);
+                t[i] = tk;
+                y[i] = xk;
+                t_max = fmaxf(t_max, tk);
+                x_max = fmaxf(x_max, xk);
+                once[i] = true;
+                for (int j = 0; j < k; ++j) if (labels[j] == id[i]) once[i] = false;
+                if (a.tail || tk != kNone) ++places;         // (without a tail a list of probabilities 0 is no distribution)
+            } else {
+                id[i] = -1;
+            }
+        }
+    }
+    const bool any = __ballot(places > 0) != 0ull;
+    RowTerms r{};
+    r.factor = weight * a.T;
+    r.live = any ? 1.0f : 0.0f;
+    if (!any) {
+        if (lane_id() == 0) a.loss[b] = 0.0f;
+        return r;
+    }
+    t_max = wave_max(t_max);
+    x_max = wave_max(x_max);
+    // the teacher
+    double q[kPlaces], sum = 0.0;
+    const double t0 = a.tail || t_max == kNone ? 0.0 : static_cast<double>(t_max);
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) {
+        q[i] = id[i] >= 0 ? exp(t[i] - t0) : 0.0;
+        sum += q[i];
+    }
+    sum = wave_sum(sum);
+    const double t_log = a.tail ? 0.0 : log(sum);
+    if (!a.tail) {
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i) q[i] /= sum;
+    }
+    // the student
+    const float m_all = fmaxf(s.m, x_max);
+    const double ref = m_all == kNone ? 0.0 : static_cast<double>(m_all);
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i) y[i] = (y[i] - ref) * invT;
+    const double sum_log = log(static_cast<double>(s.s));
+    const double rest_log = s.s == 0.0f ? sum_log : sum_log + (static_cast<double>(s.m) - ref) * invT;        // of the labels that s is about
+    double lse = rest_log;
+    if (a.tail) {
+        double listed = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPlaces; ++i) if (once[i]) listed += exp(y[i]);
+        listed = wave_sum(listed);
+        if (s.s != 0.0f) listed += exp(rest_log);
+        lse = log(listed);
+    }
+    double q_r = 0.0;
+    if (a.tail && s.s != 0.0f) {                             // (no label but the listed ones: nothing to compare)
+        q_r = 1.0 - sum;
+        if (q_r < 0.0) q_r = 0.0;
+    }
+    const double mass = a.tail ? sum + q_r : sum == sum ? 1.0 : sum;
+    double loss = 0.0;
+#pragma unroll
+    for (int i = 0; i < kPlaces; ++i)
+        if (id[i] >= 0 && !(q[i] == 0.0)) loss += q[i] * ((t[i] - t0 - t_log) - (lse == -INFINITY ? lse : y[i] - lse));
+    loss = wave_sum(loss);
+    if (!(q_r == 0.0)) loss += q_r * (log(q_r) - (rest_log - lse));
+    const double T2 = static_cast<double>(a.T) * static_cast<double>(a.T);
+    if (lane_id() == 0) a.loss[b] = static_cast<float>(static_cast<double>(weight) * T2 * loss);
+    const double log2e = 1.4426950408889634;
+    r.m = s.m == kNone ? 0.0f : s.m;
+    r.l = s.s == 0.0f ? 0.0f : static_cast<float>(sum_log * log2e);
+    r.mass = static_cast<float>(mass);
+    r.m_all = m_all == kNone ? 0.0f : m_all;
+    r.l_all = static_cast<float>(lse * log2e);
+    r.t = static_cast<float>(t0);
+    r.t_log = static_cast<float>(t_log);
+    const double factor = static_cast<double>(weight) * static_cast<double>(a.T);
+    r.other = static_cast<float>(factor * (a.tail ? (s.s == 0.0f ? 0.0 : mass * exp(rest_log - lse)) - q_r : mass));
+    return r;
+}
+
+__device__ __forceinline__ float q_of(const DistillArgs& a, const RowTerms& r, float t) {
+    return __builtin_amdgcn_exp2f(((t - r.t) - r.t_log) * 1.4426950408889634f);
+}
+__device__ __forceinline__ float other_gradient(const RowTerms& r, float x, float c) {
+    return r.other * __builtin_amdgcn_exp2f(fmaf(x - r.m, c, -r.l));
+}
+// Of the listed label at place k, the first of its label in the list: all places of it count.
+__device__ __forceinline__ float listed_gradient(const DistillArgs& a, const RowTerms& r, int64_t b, int k, int32_t id, float x) {
+    float q = 0.0f;
+    for (int j = k; j < a.K; ++j) if (a.labels[b * a.K + j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
+    const float p = r.l_all == kNone ? 0.0f : __builtin_amdgcn_exp2f(fmaf(x - r.m_all, a.c, -r.l_all));
+    return r.factor * fmaf(r.mass, p, -q);
+}
+__device__ __forceinline__ bool listed_before(const DistillArgs& a, int64_t b, int k, int32_t id) {
+    for (int j = 0; j < k; ++j) if (a.labels[b * a.K + j] == id) return true;
+    return false;
+}
+
+// Sums of a segment.  With a tail the listed labels of the segment are marked, a bit each, before its pieces are looked at.
+template <typename T, int W, int C>
+__global__ __launch_bounds__(W * kWave)
+void distill_sums_kernel(const DistillArgs a) {
+    constexpr int N = PiecedRow<T>::N, kThreads = W * kWave;
+    __shared__ Sums sums[W];
+    __shared__ uint32_t marks[kThreads * C / 4 + 1];         // a byte per piece; the edges
+    const int64_t b = blockIdx.x / static_cast<uint32_t>(a.segments), seg = blockIdx.x - b * a.segments;
+    if (a.weight != nullptr && a.weight[b] == 0.0f) return;  // uniform
+    const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
+    const int64_t first = seg * a.length, end = first + a.length < row.pieces ? first + a.length : row.pieces;
+    uint4 v[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int64_t at = first + i * kThreads + threadIdx.x;
+        v[i] = at < end ? row.load(at) : Elem<T>::none();
+    }
+    const int64_t edge = seg == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
+    float more = edge >= 0 ? Elem<T>::get(row.p + edge) : kNone;
+    if (a.tail) {
+        for (int i = threadIdx.x; i <= kThreads * C / 4; i += kThreads) marks[i] = 0;
+        __syncthreads();
+        for (int k = threadIdx.x; k < a.K; k += kThreads) {
+            const int32_t id = a.labels[b * a.K + k];
+            if (!is_label(id, a.V)) continue;
+            const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
+            if (piece >= 0 && piece < row.pieces) {
+                if (piece >= first && piece < end) {
+                    const int at = static_cast<int>(piece - first);
+                    atomicOr(&marks[at >> 2], 1u << ((at & 3) * 8 + static_cast<int>(id - row.first(piece))));
+                }
+            } else {
+                atomicOr(&marks[kThreads * C / 4], 1u << (id < row.head ? static_cast<int>(id) : static_cast<int>(id - row.pieces * N)));
+            }
+        }
+        __syncthreads();
+        if (edge >= 0 && ((marks[kThreads * C / 4] >> threadIdx.x) & 1u) != 0u) more = kNone;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const uint32_t m = reinterpret_cast<const unsigned char*>(marks)[i * kThreads + threadIdx.x];
+            if (__ballot(m != 0u) == 0ull) continue;
+            uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (N == 4) {
+                    if ((m >> e) & 1u) w[e] = 0xff800000u;
+                } else {
+                    if ((m >> (2 * e)) & 1u) w[e] = (w[e] & 0xffff0000u) | 0xff80u;
+                    if ((m >> (2 * e + 1)) & 1u) w[e] = (w[e] & 0xffffu) | 0xff800000u;
+                }
+            }
+            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    const Sums s = block_sums<W>(thread_sums<false, C, T>(v, more, a.c), a.c, sums);
+    if (threadIdx.x == 0) a.parts[b * a.segments + seg] = make_float4(s.m, s.s, 0.0f, 0.0f);
+}
+
+// A wave per row: its segments joined, its loss and terms.
+constexpr int kTermWaves = 4;
+template <typename T>
+__global__ __launch_bounds__(kTermWaves * kWave)
+void distill_terms_kernel(const DistillArgs a) {
+    const int64_t b = static_cast<int64_t>(blockIdx.x) * kTermWaves + (threadIdx.x >> 6);
+    if (b >= a.B) return;
+    const float weight = a.weight != nullptr ? a.weight[b] : 1.0f;
+    RowTerms r{};
+    if (weight == 0.0f) {                                    // counts for nothing, whatever it holds
+        if (lane_id() == 0) a.loss[b] = 0.0f;
+    } else {
+        Sums t{kNone, 0.0f, 0.0f};
+        for (int64_t i = lane_id(); i < a.segments; i += kWave) {
+            const float4 p = a.parts[b * a.segments + i];
+            const Sums q{p.x, p.y, 0.0f};
+            const float m = fmaxf(t.m, q.m);
+            const Sums u = joined(t, m, a.c), w = joined(q, m, a.c);
+            t = Sums{m, u.s + w.s, 0.0f};
+        }
+        r = row_terms<T>(a, b, wave_sums(t, a.c), weight);
+    }
+    if (lane_id() == 0) a.terms[b] = r;
+}
+
+// The gradient of a chunk of a row, then that of the listed labels in it (their scores are read before anything is stored: dX may be X).
+constexpr int kDistillThreads = 256, kDistillEach = 4, kDistillPieces = kDistillThreads * kDistillEach;
+template <typename T, typename TO>
+__global__ __launch_bounds__(kDistillThreads)
+void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
+    constexpr int N = PiecedRow<T>::N;
+    const int64_t b = blockIdx.x / static_cast<uint32_t>(chunks), chunk = blockIdx.x - b * chunks;
+    const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
+    TO* out = static_cast<TO*>(a.dX) + b * a.ldd;
+    const int64_t first = chunk * kDistillPieces, end = first + kDistillPieces < row.pieces ? first + kDistillPieces : row.pieces;
+    const RowTerms r = a.terms[b];
+    const bool live = r.live != 0.0f;                        // uniform
+    uint4 v[kDistillEach];
+#pragma unroll
+    for (int i = 0; i < kDistillEach; ++i) {
+        const int64_t at = first + i * kDistillThreads + threadIdx.x;
+        v[i] = live && at < end ? row.load(at) : make_uint4(0, 0, 0, 0);
+    }
+    const int64_t edge = chunk == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
+    const float more = live && edge >= 0 ? Elem<T>::get(row.p + edge) : 0.0f;
+    static_assert(XC_MAX_TEACHER <= kDistillThreads, "a thread per listed label");
+    int64_t listed = -1;
+    float value = 0.0f;
+    if (live && static_cast<int>(threadIdx.x) < a.K) {
+        const int32_t id = a.labels[b * a.K + threadIdx.x];
+        const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
+        if (is_label(id, a.V) && (id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) &&
+            !listed_before(a, b, threadIdx.x, id)) {
+            listed = id;
+            value = listed_gradient(a, r, b, threadIdx.x, id, Elem<T>::get(row.p + id));
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kDistillEach; ++i) {
+        const int64_t at = first + i * kDistillThreads + threadIdx.x;
+        if (at < end) {
+            float x[N];
+            Elem<T>::values(v[i], x);
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = live ? other_gradient(r, x[e], a.c) : 0.0f;
+            put_elements<N>(out + row.first(at), x);
+        }
+    }
+    if (edge >= 0) Elem<TO>::put(out + edge, live ? other_gradient(r, more, a.c) : 0.0f);
+    __syncthreads();                                         // (waits for the stores as well)
+    if (listed >= 0) Elem<TO>::put(out + listed, value);
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+static size_t distill_bytes(int64_t B, int64_t V, xc_dtype t) {
+    return static_cast<size_t>(B) * (sizeof(RowTerms) + static_cast<size_t>(cut_rows(B, V, t == XC_F32 ? 4 : 2).segments) * sizeof(float4));
+}
+
+template <typename T, typename TO>
+static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_t st) {
+    const int64_t pieces = all.V / static_cast<int64_t>(16 / sizeof(T)), chunks = pieces > kDistillPieces ? (pieces + kDistillPieces - 1) / kDistillPieces : 1;
+    int64_t rows = kSoftmaxGrid / (chunks > cut.segments ? chunks : cut.segments);
+    if (rows < 1) rows = 1;
+    for (int64_t b0 = 0; b0 < all.B; b0 += rows) {
+        DistillArgs a = all;
+        const int64_t nb = all.B - b0 < rows ? all.B - b0 : rows;
+        a.B = nb;
+        a.X = static_cast<const T*>(all.X) + b0 * all.ld;
+        if (all.dX != nullptr) a.dX = static_cast<TO*>(all.dX) + b0 * all.ldd;
+        a.labels += b0 * all.K;
+        a.teacher += b0 * all.K;
+        if (all.weight != nullptr) a.weight += b0;
+        a.loss += b0;
+        a.parts += b0 * cut.segments;
+        a.terms += b0;
+        const unsigned grid = static_cast<unsigned>(nb * cut.segments);
+        auto go = [&](auto kernel, int waves) { XC_LAUNCH(K_DISTILL_SUMS, st, (kernel<<<grid, waves * kWave, 0, st>>>(a))); };
+        if (cut.waves == 4) go(distill_sums_kernel<T, 4, 2>, 4);
+        else if (cut.each == 2) go(distill_sums_kernel<T, 8, 2>, 8);
+        else if (cut.each == 4) go(distill_sums_kernel<T, 8, 4>, 8);
+        else go(distill_sums_kernel<T, 8, 8>, 8);
+        XC_LAUNCH(K_DISTILL_TERMS, st, (distill_terms_kernel<T><<<static_cast<unsigned>((nb + kTermWaves - 1) / kTermWaves), kTermWaves * kWave, 0, st>>>(a)));
+        if (all.dX != nullptr)
+            XC_LAUNCH(K_DISTILL_GRAD, st, (distill_grad_kernel<T, TO><<<static_cast<unsigned>(nb * chunks), kDistillThreads, 0, st>>>(a, chunks)));
+    }
+}
+
+}  // namespace xc
+
+extern "C" int xc_distill_workspace(int64_t B, int64_t V, xc_dtype t, size_t* bytes) {
+    using namespace xc;
+    if (!bytes) return XC_EINVAL;
+    if (t != XC_F32 && t != XC_BF16) return XC_EDTYPE;
+    if (!softmax_shape(B, V, V)) return XC_ESHAPE;
+    *bytes = distill_bytes(B, V, t);
+    return XC_OK;
+}
+
+extern "C" int xc_distill(const void* X, int64_t ld, int64_t B, int64_t V, xc_dtype t, float temperature, const int32_t* labels, const float* teacher, int K,
+                          int tail, const float* weight, float* loss, void* dX, int64_t ldd, xc_dtype out_t, void* ws, size_t ws_bytes, void* stream) {
+    using namespace xc;
+    if ((t != XC_F32 && t != XC_BF16) || (dX != nullptr && out_t != XC_F32 && out_t != XC_BF16)) return XC_EDTYPE;
+    if (!softmax_shape(B, V, ld) || (dX != nullptr && !softmax_shape(B, V, ldd)) || K < 1 || K > XC_MAX_TEACHER) return XC_ESHAPE;
+    if (!softmax_temperature(temperature) || (tail != 0 && tail != 1)) return XC_EINVAL;
+    if (!X || !labels || !teacher || !loss || !ws) return XC_EINVAL;
+    for (const void* p : {X, static_cast<const void*>(labels), static_cast<const void*>(teacher), static_cast<const void*>(weight), static_cast<const void*>(loss),
+                          static_cast<const void*>(dX), static_cast<const void*>(ws)})
+        if (!aligned16(p)) return XC_EINVAL;
+    const size_t need = distill_bytes(B, V, t);
+    if (ws_bytes < need) return XC_EWORKSPACE;
+    const size_t per = static_cast<size_t>(B) * 4;
+    const Span x(X, rows_span(B, V, ld, t)), d(dX, dX != nullptr ? rows_span(B, V, ldd, out_t) : 0);
+    const bool in_place = dX == X && t == out_t && ld == ldd;
+    if ((!in_place && d.meets(x)) ||
+        overlap({Span(loss, per), Span(ws, need)}, {x, d, Span(labels, per * K), Span(teacher, per * K), Span(weight, per)}) ||
+        overlap({d}, {Span(labels, per * K), Span(teacher, per * K), Span(weight, per)}))
+        return XC_EINVAL;
+    const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2);
+    RowTerms* terms = static_cast<RowTerms*>(ws);
+    const DistillArgs a{X, labels, teacher, weight, loss, dX, reinterpret_cast<float4*>(terms + B), terms, B, V, ld, ldd, cut.segments, cut.length,
+                        temperature, softmax_scale(temperature), K, tail != 0};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if (t == XC_F32 && (dX == nullptr || out_t == XC_F32)) launch_distill<float, float>(a, cut, st);
+    else if (t == XC_F32) launch_distill<float, bf16_t>(a, cut, st);
+    else if (dX != nullptr && out_t == XC_F32) launch_distill<bf16_t, float>(a, cut, st);
+    else launch_distill<bf16_t, bf16_t>(a, cut, st);
+    XC_HIP_CHECK(hipGetLastError());
+    return XC_OK;
+}

@@ -1,0 +1,148 @@
+"""The operators on scores one after the other, as they are used: a teacher's classifier in 4 bits, its scores, their top labels and log
+probabilities, the student's loss against them and its gradient; training on labels drawn from the scores; on other streams and in graphs."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import answers_oracle as ao
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _inputs(seed, B, L, d, dtype=BF16):
+    g = torch.Generator().manual_seed(seed)
+    W = (torch.randn((L, d), generator=g) * 3 * d ** -0.5).to(dtype)
+    S = (W.float() + torch.randn((L, d), generator=g) * d ** -0.5).to(dtype)
+    Z = torch.randn((B, d), generator=g).to(dtype)
+    return W.to(DEV), S.to(DEV), Z.to(DEV)
+
+
+class Chain:
+    """Buffers of one chain, allocated once."""
+
+    def __init__(self, B, L, d, k):
+        import paper_2409_20156_amd as xc
+        self.xc, self.k = xc, k
+        pitch = xc.microscaled_pitch(d)
+        self.rows = (torch.empty((L, pitch // 2), dtype=torch.uint8, device=DEV), torch.empty((L, pitch // 32), dtype=torch.uint8, device=DEV))
+        self.scores = torch.empty((B, L), dtype=F32, device=DEV)
+        self.student = torch.empty((B, L), dtype=BF16, device=DEV)
+        self.ws = [torch.empty(n, dtype=torch.uint8, device=DEV) for n in (
+            xc.scores_microscaled_workspace(B, d), xc.label_logprobs_workspace(B, L, k, xc.XC_F32), xc.distill_workspace(B, L, xc.XC_BF16),
+            xc.label_logprobs_workspace(B, L, 0, xc.XC_BF16))]
+        f = dict(device=DEV, dtype=F32)
+        self.out = {"logp": torch.empty((B, 1), **f), "entropy": torch.empty(B, **f), "norm": torch.empty((B, 2), **f),
+                    "top": torch.empty((B, k), dtype=torch.int32, device=DEV), "top_logp": torch.empty((B, k), **f)}
+        self.back = {"logp": torch.empty((B, k), **f), "entropy": torch.empty(B, **f), "norm": torch.empty((B, 2), **f)}
+        self.loss, self.dX, self.dlogp = torch.empty(B, **f), torch.empty((B, L), dtype=BF16, device=DEV), torch.full((B, k), -0.1, **f)
+        self.dX2, self.one = torch.empty((B, L), dtype=BF16, device=DEV), torch.zeros((B, 1), dtype=torch.int32, device=DEV)
+
+    def run(self, W, S, Z):
+        xc = self.xc
+        xc.microscale_rows(W, out=self.rows)
+        xc.scores_microscaled(Z, *self.rows, workspace=self.ws[0], out=self.scores)
+        r = xc.label_logprobs(self.scores, self.one, top=self.k, workspace=self.ws[1], out=self.out)
+        self.student.copy_(Z.float() @ S.float().t())
+        xc.distill(self.student, r["top"], r["top_logp"], tail=True, workspace=self.ws[2], out=(self.loss, self.dX))
+        b = xc.label_logprobs(self.student, r["top"], workspace=self.ws[3], out=self.back)
+        xc.label_logprobs_grad(self.student, r["top"], self.dlogp, b["norm"], out=self.dX2)
+
+    def results(self):
+        torch.cuda.synchronize()
+        return [t.clone() for t in (self.scores, *self.out.values(), *self.back.values(), self.loss, self.dX, self.dX2)]
+
+
+def _same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("B,L,d,k", [(3, 500, 64, 5), (40, 9001, 136, 32)])
+def test_a_student_learns_from_a_teacher_in_4_bits(B, L, d, k):
+    W, S, Z = _inputs(B, B, L, d)
+    c = Chain(B, L, d, k)
+    c.run(W, S, Z)
+    torch.cuda.synchronize()
+    z, w = (ao.values(*ao.microscale_rows(t.double().cpu().numpy())) for t in (Z, W))
+    scores = z @ w.T
+    # (fp32 sums of 2 to 5 products of 128; the scores reach about 20)
+    assert np.abs(c.scores.double().cpu().numpy() - scores).max() < 1e-4
+    shown = c.scores.double().cpu().numpy()
+    r = ao.label_logprobs(shown, np.zeros((B, 1), dtype=int), 1.0, k)
+    assert (c.out["top"].cpu().numpy() == r["top"]).all()
+    # (2^-24 (60 + 3 E|d| + |log S|) with E|d| and |log S| below 20 is 8e-6; the loss's and the gradients' sums are no further off)
+    assert np.abs(c.out["top_logp"].cpu().numpy() - r["top_logp"]).max() < 2e-5
+    student = c.student.double().cpu().numpy()
+    loss, dX, _ = ao.distill(student, r["top"], c.out["top_logp"].double().cpu().numpy(), 1.0, True)
+    assert np.abs(c.loss.cpu().numpy() - loss).max() < 2e-5
+    assert np.abs(c.dX.double().cpu().numpy() - dX).max() < 2.0 ** -8
+    back = ao.label_logprobs_grad(student, r["top"], np.full((B, k), float(np.float32(-0.1))), 1.0)
+    assert np.abs(c.dX2.double().cpu().numpy() - back).max() < 2.0 ** -8 * np.abs(back).max() + 1e-6
+
+
+def test_other_streams_give_the_same():
+    W, S, Z = _inputs(1, 20, 4001, 128)
+    a, b = Chain(20, 4001, 128, 16), Chain(20, 4001, 128, 16)
+    a.run(W, S, Z)
+    want = a.results()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        b.run(W, S, Z)
+    a.run(W, S, Z)                                         # at the same time, on buffers of its own
+    torch.cuda.synchronize()
+    assert _same(a.results(), want) and _same(b.results(), want)
+
+
+def test_captured_and_replayed():
+    W, S, Z = _inputs(2, 24, 20003, 256)
+    a, b = Chain(24, 20003, 256, 20), Chain(24, 20003, 256, 20)
+    graphs = []
+    for c in (a, b):
+        c.run(W, S, Z)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.run(W, S, Z)
+        graphs.append(graph)
+    eager = Chain(24, 20003, 256, 20)
+    for turn in range(5):
+        V, R, Y = _inputs(10 + turn, 24, 20003, 256)
+        W.copy_(V), S.copy_(R), Z.copy_(Y)
+        eager.run(W, S, Z)
+        want = eager.results()
+        for graph in graphs:
+            graph.replay()
+        for c in (a, b):
+            assert _same(c.results(), want), turn
+        (torch.randn((512, 512), device=DEV) @ torch.randn((512, 512), device=DEV)).sum().item()
+        graphs[turn % 2].replay()                          # once more, and each by itself
+        assert _same((a, b)[turn % 2].results(), want)
+
+
+def test_a_search_teaches_the_student():
+    """`mine_negatives` gives a teacher's top labels and logits as they are."""
+    import paper_2409_20156_amd as xc
+    W, S, Z = _inputs(5, 30, 3000, 64)
+    ids, logits = xc.mine_negatives(Z, W, 16, want_scores=True)
+    student = (Z.float() @ S.float().t()).contiguous()
+    loss, dX = xc.distill(student, ids, logits)
+    want, grad, _ = ao.distill(student.double().cpu().numpy(), ids.cpu().numpy(), logits.double().cpu().numpy())
+    # (log S is off by u (60 + 3 E|d|), E|d| below 20; a gradient by 1e-5 of p at most)
+    assert np.abs(loss.cpu().numpy() - want).max() < 1e-5 and np.abs(dX.cpu().numpy() - grad).max() < 1e-5
+
+
+def test_nothing_is_allocated_with_buffers():
+    W, S, Z = _inputs(3, 16, 5000, 128)
+    c = Chain(16, 5000, 128, 8)
+    xc = c.xc
+    c.run(W, S, Z)
+    torch.cuda.synchronize()
+    before = torch.cuda.memory_stats()["allocation.all.allocated"]
+    xc.microscale_rows(W, out=c.rows)
+    xc.scores_microscaled(Z, *c.rows, workspace=c.ws[0], out=c.scores)
+    xc.label_logprobs(c.scores, c.one, top=8, workspace=c.ws[1], out=c.out)
+    xc.distill(c.student, c.out["top"], c.out["top_logp"], tail=True, workspace=c.ws[2], out=(c.loss, c.dX))
+    xc.label_logprobs_grad(c.student, c.out["top"], c.dlogp, c.back["norm"], out=c.dX2)
+    assert torch.cuda.memory_stats()["allocation.all.allocated"] == before

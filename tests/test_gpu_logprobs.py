@@ -1,0 +1,259 @@
+"""Log probabilities of given labels, entropy and top labels under the soft-max of scores, and their gradient, against the oracle.
+
+Bounds (u = 2^-24).  An exponential is formed from (x - m) c with three roundings (difference, product, c) of relative u each and by
+an instruction that is off by at most 2 u: relative error u (2 + 3 |d|), d = (x - m) / T.  Sums: at most 40 additions in a chain, 12
+joins.  So S is off by u (60 + 3 E|d|) relative, E the mean under the soft-max; log S by as much plus u |log S|; logp by that and
+3 u |d|; the entropy by u (120 + 6 E|d|) (1 + E|d|).  In the gradient p is off by u (80 + 3 E|d| + 8 |logp|) relative (its exponent is
+formed from x - m, log S and log2(e)), the factor behind it by u times 8 of its parts and by the entropy's own error.  A result in bf16 is
+rounded once more: 2^-8 of it."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import answers_oracle as ao
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+U = 2.0 ** -24
+
+
+def _case(seed, B, V, n, dtype, masked=0.0, sigma=2.5):
+    g = torch.Generator().manual_seed(seed)
+    X = sigma * torch.randn((B, V), generator=g)
+    X[torch.rand((B, V), generator=g) < masked] = -float("inf")
+    labels = torch.randint(-1, V + 1, (B, n), generator=g).to(torch.int32)
+    return X.to(dtype), labels
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _sizes(X, T):
+    """|d| and E|d| per row, from the oracle's own log probabilities; rows that are no numbers give 0."""
+    m = np.where(np.isnan(X), -np.inf, X).max(1, keepdims=True)
+    with np.errstate(invalid="ignore", over="ignore"):
+        d = np.abs(X - m) / T
+        p = np.exp(np.stack([ao.log_softmax(x, T) for x in X]))
+        mean = np.where(p > 0, p * np.where(np.isfinite(d), d, 0), 0).sum(1)
+    return d, np.where(np.isnan(mean), 0, mean)
+
+
+def _close(got, want, tol):
+    bad = ~np.isfinite(want)
+    assert (np.isnan(got) == np.isnan(want)).all()
+    inf = np.isinf(want)
+    assert (got[inf] == want[inf]).all()
+    off, tol = np.abs(got - want)[~bad], np.broadcast_to(tol, want.shape)[~bad]
+    assert (off <= tol).all(), (off.max(), (off / np.maximum(tol, 1e-300)).max())
+
+
+def _check(X, labels, T=1.0, top=0, given=None):
+    import paper_2409_20156_amd as xc
+    r = xc.label_logprobs(X.to(DEV) if given is None else given, labels.to(DEV), top=top, temperature=T)
+    torch.cuda.synchronize()
+    x = _np(X)
+    want = ao.label_logprobs(x, labels.numpy(), T, top)
+    d, mean = _sizes(x, T)
+    ls = np.abs(np.where(np.isfinite(want["norm"][:, 1]), want["norm"][:, 1], 0))
+    tol = U * (60 + 3 * mean + ls)
+    _close(_np(r["norm"])[:, 0], want["norm"][:, 0], 0.0)
+    _close(_np(r["norm"])[:, 1], want["norm"][:, 1], tol)
+    _close(_np(r["entropy"]), want["entropy"], U * (120 + 6 * mean) * (1 + mean) + 2 * tol)
+    B, n = labels.shape
+    V = x.shape[1]
+    at = np.clip(labels.numpy(), 0, V - 1)
+    far = np.take_along_axis(np.where(np.isfinite(d), d, 0), at, 1) if n else np.zeros((B, 0))
+    _close(_np(r["logp"]), want["logp"], tol[:, None] + 5 * U * far)
+    if top:
+        assert (r["top"].cpu().numpy() == want["top"]).all()
+        far = np.take_along_axis(np.where(np.isfinite(d), d, 0), np.clip(want["top"], 0, V - 1), 1)
+        _close(_np(r["top_logp"]), want["top_logp"], tol[:, None] + 5 * U * far)
+    else:
+        assert r["top"] is None and r["top_logp"] is None
+    return r
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,V,n,top", [(1, 1, 1, 1), (1, 2, 0, 2), (3, 3, 2, 3), (2, 5, 1, 5), (5, 7, 3, 0), (4, 8, 2, 8), (4, 9, 2, 1), (3, 15, 1, 15), (3, 17, 1, 4),
+                                       (33, 100, 7, 3), (2, 1000, 256, 128), (7, 1023, 1, 20), (7, 2049, 1, 20), (9, 4095, 2, 5), (2, 4096, 1, 128), (2, 4103, 1, 64),
+                                       (6, 8192, 1, 10), (3, 8200, 1, 100), (2, 16384, 2, 128), (2, 20011, 3, 7), (2, 50021, 1, 20), (1, 131072, 1, 20),
+                                       (1, 262144 + 3, 1, 128), (300, 4001, 1, 16), (700, 2100, 2, 9), (1, 600011, 4, 128)])
+def test_matches_the_oracle(B, V, n, top, dtype):
+    _check(*_case(B * 7 + V, B, V, n, dtype), top=top)
+
+
+@pytest.mark.parametrize("T", [0.05, 0.7, 2.0, 30.0])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_temperatures(T, dtype):
+    _check(*_case(5, 6, 3001, 4, dtype), T=T, top=11)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [6, 777, 9001, 40003])
+def test_rows_with_masks_infinities_and_nan(V, dtype):
+    X, labels = _case(V, 24, V, 5, dtype, masked=0.5)
+    low = torch.finfo(dtype).min
+    X[0] = -float("inf")                                   # nothing is left
+    X[1] = low                                             # the type's lowest value everywhere: as likely as each other
+    X[2, X[2] == -float("inf")] = low
+    X[3] = -float("inf")
+    X[3, V - 1] = 0.5                                      # one label
+    X[4] = -float("inf")
+    X[4, 0] = low
+    X[5, V // 2] = float("nan")
+    X[6] = float("nan")
+    X[7, 0] = float("inf")
+    X[8] = float("inf")
+    X[9] = 0.0
+    X[9, 1::2] = -0.0                                      # equal scores: the lowest labels
+    X[10] = torch.finfo(dtype).max
+    X[11, :] = X[11, 0] if X[11, 0] > -float("inf") else 1.0
+    X[12] = X[12].clamp(min=-1.0) * 1e30
+    X[13, : V // 2] = -float("inf")
+    X[14, V // 2:] = -float("inf")
+    X[15] = torch.arange(V) * 0.01 - 3                     # growing, falling
+    X[16] = -torch.arange(V) * 0.01
+    _check(X, labels, top=min(V, 6))
+    _check(X, labels, top=min(V, 128), T=1.5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [3000, 33000])
+@pytest.mark.parametrize("k", [1, 5, 37, 128])
+def test_many_equal_scores(V, k, dtype):
+    """More labels reach the k-th score than a workgroup ranks at a time."""
+    g = torch.Generator().manual_seed(k)
+    X = torch.randint(0, 3, (6, V), generator=g).float()
+    X[0] = 1.0
+    X[1] = 0.0
+    X[1, V // 3: V // 3 + 3] = 5.0
+    X[2] = -float("inf")
+    X[2, 10: V - 7: 2] = -2.5
+    _check(X.to(dtype), torch.zeros((6, 1), dtype=torch.int32), top=k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,ld,shift", [(77, 80, 0), (1001, 1003, 0), (5000, 5013, 0), (130, 131, 0), (8193, 9000, 0)])
+def test_rows_further_apart(V, ld, shift, dtype):
+    X, labels = _case(V, 9, V, 3, dtype)
+    buf = torch.full((9, ld), 1e4, dtype=dtype, device=DEV)                      # what lies between the rows would win
+    buf[:, :V] = X.to(DEV)
+    _check(X, labels, top=7, given=buf[:, :V])
+
+
+def _check_grad(X, labels, T=1.0, entropy=True, out=BF16, given=None, target=None):
+    import paper_2409_20156_amd as xc
+    B, V = X.shape
+    g = torch.Generator().manual_seed(B + V)
+    dlogp = torch.randn(labels.shape, generator=g)
+    dent = torch.randn(B, generator=g) if entropy else None
+    xd = X.to(DEV) if given is None else given
+    r = xc.label_logprobs(xd, labels.to(DEV), temperature=T)
+    x = _np(X)
+    got = xc.label_logprobs_grad(xd, labels.to(DEV), dlogp.to(DEV), r["norm"], temperature=T, dtype=out, out=target,
+                                 **({"entropy": r["entropy"], "dentropy": dent.to(DEV)} if entropy else {}))
+    torch.cuda.synchronize()
+    want = ao.label_logprobs_grad(x, labels.numpy(), dlogp.double().numpy(), T, dent.double().numpy() if entropy else None)
+    lp = np.stack([ao.log_softmax(row, T) for row in x])
+    with np.errstate(invalid="ignore"):
+        p = np.exp(lp)
+        lp = np.where(np.isfinite(lp), np.abs(lp), 0)
+    _, mean = _sizes(x, T)
+    there = (labels.numpy() >= 0) & (labels.numpy() < V)
+    G = np.abs(np.where(there, dlogp.numpy(), 0)).sum(1)[:, None]
+    h = np.abs(dent.double().numpy())[:, None] if entropy else 0.0
+    H = np.where(np.isfinite(r["entropy"].cpu().numpy()), r["entropy"].cpu().numpy(), 0)[:, None]
+    factor = G + h * (lp + H)
+    tol = p / T * (U * (88 + 3 * mean[:, None] + 8 * lp) * factor + h * U * (120 + 6 * mean[:, None]) * (1 + mean[:, None]))
+    given_size = np.zeros_like(x)
+    np.add.at(given_size, (np.repeat(np.arange(B), labels.shape[1]), np.clip(labels.numpy(), 0, V - 1).ravel()),
+              np.where(there, np.abs(dlogp.numpy()), 0).ravel())
+    tol = tol + U * 8 * given_size / T + (2.0 ** -8 if out == BF16 else U) * np.abs(want) + 1e-35
+    _close(_np(got), want, np.where(np.isfinite(tol), tol, 0))
+    return got
+
+
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
+@pytest.mark.parametrize("B,V,n", [(1, 1, 1), (2, 2, 1), (3, 5, 2), (4, 8, 0), (5, 9, 3), (3, 17, 256), (33, 100, 7), (2, 4096, 1), (7, 4103, 5), (9, 8193, 2), (2, 50021, 16),
+                                   (1, 131072, 1), (600, 777, 1)])
+def test_gradient_matches_the_oracle(B, V, n, dtype, out):
+    X, labels = _case(B + 3 * V, B, V, n, dtype)
+    _check_grad(X, labels, out=out)
+    _check_grad(X, labels, T=0.7, entropy=False, out=out)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V", [6, 777, 9001])
+def test_gradient_of_rows_with_masks_infinities_and_nan(V, dtype):
+    X, labels = _case(V, 12, V, 5, dtype, masked=0.4)
+    X[0] = -float("inf")
+    X[1] = torch.finfo(dtype).min
+    X[2, X[2] == -float("inf")] = torch.finfo(dtype).min
+    X[3] = -float("inf")
+    X[3, V - 1] = 0.5
+    X[4, V // 2] = float("nan")
+    X[5, 0] = float("inf")
+    labels[6] = labels[6, 0]                               # the same label at every place
+    labels[7] = -1
+    labels[8] = torch.tensor([0, V - 1, 0, V - 1, V])
+    X[6:9, 0] = 0.25
+    got = _check_grad(X, labels, out=dtype, T=1.5)
+    assert (got[0] == 0).all()
+
+
+def test_gradient_against_differences():
+    X, labels = _case(11, 3, 40, 4, F32)
+    import paper_2409_20156_amd as xc
+    g = torch.Generator().manual_seed(1)
+    dlogp, dent = torch.randn((3, 4), generator=g), torch.randn(3, generator=g)
+    r = xc.label_logprobs(X.to(DEV), labels.to(DEV))
+    got = _np(xc.label_logprobs_grad(X.to(DEV), labels.to(DEV), dlogp.to(DEV), r["norm"], entropy=r["entropy"], dentropy=dent.to(DEV)))
+    h = 2.0 ** -6                                          # the result is off by 2^-20 or so, h^2 / 6 of a third derivative by 4e-5
+    for v in range(0, 40, 7):
+        f = []
+        for sign in (1, -1):
+            Y = X.clone()
+            Y[:, v] += sign * h
+            q = xc.label_logprobs(Y.to(DEV), labels.to(DEV))
+            f.append((_np(q["logp"]) * dlogp.double().numpy()).sum(1) + _np(q["entropy"]) * dent.double().numpy())
+        assert np.abs((f[0] - f[1]) / (2 * h) - got[:, v]).max() < 2e-3
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,ld", [(64, 64), (1001, 1001), (1001, 1005), (9001, 9009)])
+def test_gradient_in_place_and_rows_further_apart(V, ld, dtype):
+    X, labels = _case(V, 7, V, 3, dtype)
+    want = _check_grad(X, labels, out=dtype)
+    buf = torch.full((7, ld), 9.0, dtype=dtype, device=DEV)
+    buf[:, :V] = X.to(DEV)
+    got = _check_grad(X, labels, out=dtype, given=buf[:, :V], target=buf[:, :V])
+    assert torch.equal(got, want) and (buf[:, V:] == 9).all()
+    wide = torch.full((9, ld + 3), 9.0, dtype=F32, device=DEV)                   # another distance and type
+    got = _check_grad(X, labels, out=F32, target=wide[:7, :V])
+    assert (wide[:, V:] == 9).all() and (wide[7:] == 9).all()
+
+
+def test_the_dense_soft_max_loss():
+    """dlogp = -1 / B: the gradient of the mean cross entropy, against torch's in 64 bits."""
+    import paper_2409_20156_amd as xc
+    X, _ = _case(2, 16, 500, 1, F32)
+    y = torch.randint(0, 500, (16, 1), dtype=torch.int32)
+    r = xc.label_logprobs(X.to(DEV), y.to(DEV))
+    got = xc.label_logprobs_grad(X.to(DEV), y.to(DEV), torch.full((16, 1), -1.0 / 16, device=DEV), r["norm"])
+    x64 = X.double().requires_grad_()
+    loss = torch.nn.functional.cross_entropy(x64, y[:, 0].long())
+    loss.backward()
+    assert abs(float(-r["logp"].double().mean()) - float(loss)) < 1e-6
+    assert (got.cpu().double() - x64.grad).abs().max() < 1e-6 / 16
+
+
+def test_runs_repeat_bit_for_bit_and_rows_do_not_depend_on_each_other():
+    import paper_2409_20156_amd as xc
+    X, labels = _case(8, 40, 9000, 4, BF16)
+    X, labels = X.to(DEV), labels.to(DEV)
+    a = xc.label_logprobs(X, labels, top=30)
+    b = xc.label_logprobs(X, labels, top=30)
+    for k in a:
+        assert torch.equal(a[k], b[k])

@@ -1,0 +1,174 @@
+"""Rows in 4-bit floating point against the oracle, code by code, and the scores of all labels from them.
+
+Bound of a score: products of codes and their sums within a block of 32 are exact (multiples of 1/4 below 2^11), a block's sum is scaled
+exactly, and the blocks' sums are added in fp32, each addition off by at most half a step of a partial sum, of which none exceeds S = the
+sum of the blocks' magnitudes: pitch / 32 * 2^-24 * S for a product that rounds after every block, twice that where an addition aligns
+by cutting off.  A result in bf16 is rounded once more: 2^-8 of it."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import answers_oracle as ao
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+def _matrix(seed, n, d, dtype, spread=0.5):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn((n, d), generator=g) * torch.exp(spread * torch.randn((n, 1), generator=g)) * d ** -0.5
+    return x.to(dtype)
+
+
+def _rows(X, **kw):
+    import paper_2409_20156_amd as xc
+    Q, s = xc.microscale_rows(X.to(DEV), **kw)
+    torch.cuda.synchronize()
+    return Q, s
+
+
+def _check_rows(X):
+    Q, s = _rows(X)
+    codes, scale = ao.microscale_rows(X.double().numpy())
+    assert (s.cpu().numpy() == scale).all()
+    got = Q.cpu().numpy()
+    assert (got == ao.packed(codes)).all(), np.argwhere(got != ao.packed(codes))[:4]
+    return Q, s, codes, scale
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,d", [(1, 8), (3, 24), (5, 64), (17, 120), (4, 128), (7, 136), (33, 300 // 8 * 8), (2, 768), (65, 1000), (3, 4096), (1, 8200)])
+def test_rows_match_the_oracle(N, d, dtype):
+    _check_rows(_matrix(N * 31 + d, N, d, dtype))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_at_the_edges_between_codes(dtype):
+    """Elements at, just above and just below every middle, in blocks of every scale from the smallest to the largest."""
+    mid = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 0.0, 6.0, 6.5, 7.0])
+    eps = 2.0 ** -7 if dtype == BF16 else 2.0 ** -22
+    base = torch.cat([mid, -mid, mid * (1 + eps)])[:31]
+    low = torch.cat([mid * (1 - eps), -mid * (1 - eps), torch.zeros(9)])
+    for e in (-127, -126, -125, -100, -30, 0, 1, 60, 120, 125):
+        X = torch.ldexp(torch.stack([torch.cat([base, torch.tensor([7.5])]), torch.cat([low, torch.tensor([-4.0])])]).double(), torch.tensor(e)).to(dtype)
+        _check_rows(X)
+
+
+def test_rows_that_are_zero_tiny_or_no_numbers():
+    X = _matrix(3, 8, 256, F32)
+    X[0] = 0
+    X[1, :32] = 0
+    X[2] = 2.0 ** -140
+    X[2, 0] = 2.0 ** -127
+    X[3] = 2.0 ** -149
+    X[4, 5] = float("nan")
+    X[5, 40] = float("inf")
+    X[6, 200] = -float("inf")
+    X[7] = 3.4e38
+    Q, s, _, scale = _check_rows(X)
+    assert scale[4, 0] == 255 and scale[5, 1] == 255 and scale[6, 6] == 255 and (scale[0] == 0).all()
+
+
+def test_listed_rows_leave_the_others():
+    X = _matrix(9, 50, 72, BF16)
+    Q, s = _rows(X)
+    X2 = X * 3
+    rows = torch.tensor([3, 49, -1, 50, 3, 7, 2 ** 31 - 1, 0], dtype=torch.int32, device=DEV)
+    for count, done in ((None, [3, 49, 7, 0]), (5, [3, 49]), (0, []), (100, [3, 49, 7, 0])):
+        q2, s2 = Q.clone(), s.clone()
+        kw = {} if count is None else {"count": torch.tensor([count], dtype=torch.int32, device=DEV)}
+        _rows(X2, rows=rows, out=(q2, s2), **kw)
+        want, ws = _rows(X2)
+        keep = torch.ones(50, dtype=torch.bool, device=DEV)
+        keep[done] = False
+        assert torch.equal(q2[keep], Q[keep]) and torch.equal(s2[keep], s[keep])
+        assert torch.equal(q2[done], want[done]) and torch.equal(s2[done], ws[done])
+
+
+def _bound(P, p, Q, q, got, out):
+    """Oracle's scores and the bound of the module's description, from codes and scales of both sides."""
+    z, w = ao.values(P, p), ao.values(Q, q)
+    units = z.shape[1] // 32
+    blocks = np.einsum("bkj,lkj->blk", z.reshape(z.shape[0], units, 32), w.reshape(w.shape[0], units, 32))
+    want, size = blocks.sum(2), np.abs(blocks).sum(2)
+    tol = 2 * units * 2.0 ** -24 * size + (2.0 ** -8 * np.abs(want) if out == BF16 else 0) + 1e-37
+    assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / tol).max()
+
+
+@pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("B,L,d", [(1, 1, 8), (1, 17, 64), (2, 1000, 72), (15, 100, 128), (16, 333, 256), (17, 64, 384), (33, 130, 768), (63, 129, 200), (64, 500, 512),
+                                   (65, 63, 1000), (128, 257, 768), (130, 515, 896), (200, 700, 1024), (129, 300, 1152), (257, 513, 640), (300, 65, 4096)])
+def test_scores_match_the_oracle(B, L, d, dtype, out):
+    import paper_2409_20156_amd as xc
+    Z, W = _matrix(B + d, B, d, dtype), _matrix(L + d + 7, L, d, dtype)
+    Q, s = _rows(W)
+    got = xc.scores_microscaled(Z.to(DEV), Q, s, dtype=out)
+    torch.cuda.synchronize()
+    P, p = ao.microscale_rows(Z.double().numpy())
+    w, ws = ao.microscale_rows(W.double().numpy())
+    _bound(P, p, w, ws, got.double().cpu().numpy(), out)
+
+
+def test_every_pair_of_codes_and_scales_that_differ():
+    """One code per block on either side, all 16 x 16 pairs; blocks' scales spread over 2^-20 .. 2^20."""
+    import paper_2409_20156_amd as xc
+    g = np.random.default_rng(2)
+    grid = np.array(ao.GRID + tuple(-v for v in ao.GRID))
+    W = np.zeros((16, 256))
+    Z = np.zeros((16, 256))
+    for c in range(16):
+        W[c], Z[c] = grid[c], grid[c]
+    W[:, ::32], Z[:, ::32] = 4.0, 4.0                      # every block's scale is 1
+    e = g.integers(-20, 21, size=8)
+    W *= np.ldexp(1.0, np.repeat(e, 32))[None]
+    Z *= np.ldexp(1.0, np.repeat(-e, 32))[None]
+    Q, s = _rows(torch.tensor(W, dtype=F32))
+    got = xc.scores_microscaled(torch.tensor(Z, dtype=F32).to(DEV), Q, s).cpu().double().numpy()
+    assert (got == Z @ W.T).all()                          # all partial sums are exact
+
+
+def test_scores_do_not_depend_on_the_batch_or_the_range():
+    import paper_2409_20156_amd as xc
+    for d in (72, 768, 1280):
+        Z, W = _matrix(1, 300, d, BF16).to(DEV), _matrix(2, 1500, d, BF16).to(DEV)
+        Q, s = xc.microscale_rows(W)
+        whole = xc.scores_microscaled(Z, Q, s)
+        for lo, hi in ((0, 1), (7, 23), (64, 128), (3, 132), (0, 257)):
+            assert torch.equal(xc.scores_microscaled(Z[lo:hi].clone(), Q, s), whole[lo:hi])
+        for lo, hi in ((0, 1), (16, 80), (1, 1400)):
+            assert torch.equal(xc.scores_microscaled(Z, Q[lo:hi].clone(), s[lo:hi].clone()), whole[:, lo:hi])
+        assert torch.equal(xc.scores_microscaled(Z, Q, s, dtype=BF16), whole.bfloat16())
+
+
+def test_rows_that_are_no_numbers_give_scores_that_are_none():
+    import paper_2409_20156_amd as xc
+    Z, W = _matrix(5, 80, 256, F32), _matrix(6, 90, 256, F32)
+    Z[3, 200] = float("nan")
+    W[17, 0] = float("inf")
+    W[20] = 0
+    Q, s = _rows(W)
+    got = xc.scores_microscaled(Z.to(DEV), Q, s).cpu()
+    bad = torch.zeros((80, 90), dtype=torch.bool)
+    bad[3], bad[:, 17] = True, True
+    assert torch.equal(got.isnan(), bad) and (got[:3, 20] == 0).all()
+
+
+def test_outputs_end_where_they_should():
+    """Memory around the scores and the rows keeps its values."""
+    import paper_2409_20156_amd as xc
+    for B, L, d in ((5, 77, 64), (70, 131, 768), (130, 1029, 256)):
+        for dtype in (F32, BF16):
+            Z, W = _matrix(B, B, d, BF16).to(DEV), _matrix(L, L, d, BF16).to(DEV)
+            pitch = xc.microscaled_pitch(d)
+            q = torch.full((L + 2, pitch // 2), 77, dtype=torch.uint8, device=DEV)
+            s = torch.full(((L + 2) * pitch // 32 + 32,), 77, dtype=torch.uint8, device=DEV)
+            sv = s[16:16 + L * pitch // 32].view(L, pitch // 32)
+            xc.microscale_rows(W, out=(q[1:-1], sv))
+            buf = torch.full((B * L + 64,), -7.0, dtype=dtype, device=DEV)
+            out = buf[32:32 + B * L].view(B, L)
+            xc.scores_microscaled(Z, q[1:-1], sv, out=out)
+            torch.cuda.synchronize()
+            assert (q[0] == 77).all() and (q[-1] == 77).all() and (s[:16] == 77).all() and (s[16 + L * pitch // 32:] == 77).all()
+            assert (buf[:32] == -7).all() and (buf[32 + B * L:] == -7).all()
+            assert torch.equal(out, xc.scores_microscaled(Z, q[1:-1].clone(), sv.clone(), dtype=dtype))
