@@ -18,16 +18,17 @@ struct DistillArgs {
     struct RowTerms* terms;              // [B]
     int64_t B, V, ld, ldd, segments, length;
     float T, c;
-    int K;
+    int K, blocks;
     bool tail;
 };
 
 // What a row's gradient is formed from.
 struct RowTerms {
+    // (powers of two are taken out as whole ones: the rest is in the factor, so that no large exponent is rounded)
     float other;                         // factor of 2^((x - m) c - l): w T (Q p_r - q_r), without a tail w T
     float m, l;                          // largest score of these labels, log2 of their sum
     float factor, mass;                  // w T; Q
-    float m_all, l_all;                  // listed labels: p = 2^((x - m_all) c - l_all)
+    float m_all, l_all;                  // listed labels: Q p = mass 2^((x - m_all) c - l_all)
     float t, t_log;                      // q = exp(teacher - t - t_log)
     float live;                          // 0: the row counts for nothing
     float pad[2];
@@ -52,12 +53,20 @@ __device__ __forceinline__ double wave_sum(double x) {
 __device__ __forceinline__ bool is_label(int32_t v, int64_t V) { return v >= 0 && v < V; }
 
 // Loss and terms of a row from its sums, by one wave: a lane has every 64th place of the list.  In 64 bits, which cost nothing beside
-// the row.  An entry of the list whose label occurs before it does not count to the student's sum again.
+// the row.  An entry of the list whose label occurs before it does not count to the student's sum again.  `list` holds the list's labels.
 constexpr int kPlaces = XC_MAX_TEACHER / kWave;
+__device__ __forceinline__ bool listed_before(const int32_t* list, int k, int32_t id) {      // (list: 16 bytes aligned, in LDS)
+    bool before = false;
+#pragma unroll 2
+    for (int j = 0; j < k; j += 4) {
+        const int4 l = *reinterpret_cast<const int4*>(list + j);
+        before |= (l.x == id) | (l.y == id && j + 1 < k) | (l.z == id && j + 2 < k) | (l.w == id && j + 3 < k);
+    }
+    return before;
+}
 template <typename T>
-__device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, const Sums& s, float weight) {
+__device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, const Sums& s, float weight, const int32_t* list) {
     const T* x = static_cast<const T*>(a.X) + b * a.ld;
-    const int32_t* labels = a.labels + b * a.K;
     const double invT = 1.0 / static_cast<double>(a.T);
     int32_t id[kPlaces];
     double t[kPlaces], y[kPlaces];                           // (the student's relative to the row's largest score: that may be huge)
@@ -71,15 +80,14 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, c
         t[i] = y[i] = 0.0;
         once[i] = false;
         if (k < a.K) {
-            id[i] = labels[k];
+            id[i] = list[k];
             if (is_label(id[i], a.V)) {
                 const float tk = a.teacher[b * a.K + k], xk = Elem<T>::get(x + id[i]);
                 t[i] = tk;
                 y[i] = xk;
                 t_max = fmaxf(t_max, tk);
                 x_max = fmaxf(x_max, xk);
-                once[i] = true;
-                for (int j = 0; j < k; ++j) if (labels[j] == id[i]) once[i] = false;
+                once[i] = !listed_before(list, k, id[i]);
                 if (a.tail || tk != kNone) ++places;         // (without a tail a list of probabilities 0 is no distribution)
             } else {
                 id[i] = -1;
@@ -142,14 +150,15 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, c
     if (lane_id() == 0) a.loss[b] = static_cast<float>(static_cast<double>(weight) * T2 * loss);
     const double log2e = 1.4426950408889634;
     r.m = s.m == kNone ? 0.0f : s.m;
-    r.l = s.s == 0.0f ? 0.0f : static_cast<float>(sum_log * log2e);
-    r.mass = static_cast<float>(mass);
+    const double l = s.s == 0.0f ? 0.0 : sum_log * log2e, l_all = lse * log2e;
+    r.l = static_cast<float>(rint(l));
     r.m_all = m_all == kNone ? 0.0f : m_all;
-    r.l_all = static_cast<float>(lse * log2e);
+    r.l_all = static_cast<float>(rint(l_all));
+    r.mass = static_cast<float>(l_all == -INFINITY ? mass : mass * exp2(rint(l_all) - l_all));
     r.t = static_cast<float>(t0);
     r.t_log = static_cast<float>(t_log);
     const double factor = static_cast<double>(weight) * static_cast<double>(a.T);
-    r.other = static_cast<float>(factor * (a.tail ? (s.s == 0.0f ? 0.0 : mass * exp(rest_log - lse)) - q_r : mass));
+    r.other = static_cast<float>(exp2(rint(l) - l) * factor * (a.tail ? (s.s == 0.0f ? 0.0 : mass * exp(rest_log - lse)) - q_r : mass));
     return r;
 }
 
@@ -160,72 +169,77 @@ __device__ __forceinline__ float other_gradient(const RowTerms& r, float x, floa
     return r.other * __builtin_amdgcn_exp2f(fmaf(x - r.m, c, -r.l));
 }
 // Of the listed label at place k, the first of its label in the list: all places of it count.
-__device__ __forceinline__ float listed_gradient(const DistillArgs& a, const RowTerms& r, int64_t b, int k, int32_t id, float x) {
+__device__ __forceinline__ float listed_gradient(const DistillArgs& a, const RowTerms& r, int64_t b, int k, int32_t id, float x, const int32_t* list) {
     float q = 0.0f;
-    for (int j = k; j < a.K; ++j) if (a.labels[b * a.K + j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
+    for (int j = k; j < a.K; ++j) if (list[j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
     const float p = r.l_all == kNone ? 0.0f : __builtin_amdgcn_exp2f(fmaf(x - r.m_all, a.c, -r.l_all));
     return r.factor * fmaf(r.mass, p, -q);
 }
-__device__ __forceinline__ bool listed_before(const DistillArgs& a, int64_t b, int k, int32_t id) {
-    for (int j = 0; j < k; ++j) if (a.labels[b * a.K + j] == id) return true;
-    return false;
-}
 
-// Sums of a segment.  With a tail the listed labels of the segment are marked, a bit each, before its pieces are looked at.
-template <typename T, int W, int C>
-__global__ __launch_bounds__(W * kWave)
+// Sums of a segment.  With a tail the listed labels of a block are marked, a bit each, before its elements are looked at.
+template <typename T, int C>
+__global__ __launch_bounds__(kRowThreads)
 void distill_sums_kernel(const DistillArgs a) {
-    constexpr int N = PiecedRow<T>::N, kThreads = W * kWave;
-    __shared__ Sums sums[W];
-    __shared__ uint32_t marks[kThreads * C / 4 + 1];         // a byte per piece; the edges
+    constexpr int N = PiecedRow<T>::N, E = C * N, kMarks = kRowThreads * C / 4;
+    __shared__ Sums sums[kRowWaves];
+    __shared__ uint32_t marks[2][kMarks + 1];                // a byte per piece; the edges.  A block's are set while the one before is summed
     const int64_t b = blockIdx.x / static_cast<uint32_t>(a.segments), seg = blockIdx.x - b * a.segments;
     if (a.weight != nullptr && a.weight[b] == 0.0f) return;  // uniform
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
-    const int64_t first = seg * a.length, end = first + a.length < row.pieces ? first + a.length : row.pieces;
-    uint4 v[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int64_t at = first + i * kThreads + threadIdx.x;
-        v[i] = at < end ? row.load(at) : Elem<T>::none();
-    }
+    const int64_t begin = seg * a.length, end = begin + a.length < row.pieces ? begin + a.length : row.pieces;
+    Block<T, C> block;
+    block.template load<true>(row, begin, end, kRowThreads);
     const int64_t edge = seg == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
     float more = edge >= 0 ? Elem<T>::get(row.p + edge) : kNone;
+    Running run;
+    static_assert(XC_MAX_TEACHER <= kRowThreads, "a thread per listed label");
+    int32_t id = -1;
+    int64_t piece = -1;
     if (a.tail) {
-        for (int i = threadIdx.x; i <= kThreads * C / 4; i += kThreads) marks[i] = 0;
+        if (static_cast<int>(threadIdx.x) < a.K) id = a.labels[b * a.K + threadIdx.x];
+        if (!is_label(id, a.V)) id = -1;
+        piece = id < row.head ? -1 : (id - row.head) / N;
+        for (int i = threadIdx.x; i <= kMarks; i += kRowThreads) marks[0][i] = marks[1][i] = 0;
         __syncthreads();
-        for (int k = threadIdx.x; k < a.K; k += kThreads) {
-            const int32_t id = a.labels[b * a.K + k];
-            if (!is_label(id, a.V)) continue;
-            const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
-            if (piece >= 0 && piece < row.pieces) {
-                if (piece >= first && piece < end) {
-                    const int at = static_cast<int>(piece - first);
-                    atomicOr(&marks[at >> 2], 1u << ((at & 3) * 8 + static_cast<int>(id - row.first(piece))));
-                }
-            } else {
-                atomicOr(&marks[kThreads * C / 4], 1u << (id < row.head ? static_cast<int>(id) : static_cast<int>(id - row.pieces * N)));
-            }
+        if (id >= 0 && (piece < 0 || piece >= row.pieces))
+            atomicOr(&marks[0][kMarks], 1u << (id < row.head ? id : static_cast<int>(id - row.pieces * N)));
+    }
+    auto mark = [&](int n, bool on) __attribute__((always_inline)) {       // the thread's listed label, if it lies in block n
+        const int64_t at = piece - (begin + static_cast<int64_t>(n) * (kRowThreads * C));
+        if (id >= 0 && piece >= 0 && piece < end && at >= 0 && at < kRowThreads * C) {
+            uint32_t* w = &marks[n & 1][at >> 2];
+            if (on) atomicOr(w, 1u << (static_cast<int>(at & 3) * 8 + static_cast<int>(id - row.first(piece))));
+            else *w = 0;
         }
+    };
+    if (a.tail) {
+        mark(0, true);
         __syncthreads();
-        if (edge >= 0 && ((marks[kThreads * C / 4] >> threadIdx.x) & 1u) != 0u) more = kNone;
+        if (edge >= 0 && ((marks[0][kMarks] >> threadIdx.x) & 1u) != 0u) more = kNone;
+    }
+    for (int n = 0; n < a.blocks; ++n) {
+        const int64_t first = begin + static_cast<int64_t>(n) * (kRowThreads * C);
+        float f[E];
+        block.values(f);
+        if (n + 1 < a.blocks) block.template load<true>(row, first + kRowThreads * C, end, kRowThreads);
+        if (a.tail) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const uint32_t m = reinterpret_cast<const unsigned char*>(marks)[i * kThreads + threadIdx.x];
-            if (__ballot(m != 0u) == 0ull) continue;
-            uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            for (int i = 0; i < C; ++i) {
+                const uint32_t m = reinterpret_cast<const unsigned char*>(marks[n & 1])[i * kRowThreads + threadIdx.x];
+                if (__ballot(m != 0u) == 0ull) continue;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if constexpr (N == 4) {
-                    if ((m >> e) & 1u) w[e] = 0xff800000u;
-                } else {
-                    if ((m >> (2 * e)) & 1u) w[e] = (w[e] & 0xffff0000u) | 0xff80u;
-                    if ((m >> (2 * e + 1)) & 1u) w[e] = (w[e] & 0xffffu) | 0xff800000u;
-                }
+                for (int e = 0; e < N; ++e) if ((m >> e) & 1u) f[i * N + e] = kNone;
             }
-            v[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            mark(n + 1, true);
+        }
+        run.template add<false>(f, largest_of<E>(f, 0), a.c);
+        if (a.tail && n + 1 < a.blocks) {
+            __syncthreads();                                 // (block n's marks have been read, those of n + 1 are set)
+            mark(n, false);
         }
     }
-    const Sums s = block_sums<W>(thread_sums<false, C, T>(v, more, a.c), a.c, sums);
+    run.add_one(more, a.c);
+    const Sums s = block_sums<kRowWaves>(run.sums(a.c), a.c, sums);
     if (threadIdx.x == 0) a.parts[b * a.segments + seg] = make_float4(s.m, s.s, 0.0f, 0.0f);
 }
 
@@ -234,7 +248,11 @@ constexpr int kTermWaves = 4;
 template <typename T>
 __global__ __launch_bounds__(kTermWaves * kWave)
 void distill_terms_kernel(const DistillArgs a) {
+    __shared__ __align__(16) int32_t lists[kTermWaves][XC_MAX_TEACHER];
     const int64_t b = static_cast<int64_t>(blockIdx.x) * kTermWaves + (threadIdx.x >> 6);
+    int32_t* list = lists[threadIdx.x >> 6];
+    if (b < a.B) for (int k = lane_id(); k < a.K; k += kWave) list[k] = a.labels[b * a.K + k];
+    __syncthreads();
     if (b >= a.B) return;
     const float weight = a.weight != nullptr ? a.weight[b] : 1.0f;
     RowTerms r{};
@@ -249,7 +267,7 @@ void distill_terms_kernel(const DistillArgs a) {
             const Sums u = joined(t, m, a.c), w = joined(q, m, a.c);
             t = Sums{m, u.s + w.s, 0.0f};
         }
-        r = row_terms<T>(a, b, wave_sums(t, a.c), weight);
+        r = row_terms<T>(a, b, wave_sums(t, a.c), weight, list);
     }
     if (lane_id() == 0) a.terms[b] = r;
 }
@@ -264,26 +282,28 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
     TO* out = static_cast<TO*>(a.dX) + b * a.ldd;
     const int64_t first = chunk * kDistillPieces, end = first + kDistillPieces < row.pieces ? first + kDistillPieces : row.pieces;
-    const RowTerms r = a.terms[b];
-    const bool live = r.live != 0.0f;                        // uniform
+    __shared__ __align__(16) int32_t list[XC_MAX_TEACHER];
     uint4 v[kDistillEach];
 #pragma unroll
     for (int i = 0; i < kDistillEach; ++i) {
         const int64_t at = first + i * kDistillThreads + threadIdx.x;
-        v[i] = live && at < end ? row.load(at) : make_uint4(0, 0, 0, 0);
+        v[i] = at < end ? row.template load<true>(at) : make_uint4(0, 0, 0, 0);
     }
     const int64_t edge = chunk == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
-    const float more = live && edge >= 0 ? Elem<T>::get(row.p + edge) : 0.0f;
+    const float more = edge >= 0 ? Elem<T>::get(row.p + edge) : 0.0f;
     static_assert(XC_MAX_TEACHER <= kDistillThreads, "a thread per listed label");
+    const int32_t id = static_cast<int>(threadIdx.x) < a.K ? a.labels[b * a.K + threadIdx.x] : -1;
+    list[threadIdx.x] = id;
+    const RowTerms r = a.terms[b];
+    const bool live = r.live != 0.0f;                        // uniform
+    __syncthreads();
     int64_t listed = -1;
     float value = 0.0f;
-    if (live && static_cast<int>(threadIdx.x) < a.K) {
-        const int32_t id = a.labels[b * a.K + threadIdx.x];
+    if (live && is_label(id, a.V)) {
         const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
-        if (is_label(id, a.V) && (id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) &&
-            !listed_before(a, b, threadIdx.x, id)) {
+        if ((id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) && !listed_before(list, threadIdx.x, id)) {
             listed = id;
-            value = listed_gradient(a, r, b, threadIdx.x, id, Elem<T>::get(row.p + id));
+            value = listed_gradient(a, r, b, threadIdx.x, id, Elem<T>::get(row.p + id), list);
         }
     }
     __syncthreads();
@@ -328,11 +348,9 @@ static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_
         a.parts += b0 * cut.segments;
         a.terms += b0;
         const unsigned grid = static_cast<unsigned>(nb * cut.segments);
-        auto go = [&](auto kernel, int waves) { XC_LAUNCH(K_DISTILL_SUMS, st, (kernel<<<grid, waves * kWave, 0, st>>>(a))); };
-        if (cut.waves == 4) go(distill_sums_kernel<T, 4, 2>, 4);
-        else if (cut.each == 2) go(distill_sums_kernel<T, 8, 2>, 8);
-        else if (cut.each == 4) go(distill_sums_kernel<T, 8, 4>, 8);
-        else go(distill_sums_kernel<T, 8, 8>, 8);
+        constexpr int kSmall = small_block(sizeof(T)), kLarge = large_block(sizeof(T));
+        if (cut.each == kSmall) XC_LAUNCH(K_DISTILL_SUMS, st, (distill_sums_kernel<T, kSmall><<<grid, kRowThreads, 0, st>>>(a)));
+        else XC_LAUNCH(K_DISTILL_SUMS, st, (distill_sums_kernel<T, kLarge><<<grid, kRowThreads, 0, st>>>(a)));
         XC_LAUNCH(K_DISTILL_TERMS, st, (distill_terms_kernel<T><<<static_cast<unsigned>((nb + kTermWaves - 1) / kTermWaves), kTermWaves * kWave, 0, st>>>(a)));
         if (all.dX != nullptr)
             XC_LAUNCH(K_DISTILL_GRAD, st, (distill_grad_kernel<T, TO><<<static_cast<unsigned>(nb * chunks), kDistillThreads, 0, st>>>(a, chunks)));
@@ -372,7 +390,7 @@ extern "C" int xc_distill(const void* X, int64_t ld, int64_t B, int64_t V, xc_dt
     const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2);
     RowTerms* terms = static_cast<RowTerms*>(ws);
     const DistillArgs a{X, labels, teacher, weight, loss, dX, reinterpret_cast<float4*>(terms + B), terms, B, V, ld, ldd, cut.segments, cut.length,
-                        temperature, softmax_scale(temperature), K, tail != 0};
+                        temperature, softmax_scale(temperature), K, cut.blocks, tail != 0};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (t == XC_F32 && (dX == nullptr || out_t == XC_F32)) launch_distill<float, float>(a, cut, st);
     else if (t == XC_F32) launch_distill<float, bf16_t>(a, cut, st);

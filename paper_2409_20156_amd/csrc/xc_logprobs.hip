@@ -5,8 +5,7 @@
 
 namespace xc {
 
-constexpr int kTopKeys = 1024;           // candidates that a workgroup ranks at a time
-constexpr int kJoinKeys = 2048;
+constexpr int kTopKeys = 1024;           // candidates that a workgroup holds
 
 struct LogprobArgs {
     const void* X;
@@ -18,7 +17,7 @@ struct LogprobArgs {
     uint64_t* keys;                      // [B][segments][k]: its best labels, best first; ~0 behind them
     int64_t B, V, ld, segments, length;
     float T, c;
-    int n, k;
+    int n, k, blocks;
 };
 
 struct Norm { float m, ls; };            // largest score; log of the sum (-inf: no label is there)
@@ -57,35 +56,37 @@ __device__ __forceinline__ uint64_t wave_min_u64(uint64_t v) { return ~wave_max_
 
 constexpr uint32_t kLowest = 0x00800000u;        // ordered image of the lowest number above -inf
 
-// A score (as its ordered image) that at least k of the 64 W largest scores of the threads reach, if as many are there, and that few
-// others do: found by halving the range, by one wave.  At least k labels reach it, and no more than those of k or a few more threads.
-template <int W>
-__device__ __forceinline__ uint32_t reached_by(const float* largest, int k) {
-    uint32_t o[W], lo = ~0u, hi = 0u;
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-        o[w] = float_to_ordered(largest[w * kWave + lane_id()] + 0.0f);
-        lo = o[w] < lo ? o[w] : lo;
-        hi = o[w] > hi ? o[w] : hi;
+// Of n values (ordered images of scores; value(i) reads one): one that at least k of them reach, if as many lie above -inf, and that few
+// others do; found by halving the range, by one wave.  Equal values can make these many.
+template <typename V>
+__device__ __forceinline__ uint32_t reached_by(int n, int k, V value) {
+    uint32_t lo = ~0u, hi = 0u;
+    for (int i = lane_id(); i < n; i += kWave) {
+        const uint32_t o = value(i);
+        lo = o < lo ? o : lo;
+        hi = o > hi ? o : hi;
     }
     lo = ~wave_max_u32(~lo);
     hi = wave_max_u32(hi) + 1u;
     auto count = [&](uint32_t t) __attribute__((always_inline)) {
-        int n = 0;
-#pragma unroll
-        for (int w = 0; w < W; ++w) n += __popcll(__ballot(o[w] >= t));
-        return n;
+        int c = 0;
+        for (int i0 = 0; i0 < n; i0 += kWave) {
+            const int i = i0 + lane_id();
+            c += __popcll(__ballot(i < n && value(i < n ? i : 0) >= t));
+        }
+        return c;
     };
-    if (lo < kLowest) {
-        lo = kLowest;
-        if (count(lo) <= k) return lo;
-    }
-    while (hi - lo > 1u) {
-        const uint32_t mid = lo + (hi - lo) / 2u;
-        const int n = count(mid);
-        if (n >= k) {
+    if (lo < kLowest) lo = kLowest;
+    bool enough = false;                                     // (does `lo` leave more than k?)
+    while (hi > lo && hi - lo > 1u) {
+        const uint32_t mid = enough ? lo + (hi - lo) / 2u : lo;
+        const int c = count(mid);
+        if (!enough) {
+            if (c <= k) return lo;
+            enough = true;
+        } else if (c >= k) {
             lo = mid;
-            if (n <= k + k / 4 + 3) break;
+            if (c <= k + k / 4 + 3) break;
         } else {
             hi = mid;
         }
@@ -93,127 +94,233 @@ __device__ __forceinline__ uint32_t reached_by(const float* largest, int k) {
     return lo;
 }
 
+// How many of n keys are better than this one (the keys behind them, up to a multiple of four, are ~0).
+__device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
+    int rank = 0;
+#pragma unroll 2
+    for (int j = 0; j < n; j += 4) {
+        uint64_t k[4];
+        __builtin_memcpy(k, __builtin_assume_aligned(keys + j, 16), 32);
+        rank += (k[0] < key ? 1 : 0) + (k[1] < key ? 1 : 0) + (k[2] < key ? 1 : 0) + (k[3] < key ? 1 : 0);
+    }
+    return rank;
+}
+// n places of a counter in LDS to each lane.
+__device__ __forceinline__ int take_room(int* counter, int n) {
+    const uint32_t at = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) int*)counter));
+    int before;
+    asm volatile("ds_add_rtn_u32 %0, %1, %2\n\ts_waitcnt lgkmcnt(0)" : "=&v"(before) : "v"(at), "v"(n) : "memory");
+    return before;
+}
+// Behind n keys, for the function above; before a barrier.
+__device__ __forceinline__ void end_keys(uint64_t* keys, int n) {
+    if (threadIdx.x < 3) keys[n + threadIdx.x] = kKeySentinel;
+}
+
+// Of a block's elements (read again, so that this takes few registers from what always runs) the k best, by halving the range of their keys, to
+// `keys`; k of them at least score `least` or more.  Where a threshold lets through more labels than a workgroup holds, that is where many
+// scores are equal.
+template <typename T>
+__device__ __forceinline__ void best_of_block(const PiecedRow<T>& row, int64_t first, int64_t end, int64_t edge, int k, uint32_t least, int* counts, uint64_t* keys,
+                                              int* kept) {
+    constexpr int N = PiecedRow<T>::N;
+    uint64_t lo = 0, hi = (static_cast<uint64_t>(~least) << 32) | 0xffffffffu;            // fewer than k keys up to lo, k at least up to hi
+    for (int turn = 1;; turn ^= 1) {
+        const bool done = hi - lo <= 1;
+        const uint64_t mid = done ? hi : lo + (hi - lo) / 2;
+        int n = 0;
+#pragma unroll 1
+        for (int64_t at = first + threadIdx.x - kRowThreads; at < end; at += kRowThreads) {        // (before the pieces: the edge)
+            const bool edges = at < first;
+            if (edges && edge < 0) continue;
+            const T* p = row.p + (edges ? edge : row.first(at));
+#pragma unroll 1
+            for (int e = 0; e < (edges ? 1 : N); ++e) {
+                const float x = Elem<T>::get(p + e);
+                const uint64_t key = x == x ? make_key(x + 0.0f, static_cast<int32_t>(p + e - row.p)) : kKeySentinel;
+                if (key > mid) continue;
+                ++n;
+                if (done) keys[atomicAdd(kept, 1)] = key;
+            }
+        }
+        if (done) return;                                    // uniform
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1) n += __shfl_xor(n, off, kWave);
+        if (threadIdx.x == 0) counts[turn] = 0;
+        __syncthreads();
+        if (lane_id() == 0) atomicAdd(&counts[turn], n);
+        __syncthreads();
+        if (counts[turn] >= k) hi = mid;
+        else lo = mid;
+    }
+}
+
 // A segment of a row by one workgroup: its sums, and its k best labels.
-// The labels: each thread's largest score is known, and a score that k of the threads reach is reached by all k best labels and by few
-// others (scores in no particular order: about a seventh more where k is a quarter of the threads).  These are put into LDS and ranked
-// by counting.  Where many scores are equal there may be too many of them: then the k-th best is found by halving ranges over all elements.
-template <typename T, int W, int C>
-__global__ __launch_bounds__(W * kWave)
+// The labels: of the first block each thread's largest score is known, and a score that k of the threads reach is reached by all k best
+// labels of the block and by few others.  These, and what reaches the same score in the blocks behind, are collected in LDS; when they have
+// become several times k, a higher threshold is found among them and the others are dropped.  In the end the few that are left are ranked by
+// counting.
+template <typename T, int C>
+__global__ __launch_bounds__(kRowThreads)
 void logprobs_kernel(const LogprobArgs a) {
-    constexpr int N = PiecedRow<T>::N, kThreads = W * kWave;
-    __shared__ Sums sums[W];
-    __shared__ float largest[kThreads];
-    __shared__ uint64_t keys[kTopKeys];
+    constexpr int N = PiecedRow<T>::N, E = C * N;
+    __shared__ Sums sums[kRowWaves];
+    __shared__ uint32_t largest[kRowThreads];
+    __shared__ __align__(16) uint64_t lists[2][kTopKeys + 4];
     __shared__ uint32_t reach;
-    __shared__ int found, counts[2];
+    __shared__ int found[3], counts[2], kept;
     const int64_t b = blockIdx.x / static_cast<uint32_t>(a.segments), seg = blockIdx.x - b * a.segments;
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
-    const int64_t first = seg * a.length, end = first + a.length < row.pieces ? first + a.length : row.pieces;
-    uint4 v[C];
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int64_t at = first + i * kThreads + threadIdx.x;
-        v[i] = at < end ? row.load(at) : Elem<T>::none();
-    }
+    const int64_t begin = seg * a.length, end = begin + a.length < row.pieces ? begin + a.length : row.pieces;
+    Block<T, C> block;
+    auto load = [&](int64_t first) __attribute__((always_inline)) {        // (for the top labels some pieces are read twice)
+        if (a.k == 0) block.template load<true>(row, first, end, kRowThreads);
+        else block.template load<false>(row, first, end, kRowThreads);
+    };
+    load(begin);
     const int64_t edge = seg == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
-    const float more = edge >= 0 ? Elem<T>::get(row.p + edge) : kNone;
-    const Sums mine = thread_sums<true, C, T>(v, more, a.c);
-    largest[threadIdx.x] = mine.m;
-    if (threadIdx.x == 0) found = 0;
-    const Sums s = block_sums<W>(mine, a.c, sums);
+    float more = edge >= 0 ? Elem<T>::get(row.p + edge) : kNone;
+    if (threadIdx.x == 0) found[0] = 0;
+    Running run;
+    uint64_t* keys = lists[0];
+    int have = 0;                                            // keys from the blocks before
+    // the threshold among the keys, and what reaches it, in the other list; by the whole workgroup
+    auto thin = [&]() __attribute__((always_inline)) {
+        __syncthreads();                                     // (`kept` and `reach` have been read)
+        if (threadIdx.x < kWave) {
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(keys);
+            const uint32_t r = reached_by(have, a.k, [&](int i) __attribute__((always_inline)) { return ~words[2 * i + 1]; });
+            if (threadIdx.x == 0) {
+                reach = r > reach ? r : reach;
+                kept = 0;
+            }
+        }
+        __syncthreads();
+        uint64_t* other = keys == lists[0] ? lists[1] : lists[0];
+        const uint32_t r = reach;
+        for (int i = threadIdx.x; i < have; i += kRowThreads)
+            if (~static_cast<uint32_t>(keys[i] >> 32) >= r) other[atomicAdd(&kept, 1)] = keys[i];
+        __syncthreads();
+        keys = other;
+        have = kept;
+    };
+    // the k best of the keys alone, in the other list
+    auto cut = [&]() __attribute__((always_inline)) {
+        end_keys(keys, have);
+        __syncthreads();
+        uint64_t* other = keys == lists[0] ? lists[1] : lists[0];
+        for (int i = threadIdx.x; i < have; i += kRowThreads) {
+            const int rank = rank_of(keys[i], keys, have);
+            if (rank < a.k) other[rank] = keys[i];
+        }
+        __syncthreads();                                     // (the keys as well have been read)
+        keys = other;
+        have = have < a.k ? have : a.k;
+    };
+    const int room = 3 * a.k + 32 < kTopKeys / 2 ? 3 * a.k + 32 : kTopKeys / 2;
+    for (int n = 0; n < a.blocks; ++n) {                     // (a.blocks: of a whole segment; the row may end before)
+        const int64_t first = begin + static_cast<int64_t>(n) * (kRowThreads * C), stop = first + kRowThreads * C < end ? first + kRowThreads * C : end;
+        float most = kNone, piece[C];
+        {
+            float f[E];
+            block.values(f);
+            if (n + 1 < a.blocks) load(first + kRowThreads * C);
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                piece[i] = largest_of<N>(f, i * N);
+                most = fmaxf(most, piece[i]);
+            }
+            run.template add<true>(f, most, a.c);
+        }
+        if (a.k == 0) continue;                              // uniform
+        if (n == 0) {
+            largest[threadIdx.x] = float_to_ordered(fmaxf(most, more) + 0.0f);
+            __syncthreads();
+            if (threadIdx.x < kWave) {
+                const uint32_t r = reached_by(kRowThreads, a.k, [&](int i) __attribute__((always_inline)) { return largest[i]; });
+                if (threadIdx.x == 0) reach = r;
+            }
+            __syncthreads();
+        }
+        // (three counters in turn: one is cleared that everyone has read, while another one is counted up)
+        int* counter = &found[n % 3];
+        if (threadIdx.x == 0) found[(n + 1) % 3] = 0;
+        const uint32_t threshold = reach;
+        const float least = ordered_to_float(threshold);
+        // pieces with such labels are few: they are read again, so that the elements need not be kept.  Room is taken by a lane for all
+        // of a piece's at once, by the instruction itself (the compiler would add the lanes' numbers up first).
+        uint32_t marked = 0;
+#pragma unroll
+        for (int i = 0; i < C; ++i) marked |= (piece[i] >= least ? 1u : 0u) << i;
+#pragma unroll 1
+        while (marked != 0u) {
+            const int i = __ffs(static_cast<int>(marked)) - 1;
+            marked &= marked - 1u;
+            const T* p = row.p + row.first(first + i * kRowThreads + threadIdx.x);
+            uint4 v = *reinterpret_cast<const uint4*>(p);
+            float x[N];
+            Elem<T>::values(v, x);
+            uint32_t which = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) which |= x[e] >= least ? 1u << e : 0u;
+            int at = have + take_room(counter, __popc(which));
+            const int32_t id = static_cast<int32_t>(p - row.p);
+#pragma unroll 1
+            for (; which != 0u && at < kTopKeys; which &= which - 1u, ++at) {
+                const int e = __ffs(static_cast<int>(which)) - 1;
+                keys[at] = make_key(Elem<T>::get(p + e) + 0.0f, id + e);       // (-0 and 0 are equal)
+            }
+        }
+        if (n == 0 && more >= least) {
+            const int at = have + take_room(counter, 1);
+            if (at < kTopKeys) keys[at] = make_key(more + 0.0f, static_cast<int32_t>(edge));
+        }
+        __syncthreads();
+        const int now = *counter;
+        if (__builtin_expect(have + now > kTopKeys, 0)) {    // uniform, as all of these
+            if (threadIdx.x == 0) kept = 0;
+            __syncthreads();
+            best_of_block<T>(row, first, stop, n == 0 ? edge : -1, a.k, threshold, counts, keys + have, &kept);
+            __syncthreads();
+            have += kept;
+            __syncthreads();
+        } else {
+            have += now;
+        }
+        const bool last = n + 1 == a.blocks;
+        if (have > (last ? a.k + a.k / 2 + 8 : room)) thin();
+        if (last || have > room) cut();
+    }
+    run.add_one(more, a.c);
+    __syncthreads();
+    const Sums s = block_sums<kRowWaves>(run.sums(a.c), a.c, sums);
     const bool alone = a.segments == 1;
     if (alone) write_row<T>(a, b, s);
     else if (threadIdx.x == 0) a.parts[b * a.segments + seg] = make_float4(s.m, s.s, s.h, 0.0f);
     if (a.k == 0) return;
-
-    if (threadIdx.x < kWave) {
-        const uint32_t r = reached_by<W>(largest, a.k);
-        if (threadIdx.x == 0) reach = r;
-    }
-    __syncthreads();
-    // every element of the thread, with its label
-    auto each = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            float x[N];
-            Elem<T>::values(v[i], x);
-            const int32_t id = static_cast<int32_t>(row.first(first + i * kThreads + threadIdx.x));
-#pragma unroll
-            for (int e = 0; e < N; ++e) f(x[e], id + e);
-        }
-        f(more, static_cast<int32_t>(edge));
-    };
-    auto take = [&](float x, int32_t id) __attribute__((always_inline)) {
-        const int at = atomicAdd(&found, 1);
-        if (at < kTopKeys) keys[at] = make_key(x + 0.0f, id);              // (-0 and 0 are equal)
-    };
-    const float least = ordered_to_float(reach);
-    if (mine.m >= least) each([&](float x, int32_t id) __attribute__((always_inline)) { if (x >= least) take(x, id); });
-    __syncthreads();
-    if (found > kTopKeys) {                                  // uniform
-        auto image = [](float x) __attribute__((always_inline)) { return x == x ? float_to_ordered(x + 0.0f) : 0u; };
-        int turn = 0;
-        auto count = [&](auto which) __attribute__((always_inline)) {      // of the workgroup's elements
-            int n = 0;
-            each([&](float x, int32_t id) __attribute__((always_inline)) { n += which(image(x), id) ? 1 : 0; });
-#pragma unroll
-            for (int off = kWave / 2; off > 0; off >>= 1) n += __shfl_xor(n, off, kWave);
-            turn ^= 1;
-            if (threadIdx.x == 0) counts[turn] = 0;
-            __syncthreads();
-            if (lane_id() == 0) atomicAdd(&counts[turn], n);
-            __syncthreads();
-            return counts[turn];
-        };
-        uint32_t lo = reach, hi = 0xff800001u;               // (behind infinity)
-        while (hi - lo > 1u) {
-            const uint32_t mid = lo + (hi - lo) / 2u;
-            if (count([&](uint32_t o, int32_t) __attribute__((always_inline)) { return o >= mid; }) >= a.k) lo = mid;
-            else hi = mid;
-        }
-        const int left = a.k - count([&](uint32_t o, int32_t) __attribute__((always_inline)) { return o > lo; });
-        int64_t under = -1, last = a.V - 1;                  // of the labels that score lo, the `left` lowest: up to `last`
-        while (last - under > 1) {
-            const int64_t mid = under + (last - under) / 2;
-            if (count([&](uint32_t o, int32_t id) __attribute__((always_inline)) { return o == lo && id <= mid; }) >= left) last = mid;
-            else under = mid;
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) found = 0;
-        __syncthreads();
-        each([&](float x, int32_t id) __attribute__((always_inline)) {
-            const uint32_t o = image(x);
-            if (o > lo || (o == lo && id <= last)) take(x, id);
-        });
-        __syncthreads();
-    }
-    const int n = found;
     const Norm z = norm_of(s);
     uint64_t* out = a.keys + (b * a.segments + seg) * a.k;
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const uint64_t key = keys[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] < key ? 1 : 0;
-        if (rank < a.k) {
-            if (alone) write_top(a, b, rank, key, z);
-            else out[rank] = key;
-        }
-    }
-    for (int i = n + threadIdx.x; i < a.k; i += kThreads) {
-        if (alone) write_top(a, b, i, kKeySentinel, z);
-        else out[i] = kKeySentinel;
+    for (int i = threadIdx.x; i < a.k; i += kRowThreads) {
+        const uint64_t key = i < have ? keys[i] : kKeySentinel;
+        if (alone) write_top(a, b, i, key, z);
+        else out[i] = key;
     }
 }
 
-// The segments of a row joined, by a workgroup per row.  The best labels: of every segment the labels that are no worse than the worst of
-// the segments' r-th ones, r = k / segments rounded up (k labels at least are no worse than that), ranked by counting.
-constexpr int kJoinWaves = 4;
+// The segments of a row joined, by a workgroup per row.  The best labels, of up to kJoinAtOnce segments at a time and the best of those
+// before them: of the first r of each segment (2 k labels or a few more in all) the k-th best is found by ranking; whatever is worse than
+// that is left out, and the few others are ranked.
+constexpr int kJoinWaves = 4, kJoinAtOnce = 128;
+constexpr int kJoinFirst = 2 * XC_MAX_TOP + kJoinAtOnce;     // labels of the first ranking at most
+constexpr int kJoinKeys = kJoinAtOnce * XC_MAX_TOP < 2048 ? kJoinAtOnce * XC_MAX_TOP : 2048;
 template <typename T>
 __global__ __launch_bounds__(kJoinWaves * kWave)
 void logprobs_join_kernel(const LogprobArgs a) {
     __shared__ Sums sums[kJoinWaves];
-    __shared__ uint64_t keys[kJoinKeys], best[XC_MAX_TOP];
+    __shared__ __align__(16) uint64_t keys[kJoinKeys + XC_MAX_TOP + 4], best[XC_MAX_TOP];
+    __shared__ uint64_t bound;
     __shared__ int found;
+    static_assert(kJoinFirst <= kJoinKeys, "");
     constexpr int kThreads = kJoinWaves * kWave;
     const int64_t b = blockIdx.x;
     Sums t{kNone, 0.0f, 0.0f};
@@ -229,30 +336,39 @@ void logprobs_join_kernel(const LogprobArgs a) {
     if (a.k == 0) return;
     const Norm z = norm_of(s);
     int have = 0;
-    const int64_t at_once = (kJoinKeys - a.k) / a.k;
+    const int at_once = kJoinKeys / a.k < kJoinAtOnce ? kJoinKeys / a.k : kJoinAtOnce;
     for (int64_t s0 = 0; s0 < a.segments; s0 += at_once) {
         const int g = static_cast<int>(a.segments - s0 < at_once ? a.segments - s0 : at_once);
         const uint64_t* in = a.keys + (b * a.segments + s0) * a.k;
-        uint64_t bound = 0;
-        for (int i = lane_id(); i < g; i += kWave) {
-            const uint64_t x = in[static_cast<int64_t>(i) * a.k + (a.k + g - 1) / g - 1];
-            bound = x > bound ? x : bound;
-        }
-        bound = wave_max_u64(bound);
+        const int want = (2 * a.k + g - 1) / g, r = want < a.k ? want : a.k, first = g * r;
         __syncthreads();                                     // (the round before has read its keys)
-        for (int i = threadIdx.x; i < have; i += kThreads) keys[i] = best[i];
-        if (threadIdx.x == 0) found = have;
+        for (int i = threadIdx.x; i < first; i += kThreads) {
+            const int seg = i / r;
+            keys[i] = in[seg * a.k + (i - seg * r)];
+        }
+        end_keys(keys, first);
+        if (threadIdx.x == 0) {
+            bound = kKeySentinel;
+            found = have;
+        }
         __syncthreads();
+        // (labels that are not there have the same key: where they reach the k-th place, `bound` stays what it is, theirs)
+        for (int i = threadIdx.x; i < first; i += kThreads)
+            if (keys[i] != kKeySentinel && rank_of(keys[i], keys, first) == a.k - 1) bound = keys[i];
+        __syncthreads();
+        const uint64_t limit = bound;
+        for (int i = threadIdx.x; i < have; i += kThreads) keys[i] = best[i];
         for (int i = threadIdx.x; i < g * a.k; i += kThreads) {
             const uint64_t x = in[i];
-            if (x <= bound && x != kKeySentinel) keys[atomicAdd(&found, 1)] = x;
+            if (x <= limit && x != kKeySentinel) keys[atomicAdd(&found, 1)] = x;
         }
         __syncthreads();
         const int n = found;
+        end_keys(keys, n);
+        __syncthreads();
         for (int i = threadIdx.x; i < n; i += kThreads) {
             const uint64_t key = keys[i];
-            int rank = 0;
-            for (int j = 0; j < n; ++j) rank += keys[j] < key ? 1 : 0;
+            const int rank = rank_of(key, keys, n);
             if (rank < a.k) best[rank] = key;
         }
         have = n < a.k ? n : a.k;
@@ -289,7 +405,7 @@ void logprobs_grad_kernel(const LogprobGradArgs a) {
 #pragma unroll
     for (int i = 0; i < kGradEach; ++i) {
         const int64_t at = first + i * kGradThreads + threadIdx.x;
-        v[i] = at < end ? row.load(at) : make_uint4(0, 0, 0, 0);
+        v[i] = at < end ? row.template load<true>(at) : make_uint4(0, 0, 0, 0);
     }
     const int64_t edge = chunk == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
     const float more = edge >= 0 ? Elem<T>::get(row.p + edge) : 0.0f;
@@ -372,11 +488,9 @@ static void launch_logprobs(const LogprobArgs& all, const RowCut& cut, hipStream
         a.parts += b0 * cut.segments;
         a.keys += b0 * cut.segments * all.k;
         const unsigned grid = static_cast<unsigned>(nb * cut.segments);
-        auto go = [&](auto kernel, int waves) { XC_LAUNCH(K_LOGPROBS, st, (kernel<<<grid, waves * kWave, 0, st>>>(a))); };
-        if (cut.waves == 4) go(logprobs_kernel<T, 4, 2>, 4);
-        else if (cut.each == 2) go(logprobs_kernel<T, 8, 2>, 8);
-        else if (cut.each == 4) go(logprobs_kernel<T, 8, 4>, 8);
-        else go(logprobs_kernel<T, 8, 8>, 8);
+        constexpr int kSmall = small_block(sizeof(T)), kLarge = large_block(sizeof(T));
+        if (cut.each == kSmall) XC_LAUNCH(K_LOGPROBS, st, (logprobs_kernel<T, kSmall><<<grid, kRowThreads, 0, st>>>(a)));
+        else XC_LAUNCH(K_LOGPROBS, st, (logprobs_kernel<T, kLarge><<<grid, kRowThreads, 0, st>>>(a)));
         if (cut.segments > 1)
             XC_LAUNCH(K_LOGPROBS_JOIN, st, (logprobs_join_kernel<T><<<static_cast<unsigned>(nb), kJoinWaves * kWave, 0, st>>>(a)));
     }
@@ -432,7 +546,7 @@ extern "C" int xc_label_logprobs(const void* X, int64_t ld, int64_t B, int64_t V
     const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2);
     float4* parts = static_cast<float4*>(ws);
     const LogprobArgs a{X, labels, logp, entropy, norm, top, top_logp, parts, reinterpret_cast<uint64_t*>(parts + B * cut.segments), B, V, ld, cut.segments,
-                        cut.length, temperature, softmax_scale(temperature), n, k};
+                        cut.length, temperature, softmax_scale(temperature), n, k, cut.blocks};
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (t == XC_F32) launch_logprobs<float>(a, cut, st);
     else launch_logprobs<bf16_t>(a, cut, st);
