@@ -2,7 +2,7 @@
 // 32 neighbouring elements of a row share a scale 2^(byte - 127); an element is a sign, two bits of exponent and one of mantissa: 0, 0.5, 1,
 // 1.5, 2, 3, 4 or 6.  The largest magnitude of a block decides the scale: the power of two that brings it into [4, 8).  What lies beyond 6
 // then is 6 (the format's published conversion, so that rows laid out elsewhere mean the same here).
-#include "xc_common.h"
+#include "xc_mine.h"
 
 namespace xc {
 
@@ -36,53 +36,96 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {   // of four neighbou
     return o > x ? o : x;
 }
 
-// 16 lanes bring 128 elements of a row, four lanes to a block.
-template <typename T>
+// Codes and scale byte of a lane's 8 elements; four lanes have a block.
+struct MicroLane { uint32_t codes, byte; };
+__device__ __forceinline__ MicroLane to_micro(float (&f)[8]) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t b = __float_as_uint(f[e]) & 0x7fffffffu;
+        big = b > big ? b : big;
+    }
+    big = quad_max(big);
+    const bool finite = big < 0x7f800000u;
+    const uint32_t exponent = big >> 23, byte = exponent > 2u ? exponent - 2u : 0u;
+    const float inv = __uint_as_float((254u - (finite ? byte : 0u)) << 23);            // (a power of two: products are exact, or far below 0.25)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] *= inv;
+    uint32_t codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], 1.0f, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], 1.0f, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], 1.0f, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], 1.0f, 3);
+    return MicroLane{finite ? codes : 0u, finite ? byte : 255u};
+}
+
+// Rows of 4 bits where they are kept: Q (64 bytes to 128 elements) and their scales row by row.
+struct MicroRows {
+    uint8_t *Q, *scale;
+    int units;                           // of 128 elements in a row
+    __device__ __forceinline__ void put(int64_t row, int u, int sub, const MicroLane& m) const {
+        *reinterpret_cast<uint32_t*>(Q + (row * units + u) * 64 + sub * 4) = m.codes;
+        if ((sub & 3) == 0) scale[(row * units + u) * 4 + (sub >> 2)] = static_cast<uint8_t>(m.byte);
+    }
+};
+// Queries in the workspace: rows of `pitch` bytes (an even number of units), zeros behind the last element and the last query.  A row's
+// scales are laid out as the products ask for them: block 4 u + b of unit u at b * upad + u, so that a lane finds four units' in a word.
+struct MicroQueries {
+    uint8_t *P, *scale;
+    int units, pitch, upad;
+    __device__ __forceinline__ void put(int64_t row, int u, int sub, const MicroLane& m) const {
+        *reinterpret_cast<uint32_t*>(P + row * pitch + u * 64 + sub * 4) = m.codes;
+        if ((sub & 3) == 0 && u < upad) scale[row * 4 * upad + (sub >> 2) * upad + u] = static_cast<uint8_t>(m.byte);
+    }
+};
+
+// 16 lanes bring 128 elements of a row, U of these at a time.  Rows from N on (of the queries' padding) and units behind a row are zeros.
+// Bound: memory.
+template <typename T, typename TO, int U>
 __global__ __launch_bounds__(256)
 void microscale_kernel(const unsigned char* __restrict__ X, int64_t N, int d, const int32_t* __restrict__ ids, int64_t m, const int32_t* __restrict__ count,
-                       uint8_t* __restrict__ Q, uint8_t* __restrict__ scale, int units /* of 128 elements in a row */) {
+                       const TO out, int64_t n_rows, int units /* written of a row */) {
     const int sub = threadIdx.x & 15;
-    int64_t rows = ids != nullptr ? m : N;
+    int64_t rows = ids != nullptr ? m : n_rows;
     if (ids != nullptr && count != nullptr) {
         const int64_t c = count[0];
         rows = c < rows ? c : rows;
     }
-    const int64_t total = rows * units, step = static_cast<int64_t>(gridDim.x) * 16;
-    for (int64_t u = static_cast<int64_t>(blockIdx.x) * 16 + (threadIdx.x >> 4); u < total; u += step) {
-        const int64_t i = u / units, row = ids != nullptr ? ids[i] : i;
-        const int col = static_cast<int>(u - i * units);
-        if (row < 0 || row >= N) continue;                   // (16 lanes leave together)
-        float f[8];
-        eight<T>(X + row * d * static_cast<int64_t>(sizeof(T)), col * kMxRow + sub * 8, d, f);
-        uint32_t big = 0;
+    const int64_t total = rows * units, step = static_cast<int64_t>(gridDim.x) * (16 * U);
+    for (int64_t u0 = static_cast<int64_t>(blockIdx.x) * (16 * U) + (threadIdx.x >> 4); u0 < total; u0 += step) {
+        float f[U][8];
+        int64_t row[U];
+        int col[U];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t b = __float_as_uint(f[e]) & 0x7fffffffu;
-            big = b > big ? b : big;
+        for (int k = 0; k < U; ++k) {
+            const int64_t u = u0 + k * 16;
+            row[k] = -1;
+            if (u >= total) continue;
+            const int64_t i = u / units;
+            col[k] = static_cast<int>(u - i * units);
+            row[k] = ids != nullptr ? ids[i] : i;
+            const bool there = row[k] >= 0 && row[k] < N;                  // (the same for 16 lanes)
+            if (!there && ids != nullptr) { row[k] = -1; continue; }
+            eight<T>(X + (there ? row[k] : 0) * d * static_cast<int64_t>(sizeof(T) == 4 ? 4 : 2), there ? col[k] * kMxRow + sub * 8 : d, d, f[k]);
         }
-        big = quad_max(big);
-        const bool finite = big < 0x7f800000u;
-        const uint32_t exponent = big >> 23, byte = exponent > 2u ? exponent - 2u : 0u;
-        const float inv = __uint_as_float((254u - (finite ? byte : 0u)) << 23);
-        uint32_t codes = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] *= inv;
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], 1.0f, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], 1.0f, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], 1.0f, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], 1.0f, 3);
-        *reinterpret_cast<uint32_t*>(Q + (row * units + col) * (kMxRow / 2) + sub * 4) = finite ? codes : 0u;
-        if ((sub & 3) == 0) scale[(row * units + col) * 4 + (sub >> 2)] = static_cast<uint8_t>(finite ? byte : 255u);
+        for (int k = 0; k < U; ++k)
+            if (row[k] >= 0) out.put(row[k], col[k], sub, to_micro(f[k]));
     }
 }
 
-static int launch_microscale(const void* X, int64_t N, int d, xc_dtype t, const int32_t* ids, int64_t m, const int32_t* count, uint8_t* Q, uint8_t* scale, hipStream_t st) {
-    const int units = static_cast<int>(mx_pitch(d) / kMxRow);
-    const int64_t rows = ids != nullptr ? m : N, want = (rows * units + 15) / 16;
-    const unsigned grid = static_cast<unsigned>(want < 16384 ? want : 16384);
+template <typename TO>
+static int launch_microscale(const void* X, int64_t N, int d, xc_dtype t, const int32_t* ids, int64_t m, const int32_t* count, const TO& out, int64_t n_rows, int units,
+                             hipStream_t st) {
+    const int64_t rows = ids != nullptr ? m : n_rows, total = rows * units;
     const unsigned char* x = static_cast<const unsigned char*>(X);
-    if (t == XC_F32) XC_LAUNCH(K_MICROSCALE, st, (microscale_kernel<float><<<grid, 256, 0, st>>>(x, N, d, ids, m, count, Q, scale, units)));
-    else XC_LAUNCH(K_MICROSCALE, st, (microscale_kernel<bf16_t><<<grid, 256, 0, st>>>(x, N, d, ids, m, count, Q, scale, units)));
+    auto go = [&](auto kernel, int U) {
+        const int64_t want = (total + 16 * U - 1) / (16 * U);
+        kernel<<<static_cast<unsigned>(want < 32768 ? want : 32768), 256, 0, st>>>(x, N, d, ids, m, count, out, n_rows, units);
+    };
+    const bool many = total > 256 * 16 * 8;
+    if (t == XC_F32) XC_LAUNCH(K_MICROSCALE, st, (many ? go(microscale_kernel<float, TO, 4>, 4) : go(microscale_kernel<float, TO, 1>, 1)));
+    else XC_LAUNCH(K_MICROSCALE, st, (many ? go(microscale_kernel<bf16_t, TO, 4>, 4) : go(microscale_kernel<bf16_t, TO, 1>, 1)));
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }
@@ -91,47 +134,392 @@ static int launch_microscale(const void* X, int64_t N, int d, xc_dtype t, const 
 // scores
 // ---------------------------------------------------------------------------
 struct MicroArgs {
+    const unsigned char* Z;              // queries as they came (the kernel that brings them to 4 bits itself)
     const uint8_t *P, *pscale;           // queries in 4 bits
     const uint8_t *Q, *scale;
     void* out;
-    int64_t B, L, tiles_m, tiles_n;
-    int units;                           // of 128 elements in a row
+    int64_t B, L;
+    int d, units, ppitch, upad;          // units of 128 elements in a row of Q; the queries' rows, see MicroQueries
 };
 
-// Blocks of 16 labels x 16 queries x 128 elements: lane l has the 32 elements of block l / 16 of row l % 16 of both operands; its
-// accumulator i is label 4 (l / 16) + i, query l % 16.
-__device__ __forceinline__ mx_f32x4 mx_product(const mx_i32x4& w, const mx_i32x4& z, const mx_f32x4& c, int ws, int zs) {
-    const mx_i32x8 a = {w.x, w.y, w.z, w.w, 0, 0, 0, 0}, b = {z.x, z.y, z.z, z.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4 /* fp4 */, 4, 0, ws, 0, zs);
+// Blocks of 16 queries x 16 labels x 128 elements: lane l has the 32 elements of block l / 16 of row l % 16 of both operands; its
+// accumulator i is query 4 (l / 16) + i, label l % 16 of the block.  A word of scale bytes holds four units', of which S is taken.
+// In every kernel a score is the sum over its units in order, from 0: its bits do not depend on the kernel.
+template <int S>
+__device__ __forceinline__ mx_f32x4 mx_product(const mx_i32x4& z, const mx_i32x4& w, const mx_f32x4& c, int zs, int ws) {
+    const mx_i32x8 a = {z.x, z.y, z.z, z.w, 0, 0, 0, 0}, b = {w.x, w.y, w.z, w.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4 /* fp4 */, 4, S, zs, S, ws);
 }
-template <typename TO> __device__ __forceinline__ void put_scores(TO* p, const float* v, int n);
-template <> __device__ __forceinline__ void put_scores<float>(float* p, const float* v, int n) {
-    for (int e = 0; e < n; ++e) p[e] = v[e];
-}
-template <> __device__ __forceinline__ void put_scores<bf16_t>(bf16_t* p, const float* v, int n) {
-    for (int e = 0; e < n; ++e) p[e].bits = static_cast<uint16_t>(float_to_bf16_bits(v[e]));
+__device__ __forceinline__ mx_f32x4 mx_product(int s /* known when compiled */, const mx_i32x4& z, const mx_i32x4& w, const mx_f32x4& c, int zs, int ws) {
+    switch (s & 3) {
+        case 0: return mx_product<0>(z, w, c, zs, ws);
+        case 1: return mx_product<1>(z, w, c, zs, ws);
+        case 2: return mx_product<2>(z, w, c, zs, ws);
+        default: return mx_product<3>(z, w, c, zs, ws);
+    }
 }
 
-// A wave has 64 labels x 64 queries.
+// 4 neighbouring scores of a row, the first `have` of which are there.
+typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void put_four(float* p, const float (&v)[4]) { __builtin_memcpy(p, v, 16); }
+__device__ __forceinline__ void put_four(bf16_t* p, const float (&v)[4]) {
+    const mx_bf16x2 h[2] = {__builtin_convertvector(mx_f32x2{v[0], v[1]}, mx_bf16x2), __builtin_convertvector(mx_f32x2{v[2], v[3]}, mx_bf16x2)};      // nearest, ties to even
+    __builtin_memcpy(p, h, 8);
+}
+__device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put_one(bf16_t* p, float v) {
+    const __bf16 h = static_cast<__bf16>(v);
+    __builtin_memcpy(p, &h, 2);
+}
+// (`whole` is the same for a wave: where lanes decided each for themselves, the compiler, ROCm 7.2's, let the last of fewer than four
+// scores take the fourth one's register in all lanes)
+template <typename TO> __device__ __forceinline__ void put_labels(TO* p, const float (&v)[4], bool whole, int64_t have) {
+    if (whole) {
+        put_four(p, v);
+    } else {
+#pragma unroll
+        for (int y = 0; y < 4; ++y) if (y < have) put_one(p + y, v[y]);
+    }
+}
+__device__ __forceinline__ int mx_swizzle(int row) { return (row >> 1) & 7; }
+__device__ __forceinline__ const void* mx_uniform(const void* p) {
+    const uint64_t a = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const void*>(
+        (static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a >> 32)))) << 32) |
+        static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a)))));
+}
+
+// ---- few queries: 16 MQ of them stay in LDS (rows of up to 64 KU bytes), the labels pass, 64 to a wave at a time, straight into registers,
+// two units of each under way while the two before are multiplied.  Lane l has labels 4 (l % 16) .. + 3 of the 64, so that it stores
+// neighbouring scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
+// Bound: one read of Q.
+template <typename TO, typename TZ, int MQ, int KU, int W>
+__global__ __launch_bounds__(W * kWave)
+void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
+    constexpr int kRows = 16 * MQ, kUpad = (KU + 3) / 4 * 4;
+    __shared__ __align__(1024) unsigned char codes[kRows * KU * 64];       // 128 bytes of every row, the next 128, ..; chunks of 16 swizzled
+    __shared__ __align__(16) unsigned char scales[kRows * 4 * kUpad];
+    const int lane = lane_id(), r = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t groups = (a.L + 63) / 64;
+    const int row_bytes = a.units * 64, row_scales = a.units * 4;
+    // neighbouring groups to neighbouring waves, and a contiguous part of them to each XCD
+    const int64_t per = (groups + kXcds - 1) / kXcds, g_begin = blockIdx.x % kXcds * per, g_end = g_begin + per < groups ? g_begin + per : groups;
+    const int64_t g_step = static_cast<int64_t>(gridDim.x / kXcds) * W;
+    int64_t g = g_begin + static_cast<int64_t>(blockIdx.x / kXcds) * W + wave;
+    const int steps = (a.units + 1) / 2;
+
+    mx_i32x4 w[2][2][4];
+    int ws[2][2][4];
+    auto bring = [&](int to, int64_t g, int step) __attribute__((always_inline)) {
+        const int64_t l0 = g * 64;
+        const int u = step * 2;
+        const bool second = u + 1 < a.units;
+        const int64_t last = a.L - 1 - l0;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            int64_t row = r * 4 + y;
+            row = l0 + (row < last ? row : last);
+            const uint8_t* p = a.Q + row * row_bytes + u * 64 + quarter * 16;
+            const uint8_t* s = a.scale + row * row_scales + u * 4;
+            w[to][0][y] = *reinterpret_cast<const mx_i32x4*>(p);
+            ws[to][0][y] = *reinterpret_cast<const int*>(s);
+            if (second) {                                    // uniform
+                w[to][1][y] = *reinterpret_cast<const mx_i32x4*>(p + 64);
+                ws[to][1][y] = *reinterpret_cast<const int*>(s + 4);
+            }
+        }
+    };
+    if (g < g_end) bring(0, g, 0);
+
+    // the queries
+    if constexpr (!std::is_void<TZ>::value) {
+        for (int i = threadIdx.x >> 4; i < kRows * a.units; i += W * 4) {
+            const int row = i / a.units, u = i - row * a.units, sub = threadIdx.x & 15;
+            float f[8];
+            const bool there = q0 + row < a.B;
+            eight<TZ>(a.Z + (there ? q0 + row : 0) * a.d * static_cast<int64_t>(sizeof(TZ) == 4 ? 4 : 2), there ? u * kMxRow + sub * 8 : a.d, a.d, f);
+            const MicroLane m = to_micro(f);
+            *reinterpret_cast<uint32_t*>(codes + (u >> 1) * (kRows * 128) + row * 128 + ((((u & 1) * 4 + (sub >> 2)) ^ mx_swizzle(row)) * 16) + (sub & 3) * 4) = m.codes;
+            if ((sub & 3) == 0) scales[row * (4 * kUpad) + (sub >> 2) * kUpad + u] = static_cast<unsigned char>(m.byte);
+        }
+    } else {
+        const int chunks = a.ppitch / 16;
+        for (int i = threadIdx.x; i < kRows * chunks; i += W * kWave) {
+            const int row = i / chunks, c = i - row * chunks;
+            *reinterpret_cast<uint4*>(codes + (c >> 3) * (kRows * 128) + row * 128 + (((c & 7) ^ mx_swizzle(row)) * 16)) =
+                *reinterpret_cast<const uint4*>(a.P + (q0 + row) * a.ppitch + c * 16);
+        }
+        for (int i = threadIdx.x; i < kRows * a.upad; i += W * kWave) {    // words of 4 units
+            const int row = i / a.upad, c = i - row * a.upad, b = c / (a.upad / 4), k = c - b * (a.upad / 4);
+            *reinterpret_cast<uint32_t*>(scales + row * (4 * kUpad) + b * kUpad + k * 4) =
+                *reinterpret_cast<const uint32_t*>(a.pscale + (q0 + row) * 4 * a.upad + b * a.upad + k * 4);
+        }
+    }
+    __syncthreads();
+    const unsigned char* frag = codes + r * 128 + ((quarter ^ mx_swizzle(r)) * 16);
+    auto query = [&](int x, int u) __attribute__((always_inline)) {        // 16 queries, 64 bytes of each
+        const uint32_t at = (u >> 1) * (kRows * 128) + x * 16 * 128;
+        return *reinterpret_cast<const mx_i32x4*>(codes + at + ((frag - codes) ^ ((u & 1) * 64)));
+    };
+    for (; g < g_end; g += g_step) {
+        mx_f32x4 acc[MQ][4];
+#pragma unroll
+        for (int x = 0; x < MQ; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) acc[x][y] = mx_f32x4{0, 0, 0, 0};
+        auto multiply = [&](int from, int step) __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int u = step * 2 + h;
+                if (u >= a.units) break;                     // uniform
+#pragma unroll
+                for (int x = 0; x < MQ; ++x) {
+                    const mx_i32x4 z = query(x, u);
+                    const int zs = scales[(x * 16 + r) * (4 * kUpad) + quarter * kUpad + u];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        acc[x][y] = mx_product<0>(z, w[from][h][y], acc[x][y], zs, static_cast<int>(static_cast<uint32_t>(ws[from][h][y]) >> (quarter * 8)));
+                }
+            }
+        };
+        // the next two units, of the next group behind the last ones
+        auto next = [&](int to, int step) __attribute__((always_inline)) {
+            if (step < steps) bring(to, g, step);
+            else if (g + g_step < g_end) bring(to, g + g_step, 0);
+        };
+        for (int step = 0; step < steps; step += 2) {
+            next(1, step + 1);
+            multiply(0, step);
+            if (step + 1 < steps) {
+                next(0, step + 2);
+                multiply(1, step + 1);
+            }
+        }
+        if ((steps & 1) != 0) {                              // (an odd number: the next group's first ones are in the other half)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                    w[0][h][y] = w[1][h][y];
+                    ws[0][h][y] = ws[1][h][y];
+                }
+        }
+        const int64_t l = g * 64 + r * 4, have = a.L - l;
+        const bool whole = g * 64 + 64 <= a.L;               // uniform
+#pragma unroll
+        for (int x = 0; x < MQ; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t q = q0 + x * 16 + quarter * 4 + i;
+                if (q >= a.B) continue;
+                const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
+                put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
+            }
+    }
+}
+
+// ---- many queries, rows of up to 512 bytes (1024 elements): the labels stay where they are.  A wave holds 64 labels as operands in registers
+// (NK units) and 512 labels of a workgroup meet the queries that stream through LDS, 64 at a time; a wave's scores are stored 16 queries at
+// a time, while the other wave of its SIMD multiplies.
+template <int NK_>
+struct MicroHeld {
+    static constexpr int NK = NK_, QS = 64, kUpad = NK <= 4 ? 4 : 8, kStage = QS * NK * 64, kScales = QS * 4 * kUpad;
+    static constexpr int kFit = 160 * 1024 / (kStage + kScales), R = kFit < 6 ? kFit : 6;   // stages in LDS
+    static constexpr int kLoads = kStage / 1024 / 8, kStores = QS / 4;                      // of a wave and stage
+    static constexpr int kLds = R * (kStage + kScales);
+    static_assert(kLoads * 8 * 1024 == kStage && R >= 3 && (kLoads + kStores) * (R - 3) < 64, "whole loads, and a count that the wait can hold");
+};
+constexpr int kMicroHeldLabels = 512;
+constexpr int kMicroPieces = 4;                          // of the tiles behind the last whole round, to a workgroup
+
+template <typename TO, int NK>
+__global__ __launch_bounds__(512, 2)
+void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
+    typedef MicroHeld<NK> H;
+    __shared__ __align__(1024) unsigned char smem[H::kLds];
+    __shared__ int4 last[kMicroPieces + 1];
+    const int lane = lane_id(), quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
+    // Each XCD takes neighbouring tiles of labels, a workgroup one of every 32, so that the lines that two tiles share are written at
+    // about the same time.  Of the last tiles, fewer than 32, a workgroup has an equal number of stages.
+    const int xcd = blockIdx.x % kXcds, nth = blockIdx.x / kXcds;
+    const int t_begin = static_cast<int>(static_cast<int64_t>(tiles) * xcd / kXcds) + nth;
+    const int t_count = static_cast<int>(static_cast<int64_t>(tiles) * (xcd + 1) / kXcds) + nth - t_begin, rounds = t_count / kCusPerXcd;
+    if (threadIdx.x == 0) {
+        const int rest = t_count % kCusPerXcd, first = t_begin - nth + rounds * kCusPerXcd;
+        const int64_t all = static_cast<int64_t>(rest) * stages, u1 = all * (nth + 1) / kCusPerXcd;
+        int n = 0, sum = 0;
+        for (int64_t u = all * nth / kCusPerXcd; u < u1;) {                // (less than a tile's stages: two tiles at most)
+            const int t = static_cast<int>(u / stages), s = static_cast<int>(u - static_cast<int64_t>(t) * stages);
+            const int e = stages - s < u1 - u ? stages : s + static_cast<int>(u1 - u);
+            last[n++] = make_int4(first + t, s, e, 0);
+            sum += e - s;
+            u += e - s;
+        }
+        last[0].w = rounds * stages + sum;
+    }
+    __syncthreads();
+    // the workgroup's n-th piece of work: a tile and stages of queries
+    auto piece = [&](int n, int& tile, int& begin, int& end) __attribute__((always_inline)) {
+        tile = t_begin + n * kCusPerXcd;
+        begin = 0;
+        end = stages;
+        if (n >= rounds) {
+            const int4 l = last[n - rounds];
+            tile = __builtin_amdgcn_readfirstlane(l.x);
+            begin = __builtin_amdgcn_readfirstlane(l.y);
+            end = __builtin_amdgcn_readfirstlane(l.z);
+        }
+    };
+    const int total = __builtin_amdgcn_readfirstlane(last[0].w);
+    if (total == 0) return;
+    int tile, ld_tile, st, st_end;
+    piece(0, tile, st, st_end);
+
+    uint32_t off[H::kLoads];
+#pragma unroll
+    for (int i = 0; i < H::kLoads; ++i) {
+        const int n = wave * H::kLoads + i, row = n % (H::QS / 8) * 8 + (lane >> 3);
+        off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(NK * 64) + n / (H::QS / 8) * 128 + (((lane & 7) ^ mx_swizzle(row)) * 16);
+    }
+    int n_piece = 0, ld_piece = 0;
+    int ld_st = st, ld_end = st_end, ld_slot = 0, n_issued = 0;
+    auto issue = [&]() __attribute__((always_inline)) {
+        const uint32_t dst = __builtin_amdgcn_readfirstlane(lds + ld_slot * H::kStage);
+        if (wave < H::kScales / 1024)
+            lds_dma16_sbase<0>(mx_uniform(a.pscale + static_cast<int64_t>(ld_st) * H::kScales + wave * 1024), lane * 16,
+                               __builtin_amdgcn_readfirstlane(lds + H::R * H::kStage + ld_slot * H::kScales + wave * 1024));
+        const void* from = mx_uniform(a.P + static_cast<int64_t>(ld_st) * H::kStage);
+#pragma unroll
+        for (int i = 0; i < H::kLoads; ++i) lds_dma16_sbase<0>(from, off[i], dst + (wave * H::kLoads + i) * 1024);
+        if (++ld_st == ld_end) piece(++ld_piece, ld_tile, ld_st, ld_end);
+        if (++ld_slot == H::R) ld_slot = 0;
+        ++n_issued;
+    };
+    int full = 0;                                            // stages in a row whose scores were all stored as whole blocks
+    auto publish = [&](int g_next) __attribute__((always_inline)) {
+        // (published while the stage before it still has a block to read: the slot of the one before that is filled)
+        if (n_issued - 1 - g_next < H::R - 3) wait_all_vmem();
+        else if (full >= H::R) wait_vmem_at_most<(H::kLoads + H::kStores) * (H::R - 3)>();
+        else wait_vmem_at_most<H::kLoads*(H::R - 3)>();
+        lds_barrier();
+        if (n_issued < total && n_issued < g_next + H::R - 1) issue();
+    };
+    for (int s = 0; s < H::R - 1 && s < total; ++s) issue();
+
+    mx_i32x4 w[NK][4], fa[3];
+    int sw[4][H::kUpad / 4];                                 // scale bytes of four units to a word
+    const int frag = (lane & 15) * 128 + ((quarter ^ mx_swizzle(lane & 15)) * 16);
+    auto read_a = [&](int slot, int qb, int k) __attribute__((always_inline)) {      // 16 queries, 64 bytes of each
+        return *reinterpret_cast<const mx_i32x4*>(smem + slot * H::kStage + (k >> 1) * (H::QS * 128) + qb * 2048 + (frag ^ ((k & 1) * 64)));
+    };
+    struct Words { int v[H::kUpad / 4]; };
+    auto read_s = [&](int slot, int qb) __attribute__((always_inline)) {             // their scales
+        return *reinterpret_cast<const Words*>(smem + H::R * H::kStage + slot * H::kScales + (qb * 16 + (lane & 15)) * (4 * H::kUpad) + quarter * H::kUpad);
+    };
+    auto hold = [&](int64_t l0) __attribute__((always_inline)) {                     // the wave's labels: 4 neighbouring ones to a lane
+        const int64_t l = l0 + wave * 64 + (lane & 15) * 4;
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const int64_t row = l + y < a.L ? l + y : a.L - 1;
+            const uint8_t* p = a.Q + row * (a.units * 64) + quarter * 16;
+            const uint8_t* s = a.scale + row * (a.units * 4) + quarter;
+#pragma unroll
+            for (int j = 0; j < H::kUpad / 4; ++j) sw[y][j] = 0;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                w[k][y] = mx_i32x4{0, 0, 0, 0};
+                if (k < a.units) {                           // uniform
+                    w[k][y] = *reinterpret_cast<const mx_i32x4*>(p + k * 64);
+                    sw[y][k >> 2] |= static_cast<int>(static_cast<uint32_t>(s[k * 4]) << ((k & 3) * 8));
+                }
+            }
+        }
+        // awaited here: the loop over the stages would wait for these (and for all loads and stores under way) every time round
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+#pragma unroll
+            for (int j = 0; j < H::kUpad / 4; ++j) asm volatile("" : "+v"(sw[y][j]));
+#pragma unroll
+            for (int k = 0; k < NK; ++k) asm volatile("" : "+v"(w[k][y]));
+        }
+    };
+    hold(static_cast<int64_t>(tile) * kMicroHeldLabels);
+    publish(0);
+    fa[0] = read_a(0, 0, 0);
+    fa[1] = read_a(0, 0, 1);
+    Words zs = read_s(0, 0), zs_next = zs;
+    int slot = 0;
+    constexpr int kBlocks = H::QS / 16;
+    for (int g = 0; g < total; ++g) {
+        const int64_t l0 = static_cast<int64_t>(tile) * kMicroHeldLabels + wave * 64, l = l0 + (lane & 15) * 4;
+        const int64_t q0 = static_cast<int64_t>(st) * H::QS;
+        const bool whole = q0 + H::QS <= a.B && l0 + 64 <= a.L;
+        const int slot_next = slot + 1 == H::R ? 0 : slot + 1;
+        TO* out = static_cast<TO*>(a.out) + (q0 + 4 * quarter) * a.L + l;
+#pragma unroll
+        for (int qb = 0; qb < kBlocks; ++qb) {
+            if (qb == kBlocks - 1 && g + 1 < total) publish(g + 1);
+            mx_f32x4 acc[4];
+            zs_next = qb + 1 < kBlocks ? read_s(slot, qb + 1) : read_s(slot_next, 0);
+#pragma unroll
+            for (int k = 0; k < NK; ++k) {
+                constexpr int kDepth = 2;
+                const int kn = k + kDepth < NK ? k + kDepth : k + kDepth - NK;
+                const bool over = k + kDepth >= NK;
+                const int n = qb * NK + k;                   // of the stage: NK * kBlocks is a multiple of 3 or fa is put right behind it
+                fa[(n + kDepth) % 3] = !over ? read_a(slot, qb, kn) : qb + 1 < kBlocks ? read_a(slot, qb + 1, kn) : read_a(slot_next, 0, kn);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    acc[y] = mx_product(k, fa[n % 3], w[k][y], k == 0 ? mx_f32x4{0, 0, 0, 0} : acc[y], zs.v[k >> 2], sw[y][k >> 2]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            zs = zs_next;
+            if constexpr ((NK * kBlocks) % 3 != 0) {
+                if (qb == kBlocks - 1) {                     // the next stage starts at fa[0] again
+                    const mx_i32x4 f0 = fa[(NK * kBlocks) % 3], f1 = fa[(NK * kBlocks + 1) % 3];
+                    fa[0] = f0;
+                    fa[1] = f1;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v[4] = {acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+                TO* p = out + static_cast<int64_t>(qb * 16 + i) * a.L;
+                if (whole) put_four(p, v);                   // uniform
+                else if (q0 + qb * 16 + 4 * quarter + i < a.B) put_labels(p, v, l0 + 64 <= a.L, a.L - l);
+            }
+        }
+        full = whole ? full + 1 : 0;
+        slot = slot_next;
+        if (++st == st_end) {
+            piece(++n_piece, tile, st, st_end);
+            full = 0;
+            if (g + 1 < total) hold(static_cast<int64_t>(tile) * kMicroHeldLabels);
+        }
+    }
+}
+
+// ---- any sizes, operands straight from memory: a wave has 64 labels x 64 queries.
 constexpr int kMxTile = 64;
 template <typename TO>
 __global__ __launch_bounds__(256)
 void scores_micro_kernel(const MicroArgs a) {
     const int lane = lane_id(), r = lane & 15, quarter = lane >> 4;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (t >= a.tiles_m * a.tiles_n) return;
-    const int64_t l0 = t / a.tiles_m * kMxTile, q0 = t % a.tiles_m * kMxTile;
+    const int64_t tiles_m = (a.B + kMxTile - 1) / kMxTile, tiles_n = (a.L + kMxTile - 1) / kMxTile, t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (t >= tiles_m * tiles_n) return;
+    const int64_t l0 = t / tiles_m * kMxTile, q0 = t % tiles_m * kMxTile;
     const uint8_t *w[4], *z[4], *ws[4], *zs[4];
 #pragma unroll
     for (int y = 0; y < 4; ++y) {
-        int64_t row = l0 + y * 16 + r;
+        int64_t row = l0 + r * 4 + y;
         row = row < a.L ? row : a.L - 1;
         w[y] = a.Q + row * a.units * 64 + quarter * 16;
         ws[y] = a.scale + row * a.units * 4 + quarter;
-        row = q0 + y * 16 + r;
-        row = row < a.B ? row : a.B - 1;
-        z[y] = a.P + row * a.units * 64 + quarter * 16;
-        zs[y] = a.pscale + row * a.units * 4 + quarter;
+        row = q0 + y * 16 + r;                               // (the queries are padded to whole tiles)
+        z[y] = a.P + row * a.ppitch + quarter * 16;
+        zs[y] = a.pscale + row * 4 * a.upad + quarter * a.upad;
     }
     mx_f32x4 acc[4][4];
 #pragma unroll
@@ -146,30 +534,101 @@ void scores_micro_kernel(const MicroArgs a) {
             fw[y] = *reinterpret_cast<const mx_i32x4*>(w[y] + u * 64);
             fz[y] = *reinterpret_cast<const mx_i32x4*>(z[y] + u * 64);
             sw[y] = ws[y][u * 4];
-            sz[y] = zs[y][u * 4];
+            sz[y] = zs[y][u];
         }
 #pragma unroll
         for (int x = 0; x < 4; ++x)
 #pragma unroll
-            for (int y = 0; y < 4; ++y) acc[x][y] = mx_product(fw[y], fz[x], acc[x][y], sw[y], sz[x]);
+            for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(fz[x], fw[y], acc[x][y], sz[x], sw[y]);
     }
+    const int64_t l = l0 + r * 4, have = a.L - l;
+    if (have <= 0) return;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        const int64_t q = q0 + x * 16 + r;
-        if (q >= a.B) continue;
+    for (int x = 0; x < 4; ++x)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            const int64_t l = l0 + y * 16 + quarter * 4;
-            if (l >= a.L) continue;
-            const float v[4] = {acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]};
-            put_scores<TO>(static_cast<TO*>(a.out) + q * a.L + l, v, static_cast<int>(a.L - l < 4 ? a.L - l : 4));
+        for (int i = 0; i < 4; ++i) {
+            const int64_t q = q0 + x * 16 + quarter * 4 + i;
+            if (q >= a.B) continue;
+            const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
+            put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, l0 + kMxTile <= a.L, have);
         }
-    }
 }
 
-// ---- sizes
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
 static bool micro_d(int d, xc_dtype t) { return d >= 1 && d <= XC_MAX_D_QUANTIZED && (static_cast<int64_t>(d) * (t == XC_F32 ? 4 : 2)) % 16 == 0; }
-static size_t micro_bytes(int64_t B, int d) { return static_cast<size_t>(B) * (mx_pitch(d) / 2) + round_up(static_cast<size_t>(B) * (mx_pitch(d) / 32), 16); }
+
+// The queries in the workspace: rows padded to whole pairs of units, their number to whole tiles of 64.
+struct MicroSpace { int64_t rows; int units, pitch, upad; size_t bytes; };
+static MicroSpace micro_space(int64_t B, int d) {
+    MicroSpace s;
+    s.rows = (B + 63) / 64 * 64;
+    s.units = static_cast<int>(mx_pitch(d) / kMxRow);
+    s.pitch = (s.units + 1) / 2 * 128;
+    s.upad = (s.units + 3) / 4 * 4;
+    s.bytes = static_cast<size_t>(s.rows) * (s.pitch + 4 * s.upad);
+    return s;
+}
+
+constexpr int kMicroFewUnits = 8, kMicroFewLong = 32, kMicroHeldUnits = 8;
+
+template <typename TO, typename TZ, int MQ, int KU, int W>
+static void launch_few(const MicroArgs& a, hipStream_t st) {
+    const int64_t groups = (a.L + 63) / 64, per = ((groups + kXcds - 1) / kXcds + W - 1) / W;
+    const int64_t most = kCusPerXcd * (KU <= kMicroFewUnits ? 16 / W : 8 / W);
+    for (int64_t q0 = 0; q0 < a.B; q0 += 16 * MQ)
+        scores_micro_few_kernel<TO, TZ, MQ, KU, W><<<static_cast<unsigned>(kXcds * (per < most ? per : most)), W * kWave, 0, st>>>(a, q0);
+}
+template <typename TO, int NK>
+static void launch_micro_held(const MicroArgs& a, hipStream_t st) {
+    scores_micro_held_kernel<TO, NK><<<kMineGrid, 512, 0, st>>>(a, static_cast<int>((a.L + kMicroHeldLabels - 1) / kMicroHeldLabels),
+                                                                static_cast<int>((a.B + MicroHeld<NK>::QS - 1) / MicroHeld<NK>::QS));
+}
+
+template <typename TO>
+static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& space, hipStream_t st) {
+    a.Z = static_cast<const unsigned char*>(Z);
+    if (a.B <= 16 && a.units <= kMicroFewLong) {             // every workgroup brings the queries to 4 bits for itself: one launch
+        auto go = [&]() {
+            if (a.units <= kMicroFewUnits) {
+                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewUnits, 4>(a, st);
+                else launch_few<TO, bf16_t, 1, kMicroFewUnits, 4>(a, st);
+            } else {
+                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewLong, 4>(a, st);
+                else launch_few<TO, bf16_t, 1, kMicroFewLong, 4>(a, st);
+            }
+        };
+        XC_LAUNCH(K_SCORES_MICRO, st, go());
+        XC_HIP_CHECK(hipGetLastError());
+        return XC_OK;
+    }
+    const MicroQueries queries{const_cast<uint8_t*>(a.P), const_cast<uint8_t*>(a.pscale), space.units, space.pitch, space.upad};
+    const int rc = launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, queries, space.rows, space.pitch / 64, st);
+    if (rc != XC_OK) return rc;
+    auto go = [&]() {
+        if (a.B > 64 && a.units <= kMicroHeldUnits) {
+            switch (space.pitch / 128) {
+                case 1: launch_micro_held<TO, 2>(a, st); break;
+                case 2: launch_micro_held<TO, 4>(a, st); break;
+                case 3: launch_micro_held<TO, 6>(a, st); break;
+                default: launch_micro_held<TO, 8>(a, st); break;
+            }
+        } else if (a.B <= 64 && a.units <= kMicroFewUnits) {
+            if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4>(a, st);
+            else launch_few<TO, void, 4, kMicroFewUnits, 4>(a, st);
+        } else if (a.B <= 64 && a.units <= kMicroFewLong) {
+            if (a.B <= 32) launch_few<TO, void, 2, kMicroFewLong, 8>(a, st);
+            else launch_few<TO, void, 4, kMicroFewLong, 8>(a, st);
+        } else {
+            const int64_t tiles = ((a.B + kMxTile - 1) / kMxTile) * ((a.L + kMxTile - 1) / kMxTile);
+            scores_micro_kernel<TO><<<static_cast<unsigned>((tiles + 3) / 4), 256, 0, st>>>(a);
+        }
+    };
+    XC_LAUNCH(K_SCORES_MICRO, st, go());
+    XC_HIP_CHECK(hipGetLastError());
+    return XC_OK;
+}
 
 }  // namespace xc
 
@@ -185,14 +644,15 @@ extern "C" int xc_microscale_rows(const void* X, int64_t N, int d, xc_dtype t, c
                 {Span(X, n * d * (t == XC_F32 ? 4 : 2)), Span(ids, static_cast<unsigned __int128>(m) * 4), Span(count, 4)}))
         return XC_EINVAL;
     if (ids && m == 0) return XC_OK;
-    return launch_microscale(X, N, d, t, ids, m, count, Q, scale, static_cast<hipStream_t>(stream));
+    const int units = static_cast<int>(mx_pitch(d) / kMxRow);
+    return launch_microscale(X, N, d, t, ids, m, count, MicroRows{Q, scale, units}, N, units, static_cast<hipStream_t>(stream));
 }
 
 extern "C" int xc_scores_microscaled_workspace(int64_t B, int d, size_t* bytes) {
     using namespace xc;
     if (!bytes) return XC_EINVAL;
     if (B < 1 || B > 0x7fffffffLL || d < 1 || d > XC_MAX_D_QUANTIZED) return XC_ESHAPE;
-    *bytes = micro_bytes(B, d);
+    *bytes = micro_space(B, d).bytes;
     return XC_OK;
 }
 
@@ -203,21 +663,14 @@ extern "C" int xc_scores_microscaled(const void* Z, int64_t B, int d, xc_dtype t
     if (B < 1 || B > 0x7fffffffLL || L < 1 || L > 0x7fffffffLL || !micro_d(d, t) || static_cast<unsigned __int128>(B) * L > (1ull << 40)) return XC_ESHAPE;
     if (!Z || !Q || !scale || !out || !ws) return XC_EINVAL;
     if (!aligned16(Z) || !aligned16(Q) || !aligned16(scale) || !aligned16(out) || !aligned16(ws)) return XC_EINVAL;
-    const size_t need = micro_bytes(B, d);
-    if (ws_bytes < need) return XC_EWORKSPACE;
+    const MicroSpace space = micro_space(B, d);
+    if (ws_bytes < space.bytes) return XC_EWORKSPACE;
     const unsigned __int128 b = B, l = L;
-    if (overlap({Span(out, b * l * (out_t == XC_F32 ? 4 : 2)), Span(ws, need)},
+    if (overlap({Span(out, b * l * (out_t == XC_F32 ? 4 : 2)), Span(ws, space.bytes)},
                 {Span(Z, b * d * (t == XC_F32 ? 4 : 2)), Span(Q, l * (mx_pitch(d) / 2)), Span(scale, l * (mx_pitch(d) / 32))}))
         return XC_EINVAL;
-    hipStream_t st = static_cast<hipStream_t>(stream);
     uint8_t* P = static_cast<uint8_t*>(ws);
-    uint8_t* pscale = P + B * (mx_pitch(d) / 2);
-    const int rc = launch_microscale(Z, B, d, t, nullptr, 0, nullptr, P, pscale, st);
-    if (rc != XC_OK) return rc;
-    const MicroArgs a{P, pscale, Q, scale, out, B, L, (B + kMxTile - 1) / kMxTile, (L + kMxTile - 1) / kMxTile, static_cast<int>(mx_pitch(d) / kMxRow)};
-    const unsigned grid = static_cast<unsigned>((a.tiles_m * a.tiles_n + 3) / 4);
-    if (out_t == XC_F32) XC_LAUNCH(K_SCORES_MICRO, st, (scores_micro_kernel<float><<<grid, 256, 0, st>>>(a)));
-    else XC_LAUNCH(K_SCORES_MICRO, st, (scores_micro_kernel<bf16_t><<<grid, 256, 0, st>>>(a)));
-    XC_HIP_CHECK(hipGetLastError());
-    return XC_OK;
+    const MicroArgs a{nullptr, P, P + space.rows * space.pitch, Q, scale, out, B, L, d, space.units, space.pitch, space.upad};
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return out_t == XC_F32 ? run_micro<float>(a, Z, t, space, st) : run_micro<bf16_t>(a, Z, t, space, st);
 }
