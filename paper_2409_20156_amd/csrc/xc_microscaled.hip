@@ -140,6 +140,7 @@ struct MicroArgs {
     void* out;
     int64_t B, L;
     int d, units, ppitch, upad;          // units of 128 elements in a row of Q; the queries' rows, see MicroQueries
+    bool stream;                         // scores beyond the last-level cache: stored with the non-temporal hint
 };
 
 // Blocks of 16 queries x 16 labels x 128 elements: lane l has the 32 elements of block l / 16 of row l % 16 of both operands; its
@@ -162,10 +163,20 @@ __device__ __forceinline__ mx_f32x4 mx_product(int s /* known when compiled */, 
 // 4 neighbouring scores of a row, the first `have` of which are there.
 typedef float mx_f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 mx_bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ void put_four(float* p, const float (&v)[4]) { __builtin_memcpy(p, v, 16); }
-__device__ __forceinline__ void put_four(bf16_t* p, const float (&v)[4]) {
+typedef uint32_t mx_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t mx_u32x4 __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ void put_four(float* p, const float (&v)[4], bool stream) {
+    mx_u32x4 u;
+    __builtin_memcpy(&u, v, 16);
+    if (stream) __builtin_nontemporal_store(u, reinterpret_cast<mx_u32x4*>(p));      // uniform
+    else *reinterpret_cast<mx_u32x4*>(p) = u;
+}
+__device__ __forceinline__ void put_four(bf16_t* p, const float (&v)[4], bool stream) {
     const mx_bf16x2 h[2] = {__builtin_convertvector(mx_f32x2{v[0], v[1]}, mx_bf16x2), __builtin_convertvector(mx_f32x2{v[2], v[3]}, mx_bf16x2)};      // nearest, ties to even
-    __builtin_memcpy(p, h, 8);
+    mx_u32x2 u;
+    __builtin_memcpy(&u, h, 8);
+    if (stream) __builtin_nontemporal_store(u, reinterpret_cast<mx_u32x2*>(p));
+    else *reinterpret_cast<mx_u32x2*>(p) = u;
 }
 __device__ __forceinline__ void put_one(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put_one(bf16_t* p, float v) {
@@ -176,7 +187,7 @@ __device__ __forceinline__ void put_one(bf16_t* p, float v) {
 // scores take the fourth one's register in all lanes)
 template <typename TO> __device__ __forceinline__ void put_labels(TO* p, const float (&v)[4], bool whole, int64_t have) {
     if (whole) {
-        put_four(p, v);
+        put_four(p, v, false);
     } else {
 #pragma unroll
         for (int y = 0; y < 4; ++y) if (y < have) put_one(p + y, v[y]);
@@ -190,47 +201,60 @@ __device__ __forceinline__ const void* mx_uniform(const void* p) {
         static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a)))));
 }
 
-// ---- few queries: 16 MQ of them stay in LDS (rows of up to 64 KU bytes), the labels pass, 64 to a wave at a time, straight into registers,
-// two units of each under way while the two before are multiplied.  Lane l has labels 4 (l % 16) .. + 3 of the 64, so that it stores
-// neighbouring scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
+// ---- few queries: 16 MQ of them stay in LDS (rows of up to 64 KU bytes), the labels pass, 64 to a wave at a time and two units of each to a
+// step, through a ring of R steps in LDS that the wave fills and empties by itself.  Eight neighbouring lanes bring 128 bytes of a row, so
+// that a load meets eight lines; straight into registers, where neighbouring lanes have different rows, it meets 64, and so do a row's
+// scales: 1 x 131072 x 768 14.5 us, 1 x 670000 x 768 68.  Lane l has labels 4 (l % 16) .. + 3 of the 64, so that it stores neighbouring
+// scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
 // Bound: one read of Q.
-template <typename TO, typename TZ, int MQ, int KU, int W>
+constexpr int kFewSlot = 64 * 128 + 2 * 64 * 4;          // a step of 64 labels, their scales
+constexpr int kFewLoads = 8 + 2;
+template <int N> __device__ __forceinline__ void few_wait() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
+__device__ __forceinline__ void lds_dma4_sbase(const void* sbase /* wave-uniform */, uint32_t voff, uint32_t lds_addr /* wave-uniform */) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(voff), "s"(sbase), "s"(lds_addr) : "memory");
+}
+template <typename TO, typename TZ, int MQ, int KU, int W, int R>
 __global__ __launch_bounds__(W * kWave)
 void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
     constexpr int kRows = 16 * MQ, kUpad = (KU + 3) / 4 * 4;
+    __shared__ __align__(1024) unsigned char ring[W][R][kFewSlot];
     __shared__ __align__(1024) unsigned char codes[kRows * KU * 64];       // 128 bytes of every row, the next 128, ..; chunks of 16 swizzled
     __shared__ __align__(16) unsigned char scales[kRows * 4 * kUpad];
+    static_assert((R - 1) * kFewLoads < 64, "a count that the wait can hold");
     const int lane = lane_id(), r = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t groups = (a.L + 63) / 64;
-    const int row_bytes = a.units * 64, row_scales = a.units * 4;
+    const uint32_t row_bytes = a.units * 64, row_scales = a.units * 4;
     // neighbouring groups to neighbouring waves, and a contiguous part of them to each XCD
     const int64_t per = (groups + kXcds - 1) / kXcds, g_begin = blockIdx.x % kXcds * per, g_end = g_begin + per < groups ? g_begin + per : groups;
     const int64_t g_step = static_cast<int64_t>(gridDim.x / kXcds) * W;
-    int64_t g = g_begin + static_cast<int64_t>(blockIdx.x / kXcds) * W + wave;
+    int64_t g = g_begin + static_cast<int64_t>(blockIdx.x / kXcds) * W + wave, ahead_g = g;
     const int steps = (a.units + 1) / 2;
-
-    mx_i32x4 w[2][2][4];
-    int ws[2][2][4];
-    auto bring = [&](int to, int64_t g, int step) __attribute__((always_inline)) {
-        const int64_t l0 = g * 64;
-        const int u = step * 2;
-        const bool second = u + 1 < a.units;
-        const int64_t last = a.L - 1 - l0;
+    const int64_t total = g < g_end ? ((g_end - 1 - g) / g_step + 1) * steps : 0;
+    int ahead_step = 0, ahead_slot = 0;
+    unsigned char* slots = &ring[wave][0][0];
+    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)slots));
+    auto issue = [&]() __attribute__((always_inline)) {
+        const int64_t l0 = ahead_g * 64, have = a.L - 1 - l0;
+        const uint32_t last = have < 63 ? static_cast<uint32_t>(have) : 63u;           // rows past the end: the last one again
+        const uint32_t mask = ahead_step * 2 + 1 < a.units ? 127u : 63u;                // (a single unit: it again)
+        const void* q = mx_uniform(a.Q + l0 * row_bytes + ahead_step * 128);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + ahead_slot * kFewSlot);
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            int64_t row = r * 4 + y;
-            row = l0 + (row < last ? row : last);
-            const uint8_t* p = a.Q + row * row_bytes + u * 64 + quarter * 16;
-            const uint8_t* s = a.scale + row * row_scales + u * 4;
-            w[to][0][y] = *reinterpret_cast<const mx_i32x4*>(p);
-            ws[to][0][y] = *reinterpret_cast<const int*>(s);
-            if (second) {                                    // uniform
-                w[to][1][y] = *reinterpret_cast<const mx_i32x4*>(p + 64);
-                ws[to][1][y] = *reinterpret_cast<const int*>(s + 4);
-            }
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t row = i * 8 + (lane >> 3), chunk = (lane ^ (row >> 2)) & 7;
+            lds_dma16_sbase<0>(q, (row < last ? row : last) * row_bytes + ((chunk * 16) & mask), to + i * 1024);
         }
+        const void* s = mx_uniform(a.scale + l0 * row_scales + ahead_step * 8);
+        const uint32_t at = (static_cast<uint32_t>(lane) < last ? lane : last) * row_scales;
+        lds_dma4_sbase(s, at, to + 64 * 128);
+        lds_dma4_sbase(s, at + (mask == 127u ? 4 : 0), to + 64 * 128 + 256);
+        if (++ahead_step == steps) {
+            ahead_step = 0;
+            ahead_g += g_step;
+        }
+        if (++ahead_slot == R) ahead_slot = 0;
     };
-    if (g < g_end) bring(0, g, 0);
+    for (int i = 0; i < R && i < total; ++i) issue();
 
     // the queries
     if constexpr (!std::is_void<TZ>::value) {
@@ -257,65 +281,61 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
         }
     }
     __syncthreads();
-    const unsigned char* frag = codes + r * 128 + ((quarter ^ mx_swizzle(r)) * 16);
-    auto query = [&](int x, int u) __attribute__((always_inline)) {        // 16 queries, 64 bytes of each
-        const uint32_t at = (u >> 1) * (kRows * 128) + x * 16 * 128;
-        return *reinterpret_cast<const mx_i32x4*>(codes + at + ((frag - codes) ^ ((u & 1) * 64)));
-    };
-    for (; g < g_end; g += g_step) {
-        mx_f32x4 acc[MQ][4];
+    const int frag = r * 128 + ((quarter ^ mx_swizzle(r)) * 16);
+    mx_f32x4 acc[MQ][4];
+    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < MQ; ++x)
 #pragma unroll
             for (int y = 0; y < 4; ++y) acc[x][y] = mx_f32x4{0, 0, 0, 0};
-        auto multiply = [&](int from, int step) __attribute__((always_inline)) {
+    };
+    clear();
+    int step = 0, slot = 0;
+    for (int64_t n = 0; n < total; ++n) {
+        // (the waits count loads and stores, in the order of their issue: with stores among the younger ones they end a little later)
+        if (total - 1 - n >= R - 1) few_wait<(R - 1) * kFewLoads>();
+        else few_wait<0>();
+        const unsigned char* from = slots + slot * kFewSlot;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int u = step * 2 + h;
-                if (u >= a.units) break;                     // uniform
+        for (int h = 0; h < 2; ++h) {
+            const int u = step * 2 + h;
+            if (u >= a.units) break;                         // uniform
+            mx_i32x4 w[4];
+            int ws[4];
 #pragma unroll
-                for (int x = 0; x < MQ; ++x) {
-                    const mx_i32x4 z = query(x, u);
-                    const int zs = scales[(x * 16 + r) * (4 * kUpad) + quarter * kUpad + u];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        acc[x][y] = mx_product<0>(z, w[from][h][y], acc[x][y], zs, static_cast<int>(static_cast<uint32_t>(ws[from][h][y]) >> (quarter * 8)));
-                }
+            for (int y = 0; y < 4; ++y) {
+                w[y] = *reinterpret_cast<const mx_i32x4*>(from + (r * 4 + y) * 128 + (((h * 4 + quarter) ^ (r & 7)) * 16));
+                ws[y] = from[64 * 128 + h * 256 + (r * 4 + y) * 4 + quarter];
             }
-        };
-        // the next two units, of the next group behind the last ones
-        auto next = [&](int to, int step) __attribute__((always_inline)) {
-            if (step < steps) bring(to, g, step);
-            else if (g + g_step < g_end) bring(to, g + g_step, 0);
-        };
-        for (int step = 0; step < steps; step += 2) {
-            next(1, step + 1);
-            multiply(0, step);
-            if (step + 1 < steps) {
-                next(0, step + 2);
-                multiply(1, step + 1);
+#pragma unroll
+            for (int x = 0; x < MQ; ++x) {                   // 16 queries, 64 bytes of each
+                const mx_i32x4 z = *reinterpret_cast<const mx_i32x4*>(codes + (u >> 1) * (kRows * 128) + x * 16 * 128 + (frag ^ ((u & 1) * 64)));
+                const int zs = scales[(x * 16 + r) * (4 * kUpad) + quarter * kUpad + u];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(z, w[y], acc[x][y], zs, ws[y]);
             }
         }
-        if ((steps & 1) != 0) {                              // (an odd number: the next group's first ones are in the other half)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                    w[0][h][y] = w[1][h][y];
-                    ws[0][h][y] = ws[1][h][y];
-                }
+        if (n + R < total) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // (the slot has been read)
+            issue();
         }
-        const int64_t l = g * 64 + r * 4, have = a.L - l;
-        const bool whole = g * 64 + 64 <= a.L;               // uniform
+        if (++slot == R) slot = 0;
+        if (++step == steps) {
+            step = 0;
+            const int64_t l = g * 64 + r * 4, have = a.L - l;
+            const bool whole = g * 64 + 64 <= a.L;           // uniform
 #pragma unroll
-        for (int x = 0; x < MQ; ++x)
+            for (int x = 0; x < MQ; ++x)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t q = q0 + x * 16 + quarter * 4 + i;
-                if (q >= a.B) continue;
-                const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
-                put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
-            }
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t q = q0 + x * 16 + quarter * 4 + i;
+                    if (q >= a.B) continue;
+                    const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
+                    put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
+                }
+            clear();
+            g += g_step;
+        }
     }
 }
 
@@ -408,7 +428,8 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
     };
     for (int s = 0; s < H::R - 1 && s < total; ++s) issue();
 
-    mx_i32x4 w[NK][4], fa[3];
+    constexpr int kDepth = 3;                                // units whose queries are read ahead
+    mx_i32x4 w[NK][4], fa[kDepth + 1];
     int sw[4][H::kUpad / 4];                                 // scale bytes of four units to a word
     const int frag = (lane & 15) * 128 + ((quarter ^ mx_swizzle(lane & 15)) * 16);
     auto read_a = [&](int slot, int qb, int k) __attribute__((always_inline)) {      // 16 queries, 64 bytes of each
@@ -447,11 +468,12 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
     };
     hold(static_cast<int64_t>(tile) * kMicroHeldLabels);
     publish(0);
-    fa[0] = read_a(0, 0, 0);
-    fa[1] = read_a(0, 0, 1);
+#pragma unroll
+    for (int n = 0; n < kDepth; ++n) fa[n] = read_a(0, n / NK, n % NK);
     Words zs = read_s(0, 0), zs_next = zs;
     int slot = 0;
     constexpr int kBlocks = H::QS / 16;
+    static_assert(NK * kBlocks % (kDepth + 1) == 0 && kDepth <= NK * kBlocks, "a stage begins with the same registers");
     for (int g = 0; g < total; ++g) {
         const int64_t l0 = static_cast<int64_t>(tile) * kMicroHeldLabels + wave * 64, l = l0 + (lane & 15) * 4;
         const int64_t q0 = static_cast<int64_t>(st) * H::QS;
@@ -460,34 +482,24 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
         TO* out = static_cast<TO*>(a.out) + (q0 + 4 * quarter) * a.L + l;
 #pragma unroll
         for (int qb = 0; qb < kBlocks; ++qb) {
-            if (qb == kBlocks - 1 && g + 1 < total) publish(g + 1);
+            if (qb == (NK * kBlocks - kDepth) / NK && g + 1 < total) publish(g + 1);       // (from here on the next stage is read)
             mx_f32x4 acc[4];
             zs_next = qb + 1 < kBlocks ? read_s(slot, qb + 1) : read_s(slot_next, 0);
 #pragma unroll
             for (int k = 0; k < NK; ++k) {
-                constexpr int kDepth = 2;
-                const int kn = k + kDepth < NK ? k + kDepth : k + kDepth - NK;
-                const bool over = k + kDepth >= NK;
-                const int n = qb * NK + k;                   // of the stage: NK * kBlocks is a multiple of 3 or fa is put right behind it
-                fa[(n + kDepth) % 3] = !over ? read_a(slot, qb, kn) : qb + 1 < kBlocks ? read_a(slot, qb + 1, kn) : read_a(slot_next, 0, kn);
+                const int n = qb * NK + k, ahead = n + kDepth;             // of the stage's units
+                fa[ahead % (kDepth + 1)] = ahead < NK * kBlocks ? read_a(slot, ahead / NK, ahead % NK) : read_a(slot_next, (ahead - NK * kBlocks) / NK, (ahead - NK * kBlocks) % NK);
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
-                    acc[y] = mx_product(k, fa[n % 3], w[k][y], k == 0 ? mx_f32x4{0, 0, 0, 0} : acc[y], zs.v[k >> 2], sw[y][k >> 2]);
+                    acc[y] = mx_product(k, fa[n % (kDepth + 1)], w[k][y], k == 0 ? mx_f32x4{0, 0, 0, 0} : acc[y], zs.v[k >> 2], sw[y][k >> 2]);
                 __builtin_amdgcn_sched_barrier(0);
             }
             zs = zs_next;
-            if constexpr ((NK * kBlocks) % 3 != 0) {
-                if (qb == kBlocks - 1) {                     // the next stage starts at fa[0] again
-                    const mx_i32x4 f0 = fa[(NK * kBlocks) % 3], f1 = fa[(NK * kBlocks + 1) % 3];
-                    fa[0] = f0;
-                    fa[1] = f1;
-                }
-            }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float v[4] = {acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
                 TO* p = out + static_cast<int64_t>(qb * 16 + i) * a.L;
-                if (whole) put_four(p, v);                   // uniform
+                if (whole) put_four(p, v, a.stream);         // uniform
                 else if (q0 + qb * 16 + 4 * quarter + i < a.B) put_labels(p, v, l0 + 64 <= a.L, a.L - l);
             }
         }
@@ -571,14 +583,16 @@ static MicroSpace micro_space(int64_t B, int d) {
     return s;
 }
 
+constexpr int64_t kMxCachedBytes = 256ll << 20;
 constexpr int kMicroFewUnits = 8, kMicroFewLong = 32, kMicroHeldUnits = 8;
 
-template <typename TO, typename TZ, int MQ, int KU, int W>
+template <typename TO, typename TZ, int MQ, int KU, int W, int R>
 static void launch_few(const MicroArgs& a, hipStream_t st) {
-    const int64_t groups = (a.L + 63) / 64, per = ((groups + kXcds - 1) / kXcds + W - 1) / W;
-    const int64_t most = kCusPerXcd * (KU <= kMicroFewUnits ? 16 / W : 8 / W);
+    constexpr int kLds = W * R * kFewSlot + 16 * MQ * (KU * 64 + (KU + 3) / 4 * 16), kPerCu = 160 * 1024 / (kLds + 1024);
+    static_assert(kPerCu >= 1, "");
+    const int64_t groups = (a.L + 63) / 64, per = ((groups + kXcds - 1) / kXcds + W - 1) / W, most = kCusPerXcd * kPerCu;
     for (int64_t q0 = 0; q0 < a.B; q0 += 16 * MQ)
-        scores_micro_few_kernel<TO, TZ, MQ, KU, W><<<static_cast<unsigned>(kXcds * (per < most ? per : most)), W * kWave, 0, st>>>(a, q0);
+        scores_micro_few_kernel<TO, TZ, MQ, KU, W, R><<<static_cast<unsigned>(kXcds * (per < most ? per : most)), W * kWave, 0, st>>>(a, q0);
 }
 template <typename TO, int NK>
 static void launch_micro_held(const MicroArgs& a, hipStream_t st) {
@@ -592,11 +606,11 @@ static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& s
     if (a.B <= 16 && a.units <= kMicroFewLong) {             // every workgroup brings the queries to 4 bits for itself: one launch
         auto go = [&]() {
             if (a.units <= kMicroFewUnits) {
-                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewUnits, 4>(a, st);
-                else launch_few<TO, bf16_t, 1, kMicroFewUnits, 4>(a, st);
+                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewUnits, 4, 2>(a, st);
+                else launch_few<TO, bf16_t, 1, kMicroFewUnits, 4, 2>(a, st);
             } else {
-                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewLong, 4>(a, st);
-                else launch_few<TO, bf16_t, 1, kMicroFewLong, 4>(a, st);
+                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewLong, 4, 3>(a, st);
+                else launch_few<TO, bf16_t, 1, kMicroFewLong, 4, 3>(a, st);
             }
         };
         XC_LAUNCH(K_SCORES_MICRO, st, go());
@@ -615,11 +629,10 @@ static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& s
                 default: launch_micro_held<TO, 8>(a, st); break;
             }
         } else if (a.B <= 64 && a.units <= kMicroFewUnits) {
-            if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4>(a, st);
-            else launch_few<TO, void, 4, kMicroFewUnits, 4>(a, st);
+            if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4, 3>(a, st);
+            else launch_few<TO, void, 4, kMicroFewUnits, 4, 3>(a, st);
         } else if (a.B <= 64 && a.units <= kMicroFewLong) {
-            if (a.B <= 32) launch_few<TO, void, 2, kMicroFewLong, 8>(a, st);
-            else launch_few<TO, void, 4, kMicroFewLong, 8>(a, st);
+            launch_few<TO, void, 2, kMicroFewLong, 4, 2>(a, st);
         } else {
             const int64_t tiles = ((a.B + kMxTile - 1) / kMxTile) * ((a.L + kMxTile - 1) / kMxTile);
             scores_micro_kernel<TO><<<static_cast<unsigned>((tiles + 3) / 4), 256, 0, st>>>(a);
@@ -670,7 +683,7 @@ extern "C" int xc_scores_microscaled(const void* Z, int64_t B, int d, xc_dtype t
                 {Span(Z, b * d * (t == XC_F32 ? 4 : 2)), Span(Q, l * (mx_pitch(d) / 2)), Span(scale, l * (mx_pitch(d) / 32))}))
         return XC_EINVAL;
     uint8_t* P = static_cast<uint8_t*>(ws);
-    const MicroArgs a{nullptr, P, P + space.rows * space.pitch, Q, scale, out, B, L, d, space.units, space.pitch, space.upad};
+    const MicroArgs a{nullptr, P, P + space.rows * space.pitch, Q, scale, out, B, L, d, space.units, space.pitch, space.upad, B * L * (out_t == XC_F32 ? 4 : 2) > kMxCachedBytes};
     hipStream_t st = static_cast<hipStream_t>(stream);
     return out_t == XC_F32 ? run_micro<float>(a, Z, t, space, st) : run_micro<bf16_t>(a, Z, t, space, st);
 }
