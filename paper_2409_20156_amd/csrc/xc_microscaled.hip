@@ -69,7 +69,8 @@ struct MicroRows {
     }
 };
 // Queries in the workspace: rows of `pitch` bytes (an even number of units), zeros behind the last element and the last query.  A row's
-// scales are laid out as the products ask for them: block 4 u + b of unit u at b * upad + u, so that a lane finds four units' in a word.
+// scales are laid out as the products of labels held in registers ask for them: block 4 u + b of unit u at b * upad + u, so that a lane
+// finds four units' in a word.  (Long rows are staged like the labels, and kept like them: MicroRows.)
 struct MicroQueries {
     uint8_t *P, *scale;
     int units, pitch, upad;
@@ -345,9 +346,10 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
 template <int NK_>
 struct MicroHeld {
     static constexpr int NK = NK_, QS = 64, kUpad = NK <= 4 ? 4 : 8, kStage = QS * NK * 64, kScales = QS * 4 * kUpad;
-    static constexpr int kFit = 160 * 1024 / (kStage + kScales), R = kFit < 6 ? kFit : 6;   // stages in LDS
+    static constexpr int kTurn = 2048;                                                       // of a wave, to turn its labels in
+    static constexpr int kFit = (160 * 1024 - 8 * kTurn - 1024) / (kStage + kScales), R = kFit < 6 ? kFit : 6;        // stages in LDS
     static constexpr int kLoads = kStage / 1024 / 8, kStores = QS / 4;                      // of a wave and stage
-    static constexpr int kLds = R * (kStage + kScales);
+    static constexpr int kLds = R * (kStage + kScales) + 8 * kTurn;
     static_assert(kLoads * 8 * 1024 == kStage && R >= 3 && (kLoads + kStores) * (R - 3) < 64, "whole loads, and a count that the wait can hold");
 };
 constexpr int kMicroHeldLabels = 512;
@@ -439,23 +441,44 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
     auto read_s = [&](int slot, int qb) __attribute__((always_inline)) {             // their scales
         return *reinterpret_cast<const Words*>(smem + H::R * H::kStage + slot * H::kScales + (qb * 16 + (lane & 15)) * (4 * H::kUpad) + quarter * H::kUpad);
     };
-    auto hold = [&](int64_t l0) __attribute__((always_inline)) {                     // the wave's labels: 4 neighbouring ones to a lane
-        const int64_t l = l0 + wave * 64 + (lane & 15) * 4;
+    unsigned char* turn = smem + H::R * (H::kStage + H::kScales) + wave * H::kTurn;
+    // The wave's labels: 4 neighbouring ones to a lane.  Four neighbouring lanes load 64 bytes of a row, so that a load meets 16 lines and
+    // not 64, and are turned into the operands' order through LDS.
+    auto hold = [&](int64_t l0) __attribute__((always_inline)) {
+        const int64_t l = l0 + wave * 64;
+        const int64_t past = a.L - 1 - l;                    // (a wave behind the last label: that one again)
+        const int64_t row_bytes = a.units * 64, row_scales = a.units * 4;
+        uint32_t words[NK];
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
-            const int64_t row = l + y < a.L ? l + y : a.L - 1;
-            const uint8_t* p = a.Q + row * (a.units * 64) + quarter * 16;
-            const uint8_t* s = a.scale + row * (a.units * 4) + quarter;
+            const int64_t row = (lane >> 2) * 4 + y, at = l + (row < past ? row : past);
+            const uint8_t* p = a.Q + at * row_bytes + (lane & 3) * 16;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) w[k][y] = *reinterpret_cast<const mx_i32x4*>(p + (k < a.units ? k : a.units - 1) * 64);
+        }
+        {
+            const uint8_t* p = a.scale + (l + (lane < past ? lane : past)) * row_scales;
+#pragma unroll
+            for (int k = 0; k < NK; ++k) words[k] = *reinterpret_cast<const uint32_t*>(p + (k < a.units ? k : a.units - 1) * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < NK; ++k)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                unsigned char* t = turn + (y & 1) * 1024;
+                *reinterpret_cast<mx_i32x4*>(t + lane * 16) = w[k][y];
+                w[k][y] = *reinterpret_cast<const mx_i32x4*>(t + ((lane & 15) * 4 + quarter) * 16);
+                if (k >= a.units) w[k][y] = mx_i32x4{0, 0, 0, 0};          // uniform
+            }
+#pragma unroll
+        for (int k = 0; k < NK; ++k) *reinterpret_cast<uint32_t*>(turn + k * 256 + lane * 4) = words[k];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
 #pragma unroll
             for (int j = 0; j < H::kUpad / 4; ++j) sw[y][j] = 0;
 #pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                w[k][y] = mx_i32x4{0, 0, 0, 0};
-                if (k < a.units) {                           // uniform
-                    w[k][y] = *reinterpret_cast<const mx_i32x4*>(p + k * 64);
-                    sw[y][k >> 2] |= static_cast<int>(static_cast<uint32_t>(s[k * 4]) << ((k & 3) * 8));
-                }
-            }
+            for (int k = 0; k < NK; ++k)
+                if (k < a.units) sw[y][k >> 2] |= static_cast<int>(static_cast<uint32_t>(turn[k * 256 + ((lane & 15) * 4 + y) * 4 + quarter]) << ((k & 3) * 8));
         }
         // awaited here: the loop over the stages would wait for these (and for all loads and stores under way) every time round
 #pragma unroll
@@ -513,56 +536,105 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
     }
 }
 
-// ---- any sizes, operands straight from memory: a wave has 64 labels x 64 queries.
-constexpr int kMxTile = 64;
-template <typename TO>
-__global__ __launch_bounds__(256)
-void scores_micro_kernel(const MicroArgs a) {
-    const int lane = lane_id(), r = lane & 15, quarter = lane >> 4;
-    const int64_t tiles_m = (a.B + kMxTile - 1) / kMxTile, tiles_n = (a.L + kMxTile - 1) / kMxTile, t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-    if (t >= tiles_m * tiles_n) return;
-    const int64_t l0 = t / tiles_m * kMxTile, q0 = t % tiles_m * kMxTile;
-    const uint8_t *w[4], *z[4], *ws[4], *zs[4];
+// ---- longer rows: tiles of 64 WQ queries x 64 WL labels, two units of both to a stage, three stages in LDS, a wave with 64 x 64.  Rows of
+// labels lie in the order of the products' blocks (block y, column j: label 4 j + y of 64), so that a lane stores neighbouring scores.
+// Consecutive workgroups of an XCD take the query tiles of one label tile.
+template <int WQ, int WL>
+struct MicroTile {
+    static constexpr int kWaves = WQ * WL, BM = 64 * WQ, BN = 64 * WL, kRows = BM + BN, R = 3;
+    static constexpr int kStage = kRows * (128 + 8), kParts = kRows / 64 * 2 /* of 64 scale words */, kScaleLoads = (kParts + kWaves - 1) / kWaves;
+    static constexpr int kRowLoads = kRows / 8 / kWaves, kLoads = kRowLoads + kScaleLoads;
+    static_assert(kRowLoads * 8 * kWaves == kRows && R * kStage <= 160 * 1024, "whole loads");
+};
+template <typename TO, int WQ, int WL>
+__global__ __launch_bounds__(WQ * WL * kWave, 2)
+void scores_micro_tile_kernel(const MicroArgs a, uint32_t tiles_m, uint32_t tiles_n) {
+    typedef MicroTile<WQ, WL> T;
+    __shared__ __align__(1024) unsigned char smem[T::R * T::kStage];
+    const int lane = lane_id(), r = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wq = wave / WL, wl = wave % WL;
+    const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
+    const uint32_t n_tiles = tiles_m * tiles_n, per = (n_tiles + kXcds - 1) / kXcds, t = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
+    if (blockIdx.x / kXcds >= per || t >= n_tiles) return;   // uniform
+    const int64_t q0 = static_cast<int64_t>(t % tiles_m) * T::BM, l0 = static_cast<int64_t>(t / tiles_m) * T::BN;
+    const uint32_t row_bytes = a.units * 64, row_scales = a.units * 4;
+    const uint32_t last_q = static_cast<uint32_t>(a.B - 1 - q0 < T::BM ? a.B - 1 - q0 : T::BM - 1), last_l = static_cast<uint32_t>(a.L - 1 - l0 < T::BN ? a.L - 1 - l0 : T::BN - 1);
+    // row of the tile's queries or labels in place p of the stage, rows past the end: the last one again
+    auto row_of = [&](uint32_t p) __attribute__((always_inline)) {
+        if (p < T::BM) return p < last_q ? p : last_q;
+        const uint32_t q = p - T::BM, l = (q & ~63u) + (q & 15) * 4 + ((q >> 4) & 3);
+        return l < last_l ? l : last_l;
+    };
+    uint32_t at[T::kRowLoads], scale_at[T::kScaleLoads];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) {
-        int64_t row = l0 + r * 4 + y;
-        row = row < a.L ? row : a.L - 1;
-        w[y] = a.Q + row * a.units * 64 + quarter * 16;
-        ws[y] = a.scale + row * a.units * 4 + quarter;
-        row = q0 + y * 16 + r;                               // (the queries are padded to whole tiles)
-        z[y] = a.P + row * a.ppitch + quarter * 16;
-        zs[y] = a.pscale + row * 4 * a.upad + quarter * a.upad;
-    }
+    for (int i = 0; i < T::kRowLoads; ++i) at[i] = row_of((wave * T::kRowLoads + i) * 8 + (lane >> 3)) * row_bytes;
+#pragma unroll
+    for (int i = 0; i < T::kScaleLoads; ++i) scale_at[i] = row_of((wave + i * T::kWaves) % T::kParts / 2 * 64 + lane) * row_scales;
+    const uint8_t *rows_q = a.P + q0 * row_bytes, *rows_l = a.Q + l0 * row_bytes, *scale_q = a.pscale + q0 * row_scales, *scale_l = a.scale + l0 * row_scales;
+    const int steps = (a.units + 1) / 2;
+    int ahead = 0, ahead_slot = 0;
+    auto issue = [&]() __attribute__((always_inline)) {
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds + ahead_slot * T::kStage), mask = ahead * 2 + 1 < a.units ? 127u : 63u;       // (a single unit: it again)
+#pragma unroll
+        for (int i = 0; i < T::kRowLoads; ++i) {
+            const int n = wave * T::kRowLoads + i;           // (of one operand: a load's 8 rows)
+            const uint32_t p = n * 8 + (lane >> 3), chunk = (lane ^ (p >> 1)) & 7;
+            lds_dma16_sbase<0>(mx_uniform((n * 8 < T::BM ? rows_q : rows_l) + ahead * 128), at[i] + ((chunk * 16) & mask), to + n * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < T::kScaleLoads; ++i) {
+            const int n = (wave + i * T::kWaves) % T::kParts;          // (where they do not divide evenly, some twice)
+            const uint32_t second = (n & 1) != 0 && mask == 127u ? 4 : 0;
+            lds_dma4_sbase(mx_uniform((n / 2 * 64 < T::BM ? scale_q : scale_l) + ahead * 8), scale_at[i] + second,
+                           __builtin_amdgcn_readfirstlane(to + T::kRows * 128 + n * 256));
+        }
+        ++ahead;
+        if (++ahead_slot == T::R) ahead_slot = 0;
+    };
+    issue();
+    if (steps > 1) issue();
     mx_f32x4 acc[4][4];
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int y = 0; y < 4; ++y) acc[x][y] = mx_f32x4{0, 0, 0, 0};
-    for (int u = 0; u < a.units; ++u) {
-        mx_i32x4 fw[4], fz[4];
-        int sw[4], sz[4];
+    const int frag = r * 128 + ((quarter ^ mx_swizzle(r)) * 16);
+    int slot = 0;
+    for (int step = 0; step < steps; ++step) {
+        if (step + 1 < steps) few_wait<T::kLoads>();
+        else few_wait<0>();
+        lds_barrier();                                       // the stage is there for everyone, the one before it has been read by everyone
+        if (step + 2 < steps) issue();
+        const unsigned char* stage = smem + slot * T::kStage;
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
-            fw[y] = *reinterpret_cast<const mx_i32x4*>(w[y] + u * 64);
-            fz[y] = *reinterpret_cast<const mx_i32x4*>(z[y] + u * 64);
-            sw[y] = ws[y][u * 4];
-            sz[y] = zs[y][u];
+        for (int h = 0; h < 2; ++h) {
+            if (step * 2 + h >= a.units) break;              // uniform
+            mx_i32x4 w[4], z[4];
+            int ws[4], zs[4];
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                w[y] = *reinterpret_cast<const mx_i32x4*>(stage + (T::BM + wl * 64 + y * 16) * 128 + (frag ^ (h * 64)));
+                ws[y] = stage[T::kRows * 128 + ((WQ + wl) * 2 + h) * 256 + (y * 16 + r) * 4 + quarter];
+                z[y] = *reinterpret_cast<const mx_i32x4*>(stage + (wq * 64 + y * 16) * 128 + (frag ^ (h * 64)));
+                zs[y] = stage[T::kRows * 128 + (wq * 2 + h) * 256 + (y * 16 + r) * 4 + quarter];
+            }
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(z[x], w[y], acc[x][y], zs[x], ws[y]);
         }
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(fz[x], fw[y], acc[x][y], sz[x], sw[y]);
+        if (++slot == T::R) slot = 0;
     }
-    const int64_t l = l0 + r * 4, have = a.L - l;
-    if (have <= 0) return;
+    const int64_t lw = l0 + wl * 64, l = lw + r * 4, have = a.L - l;
+    const bool whole = lw + 64 <= a.L;                       // uniform
 #pragma unroll
     for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int64_t q = q0 + x * 16 + quarter * 4 + i;
+            const int64_t q = q0 + wq * 64 + x * 16 + quarter * 4 + i;
             if (q >= a.B) continue;
             const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
-            put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, l0 + kMxTile <= a.L, have);
+            put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
         }
 }
 
@@ -600,6 +672,24 @@ static void launch_micro_held(const MicroArgs& a, hipStream_t st) {
                                                                 static_cast<int>((a.B + MicroHeld<NK>::QS - 1) / MicroHeld<NK>::QS));
 }
 
+template <typename TO, int WQ, int WL>
+static void launch_micro_tile(const MicroArgs& a, hipStream_t st) {
+    typedef MicroTile<WQ, WL> T;
+    // (launches of queries that leave the tiles countable)
+    const int64_t tiles_n = (a.L + T::BN - 1) / T::BN, rows = ((1 << 24) / tiles_n > 1 ? (1 << 24) / tiles_n : 1) * T::BM;
+    for (int64_t q0 = 0; q0 < a.B; q0 += rows) {
+        MicroArgs p = a;
+        p.B = a.B - q0 < rows ? a.B - q0 : rows;
+        p.P += q0 * a.units * 64;
+        p.pscale += q0 * a.units * 4;
+        p.out = static_cast<TO*>(a.out) + q0 * a.L;
+        const uint32_t tiles_m = static_cast<uint32_t>((p.B + T::BM - 1) / T::BM), per = (tiles_m * static_cast<uint32_t>(tiles_n) + kXcds - 1) / kXcds;
+        scores_micro_tile_kernel<TO, WQ, WL><<<kXcds * per, T::kWaves * kWave, 0, st>>>(p, tiles_m, static_cast<uint32_t>(tiles_n));
+    }
+}
+
+constexpr int kMicroTileQueries = 128;
+
 template <typename TO>
 static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& space, hipStream_t st) {
     a.Z = static_cast<const unsigned char*>(Z);
@@ -617,25 +707,27 @@ static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& s
         XC_HIP_CHECK(hipGetLastError());
         return XC_OK;
     }
-    const MicroQueries queries{const_cast<uint8_t*>(a.P), const_cast<uint8_t*>(a.pscale), space.units, space.pitch, space.upad};
-    const int rc = launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, queries, space.rows, space.pitch / 64, st);
+    const bool held = a.B > 64 && a.units <= kMicroHeldUnits, few = a.B <= 64 && (a.units <= kMicroFewUnits || (a.B <= 32 && a.units <= kMicroFewLong));
+    uint8_t *P = const_cast<uint8_t*>(a.P), *pscale = const_cast<uint8_t*>(a.pscale);
+    const int rc = held || few ? launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroQueries{P, pscale, space.units, space.pitch, space.upad}, space.rows, space.pitch / 64, st)
+                               : launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroRows{P, pscale, space.units}, a.B, space.units, st);
     if (rc != XC_OK) return rc;
     auto go = [&]() {
-        if (a.B > 64 && a.units <= kMicroHeldUnits) {
+        if (held) {
             switch (space.pitch / 128) {
                 case 1: launch_micro_held<TO, 2>(a, st); break;
                 case 2: launch_micro_held<TO, 4>(a, st); break;
                 case 3: launch_micro_held<TO, 6>(a, st); break;
                 default: launch_micro_held<TO, 8>(a, st); break;
             }
-        } else if (a.B <= 64 && a.units <= kMicroFewUnits) {
-            if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4, 3>(a, st);
+        } else if (few) {
+            if (a.units > kMicroFewUnits) launch_few<TO, void, 2, kMicroFewLong, 4, 2>(a, st);
+            else if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4, 3>(a, st);
             else launch_few<TO, void, 4, kMicroFewUnits, 4, 3>(a, st);
-        } else if (a.B <= 64 && a.units <= kMicroFewLong) {
-            launch_few<TO, void, 2, kMicroFewLong, 4, 2>(a, st);
+        } else if (a.B <= kMicroTileQueries) {
+            launch_micro_tile<TO, 1, 2>(a, st);
         } else {
-            const int64_t tiles = ((a.B + kMxTile - 1) / kMxTile) * ((a.L + kMxTile - 1) / kMxTile);
-            scores_micro_kernel<TO><<<static_cast<unsigned>((tiles + 3) / 4), 256, 0, st>>>(a);
+            launch_micro_tile<TO, 4, 2>(a, st);
         }
     };
     XC_LAUNCH(K_SCORES_MICRO, st, go());

@@ -98,7 +98,8 @@ def _bound(P, p, Q, q, got, out):
 
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32)])
 @pytest.mark.parametrize("B,L,d", [(1, 1, 8), (1, 17, 64), (2, 1000, 72), (15, 100, 128), (16, 333, 256), (17, 64, 384), (33, 130, 768), (63, 129, 200), (64, 500, 512),
-                                   (65, 63, 1000), (128, 257, 768), (130, 515, 896), (200, 700, 1024), (129, 300, 1152), (257, 513, 640), (300, 65, 4096)])
+                                   (65, 63, 1000), (128, 257, 768), (130, 515, 896), (200, 700, 1024), (129, 300, 1152), (257, 513, 640), (300, 65, 4096), (5, 100, 5000), (20, 500, 2048),
+                                   (31, 200, 1160), (40, 300, 2048), (100, 129, 1800), (129, 257, 1288), (2, 65, 20000), (260, 1000, 1536)])
 def test_scores_match_the_oracle(B, L, d, dtype, out):
     import paper_2409_20156_amd as xc
     Z, W = _matrix(B + d, B, d, dtype), _matrix(L + d + 7, L, d, dtype)
@@ -130,7 +131,7 @@ def test_every_pair_of_codes_and_scales_that_differ():
 
 def test_scores_do_not_depend_on_the_batch_or_the_range():
     import paper_2409_20156_amd as xc
-    for d in (72, 768, 1280):
+    for d in (72, 768, 1280, 4200):
         Z, W = _matrix(1, 300, d, BF16).to(DEV), _matrix(2, 1500, d, BF16).to(DEV)
         Q, s = xc.microscale_rows(W)
         whole = xc.scores_microscaled(Z, Q, s)
