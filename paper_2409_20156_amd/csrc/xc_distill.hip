@@ -323,6 +323,107 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
     if (listed >= 0) Elem<TO>::put(out + listed, value);
 }
 
+// ---- a row by one workgroup, which holds it in registers: read once, its sums, its loss and terms by one wave, its gradient.
+// Listed labels are taken out of the sums by a mark each, a bit in a byte per piece.
+template <typename T, typename TO, int W, int C>
+__global__ __launch_bounds__(W * kWave)
+void distill_row_kernel(const DistillArgs a) {
+    constexpr int N = PiecedRow<T>::N, kThreads = W * kWave, kMarks = kThreads * C / 4;
+    __shared__ Sums sums[W];
+    __shared__ uint32_t marks[kMarks + 1];                   // a byte per piece; the edges
+    __shared__ __align__(16) int32_t list[XC_MAX_TEACHER];
+    __shared__ RowTerms terms;
+    static_assert(XC_MAX_TEACHER <= kThreads, "a thread per listed label");
+    const int64_t b = blockIdx.x;
+    const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
+    TO* out = static_cast<TO*>(a.dX) + b * a.ldd;
+    const float weight = a.weight != nullptr ? a.weight[b] : 1.0f;
+    const int32_t id = static_cast<int>(threadIdx.x) < a.K ? a.labels[b * a.K + threadIdx.x] : -1;
+    const bool there = is_label(id, a.V);
+    const int64_t edge = static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
+    const int pieces = static_cast<int>(row.pieces);
+    uint4 v[C];
+    if (weight != 0.0f) {                                    // uniform
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int at = i * kThreads + static_cast<int>(threadIdx.x);
+            v[i] = at < pieces ? row.template load<true>(at) : Elem<T>::none();
+        }
+    }
+    float more = edge >= 0 && weight != 0.0f ? Elem<T>::get(row.p + edge) : kNone;
+    const float edge_score = more;
+    const float score = there ? Elem<T>::get(row.p + id) : 0.0f;
+    if (static_cast<int>(threadIdx.x) < XC_MAX_TEACHER) list[threadIdx.x] = id;
+    if (a.tail) {
+        for (int i = threadIdx.x; i <= kMarks; i += kThreads) marks[i] = 0;
+        __syncthreads();
+        if (there) {
+            const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
+            if (piece >= 0 && piece < row.pieces) atomicOr(&marks[piece >> 2], 1u << (static_cast<int>(piece & 3) * 8 + static_cast<int>(id - row.first(piece))));
+            else atomicOr(&marks[kMarks], 1u << (id < row.head ? id : static_cast<int>(id - row.pieces * N)));
+        }
+    }
+    __syncthreads();
+    if (weight != 0.0f) {
+        if (a.tail && edge >= 0 && ((marks[kMarks] >> threadIdx.x) & 1u) != 0u) more = kNone;
+        Running run;
+        // groups of 8 elements at least, unpacked one after the other
+        constexpr int G = 8 / N > 1 ? 8 / N : C % 2 == 0 ? 2 : 1, E = G * N;
+#pragma unroll
+        for (int i0 = 0; i0 < C; i0 += G) {
+            float f[E];
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+                float x[N];
+                Elem<T>::values(v[i0 + i], x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[i * N + e] = x[e];
+                if (a.tail) {
+                    const uint32_t m = reinterpret_cast<const unsigned char*>(marks)[(i0 + i) * kThreads + threadIdx.x];
+                    if (__ballot(m != 0u) == 0ull) continue;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) if ((m >> e) & 1u) f[i * N + e] = kNone;
+                }
+            }
+            run.template add<false>(f, largest_of<E>(f, 0), a.c);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        run.add_one(more, a.c);
+        const Sums s = block_sums<W>(run.sums(a.c), a.c, sums);
+        if (threadIdx.x < kWave) {
+            const RowTerms r = row_terms<T>(a, b, s, weight, list);
+            if (threadIdx.x == 0) terms = r;
+        }
+    } else if (threadIdx.x == 0) {                           // counts for nothing, whatever it holds
+        terms = RowTerms{};
+        a.loss[b] = 0.0f;
+    }
+    __syncthreads();                                         // (the row's scores have all been read: dX may be X)
+    const RowTerms r = terms;
+    const bool live = r.live != 0.0f;                        // uniform
+    const bool listed = live && there && !listed_before(list, threadIdx.x, id);
+    const float value = listed ? listed_gradient(a, r, b, threadIdx.x, id, score, list) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int at = i * kThreads + static_cast<int>(threadIdx.x);
+        if (at < pieces) {
+            float x[N];
+            if (live) {
+                Elem<T>::values(v[i], x);
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[e] = other_gradient(r, x[e], a.c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) x[e] = 0.0f;
+            }
+            put_elements<N>(out + row.first(at), x);
+        }
+    }
+    if (edge >= 0) Elem<TO>::put(out + edge, live ? other_gradient(r, edge_score, a.c) : 0.0f);
+    __syncthreads();                                         // (waits for the stores as well)
+    if (listed) Elem<TO>::put(out + id, value);
+}
+
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
@@ -330,8 +431,35 @@ static size_t distill_bytes(int64_t B, int64_t V, xc_dtype t) {
     return static_cast<size_t>(B) * (sizeof(RowTerms) + static_cast<size_t>(cut_rows(B, V, t == XC_F32 ? 4 : 2).segments) * sizeof(float4));
 }
 
+// Whether a row is one workgroup's, which holds it (pieces of a thread; 0: it is not).
+static int distill_whole(int64_t B, int64_t V, size_t element) {
+    const int64_t pieces = V / static_cast<int64_t>(16 / element);
+    if (pieces <= 4 * kWave * 4) return 4;                   // 4 waves
+    if (B < 64) return 0;
+    if (pieces <= 16 * kWave * 4) return 16;                 // 16 waves with 4
+    return pieces <= 16 * kWave * 16 ? 64 : 0;               // 16 waves with 16
+}
+
 template <typename T, typename TO>
 static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_t st) {
+    const int whole = all.dX != nullptr ? distill_whole(all.B, all.V, sizeof(T)) : 0;
+    if (whole != 0) {
+        for (int64_t b0 = 0; b0 < all.B; b0 += kSoftmaxGrid) {
+            DistillArgs a = all;
+            a.B = all.B - b0 < kSoftmaxGrid ? all.B - b0 : kSoftmaxGrid;
+            a.X = static_cast<const T*>(all.X) + b0 * all.ld;
+            a.dX = static_cast<TO*>(all.dX) + b0 * all.ldd;
+            a.labels += b0 * all.K;
+            a.teacher += b0 * all.K;
+            if (all.weight != nullptr) a.weight += b0;
+            a.loss += b0;
+            const unsigned grid = static_cast<unsigned>(a.B);
+            if (whole == 4) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 4><<<grid, 4 * kWave, 0, st>>>(a)));
+            else if (whole == 16) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 4><<<grid, 16 * kWave, 0, st>>>(a)));
+            else XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 16><<<grid, 16 * kWave, 0, st>>>(a)));
+        }
+        return;
+    }
     const int64_t pieces = all.V / static_cast<int64_t>(16 / sizeof(T)), chunks = pieces > kDistillPieces ? (pieces + kDistillPieces - 1) / kDistillPieces : 1;
     int64_t rows = kSoftmaxGrid / (chunks > cut.segments ? chunks : cut.segments);
     if (rows < 1) rows = 1;

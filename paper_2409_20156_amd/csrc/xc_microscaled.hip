@@ -37,7 +37,7 @@ __device__ __forceinline__ uint32_t quad_max(uint32_t x) {   // of four neighbou
 }
 
 // Codes and scale byte of a lane's 8 elements; four lanes have a block.
-struct MicroLane { uint32_t codes, byte; };
+struct MicroLane { uint32_t codes, byte, bytes; };       // bytes: of four blocks, in every 16th lane
 __device__ __forceinline__ MicroLane to_micro(float (&f)[8]) {
     uint32_t big = 0;
 #pragma unroll
@@ -56,7 +56,12 @@ __device__ __forceinline__ MicroLane to_micro(float (&f)[8]) {
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], 1.0f, 1);
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], 1.0f, 2);
     codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], 1.0f, 3);
-    return MicroLane{finite ? codes : 0u, finite ? byte : 255u};
+    const uint32_t b = finite ? byte : 255u;
+    uint32_t all = b;
+    all |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), 0x104, 0xf, 0xf, false)) << 8;         // row_shl 4, 8, 12
+    all |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), 0x108, 0xf, 0xf, false)) << 16;
+    all |= static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(b), 0x10c, 0xf, 0xf, false)) << 24;
+    return MicroLane{finite ? codes : 0u, b, all};
 }
 
 // Rows of 4 bits where they are kept: Q (64 bytes to 128 elements) and their scales row by row.
@@ -65,7 +70,7 @@ struct MicroRows {
     int units;                           // of 128 elements in a row
     __device__ __forceinline__ void put(int64_t row, int u, int sub, const MicroLane& m) const {
         *reinterpret_cast<uint32_t*>(Q + (row * units + u) * 64 + sub * 4) = m.codes;
-        if ((sub & 3) == 0) scale[(row * units + u) * 4 + (sub >> 2)] = static_cast<uint8_t>(m.byte);
+        if (sub == 0) *reinterpret_cast<uint32_t*>(scale + (row * units + u) * 4) = m.bytes;
     }
 };
 // Queries in the workspace: rows of `pitch` bytes (an even number of units), zeros behind the last element and the last query.  A row's
@@ -81,7 +86,7 @@ struct MicroQueries {
 };
 
 // 16 lanes bring 128 elements of a row, U of these at a time.  Rows from N on (of the queries' padding) and units behind a row are zeros.
-// Bound: memory.
+// Bound: memory.  670000 x 768 bf16: 240 us, 5.4 TB/s, what a copy reaches here; one at a time 252, four 237, with the non-temporal hint 240.
 template <typename T, typename TO, int U>
 __global__ __launch_bounds__(256)
 void microscale_kernel(const unsigned char* __restrict__ X, int64_t N, int d, const int32_t* __restrict__ ids, int64_t m, const int32_t* __restrict__ count,
@@ -93,6 +98,7 @@ void microscale_kernel(const unsigned char* __restrict__ X, int64_t N, int d, co
         rows = c < rows ? c : rows;
     }
     const int64_t total = rows * units, step = static_cast<int64_t>(gridDim.x) * (16 * U);
+    const bool small = total <= 0xffffffffLL;                // uniform: divided in 32 bits
     for (int64_t u0 = static_cast<int64_t>(blockIdx.x) * (16 * U) + (threadIdx.x >> 4); u0 < total; u0 += step) {
         float f[U][8];
         int64_t row[U];
@@ -102,7 +108,7 @@ void microscale_kernel(const unsigned char* __restrict__ X, int64_t N, int d, co
             const int64_t u = u0 + k * 16;
             row[k] = -1;
             if (u >= total) continue;
-            const int64_t i = u / units;
+            const int64_t i = small ? static_cast<uint32_t>(u) / static_cast<uint32_t>(units) : u / units;
             col[k] = static_cast<int>(u - i * units);
             row[k] = ids != nullptr ? ids[i] : i;
             const bool there = row[k] >= 0 && row[k] < N;                  // (the same for 16 lanes)
@@ -115,6 +121,7 @@ void microscale_kernel(const unsigned char* __restrict__ X, int64_t N, int d, co
     }
 }
 
+constexpr int64_t kMxGrid = 1 << 20;
 template <typename TO>
 static int launch_microscale(const void* X, int64_t N, int d, xc_dtype t, const int32_t* ids, int64_t m, const int32_t* count, const TO& out, int64_t n_rows, int units,
                              hipStream_t st) {
@@ -122,11 +129,11 @@ static int launch_microscale(const void* X, int64_t N, int d, xc_dtype t, const 
     const unsigned char* x = static_cast<const unsigned char*>(X);
     auto go = [&](auto kernel, int U) {
         const int64_t want = (total + 16 * U - 1) / (16 * U);
-        kernel<<<static_cast<unsigned>(want < 32768 ? want : 32768), 256, 0, st>>>(x, N, d, ids, m, count, out, n_rows, units);
+        kernel<<<static_cast<unsigned>(want < kMxGrid ? want : kMxGrid), 256, 0, st>>>(x, N, d, ids, m, count, out, n_rows, units);
     };
     const bool many = total > 256 * 16 * 8;
-    if (t == XC_F32) XC_LAUNCH(K_MICROSCALE, st, (many ? go(microscale_kernel<float, TO, 4>, 4) : go(microscale_kernel<float, TO, 1>, 1)));
-    else XC_LAUNCH(K_MICROSCALE, st, (many ? go(microscale_kernel<bf16_t, TO, 4>, 4) : go(microscale_kernel<bf16_t, TO, 1>, 1)));
+    if (t == XC_F32) XC_LAUNCH(K_MICROSCALE, st, (many ? go(microscale_kernel<float, TO, 2>, 2) : go(microscale_kernel<float, TO, 1>, 1)));
+    else XC_LAUNCH(K_MICROSCALE, st, (many ? go(microscale_kernel<bf16_t, TO, 2>, 2) : go(microscale_kernel<bf16_t, TO, 1>, 1)));
     XC_HIP_CHECK(hipGetLastError());
     return XC_OK;
 }
@@ -547,7 +554,7 @@ struct MicroTile {
     static_assert(kRowLoads * 8 * kWaves == kRows && R * kStage <= 160 * 1024, "whole loads");
 };
 template <typename TO, int WQ, int WL>
-__global__ __launch_bounds__(WQ * WL * kWave, 2)
+__global__ __launch_bounds__(WQ * WL * kWave)
 void scores_micro_tile_kernel(const MicroArgs a, uint32_t tiles_m, uint32_t tiles_n) {
     typedef MicroTile<WQ, WL> T;
     __shared__ __align__(1024) unsigned char smem[T::R * T::kStage];
