@@ -52,10 +52,13 @@ __device__ __forceinline__ double wave_sum(double x) {
 }
 __device__ __forceinline__ bool is_label(int32_t v, int64_t V) { return v >= 0 && v < V; }
 
-// Loss and terms of a row from its sums, by one wave: a lane has every 64th place of the list.  In 64 bits, which cost nothing beside
-// the row.  An entry of the list whose label occurs before it does not count to the student's sum again.  `list` holds the list's labels.
-constexpr int kPlaces = XC_MAX_TEACHER / kWave;
-__device__ __forceinline__ bool listed_before(const int32_t* list, int k, int32_t id) {      // (list: 16 bytes aligned, in LDS)
+// The list of a row in LDS: its labels, and what one wave has made of each place.
+struct Place { double q; float t, x; float q_all; bool once; };           // q_all: of all places with the label, at the first of them (once)
+struct List {
+    int32_t labels[XC_MAX_TEACHER];      // (read 16 bytes at a time)
+    Place places[XC_MAX_TEACHER];
+};
+__device__ __forceinline__ bool listed_before(const int32_t* list, int k, int32_t id) {
     bool before = false;
 #pragma unroll 2
     for (int j = 0; j < k; j += 4) {
@@ -64,87 +67,110 @@ __device__ __forceinline__ bool listed_before(const int32_t* list, int k, int32_
     }
     return before;
 }
+
+// What does not depend on the row's sums, by one wave (a lane has every 64th place), while the row is on its way: the teacher's
+// probabilities, in 64 bits as all that is formed from the sums, which costs nothing beside the row.  labels are in the list.
+struct Teacher {
+    double sum, entropy;                 // sum of q before it is normalised; sum of q log q behind that
+    float t0, x_max;
+    bool any;
+};
 template <typename T>
-__device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, const Sums& s, float weight, const int32_t* list) {
+__device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t b, List& list) {
     const T* x = static_cast<const T*>(a.X) + b * a.ld;
-    const double invT = 1.0 / static_cast<double>(a.T);
-    int32_t id[kPlaces];
-    double t[kPlaces], y[kPlaces];                           // (the student's relative to the row's largest score: that may be huge)
-    bool once[kPlaces];
-    float t_max = kNone, x_max = kNone;
-    int places = 0;
-#pragma unroll
-    for (int i = 0; i < kPlaces; ++i) {
-        const int k = i * kWave + lane_id();
-        id[i] = -1;
-        t[i] = y[i] = 0.0;
-        once[i] = false;
-        if (k < a.K) {
-            id[i] = list[k];
-            if (is_label(id[i], a.V)) {
-                const float tk = a.teacher[b * a.K + k], xk = Elem<T>::get(x + id[i]);
-                t[i] = tk;
-                y[i] = xk;
-                t_max = fmaxf(t_max, tk);
-                x_max = fmaxf(x_max, xk);
-                once[i] = !listed_before(list, k, id[i]);
-                if (a.tail || tk != kNone) ++places;         // (without a tail a list of probabilities 0 is no distribution)
-            } else {
-                id[i] = -1;
-            }
+    Teacher r;
+    float t_max = kNone;
+    r.x_max = kNone;
+    bool some = false;
+#pragma unroll 1
+    for (int k = lane_id(); k < a.K; k += kWave) {
+        const int32_t id = list.labels[k];
+        Place p{0.0, 0.0f, 0.0f, 0.0f, false};
+        if (is_label(id, a.V)) {
+            p.t = a.teacher[b * a.K + k];
+            p.x = Elem<T>::get(x + id);
+            p.once = !listed_before(list.labels, k, id);
+            t_max = fmaxf(t_max, p.t);
+            r.x_max = fmaxf(r.x_max, p.x);
+            some |= a.tail || p.t != kNone;                  // (without a tail a list of probabilities 0 is no distribution)
         }
+        list.places[k] = p;
     }
-    const bool any = __ballot(places > 0) != 0ull;
+    r.any = __ballot(some) != 0ull;
+    t_max = wave_max(t_max);
+    r.x_max = wave_max(r.x_max);
+    r.t0 = a.tail || t_max == kNone ? 0.0f : t_max;
+    r.sum = 0.0;
+#pragma unroll 1
+    for (int k = lane_id(); k < a.K; k += kWave) {
+        if (!is_label(list.labels[k], a.V)) continue;
+        const double q = exp(static_cast<double>(list.places[k].t) - static_cast<double>(r.t0));
+        list.places[k].q = q;
+        r.sum += q;
+    }
+    r.sum = wave_sum(r.sum);
+    const double scale = a.tail ? 1.0 : 1.0 / r.sum, t_log = a.tail ? 0.0 : log(r.sum);
+    r.entropy = 0.0;
+#pragma unroll 1
+    for (int k = lane_id(); k < a.K; k += kWave) {
+        if (!is_label(list.labels[k], a.V)) continue;
+        const double q = list.places[k].q * scale;
+        list.places[k].q = q;
+        if (!(q == 0.0)) r.entropy += q * (static_cast<double>(list.places[k].t) - static_cast<double>(r.t0) - t_log);
+    }
+    r.entropy = wave_sum(r.entropy);
+#pragma unroll 1
+    for (int k = lane_id(); k < a.K; k += kWave) {
+        if (!list.places[k].once) continue;
+        double q = 0.0;
+        const int32_t id = list.labels[k];
+        for (int j = k; j < a.K; ++j) if (list.labels[j] == id) q += list.places[j].q;
+        list.places[k].q_all = static_cast<float>(q);
+    }
+    return r;
+}
+
+// Loss and terms of a row from its sums, by the same wave.  A place whose label occurs before it does not count to the student's sum again.
+template <typename T>
+__device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, const Sums& s, float weight, const Teacher& t, const List& list) {
     RowTerms r{};
     r.factor = weight * a.T;
-    r.live = any ? 1.0f : 0.0f;
-    if (!any) {
+    r.live = t.any ? 1.0f : 0.0f;
+    if (!t.any) {
         if (lane_id() == 0) a.loss[b] = 0.0f;
         return r;
     }
-    t_max = wave_max(t_max);
-    x_max = wave_max(x_max);
-    // the teacher
-    double q[kPlaces], sum = 0.0;
-    const double t0 = a.tail || t_max == kNone ? 0.0 : static_cast<double>(t_max);
-#pragma unroll
-    for (int i = 0; i < kPlaces; ++i) {
-        q[i] = id[i] >= 0 ? exp(t[i] - t0) : 0.0;
-        sum += q[i];
-    }
-    sum = wave_sum(sum);
-    const double t_log = a.tail ? 0.0 : log(sum);
-    if (!a.tail) {
-#pragma unroll
-        for (int i = 0; i < kPlaces; ++i) q[i] /= sum;
-    }
-    // the student
-    const float m_all = fmaxf(s.m, x_max);
+    // (the student's scores relative to the largest one: that may be huge)
+    const double invT = 1.0 / static_cast<double>(a.T);
+    const float m_all = fmaxf(s.m, t.x_max);
     const double ref = m_all == kNone ? 0.0 : static_cast<double>(m_all);
-#pragma unroll
-    for (int i = 0; i < kPlaces; ++i) y[i] = (y[i] - ref) * invT;
+    double listed = 0.0, cross = 0.0;
+#pragma unroll 1
+    for (int k = lane_id(); k < a.K; k += kWave) {
+        if (!is_label(list.labels[k], a.V)) continue;
+        const Place p = list.places[k];
+        const double y = (static_cast<double>(p.x) - ref) * invT;
+        if (a.tail && p.once) listed += exp(y);
+        if (!(p.q == 0.0)) cross += p.q * y;
+    }
+    cross = wave_sum(cross);
     const double sum_log = log(static_cast<double>(s.s));
     const double rest_log = s.s == 0.0f ? sum_log : sum_log + (static_cast<double>(s.m) - ref) * invT;        // of the labels that s is about
     double lse = rest_log;
     if (a.tail) {
-        double listed = 0.0;
-#pragma unroll
-        for (int i = 0; i < kPlaces; ++i) if (once[i]) listed += exp(y[i]);
         listed = wave_sum(listed);
         if (s.s != 0.0f) listed += exp(rest_log);
         lse = log(listed);
     }
     double q_r = 0.0;
     if (a.tail && s.s != 0.0f) {                             // (no label but the listed ones: nothing to compare)
-        q_r = 1.0 - sum;
+        q_r = 1.0 - t.sum;
         if (q_r < 0.0) q_r = 0.0;
     }
-    const double mass = a.tail ? sum + q_r : sum == sum ? 1.0 : sum;
+    const double q_sum = a.tail ? t.sum : t.sum == t.sum ? 1.0 : t.sum, mass = q_sum + q_r;
     double loss = 0.0;
-#pragma unroll
-    for (int i = 0; i < kPlaces; ++i)
-        if (id[i] >= 0 && !(q[i] == 0.0)) loss += q[i] * ((t[i] - t0 - t_log) - (lse == -INFINITY ? lse : y[i] - lse));
-    loss = wave_sum(loss);
+    if (lse == -INFINITY) loss = q_sum == 0.0 ? 0.0 : q_sum == q_sum ? INFINITY : q_sum;       // no label at all
+    else if (!(q_sum == 0.0)) loss = t.entropy - cross + q_sum * lse;
     if (!(q_r == 0.0)) loss += q_r * (log(q_r) - (rest_log - lse));
     const double T2 = static_cast<double>(a.T) * static_cast<double>(a.T);
     if (lane_id() == 0) a.loss[b] = static_cast<float>(static_cast<double>(weight) * T2 * loss);
@@ -155,8 +181,8 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, c
     r.m_all = m_all == kNone ? 0.0f : m_all;
     r.l_all = static_cast<float>(rint(l_all));
     r.mass = static_cast<float>(l_all == -INFINITY ? mass : mass * exp2(rint(l_all) - l_all));
-    r.t = static_cast<float>(t0);
-    r.t_log = static_cast<float>(t_log);
+    r.t = t.t0;
+    r.t_log = a.tail ? 0.0f : static_cast<float>(log(t.sum));
     const double factor = static_cast<double>(weight) * static_cast<double>(a.T);
     r.other = static_cast<float>(exp2(rint(l) - l) * factor * (a.tail ? (s.s == 0.0f ? 0.0 : mass * exp(rest_log - lse)) - q_r : mass));
     return r;
@@ -168,10 +194,8 @@ __device__ __forceinline__ float q_of(const DistillArgs& a, const RowTerms& r, f
 __device__ __forceinline__ float other_gradient(const RowTerms& r, float x, float c) {
     return r.other * __builtin_amdgcn_exp2f(fmaf(x - r.m, c, -r.l));
 }
-// Of the listed label at place k, the first of its label in the list: all places of it count.
-__device__ __forceinline__ float listed_gradient(const DistillArgs& a, const RowTerms& r, int64_t b, int k, int32_t id, float x, const int32_t* list) {
-    float q = 0.0f;
-    for (int j = k; j < a.K; ++j) if (list[j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
+// Of a listed label with score x, q the teacher's probability.
+__device__ __forceinline__ float listed_gradient(const DistillArgs& a, const RowTerms& r, float x, float q) {
     const float p = r.l_all == kNone ? 0.0f : __builtin_amdgcn_exp2f(fmaf(x - r.m_all, a.c, -r.l_all));
     return r.factor * fmaf(r.mass, p, -q);
 }
@@ -248,10 +272,10 @@ constexpr int kTermWaves = 4;
 template <typename T>
 __global__ __launch_bounds__(kTermWaves * kWave)
 void distill_terms_kernel(const DistillArgs a) {
-    __shared__ __align__(16) int32_t lists[kTermWaves][XC_MAX_TEACHER];
+    __shared__ __align__(16) List lists[kTermWaves];
     const int64_t b = static_cast<int64_t>(blockIdx.x) * kTermWaves + (threadIdx.x >> 6);
-    int32_t* list = lists[threadIdx.x >> 6];
-    if (b < a.B) for (int k = lane_id(); k < a.K; k += kWave) list[k] = a.labels[b * a.K + k];
+    List& list = lists[threadIdx.x >> 6];
+    if (b < a.B) for (int k = lane_id(); k < a.K; k += kWave) list.labels[k] = a.labels[b * a.K + k];
     __syncthreads();
     if (b >= a.B) return;
     const float weight = a.weight != nullptr ? a.weight[b] : 1.0f;
@@ -267,7 +291,7 @@ void distill_terms_kernel(const DistillArgs a) {
             const Sums u = joined(t, m, a.c), w = joined(q, m, a.c);
             t = Sums{m, u.s + w.s, 0.0f};
         }
-        r = row_terms<T>(a, b, wave_sums(t, a.c), weight, list);
+        r = row_terms<T>(a, b, wave_sums(t, a.c), weight, teacher_of<T>(a, b, list), list);
     }
     if (lane_id() == 0) a.terms[b] = r;
 }
@@ -303,7 +327,9 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
         const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
         if ((id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) && !listed_before(list, threadIdx.x, id)) {
             listed = id;
-            value = listed_gradient(a, r, b, threadIdx.x, id, Elem<T>::get(row.p + id), list);
+            float q = 0.0f;                                  // (all places of the label count)
+            for (int j = threadIdx.x; j < a.K; ++j) if (list[j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
+            value = listed_gradient(a, r, Elem<T>::get(row.p + id), q);
         }
     }
     __syncthreads();
@@ -326,12 +352,12 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
 // ---- a row by one workgroup, which holds it in registers: read once, its sums, its loss and terms by one wave, its gradient.
 // Listed labels are taken out of the sums by a mark each, a bit in a byte per piece.
 template <typename T, typename TO, int W, int C>
-__global__ __launch_bounds__(W * kWave)
+__global__ __launch_bounds__(W * kWave, C == 16 ? 4 : 1)
 void distill_row_kernel(const DistillArgs a) {
     constexpr int N = PiecedRow<T>::N, kThreads = W * kWave, kMarks = kThreads * C / 4;
     __shared__ Sums sums[W];
     __shared__ uint32_t marks[kMarks + 1];                   // a byte per piece; the edges
-    __shared__ __align__(16) int32_t list[XC_MAX_TEACHER];
+    __shared__ __align__(16) List list;
     __shared__ RowTerms terms;
     static_assert(XC_MAX_TEACHER <= kThreads, "a thread per listed label");
     const int64_t b = blockIdx.x;
@@ -352,8 +378,7 @@ void distill_row_kernel(const DistillArgs a) {
     }
     float more = edge >= 0 && weight != 0.0f ? Elem<T>::get(row.p + edge) : kNone;
     const float edge_score = more;
-    const float score = there ? Elem<T>::get(row.p + id) : 0.0f;
-    if (static_cast<int>(threadIdx.x) < XC_MAX_TEACHER) list[threadIdx.x] = id;
+    if (static_cast<int>(threadIdx.x) < XC_MAX_TEACHER) list.labels[threadIdx.x] = id;
     if (a.tail) {
         for (int i = threadIdx.x; i <= kMarks; i += kThreads) marks[i] = 0;
         __syncthreads();
@@ -365,6 +390,8 @@ void distill_row_kernel(const DistillArgs a) {
     }
     __syncthreads();
     if (weight != 0.0f) {
+        Teacher teacher{};
+        if (threadIdx.x < kWave) teacher = teacher_of<T>(a, b, list);      // (while the row's pieces are under way)
         if (a.tail && edge >= 0 && ((marks[kMarks] >> threadIdx.x) & 1u) != 0u) more = kNone;
         Running run;
         // groups of 8 elements at least, unpacked one after the other
@@ -391,7 +418,7 @@ void distill_row_kernel(const DistillArgs a) {
         run.add_one(more, a.c);
         const Sums s = block_sums<W>(run.sums(a.c), a.c, sums);
         if (threadIdx.x < kWave) {
-            const RowTerms r = row_terms<T>(a, b, s, weight, list);
+            const RowTerms r = row_terms<T>(a, b, s, weight, teacher, list);
             if (threadIdx.x == 0) terms = r;
         }
     } else if (threadIdx.x == 0) {                           // counts for nothing, whatever it holds
@@ -401,8 +428,8 @@ void distill_row_kernel(const DistillArgs a) {
     __syncthreads();                                         // (the row's scores have all been read: dX may be X)
     const RowTerms r = terms;
     const bool live = r.live != 0.0f;                        // uniform
-    const bool listed = live && there && !listed_before(list, threadIdx.x, id);
-    const float value = listed ? listed_gradient(a, r, b, threadIdx.x, id, score, list) : 0.0f;
+    const bool listed = live && there && list.places[threadIdx.x].once;
+    const float value = listed ? listed_gradient(a, r, list.places[threadIdx.x].x, list.places[threadIdx.x].q_all) : 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         const int at = i * kThreads + static_cast<int>(threadIdx.x);
@@ -434,9 +461,11 @@ static size_t distill_bytes(int64_t B, int64_t V, xc_dtype t) {
 // Whether a row is one workgroup's, which holds it (pieces of a thread; 0: it is not).
 static int distill_whole(int64_t B, int64_t V, size_t element) {
     const int64_t pieces = V / static_cast<int64_t>(16 / element);
-    if (pieces <= 4 * kWave * 4) return 4;                   // 4 waves
+    if (pieces <= 4 * kWave * 4) return 4;                   // 4 waves with 4
     if (B < 64) return 0;
+    if (B >= 512 && pieces <= 4 * kWave * 16) return 17;     // 4 waves with 16
     if (pieces <= 16 * kWave * 4) return 16;                 // 16 waves with 4
+    if (pieces <= 8 * kWave * 16) return 32;                 // 8 waves with 16
     return pieces <= 16 * kWave * 16 ? 64 : 0;               // 16 waves with 16
 }
 
@@ -456,6 +485,8 @@ static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_
             const unsigned grid = static_cast<unsigned>(a.B);
             if (whole == 4) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 4><<<grid, 4 * kWave, 0, st>>>(a)));
             else if (whole == 16) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 4><<<grid, 16 * kWave, 0, st>>>(a)));
+            else if (whole == 17) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 16><<<grid, 4 * kWave, 0, st>>>(a)));
+            else if (whole == 32) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 8, 16><<<grid, 8 * kWave, 0, st>>>(a)));
             else XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 16><<<grid, 16 * kWave, 0, st>>>(a)));
         }
         return;
