@@ -137,7 +137,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, c
     r.factor = weight * a.T;
     r.live = t.any ? 1.0f : 0.0f;
     if (!t.any) {
-        if (lane_id() == 0) a.loss[b] = 0.0f;
+        if (lane_id() == 0 && a.loss != nullptr) a.loss[b] = 0.0f;
         return r;
     }
     // (the student's scores relative to the largest one: that may be huge)
@@ -173,7 +173,7 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, c
     else if (!(q_sum == 0.0)) loss = t.entropy - cross + q_sum * lse;
     if (!(q_r == 0.0)) loss += q_r * (log(q_r) - (rest_log - lse));
     const double T2 = static_cast<double>(a.T) * static_cast<double>(a.T);
-    if (lane_id() == 0) a.loss[b] = static_cast<float>(static_cast<double>(weight) * T2 * loss);
+    if (lane_id() == 0 && a.loss != nullptr) a.loss[b] = static_cast<float>(static_cast<double>(weight) * T2 * loss);
     const double log2e = 1.4426950408889634;
     r.m = s.m == kNone ? 0.0f : s.m;
     const double l = s.s == 0.0f ? 0.0 : sum_log * log2e, l_all = lse * log2e;
@@ -267,6 +267,19 @@ void distill_sums_kernel(const DistillArgs a) {
     if (threadIdx.x == 0) a.parts[b * a.segments + seg] = make_float4(s.m, s.s, 0.0f, 0.0f);
 }
 
+// A row's segments joined, by a wave.
+__device__ __forceinline__ Sums joined_segments(const DistillArgs& a, int64_t b) {
+    Sums t{kNone, 0.0f, 0.0f};
+    for (int64_t i = lane_id(); i < a.segments; i += kWave) {
+        const float4 p = a.parts[b * a.segments + i];
+        const Sums q{p.x, p.y, 0.0f};
+        const float m = fmaxf(t.m, q.m);
+        const Sums u = joined(t, m, a.c), w = joined(q, m, a.c);
+        t = Sums{m, u.s + w.s, 0.0f};
+    }
+    return wave_sums(t, a.c);
+}
+
 // A wave per row: its segments joined, its loss and terms.
 constexpr int kTermWaves = 4;
 template <typename T>
@@ -283,22 +296,17 @@ void distill_terms_kernel(const DistillArgs a) {
     if (weight == 0.0f) {                                    // counts for nothing, whatever it holds
         if (lane_id() == 0) a.loss[b] = 0.0f;
     } else {
-        Sums t{kNone, 0.0f, 0.0f};
-        for (int64_t i = lane_id(); i < a.segments; i += kWave) {
-            const float4 p = a.parts[b * a.segments + i];
-            const Sums q{p.x, p.y, 0.0f};
-            const float m = fmaxf(t.m, q.m);
-            const Sums u = joined(t, m, a.c), w = joined(q, m, a.c);
-            t = Sums{m, u.s + w.s, 0.0f};
-        }
-        r = row_terms<T>(a, b, wave_sums(t, a.c), weight, teacher_of<T>(a, b, list), list);
+        r = row_terms<T>(a, b, joined_segments(a, b), weight, teacher_of<T>(a, b, list), list);
     }
     if (lane_id() == 0) a.terms[b] = r;
 }
 
 // The gradient of a chunk of a row, then that of the listed labels in it (their scores are read before anything is stored: dX may be X).
+// INLINE: every workgroup makes the row's terms for itself from the segments' sums, while its chunk is on its way, and the first one the
+// loss: a launch less, where few rows leave the device idle anyway (16 x 131072 bf16 24 us with it).  Not in place: the list's scores lie
+// in other workgroups' chunks.
 constexpr int kDistillThreads = 256, kDistillEach = 4, kDistillPieces = kDistillThreads * kDistillEach;
-template <typename T, typename TO>
+template <typename T, typename TO, bool INLINE>
 __global__ __launch_bounds__(kDistillThreads)
 void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
     constexpr int N = PiecedRow<T>::N;
@@ -306,29 +314,39 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
     TO* out = static_cast<TO*>(a.dX) + b * a.ldd;
     const int64_t first = chunk * kDistillPieces, end = first + kDistillPieces < row.pieces ? first + kDistillPieces : row.pieces;
-    __shared__ __align__(16) int32_t list[XC_MAX_TEACHER];
-    uint4 v[kDistillEach];
-#pragma unroll
-    for (int i = 0; i < kDistillEach; ++i) {
-        const int64_t at = first + i * kDistillThreads + threadIdx.x;
-        v[i] = at < end ? row.template load<true>(at) : make_uint4(0, 0, 0, 0);
-    }
+    __shared__ __align__(16) List list;
+    __shared__ RowTerms terms;
+    Block<T, kDistillEach> block;
+    block.template load<true>(row, first, end, kDistillThreads);
     const int64_t edge = chunk == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
     const float more = edge >= 0 ? Elem<T>::get(row.p + edge) : 0.0f;
     static_assert(XC_MAX_TEACHER <= kDistillThreads, "a thread per listed label");
     const int32_t id = static_cast<int>(threadIdx.x) < a.K ? a.labels[b * a.K + threadIdx.x] : -1;
-    list[threadIdx.x] = id;
-    const RowTerms r = a.terms[b];
-    const bool live = r.live != 0.0f;                        // uniform
+    list.labels[threadIdx.x] = id;
+    if constexpr (!INLINE) { if (threadIdx.x == 0) terms = a.terms[b]; }
     __syncthreads();
+    if constexpr (INLINE) {
+        const float weight = a.weight != nullptr ? a.weight[b] : 1.0f;
+        if (threadIdx.x < kWave) {
+            RowTerms r{};
+            DistillArgs mine = a;
+            if (chunk != 0) mine.loss = nullptr;
+            if (weight != 0.0f) r = row_terms<T>(mine, b, joined_segments(a, b), weight, teacher_of<T>(a, b, list), list);
+            else if (threadIdx.x == 0 && chunk == 0) a.loss[b] = 0.0f;
+            if (threadIdx.x == 0) terms = r;
+        }
+        __syncthreads();
+    }
+    const RowTerms r = terms;
+    const bool live = r.live != 0.0f;                        // uniform
     int64_t listed = -1;
     float value = 0.0f;
     if (live && is_label(id, a.V)) {
         const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
-        if ((id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) && !listed_before(list, threadIdx.x, id)) {
+        if ((id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) && !listed_before(list.labels, threadIdx.x, id)) {
             listed = id;
             float q = 0.0f;                                  // (all places of the label count)
-            for (int j = threadIdx.x; j < a.K; ++j) if (list[j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
+            for (int j = threadIdx.x; j < a.K; ++j) if (list.labels[j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
             value = listed_gradient(a, r, Elem<T>::get(row.p + id), q);
         }
     }
@@ -338,7 +356,7 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
         const int64_t at = first + i * kDistillThreads + threadIdx.x;
         if (at < end) {
             float x[N];
-            Elem<T>::values(v[i], x);
+            Elem<T>::values(block.v[i], x);
 #pragma unroll
             for (int e = 0; e < N; ++e) x[e] = live ? other_gradient(r, x[e], a.c) : 0.0f;
             put_elements<N>(out + row.first(at), x);
@@ -458,11 +476,12 @@ static size_t distill_bytes(int64_t B, int64_t V, xc_dtype t) {
     return static_cast<size_t>(B) * (sizeof(RowTerms) + static_cast<size_t>(cut_rows(B, V, t == XC_F32 ? 4 : 2).segments) * sizeof(float4));
 }
 
+constexpr unsigned kInlineGrid = 1024;
 // Whether a row is one workgroup's, which holds it (pieces of a thread; 0: it is not).
 static int distill_whole(int64_t B, int64_t V, size_t element) {
     const int64_t pieces = V / static_cast<int64_t>(16 / element);
     if (pieces <= 4 * kWave * 4) return 4;                   // 4 waves with 4
-    if (B < 64) return 0;
+    if (B < 64) return pieces <= 16 * kWave * 4 ? 16 : 0;
     if (B >= 512 && pieces <= 4 * kWave * 16) return 17;     // 4 waves with 16
     if (pieces <= 16 * kWave * 4) return 16;                 // 16 waves with 4
     if (pieces <= 8 * kWave * 16) return 32;                 // 8 waves with 16
@@ -510,9 +529,13 @@ static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_
         constexpr int kSmall = small_block(sizeof(T)), kLarge = large_block(sizeof(T));
         if (cut.each == kSmall) XC_LAUNCH(K_DISTILL_SUMS, st, (distill_sums_kernel<T, kSmall><<<grid, kRowThreads, 0, st>>>(a)));
         else XC_LAUNCH(K_DISTILL_SUMS, st, (distill_sums_kernel<T, kLarge><<<grid, kRowThreads, 0, st>>>(a)));
+        const unsigned chunk_grid = static_cast<unsigned>(nb * chunks);
+        if (all.dX != nullptr && all.dX != all.X && chunk_grid <= kInlineGrid) {
+            XC_LAUNCH(K_DISTILL_GRAD, st, (distill_grad_kernel<T, TO, true><<<chunk_grid, kDistillThreads, 0, st>>>(a, chunks)));
+            continue;
+        }
         XC_LAUNCH(K_DISTILL_TERMS, st, (distill_terms_kernel<T><<<static_cast<unsigned>((nb + kTermWaves - 1) / kTermWaves), kTermWaves * kWave, 0, st>>>(a)));
-        if (all.dX != nullptr)
-            XC_LAUNCH(K_DISTILL_GRAD, st, (distill_grad_kernel<T, TO><<<static_cast<unsigned>(nb * chunks), kDistillThreads, 0, st>>>(a, chunks)));
+        if (all.dX != nullptr) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_grad_kernel<T, TO, false><<<chunk_grid, kDistillThreads, 0, st>>>(a, chunks)));
     }
 }
 

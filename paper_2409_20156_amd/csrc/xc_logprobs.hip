@@ -157,18 +157,21 @@ __device__ __forceinline__ void best_of_block(const PiecedRow<T>& row, int64_t f
 
 // A segment of a row by one workgroup: its sums, and its k best labels.
 // The labels: of the first block each thread's largest score is known, and a score that k of the threads reach is reached by all k best
-// labels of the block and by few others.  These, and what reaches the same score in the blocks behind, are collected in LDS; when they have
-// become several times k, a higher threshold is found among them and the others are dropped.  In the end the few that are left are ranked by
-// counting.
+// labels of the block and by few others.  These, and what reaches the same score in the blocks behind, are collected in LDS; behind 1, 2,
+// 4, 8, .. blocks a higher threshold is found among them and the others are dropped, so that as many labels are collected in each of these
+// stretches.  In the end the few that are left are ranked by counting.
+// A piece with such a label is noted in a list of its wave, 64 of them are looked at together: most blocks have a few, and a wave would
+// spend as much on these as on 64.
 template <typename T, int C>
-__global__ __launch_bounds__(kRowThreads)
+__global__ __launch_bounds__(kRowThreads, 4)
 void logprobs_kernel(const LogprobArgs a) {
     constexpr int N = PiecedRow<T>::N, E = C * N;
     __shared__ Sums sums[kRowWaves];
     __shared__ uint32_t largest[kRowThreads];
     __shared__ __align__(16) uint64_t lists[2][kTopKeys + 4];
+    __shared__ int noted[kRowWaves][kWave + kWave * C];      // pieces, counted from the segment's first
     __shared__ uint32_t reach;
-    __shared__ int found[3], counts[2], kept;
+    __shared__ int found, counts[2], kept;
     const int64_t b = blockIdx.x / static_cast<uint32_t>(a.segments), seg = blockIdx.x - b * a.segments;
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
     const int64_t begin = seg * a.length, end = begin + a.length < row.pieces ? begin + a.length : row.pieces;
@@ -180,7 +183,7 @@ void logprobs_kernel(const LogprobArgs a) {
     load(begin);
     const int64_t edge = seg == 0 && static_cast<int>(threadIdx.x) < row.edges ? row.edge(threadIdx.x) : -1;
     float more = edge >= 0 ? Elem<T>::get(row.p + edge) : kNone;
-    if (threadIdx.x == 0) found[0] = 0;
+    if (threadIdx.x == 0) found = 0;
     Running run;
     uint64_t* keys = lists[0];
     int have = 0;                                            // keys from the blocks before
@@ -217,7 +220,31 @@ void logprobs_kernel(const LogprobArgs a) {
         keys = other;
         have = have < a.k ? have : a.k;
     };
-    const int room = 3 * a.k + 32 < kTopKeys / 2 ? 3 * a.k + 32 : kTopKeys / 2;
+    int* notes = noted[threadIdx.x >> 6];
+    int n_notes = 0;
+    int64_t since = begin;                                   // where the present stretch of blocks began
+    // up to 64 of the noted pieces, the last ones; room is taken by a lane for all of a piece's labels at once, by the instruction itself (the
+    // compiler would add the lanes' numbers up first)
+    auto look = [&](float least) __attribute__((always_inline)) {
+        const int take = n_notes < kWave ? n_notes : kWave;
+        n_notes -= take;
+        if (lane_id() < take) {
+            const T* p = row.p + row.first(begin + notes[n_notes + lane_id()]);
+            float x[N];
+            Elem<T>::values(*reinterpret_cast<const uint4*>(p), x);
+            uint32_t which = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) which |= x[e] >= least ? 1u << e : 0u;
+            int at = have + take_room(&found, __popc(which));
+            const int32_t id = static_cast<int32_t>(p - row.p);
+#pragma unroll 1
+            for (; which != 0u && at < kTopKeys; which &= which - 1u, ++at) {
+                const int e = __ffs(static_cast<int>(which)) - 1;
+                keys[at] = make_key(Elem<T>::get(p + e) + 0.0f, id + e);       // (-0 and 0 are equal)
+            }
+        }
+    };
+    float least = kNone;
     for (int n = 0; n < a.blocks; ++n) {                     // (a.blocks: of a whole segment; the row may end before)
         const int64_t first = begin + static_cast<int64_t>(n) * (kRowThreads * C), stop = first + kRowThreads * C < end ? first + kRowThreads * C : end;
         float most = kNone, piece[C];
@@ -242,54 +269,40 @@ void logprobs_kernel(const LogprobArgs a) {
             }
             __syncthreads();
         }
-        // (three counters in turn: one is cleared that everyone has read, while another one is counted up)
-        int* counter = &found[n % 3];
-        if (threadIdx.x == 0) found[(n + 1) % 3] = 0;
-        const uint32_t threshold = reach;
-        const float least = ordered_to_float(threshold);
-        // pieces with such labels are few: they are read again, so that the elements need not be kept.  Room is taken by a lane for all
-        // of a piece's at once, by the instruction itself (the compiler would add the lanes' numbers up first).
-        uint32_t marked = 0;
+        if (n == 0) least = ordered_to_float(reach);
 #pragma unroll
-        for (int i = 0; i < C; ++i) marked |= (piece[i] >= least ? 1u : 0u) << i;
-#pragma unroll 1
-        while (marked != 0u) {
-            const int i = __ffs(static_cast<int>(marked)) - 1;
-            marked &= marked - 1u;
-            const T* p = row.p + row.first(first + i * kRowThreads + threadIdx.x);
-            uint4 v = *reinterpret_cast<const uint4*>(p);
-            float x[N];
-            Elem<T>::values(v, x);
-            uint32_t which = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) which |= x[e] >= least ? 1u << e : 0u;
-            int at = have + take_room(counter, __popc(which));
-            const int32_t id = static_cast<int32_t>(p - row.p);
-#pragma unroll 1
-            for (; which != 0u && at < kTopKeys; which &= which - 1u, ++at) {
-                const int e = __ffs(static_cast<int>(which)) - 1;
-                keys[at] = make_key(Elem<T>::get(p + e) + 0.0f, id + e);       // (-0 and 0 are equal)
-            }
+        for (int i = 0; i < C; ++i) {
+            const bool here = piece[i] >= least;
+            const uint64_t all = __ballot(here);
+            if (all == 0ull) continue;                       // uniform
+            if (here) notes[n_notes + __popcll(all & lanemask_lt())] = static_cast<int>(first - begin) + i * kRowThreads + static_cast<int>(threadIdx.x);
+            n_notes += __popcll(all);
         }
+        const bool last = n + 1 == a.blocks, ends = last || (n & (n + 1)) == 0;          // uniform
+        while (n_notes >= kWave || (ends && n_notes > 0)) look(least);
         if (n == 0 && more >= least) {
-            const int at = have + take_room(counter, 1);
+            const int at = have + take_room(&found, 1);
             if (at < kTopKeys) keys[at] = make_key(more + 0.0f, static_cast<int32_t>(edge));
         }
+        if (!ends) continue;
         __syncthreads();
-        const int now = *counter;
+        const int now = found;
         if (__builtin_expect(have + now > kTopKeys, 0)) {    // uniform, as all of these
             if (threadIdx.x == 0) kept = 0;
             __syncthreads();
-            best_of_block<T>(row, first, stop, n == 0 ? edge : -1, a.k, threshold, counts, keys + have, &kept);
+            best_of_block<T>(row, since, stop, n == 0 ? edge : -1, a.k, reach, counts, keys + have, &kept);
             __syncthreads();
             have += kept;
-            __syncthreads();
         } else {
             have += now;
         }
-        const bool last = n + 1 == a.blocks;
-        if (have > (last ? a.k + a.k / 2 + 8 : room)) thin();
-        if (last || have > room) cut();
+        if (have > a.k + a.k / 2 + 8) thin();
+        if (last || have > kTopKeys / 2) cut();
+        __syncthreads();                                     // (everyone has read `found`)
+        if (threadIdx.x == 0) found = 0;
+        __syncthreads();
+        least = ordered_to_float(reach);
+        since = stop;
     }
     run.add_one(more, a.c);
     __syncthreads();
@@ -312,7 +325,6 @@ void logprobs_kernel(const LogprobArgs a) {
 // that is left out, and the few others are ranked.
 constexpr int kJoinWaves = 4, kJoinAtOnce = 128;
 constexpr int kJoinFirst = 2 * XC_MAX_TOP + kJoinAtOnce;     // labels of the first ranking at most
-constexpr int kJoinKeys = kJoinAtOnce * XC_MAX_TOP < 2048 ? kJoinAtOnce * XC_MAX_TOP : 2048;
 template <typename T>
 __global__ __launch_bounds__(kJoinWaves * kWave)
 void logprobs_join_kernel(const LogprobArgs a) {
@@ -466,7 +478,7 @@ void logprobs_grad_kernel(const LogprobGradArgs a) {
 // host
 // ---------------------------------------------------------------------------
 static size_t logprobs_bytes(int64_t B, int64_t V, int k, xc_dtype t) {
-    const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2);
+    const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2, k);
     if (cut.segments == 1) return 16;
     return static_cast<size_t>(B) * cut.segments * (sizeof(float4) + static_cast<size_t>(k) * sizeof(uint64_t));
 }
@@ -543,7 +555,7 @@ extern "C" int xc_label_logprobs(const void* X, int64_t ld, int64_t B, int64_t V
     if (overlap({Span(logp, per * n), Span(entropy, per), Span(norm, per * 2), Span(top, per * k), Span(top_logp, per * k), Span(ws, need)},
                 {Span(X, rows_span(B, V, ld, t)), Span(labels, per * n)}))
         return XC_EINVAL;
-    const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2);
+    const RowCut cut = cut_rows(B, V, t == XC_F32 ? 4 : 2, k);
     float4* parts = static_cast<float4*>(ws);
     const LogprobArgs a{X, labels, logp, entropy, norm, top, top_logp, parts, reinterpret_cast<uint64_t*>(parts + B * cut.segments), B, V, ld, cut.segments,
                         cut.length, temperature, softmax_scale(temperature), n, k, cut.blocks};

@@ -99,6 +99,12 @@ struct Block {
     static constexpr int N = PiecedRow<T>::N, E = C * N;
     uint4 v[C];
     template <bool STREAM> __device__ __forceinline__ void load(const PiecedRow<T>& row, int64_t first, int64_t end, int threads) {
+        if (first + C * threads <= end) {                    // uniform: nothing to form for each piece but an offset
+            const uint4* p = reinterpret_cast<const uint4*>(row.p + row.first(first));
+#pragma unroll
+            for (int i = 0; i < C; ++i) v[i] = load16<STREAM>(p + (static_cast<uint32_t>(threadIdx.x) + i * threads));
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const int64_t at = first + i * threads + threadIdx.x;
@@ -233,14 +239,19 @@ constexpr int kRowWaves = 4, kRowThreads = kRowWaves * kWave;
 constexpr int small_block(size_t element) { return element == 4 ? 2 : 1; }        // pieces to a thread: 8 elements,
 constexpr int large_block(size_t) { return 4; }                                  // 16 (fp32), 32
 struct RowCut { int each, blocks; int64_t segments, length /* pieces of a segment */; };
-inline RowCut cut_rows(int64_t B, int64_t V, size_t element) {
+// Segments: as many as give every compute unit several workgroups, of 4096 elements at least (8 x 131072 fp32 with 20 top labels 13.8 us,
+// of 2048 15.1), and no more than the kernel that joins their top labels takes at a time (1 x 262144 bf16, 128 labels: 16 segments 30 us,
+// 128 of them 102).
+constexpr int kJoinKeys = 2048;
+inline RowCut cut_rows(int64_t B, int64_t V, size_t element, int k = 0) {
     const int64_t pieces = V / static_cast<int64_t>(16 / element);
     const int small = small_block(element), large = large_block(element);
     RowCut r{};
     const int64_t wanted = 1024;                                           // workgroups
     int64_t segments = B >= wanted / 2 ? 1 : wanted / B;
-    const int64_t most = (pieces + kRowThreads * small - 1) / (kRowThreads * small);
+    const int64_t most = (pieces + 2 * kRowThreads * small - 1) / (2 * kRowThreads * small);
     if (segments > most) segments = most;
+    if (k > 0 && segments > kJoinKeys / k) segments = kJoinKeys / k;
     if (pieces <= kRowThreads * large || segments < 1) segments = 1;
     r.length = pieces > 0 ? (pieces + segments - 1) / segments : 1;
     r.segments = pieces > 0 ? (pieces + r.length - 1) / r.length : 1;
