@@ -58,77 +58,114 @@ struct List {
     int32_t labels[XC_MAX_TEACHER];      // (read 16 bytes at a time)
     Place places[XC_MAX_TEACHER];
 };
-__device__ __forceinline__ bool listed_before(const int32_t* list, int k, int32_t id) {
-    bool before = false;
-#pragma unroll 2
-    for (int j = 0; j < k; j += 4) {
+// Whether the label of place k is in the list before it, or behind it (16 bytes aligned, -1 behind the last place up to a multiple of 4).
+struct Elsewhere { bool before, behind; };
+__device__ __forceinline__ Elsewhere listed_elsewhere(const int32_t* list, int K, int k, int32_t id) {
+    Elsewhere r{false, false};
+#pragma unroll 4
+    for (int j = 0; j < K; j += 4) {
         const int4 l = *reinterpret_cast<const int4*>(list + j);
-        before |= (l.x == id) | (l.y == id && j + 1 < k) | (l.z == id && j + 2 < k) | (l.w == id && j + 3 < k);
+        const int n = (l.x == id ? 1 : 0) | (l.y == id ? 2 : 0) | (l.z == id ? 4 : 0) | (l.w == id ? 8 : 0);
+        const int below = k - j >= 4 ? 15 : k > j ? (1 << (k - j)) - 1 : 0, at = k >= j && k - j < 4 ? 1 << (k - j) : 0;
+        r.before |= (n & below) != 0;
+        r.behind |= (n & ~(below | at)) != 0;
     }
-    return before;
+    return r;
 }
 
 // What does not depend on the row's sums, by one wave (a lane has every 64th place), while the row is on its way: the teacher's
-// probabilities, in 64 bits as all that is formed from the sums, which costs nothing beside the row.  labels are in the list.
+// probabilities, in 64 bits as all that is formed from the sums.  labels are in the list.
+// These two functions are a chain of dependent steps, not work: logarithms that are needed together are taken by neighbouring lanes at
+// once, quotients of sums stand where differences of their logarithms would (200 x 131072 fp32: 11.8 us with a logarithm, an exponential
+// after the other and a loop over the list for each place).
 struct Teacher {
-    double sum, entropy;                 // sum of q before it is normalised; sum of q log q behind that
+    double sum, weighted;                // of the list: sum of q = exp(t - t0), of q (t - t0)
     float t0, x_max;
     bool any;
 };
 template <typename T>
 __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t b, List& list) {
+    constexpr int kGroups = XC_MAX_TEACHER / kWave;
     const T* x = static_cast<const T*>(a.X) + b * a.ld;
+    const int groups = (a.K + kWave - 1) / kWave;
     Teacher r;
+    int32_t ids[kGroups];
     float t_max = kNone;
     r.x_max = kNone;
     bool some = false;
-#pragma unroll 1
-    for (int k = lane_id(); k < a.K; k += kWave) {
-        const int32_t id = list.labels[k];
-        Place p{0.0, 0.0f, 0.0f, 0.0f, false};
-        if (is_label(id, a.V)) {
-            p.t = a.teacher[b * a.K + k];
-            p.x = Elem<T>::get(x + id);
-            p.once = !listed_before(list.labels, k, id);
-            t_max = fmaxf(t_max, p.t);
-            r.x_max = fmaxf(r.x_max, p.x);
-            some |= a.tail || p.t != kNone;                  // (without a tail a list of probabilities 0 is no distribution)
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+        ids[g] = -1;
+        if (g >= groups) continue;                           // uniform
+        const int k = g * kWave + lane_id();
+        if (k < a.K) {
+            ids[g] = list.labels[k];
+            Place p{0.0, 0.0f, 0.0f, 0.0f, false};
+            if (is_label(ids[g], a.V)) {
+                p.t = a.teacher[b * a.K + k];
+                p.x = Elem<T>::get(x + ids[g]);
+                t_max = fmaxf(t_max, p.t);
+                r.x_max = fmaxf(r.x_max, p.x);
+                some |= a.tail || p.t != kNone;              // (without a tail a list of probabilities 0 is no distribution)
+            }
+            list.places[k] = p;
         }
-        list.places[k] = p;
+    }
+    // places whose label occurs before them
+    uint64_t again[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) again[g] = 0ull;
+#pragma unroll
+    for (int h = 0; h < kGroups; ++h) {
+        if (h >= groups) continue;
+        const int n = a.K - h * kWave < kWave ? a.K - h * kWave : kWave;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const int32_t id = __builtin_amdgcn_readlane(ids[h], j);
+            again[h] |= __ballot(ids[h] == id) & (~1ull << j);
+#pragma unroll
+            for (int g = h + 1; g < kGroups; ++g) if (g < groups) again[g] |= __ballot(ids[g] == id);
+        }
     }
     r.any = __ballot(some) != 0ull;
     t_max = wave_max(t_max);
     r.x_max = wave_max(r.x_max);
     r.t0 = a.tail || t_max == kNone ? 0.0f : t_max;
-    r.sum = 0.0;
+    r.sum = r.weighted = 0.0;
+    bool twice = false;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g)
+        if (g < groups && is_label(ids[g], a.V)) {
+            const bool once = ((again[g] >> lane_id()) & 1ull) == 0ull;
+            list.places[g * kWave + lane_id()].once = once;
+            twice |= !once;
+        }
+    // (one exponential in the code for all places: a kernel that runs once per row waits for its own instructions as well)
 #pragma unroll 1
     for (int k = lane_id(); k < a.K; k += kWave) {
         if (!is_label(list.labels[k], a.V)) continue;
-        const double q = exp(static_cast<double>(list.places[k].t) - static_cast<double>(r.t0));
+        const double d = static_cast<double>(list.places[k].t) - static_cast<double>(r.t0), q = exp(d);
         list.places[k].q = q;
         r.sum += q;
+        if (!(q == 0.0)) r.weighted += q * d;
     }
     r.sum = wave_sum(r.sum);
-    const double scale = a.tail ? 1.0 : 1.0 / r.sum, t_log = a.tail ? 0.0 : log(r.sum);
-    r.entropy = 0.0;
+    r.weighted = wave_sum(r.weighted);
+    const double scale = a.tail ? 1.0 : 1.0 / r.sum;
+    const bool dup = __ballot(twice) != 0ull;
 #pragma unroll 1
     for (int k = lane_id(); k < a.K; k += kWave) {
-        if (!is_label(list.labels[k], a.V)) continue;
-        const double q = list.places[k].q * scale;
-        list.places[k].q = q;
-        if (!(q == 0.0)) r.entropy += q * (static_cast<double>(list.places[k].t) - static_cast<double>(r.t0) - t_log);
-    }
-    r.entropy = wave_sum(r.entropy);
-#pragma unroll 1
-    for (int k = lane_id(); k < a.K; k += kWave) {
-        if (!list.places[k].once) continue;
-        double q = 0.0;
-        const int32_t id = list.labels[k];
-        for (int j = k; j < a.K; ++j) if (list.labels[j] == id) q += list.places[j].q;
-        list.places[k].q_all = static_cast<float>(q);
+        double q = list.places[k].q;
+        if (dup && list.places[k].once) {
+            const int32_t id = list.labels[k];
+            for (int j = k + 1; j < a.K; ++j) if (list.labels[j] == id) q += list.places[j].q;
+        }
+        list.places[k].q_all = static_cast<float>(q * scale);
     }
     return r;
 }
+// 2^n of the size of x (or 1), by which factors are kept from being rounded in an exponent.
+__device__ __forceinline__ int size_of(double x) { return x > 0.0 && x < static_cast<double>(INFINITY) ? ilogb(x) : 0; }
 
 // Loss and terms of a row from its sums, by the same wave.  A place whose label occurs before it does not count to the student's sum again.
 template <typename T>
@@ -141,54 +178,63 @@ __device__ __forceinline__ RowTerms row_terms(const DistillArgs& a, int64_t b, c
         return r;
     }
     // (the student's scores relative to the largest one: that may be huge)
-    const double invT = 1.0 / static_cast<double>(a.T);
+    const double invT = 1.0 / static_cast<double>(a.T), none = -static_cast<double>(INFINITY);
     const float m_all = fmaxf(s.m, t.x_max);
     const double ref = m_all == kNone ? 0.0 : static_cast<double>(m_all);
-    double listed = 0.0, cross = 0.0;
+    // sums relative to the largest score: of the listed labels, of those that s is about (as one more place, where that score is another)
+    const double below = s.s == 0.0f || s.m == m_all ? 0.0 : (static_cast<double>(s.m) - ref) * invT;
+    double listed = 0.0, cross = 0.0, rest = below != 0.0 ? 0.0 : static_cast<double>(s.s);
+    const int n = a.tail ? a.K + (below != 0.0 ? 1 : 0) : a.K;
 #pragma unroll 1
-    for (int k = lane_id(); k < a.K; k += kWave) {
-        if (!is_label(list.labels[k], a.V)) continue;
-        const Place p = list.places[k];
-        const double y = (static_cast<double>(p.x) - ref) * invT;
-        if (a.tail && p.once) listed += exp(y);
-        if (!(p.q == 0.0)) cross += p.q * y;
+    for (int k = lane_id(); k < n; k += kWave) {
+        const bool place = k < a.K;
+        if (place && !is_label(list.labels[k], a.V)) continue;
+        const double y = place ? (static_cast<double>(list.places[k].x) - ref) * invT : below;
+        const double e = a.tail ? exp(y) : 0.0;
+        if (!place) {
+            rest = static_cast<double>(s.s) * e;
+        } else {
+            if (list.places[k].once) listed += e;
+            const double q = list.places[k].q;
+            if (!(q == 0.0)) cross += q * y;
+        }
     }
     cross = wave_sum(cross);
-    const double sum_log = log(static_cast<double>(s.s));
-    const double rest_log = s.s == 0.0f ? sum_log : sum_log + (static_cast<double>(s.m) - ref) * invT;        // of the labels that s is about
-    double lse = rest_log;
-    if (a.tail) {
-        listed = wave_sum(listed);
-        if (s.s != 0.0f) listed += exp(rest_log);
-        lse = log(listed);
-    }
+    if (below != 0.0) rest = __shfl(rest, a.K & (kWave - 1), kWave);       // uniform (without a tail the largest score is s's)
+    double all = rest;
+    if (a.tail) all += wave_sum(listed);
+    const double p_r = a.tail ? (s.s == 0.0f ? 0.0 : rest / all) : 1.0;
     double q_r = 0.0;
     if (a.tail && s.s != 0.0f) {                             // (no label but the listed ones: nothing to compare)
         q_r = 1.0 - t.sum;
         if (q_r < 0.0) q_r = 0.0;
     }
-    const double q_sum = a.tail ? t.sum : t.sum == t.sum ? 1.0 : t.sum, mass = q_sum + q_r;
+    // log of the sum over all, of q_r / p_r, of the teacher's sum
+    const double logs = log(lane_id() == 0 ? all : lane_id() == 1 ? q_r / p_r : t.sum);
+    const double lse = __shfl(logs, 0, kWave), t_log = a.tail ? 0.0 : __shfl(logs, 2, kWave);
+    double ratio = __shfl(logs, 1, kWave);
+    if (p_r == 0.0 && q_r != 0.0) ratio = log(q_r) - (log(static_cast<double>(s.s)) + below - lse);          // (beyond what 64 bits hold)
+    const double scale = a.tail ? 1.0 : 1.0 / t.sum, q_sum = a.tail ? t.sum : t.sum == t.sum ? 1.0 : t.sum, mass = q_sum + q_r;
     double loss = 0.0;
-    if (lse == -INFINITY) loss = q_sum == 0.0 ? 0.0 : q_sum == q_sum ? INFINITY : q_sum;       // no label at all
-    else if (!(q_sum == 0.0)) loss = t.entropy - cross + q_sum * lse;
-    if (!(q_r == 0.0)) loss += q_r * (log(q_r) - (rest_log - lse));
+    if (lse == none) loss = q_sum == 0.0 ? 0.0 : q_sum == q_sum ? -none : q_sum;               // no label at all
+    else if (!(q_sum == 0.0)) loss = (t.weighted - cross) * scale + q_sum * (lse - t_log);
+    if (!(q_r == 0.0)) loss += q_r * ratio;
     const double T2 = static_cast<double>(a.T) * static_cast<double>(a.T);
     if (lane_id() == 0 && a.loss != nullptr) a.loss[b] = static_cast<float>(static_cast<double>(weight) * T2 * loss);
-    const double log2e = 1.4426950408889634;
     r.m = s.m == kNone ? 0.0f : s.m;
-    const double l = s.s == 0.0f ? 0.0 : sum_log * log2e, l_all = lse * log2e;
-    r.l = static_cast<float>(rint(l));
+    const int l = size_of(static_cast<double>(s.s)), l_all = size_of(all);
+    r.l = static_cast<float>(l);
     r.m_all = m_all == kNone ? 0.0f : m_all;
-    r.l_all = static_cast<float>(rint(l_all));
-    r.mass = static_cast<float>(l_all == -INFINITY ? mass : mass * exp2(rint(l_all) - l_all));
+    r.l_all = lse == none ? kNone : static_cast<float>(l_all);
+    r.mass = static_cast<float>(lse == none ? mass : mass * (ldexp(1.0, l_all) / all));
     r.t = t.t0;
-    r.t_log = a.tail ? 0.0f : static_cast<float>(log(t.sum));
+    r.t_log = a.tail ? 0.0f : static_cast<float>(t_log);
     const double factor = static_cast<double>(weight) * static_cast<double>(a.T);
-    r.other = static_cast<float>(exp2(rint(l) - l) * factor * (a.tail ? (s.s == 0.0f ? 0.0 : mass * exp(rest_log - lse)) - q_r : mass));
+    r.other = s.s == 0.0f ? 0.0f : static_cast<float>(factor * (mass * p_r - q_r) * (ldexp(1.0, l) / static_cast<double>(s.s)));
     return r;
 }
 
-__device__ __forceinline__ float q_of(const DistillArgs& a, const RowTerms& r, float t) {
+__device__ __forceinline__ float q_of(const RowTerms& r, float t) {
     return __builtin_amdgcn_exp2f(((t - r.t) - r.t_log) * 1.4426950408889634f);
 }
 __device__ __forceinline__ float other_gradient(const RowTerms& r, float x, float c) {
@@ -268,10 +314,13 @@ void distill_sums_kernel(const DistillArgs a) {
 }
 
 // A row's segments joined, by a wave.
-__device__ __forceinline__ Sums joined_segments(const DistillArgs& a, int64_t b) {
+__device__ __forceinline__ float4 first_part(const DistillArgs& a, int64_t b) {       // asked for before the teacher's part, which does not need it
+    return lane_id() < a.segments ? a.parts[b * a.segments + lane_id()] : make_float4(kNone, 0.0f, 0.0f, 0.0f);
+}
+__device__ __forceinline__ Sums joined_segments(const DistillArgs& a, int64_t b, const float4& first) {
     Sums t{kNone, 0.0f, 0.0f};
     for (int64_t i = lane_id(); i < a.segments; i += kWave) {
-        const float4 p = a.parts[b * a.segments + i];
+        const float4 p = i < kWave ? first : a.parts[b * a.segments + i];
         const Sums q{p.x, p.y, 0.0f};
         const float m = fmaxf(t.m, q.m);
         const Sums u = joined(t, m, a.c), w = joined(q, m, a.c);
@@ -296,7 +345,9 @@ void distill_terms_kernel(const DistillArgs a) {
     if (weight == 0.0f) {                                    // counts for nothing, whatever it holds
         if (lane_id() == 0) a.loss[b] = 0.0f;
     } else {
-        r = row_terms<T>(a, b, joined_segments(a, b), weight, teacher_of<T>(a, b, list), list);
+        const float4 part = first_part(a, b);
+        const Teacher teacher = teacher_of<T>(a, b, list);
+        r = row_terms<T>(a, b, joined_segments(a, b, part), weight, teacher, list);
     }
     if (lane_id() == 0) a.terms[b] = r;
 }
@@ -331,8 +382,13 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
             RowTerms r{};
             DistillArgs mine = a;
             if (chunk != 0) mine.loss = nullptr;
-            if (weight != 0.0f) r = row_terms<T>(mine, b, joined_segments(a, b), weight, teacher_of<T>(a, b, list), list);
-            else if (threadIdx.x == 0 && chunk == 0) a.loss[b] = 0.0f;
+            if (weight != 0.0f) {
+                const float4 part = first_part(a, b);
+                const Teacher teacher = teacher_of<T>(a, b, list);
+                r = row_terms<T>(mine, b, joined_segments(a, b, part), weight, teacher, list);
+            } else if (threadIdx.x == 0 && chunk == 0) {
+                a.loss[b] = 0.0f;
+            }
             if (threadIdx.x == 0) terms = r;
         }
         __syncthreads();
@@ -343,11 +399,18 @@ void distill_grad_kernel(const DistillArgs a, int64_t chunks) {
     float value = 0.0f;
     if (live && is_label(id, a.V)) {
         const int64_t piece = id < row.head ? -1 : (id - row.head) / N;
-        if ((id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) && !listed_before(list.labels, threadIdx.x, id)) {
-            listed = id;
-            float q = 0.0f;                                  // (all places of the label count)
-            for (int j = threadIdx.x; j < a.K; ++j) if (list.labels[j] == id) q += q_of(a, r, a.teacher[b * a.K + j]);
-            value = listed_gradient(a, r, Elem<T>::get(row.p + id), q);
+        if (id < row.head || piece >= row.pieces ? chunk == 0 : piece >= first && piece < end) {
+            float q = 0.0f;                                  // (all places of the label count, at the first of them)
+            if constexpr (INLINE) {
+                if (list.places[threadIdx.x].once) listed = id;
+                q = list.places[threadIdx.x].q_all;
+            } else {
+                const Elsewhere e = listed_elsewhere(list.labels, a.K, threadIdx.x, id);
+                if (!e.before) listed = id;
+                q = q_of(r, a.teacher[b * a.K + threadIdx.x]);
+                if (e.behind) for (int j = threadIdx.x + 1; j < a.K; ++j) if (list.labels[j] == id) q += q_of(r, a.teacher[b * a.K + j]);
+            }
+            if (listed >= 0) value = listed_gradient(a, r, Elem<T>::get(row.p + id), q);
         }
     }
     __syncthreads();
