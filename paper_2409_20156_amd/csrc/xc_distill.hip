@@ -479,6 +479,7 @@ void distill_row_kernel(const DistillArgs a) {
         constexpr int G = 8 / N > 1 ? 8 / N : C % 2 == 0 ? 2 : 1, E = G * N;
 #pragma unroll
         for (int i0 = 0; i0 < C; i0 += G) {
+            if (i0 * kThreads >= pieces) break;              // uniform: the row ends before
             float f[E];
 #pragma unroll
             for (int i = 0; i < G; ++i) {

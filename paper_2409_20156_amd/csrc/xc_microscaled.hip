@@ -264,16 +264,31 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
     };
     for (int i = 0; i < R && i < total; ++i) issue();
 
-    // the queries
+    // the queries; rows past the last one are zeros
     if constexpr (!std::is_void<TZ>::value) {
-        for (int i = threadIdx.x >> 4; i < kRows * a.units; i += W * 4) {
-            const int row = i / a.units, u = i - row * a.units, sub = threadIdx.x & 15;
-            float f[8];
-            const bool there = q0 + row < a.B;
-            eight<TZ>(a.Z + (there ? q0 + row : 0) * a.d * static_cast<int64_t>(sizeof(TZ) == 4 ? 4 : 2), there ? u * kMxRow + sub * 8 : a.d, a.d, f);
-            const MicroLane m = to_micro(f);
-            *reinterpret_cast<uint32_t*>(codes + (u >> 1) * (kRows * 128) + row * 128 + ((((u & 1) * 4 + (sub >> 2)) ^ mx_swizzle(row)) * 16) + (sub & 3) * 4) = m.codes;
-            if ((sub & 3) == 0) scales[row * (4 * kUpad) + (sub >> 2) * kUpad + u] = static_cast<unsigned char>(m.byte);
+        const int rows = a.B - q0 < kRows ? static_cast<int>(a.B - q0) : kRows, all = rows * a.units;
+        if (rows < kRows) {
+            for (int i = threadIdx.x; i < kRows * KU * 4; i += W * kWave)
+                if ((i >> 3) % kRows >= rows) *reinterpret_cast<uint4*>(codes + i * 16) = make_uint4(0, 0, 0, 0);
+            for (int i = rows * kUpad + static_cast<int>(threadIdx.x); i < kRows * kUpad; i += W * kWave) *reinterpret_cast<uint32_t*>(scales + i * 4) = 0;
+        }
+        constexpr int U = 4;                                 // of 128 elements, under way together
+        const int sub = threadIdx.x & 15;
+        for (int i0 = threadIdx.x >> 4; i0 < all; i0 += W * 4 * U) {
+            float f[U][8];
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + k * W * 4, row = i / a.units, u = i - row * a.units;
+                if (i < all) eight<TZ>(a.Z + (q0 + row) * a.d * static_cast<int64_t>(sizeof(TZ) == 4 ? 4 : 2), u * kMxRow + sub * 8, a.d, f[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                const int i = i0 + k * W * 4, row = i / a.units, u = i - row * a.units;
+                if (i >= all) break;
+                const MicroLane m = to_micro(f[k]);
+                *reinterpret_cast<uint32_t*>(codes + (u >> 1) * (kRows * 128) + row * 128 + ((((u & 1) * 4 + (sub >> 2)) ^ mx_swizzle(row)) * 16) + (sub & 3) * 4) = m.codes;
+                if ((sub & 3) == 0) scales[row * (4 * kUpad) + (sub >> 2) * kUpad + u] = static_cast<unsigned char>(m.byte);
+            }
         }
     } else {
         const int chunks = a.ppitch / 16;
@@ -543,44 +558,57 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
     }
 }
 
-// ---- longer rows: tiles of 64 WQ queries x 64 WL labels, two units of both to a stage, three stages in LDS, a wave with 64 x 64.  Rows of
-// labels lie in the order of the products' blocks (block y, column j: label 4 j + y of 64), so that a lane stores neighbouring scores.
-// Consecutive workgroups of an XCD take the query tiles of one label tile.
-template <int WQ, int WL>
+// ---- longer rows: tiles of 16 MQ WQ queries x 64 WL labels, two units of both to a stage, two stages in LDS, a wave with 16 MQ x 64.  A
+// workgroup takes one tile after the other, the first stage of the next one under way while the last is multiplied and the scores are
+// stored.  Rows of labels lie in the order of the products' blocks (block y, column j: label 4 j + y of 64), so that a lane stores
+// neighbouring scores.  Consecutive workgroups of an XCD take the query tiles of one label tile.
+// Bound: what brings the operands out of LDS (96 bytes a cycle of 128 with 128 x 64 to a wave), and the stores.
+template <int WQ, int WL, int MQ>
 struct MicroTile {
-    static constexpr int kWaves = WQ * WL, BM = 64 * WQ, BN = 64 * WL, kRows = BM + BN, R = 3;
+    static constexpr int kWaves = WQ * WL, BM = 16 * MQ * WQ, BN = 64 * WL, kRows = BM + BN, R = 2;
     static constexpr int kStage = kRows * (128 + 8), kParts = kRows / 64 * 2 /* of 64 scale words */, kScaleLoads = (kParts + kWaves - 1) / kWaves;
-    static constexpr int kRowLoads = kRows / 8 / kWaves, kLoads = kRowLoads + kScaleLoads;
-    static_assert(kRowLoads * 8 * kWaves == kRows && R * kStage <= 160 * 1024, "whole loads");
+    static constexpr int kRowLoads = kRows / 8 / kWaves, kStores = 4 * MQ, kPerCu = 160 * 1024 / (R * kStage + 512);
+    static_assert(kRowLoads * 8 * kWaves == kRows && BM % 64 == 0 && kPerCu >= 1 && kStores < 64, "whole loads, a count that the wait can hold");
 };
-template <typename TO, int WQ, int WL>
+template <typename TO, int WQ, int WL, int MQ>
 __global__ __launch_bounds__(WQ * WL * kWave)
 void scores_micro_tile_kernel(const MicroArgs a, uint32_t tiles_m, uint32_t tiles_n) {
-    typedef MicroTile<WQ, WL> T;
+    typedef MicroTile<WQ, WL, MQ> T;
     __shared__ __align__(1024) unsigned char smem[T::R * T::kStage];
     const int lane = lane_id(), r = lane & 15, quarter = lane >> 4, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wq = wave / WL, wl = wave % WL;
     const uint32_t lds = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) unsigned char*)smem));
-    const uint32_t n_tiles = tiles_m * tiles_n, per = (n_tiles + kXcds - 1) / kXcds, t = blockIdx.x % kXcds * per + blockIdx.x / kXcds;
-    if (blockIdx.x / kXcds >= per || t >= n_tiles) return;   // uniform
-    const int64_t q0 = static_cast<int64_t>(t % tiles_m) * T::BM, l0 = static_cast<int64_t>(t / tiles_m) * T::BN;
+    const uint32_t n_tiles = tiles_m * tiles_n, per = (n_tiles + kXcds - 1) / kXcds;
+    const uint32_t t_begin = blockIdx.x % kXcds * per, t_end = t_begin + per < n_tiles ? t_begin + per : n_tiles, t_step = gridDim.x / kXcds;
+    uint32_t t = t_begin + blockIdx.x / kXcds;
+    if (t >= t_end) return;                                  // uniform
     const uint32_t row_bytes = a.units * 64, row_scales = a.units * 4;
-    const uint32_t last_q = static_cast<uint32_t>(a.B - 1 - q0 < T::BM ? a.B - 1 - q0 : T::BM - 1), last_l = static_cast<uint32_t>(a.L - 1 - l0 < T::BN ? a.L - 1 - l0 : T::BN - 1);
-    // row of the tile's queries or labels in place p of the stage, rows past the end: the last one again
-    auto row_of = [&](uint32_t p) __attribute__((always_inline)) {
-        if (p < T::BM) return p < last_q ? p : last_q;
-        const uint32_t q = p - T::BM, l = (q & ~63u) + (q & 15) * 4 + ((q >> 4) & 3);
-        return l < last_l ? l : last_l;
-    };
-    uint32_t at[T::kRowLoads], scale_at[T::kScaleLoads];
-#pragma unroll
-    for (int i = 0; i < T::kRowLoads; ++i) at[i] = row_of((wave * T::kRowLoads + i) * 8 + (lane >> 3)) * row_bytes;
-#pragma unroll
-    for (int i = 0; i < T::kScaleLoads; ++i) scale_at[i] = row_of((wave + i * T::kWaves) % T::kParts / 2 * 64 + lane) * row_scales;
-    const uint8_t *rows_q = a.P + q0 * row_bytes, *rows_l = a.Q + l0 * row_bytes, *scale_q = a.pscale + q0 * row_scales, *scale_l = a.scale + l0 * row_scales;
     const int steps = (a.units + 1) / 2;
+
+    uint32_t at[T::kRowLoads], scale_at[T::kScaleLoads], ahead_t = t;
+    const uint8_t *rows_q = nullptr, *rows_l = nullptr, *scale_q = nullptr, *scale_l = nullptr;
     int ahead = 0, ahead_slot = 0;
     auto issue = [&]() __attribute__((always_inline)) {
+        if (ahead_t >= t_end) return;                        // uniform
+        if (ahead == 0) {                                    // another tile
+            const int64_t q0 = static_cast<int64_t>(ahead_t % tiles_m) * T::BM, l0 = static_cast<int64_t>(ahead_t / tiles_m) * T::BN;
+            const uint32_t last_q = static_cast<uint32_t>(a.B - 1 - q0 < T::BM ? a.B - 1 - q0 : T::BM - 1);
+            const uint32_t last_l = static_cast<uint32_t>(a.L - 1 - l0 < T::BN ? a.L - 1 - l0 : T::BN - 1);
+            // row of the tile's queries or labels in place p of the stage, rows past the end: the last one again
+            auto row_of = [&](uint32_t p) __attribute__((always_inline)) {
+                if (p < T::BM) return p < last_q ? p : last_q;
+                const uint32_t q = p - T::BM, l = (q & ~63u) + (q & 15) * 4 + ((q >> 4) & 3);
+                return l < last_l ? l : last_l;
+            };
+#pragma unroll
+            for (int i = 0; i < T::kRowLoads; ++i) at[i] = row_of((wave * T::kRowLoads + i) * 8 + (lane >> 3)) * row_bytes;
+#pragma unroll
+            for (int i = 0; i < T::kScaleLoads; ++i) scale_at[i] = row_of((wave + i * T::kWaves) % T::kParts / 2 * 64 + lane) * row_scales;
+            rows_q = a.P + q0 * row_bytes;
+            rows_l = a.Q + l0 * row_bytes;
+            scale_q = a.pscale + q0 * row_scales;
+            scale_l = a.scale + l0 * row_scales;
+        }
         const uint32_t to = __builtin_amdgcn_readfirstlane(lds + ahead_slot * T::kStage), mask = ahead * 2 + 1 < a.units ? 127u : 63u;       // (a single unit: it again)
 #pragma unroll
         for (int i = 0; i < T::kRowLoads; ++i) {
@@ -595,54 +623,71 @@ void scores_micro_tile_kernel(const MicroArgs a, uint32_t tiles_m, uint32_t tile
             lds_dma4_sbase(mx_uniform((n / 2 * 64 < T::BM ? scale_q : scale_l) + ahead * 8), scale_at[i] + second,
                            __builtin_amdgcn_readfirstlane(to + T::kRows * 128 + n * 256));
         }
-        ++ahead;
-        if (++ahead_slot == T::R) ahead_slot = 0;
+        if (++ahead == steps) {
+            ahead = 0;
+            ahead_t += t_step;
+        }
+        ahead_slot ^= 1;
     };
     issue();
-    if (steps > 1) issue();
-    mx_f32x4 acc[4][4];
+    mx_f32x4 acc[MQ][4];
+    auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+        for (int x = 0; x < MQ; ++x)
 #pragma unroll
-        for (int y = 0; y < 4; ++y) acc[x][y] = mx_f32x4{0, 0, 0, 0};
+            for (int y = 0; y < 4; ++y) acc[x][y] = mx_f32x4{0, 0, 0, 0};
+    };
+    clear();
     const int frag = r * 128 + ((quarter ^ mx_swizzle(r)) * 16);
-    int slot = 0;
-    for (int step = 0; step < steps; ++step) {
-        if (step + 1 < steps) few_wait<T::kLoads>();
+    int slot = 0, step = 0;
+    bool stored = false;                                     // a whole tile's scores, behind the loads that are waited for
+    while (t < t_end) {
+        if (stored) few_wait<T::kStores>();
         else few_wait<0>();
+        stored = false;
         lds_barrier();                                       // the stage is there for everyone, the one before it has been read by everyone
-        if (step + 2 < steps) issue();
+        issue();
         const unsigned char* stage = smem + slot * T::kStage;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             if (step * 2 + h >= a.units) break;              // uniform
-            mx_i32x4 w[4], z[4];
-            int ws[4], zs[4];
+            mx_i32x4 w[4];
+            int ws[4];
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
                 w[y] = *reinterpret_cast<const mx_i32x4*>(stage + (T::BM + wl * 64 + y * 16) * 128 + (frag ^ (h * 64)));
-                ws[y] = stage[T::kRows * 128 + ((WQ + wl) * 2 + h) * 256 + (y * 16 + r) * 4 + quarter];
-                z[y] = *reinterpret_cast<const mx_i32x4*>(stage + (wq * 64 + y * 16) * 128 + (frag ^ (h * 64)));
-                zs[y] = stage[T::kRows * 128 + (wq * 2 + h) * 256 + (y * 16 + r) * 4 + quarter];
+                ws[y] = stage[T::kRows * 128 + ((T::BM / 64 + wl) * 2 + h) * 256 + (y * 16 + r) * 4 + quarter];
             }
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
+            for (int x = 0; x < MQ; ++x) {
+                const int row = (wq * MQ + x) * 16;
+                const mx_i32x4 z = *reinterpret_cast<const mx_i32x4*>(stage + row * 128 + (frag ^ (h * 64)));
+                const int zs = stage[T::kRows * 128 + (row / 64 * 2 + h) * 256 + (row % 64 + r) * 4 + quarter];
 #pragma unroll
-                for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(z[x], w[y], acc[x][y], zs[x], ws[y]);
+                for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(z, w[y], acc[x][y], zs, ws[y]);
+            }
         }
-        if (++slot == T::R) slot = 0;
+        slot ^= 1;
+        if (++step == steps) {
+            step = 0;
+            const int64_t q0 = static_cast<int64_t>(t % tiles_m) * T::BM + wq * MQ * 16, lw = static_cast<int64_t>(t / tiles_m) * T::BN + wl * 64;
+            const int64_t l = lw + r * 4, have = a.L - l;
+            const bool whole = lw + 64 <= a.L && q0 + MQ * 16 <= a.B;          // uniform
+            TO* out = static_cast<TO*>(a.out) + (q0 + quarter * 4) * a.L + l;
+#pragma unroll
+            for (int x = 0; x < MQ; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
+                    TO* p = out + static_cast<int64_t>(x * 16 + i) * a.L;
+                    if (whole) put_four(p, v, a.stream);     // uniform
+                    else if (q0 + x * 16 + quarter * 4 + i < a.B) put_labels(p, v, lw + 64 <= a.L, have);
+                }
+            stored = whole;
+            clear();
+            t += t_step;
+        }
     }
-    const int64_t lw = l0 + wl * 64, l = lw + r * 4, have = a.L - l;
-    const bool whole = lw + 64 <= a.L;                       // uniform
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t q = q0 + wq * 64 + x * 16 + quarter * 4 + i;
-            if (q >= a.B) continue;
-            const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
-            put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
-        }
 }
 
 // ---------------------------------------------------------------------------
@@ -679,9 +724,9 @@ static void launch_micro_held(const MicroArgs& a, hipStream_t st) {
                                                                 static_cast<int>((a.B + MicroHeld<NK>::QS - 1) / MicroHeld<NK>::QS));
 }
 
-template <typename TO, int WQ, int WL>
+template <typename TO, int WQ, int WL, int MQ>
 static void launch_micro_tile(const MicroArgs& a, hipStream_t st) {
-    typedef MicroTile<WQ, WL> T;
+    typedef MicroTile<WQ, WL, MQ> T;
     // (launches of queries that leave the tiles countable)
     const int64_t tiles_n = (a.L + T::BN - 1) / T::BN, rows = ((1 << 24) / tiles_n > 1 ? (1 << 24) / tiles_n : 1) * T::BM;
     for (int64_t q0 = 0; q0 < a.B; q0 += rows) {
@@ -691,16 +736,25 @@ static void launch_micro_tile(const MicroArgs& a, hipStream_t st) {
         p.pscale += q0 * a.units * 4;
         p.out = static_cast<TO*>(a.out) + q0 * a.L;
         const uint32_t tiles_m = static_cast<uint32_t>((p.B + T::BM - 1) / T::BM), per = (tiles_m * static_cast<uint32_t>(tiles_n) + kXcds - 1) / kXcds;
-        scores_micro_tile_kernel<TO, WQ, WL><<<kXcds * per, T::kWaves * kWave, 0, st>>>(p, tiles_m, static_cast<uint32_t>(tiles_n));
+        const uint32_t most = kCusPerXcd * T::kPerCu;
+        scores_micro_tile_kernel<TO, WQ, WL, MQ><<<kXcds * (per < most ? per : most), T::kWaves * kWave, 0, st>>>(p, tiles_m, static_cast<uint32_t>(tiles_n));
     }
 }
 
-constexpr int kMicroTileQueries = 128;
+// Tiles of 128 x 128, two workgroups of them to a compute unit, or of 256 x 256: whichever's rounds take less, a round of large ones
+// 5/3 of the others' (d = 2048, small against large: 2000 x 2000 18.3 us against 27.8, 300 x 50021 40.9 against 44.3, 2000 x 6000 29.0
+// against 28.2, 4096 x 4096 35.3 against 29.5; 4096 x 131072 x 4096 1817 against 1346).
+static bool small_tiles(const MicroArgs& a) {
+    auto rounds = [&](int64_t side, int64_t at_once) { return ((a.B + side - 1) / side * ((a.L + side - 1) / side) + at_once - 1) / at_once; };
+    return rounds(MicroTile<2, 4, 8>::BM, kMineGrid * MicroTile<2, 4, 8>::kPerCu) * 5 > rounds(MicroTile<2, 2, 4>::BM, kMineGrid * MicroTile<2, 2, 4>::kPerCu) * 3;
+}
+constexpr int64_t kMicroInline = 128;                    // units of queries: two rounds of a workgroup's loads (16 x 131072 x 4096, 512 of
+                                                         // them: 81 us, in a launch of their own 64; 4 x 2487 x 3280, 104: 14.7 against 18.8 with one round)
 
 template <typename TO>
 static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& space, hipStream_t st) {
     a.Z = static_cast<const unsigned char*>(Z);
-    if (a.B <= 16 && a.units <= kMicroFewLong) {             // every workgroup brings the queries to 4 bits for itself: one launch
+    if (a.B <= 16 && a.units <= kMicroFewLong && a.B * a.units <= kMicroInline) {      // every workgroup brings the queries to 4 bits for itself: one launch
         auto go = [&]() {
             if (a.units <= kMicroFewUnits) {
                 if (t == XC_F32) launch_few<TO, float, 1, kMicroFewUnits, 4, 2>(a, st);
@@ -714,7 +768,7 @@ static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& s
         XC_HIP_CHECK(hipGetLastError());
         return XC_OK;
     }
-    const bool held = a.B > 64 && a.units <= kMicroHeldUnits, few = a.B <= 64 && (a.units <= kMicroFewUnits || (a.B <= 32 && a.units <= kMicroFewLong));
+    const bool held = a.B > 64 && a.units <= kMicroHeldUnits, few = a.units <= kMicroFewUnits ? a.B <= 64 : a.B <= 16 && a.units <= kMicroFewLong;
     uint8_t *P = const_cast<uint8_t*>(a.P), *pscale = const_cast<uint8_t*>(a.pscale);
     const int rc = held || few ? launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroQueries{P, pscale, space.units, space.pitch, space.upad}, space.rows, space.pitch / 64, st)
                                : launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroRows{P, pscale, space.units}, a.B, space.units, st);
@@ -728,13 +782,13 @@ static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& s
                 default: launch_micro_held<TO, 8>(a, st); break;
             }
         } else if (few) {
-            if (a.units > kMicroFewUnits) launch_few<TO, void, 2, kMicroFewLong, 4, 2>(a, st);
+            if (a.units > kMicroFewUnits) launch_few<TO, void, 1, kMicroFewLong, 4, 3>(a, st);
             else if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4, 3>(a, st);
             else launch_few<TO, void, 4, kMicroFewUnits, 4, 3>(a, st);
-        } else if (a.B <= kMicroTileQueries) {
-            launch_micro_tile<TO, 1, 2>(a, st);
+        } else if (small_tiles(a)) {
+            launch_micro_tile<TO, 2, 2, 4>(a, st);
         } else {
-            launch_micro_tile<TO, 4, 2>(a, st);
+            launch_micro_tile<TO, 2, 4, 8>(a, st);
         }
     };
     XC_LAUNCH(K_SCORES_MICRO, st, go());

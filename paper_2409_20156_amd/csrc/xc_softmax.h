@@ -150,24 +150,14 @@ struct Running {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] = __builtin_amdgcn_exp2f(d[e]);
                 sum += ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
-                if constexpr (ENTROPY) {
-                    float w[2] = {x[0] * d[0], x[4] * d[4]};
+                if constexpr (ENTROPY) {                     // (0 times -infinity, of a label that is not there, is no number)
+                    float w[2] = {x[0] * fmaxf(d[0], kFloor), x[4] * fmaxf(d[4], kFloor)};
 #pragma unroll
                     for (int e = 1; e < 4; ++e) {
-                        w[0] = fmaf(x[e], d[e], w[0]);
-                        w[1] = fmaf(x[4 + e], d[4 + e], w[1]);
+                        w[0] = fmaf(x[e], fmaxf(d[e], kFloor), w[0]);
+                        w[1] = fmaf(x[4 + e], fmaxf(d[4 + e], kFloor), w[1]);
                     }
                     weighted += w[0] + w[1];
-                }
-            }
-            if (ENTROPY && __builtin_expect(weighted != weighted, 0)) {    // 0 times -infinity: labels that are not there
-                weighted = 0.0f;
-                float again = k;
-                asm volatile("" : "+v"(again));          // (else the exponents of above are kept for here, in as many registers)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float d = fmaxf(fmaf(f[e], c, -again), kFloor);
-                    weighted = fmaf(__builtin_amdgcn_exp2f(d), d, weighted);
                 }
             }
             s += sum;

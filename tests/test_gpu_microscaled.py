@@ -99,7 +99,7 @@ def _bound(P, p, Q, q, got, out):
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32)])
 @pytest.mark.parametrize("B,L,d", [(1, 1, 8), (1, 17, 64), (2, 1000, 72), (15, 100, 128), (16, 333, 256), (17, 64, 384), (33, 130, 768), (63, 129, 200), (64, 500, 512),
                                    (65, 63, 1000), (128, 257, 768), (130, 515, 896), (200, 700, 1024), (129, 300, 1152), (257, 513, 640), (300, 65, 4096), (5, 100, 5000), (20, 500, 2048),
-                                   (31, 200, 1160), (40, 300, 2048), (100, 129, 1800), (129, 257, 1288), (2, 65, 20000), (260, 1000, 1536)])
+                                   (4, 300, 4096), (5, 300, 4088), (16, 70, 1032), (31, 200, 1160), (40, 300, 2048), (100, 129, 1800), (129, 257, 1288), (2, 65, 20000), (260, 1000, 1536)])
 def test_scores_match_the_oracle(B, L, d, dtype, out):
     import paper_2409_20156_amd as xc
     Z, W = _matrix(B + d, B, d, dtype), _matrix(L + d + 7, L, d, dtype)
@@ -140,6 +140,20 @@ def test_scores_do_not_depend_on_the_batch_or_the_range():
         for lo, hi in ((0, 1), (16, 80), (1, 1400)):
             assert torch.equal(xc.scores_microscaled(Z, Q[lo:hi].clone(), s[lo:hi].clone()), whole[:, lo:hi])
         assert torch.equal(xc.scores_microscaled(Z, Q, s, dtype=BF16), whole.bfloat16())
+
+
+@pytest.mark.parametrize("B,L,d", [(520, 33001, 1096), (2500, 16385, 1160), (2049, 16384, 1400), (90, 70003, 1288)])
+def test_workgroups_that_take_several_tiles(B, L, d):
+    """More tiles of long rows than there are workgroups: every tile's scores are those of the rows by themselves, 16 of them at a time."""
+    import paper_2409_20156_amd as xc
+    Z, W = _matrix(B, B, d, BF16).to(DEV), _matrix(L, L, d, BF16).to(DEV)
+    Q, s = xc.microscale_rows(W)
+    for dtype in (BF16, F32):
+        whole = xc.scores_microscaled(Z, Q, s, dtype=dtype)
+        for lo in range(0, B, 16 if B < 1000 else 208):
+            hi = min(lo + 16, B)
+            assert torch.equal(xc.scores_microscaled(Z[lo:hi].clone(), Q, s, dtype=dtype), whole[lo:hi])
+        assert torch.equal(xc.scores_microscaled(Z[-16:].clone(), Q, s, dtype=dtype), whole[-16:])
 
 
 def test_rows_that_are_no_numbers_give_scores_that_are_none():
