@@ -323,11 +323,11 @@ def _launch(fn, where: str, dev: torch.device, *args) -> None:
 
 
 def _same_device(first: torch.Tensor, *others) -> torch.device:
-    dev = first.device
+    index = first.get_device()                             # (a number: device objects cost a small call more; -1 for the host's memory)
     for t in others:
-        if t is not None and t.device != dev:
-            raise ValueError("all tensors of a call must be on one device, got %s and %s" % (dev, t.device))
-    return dev
+        if t is not None and t.get_device() != index:
+            raise ValueError("all tensors of a call must be on one device, got %s and %s" % (first.device, t.device))
+    return first.device
 
 
 def _at(t: torch.Tensor, dtype, name: str) -> int:
@@ -519,28 +519,30 @@ def label_logprobs(scores: torch.Tensor, labels: torch.Tensor, *, top: int = 0, 
     B, V = scores.shape
     n = labels.shape[1]
     dev = scores.device
-    out = {} if out is None else out
-    shapes = {"logp": (B, n), "entropy": (B,), "norm": (B, 2), "top": (B, top), "top_logp": (B, top)}
-    r = {}
-    for name, shape in shapes.items():
-        t = out.get(name)
-        if top == 0 and name in ("top", "top_logp"):
-            t = None
-        elif t is None:
-            t = torch.empty(shape, dtype=torch.int32 if name == "top" else torch.float32, device=dev)
-        else:
+    r = {} if out is None else dict(out)
+
+    def result(name, shape, dtype=torch.float32):
+        t = r.get(name)
+        if t is None:
+            r[name] = t = torch.empty(shape, dtype=dtype, device=dev)
+        elif t.shape != shape:
             _shaped(t, shape, name)
-        r[name] = t
+        return t
+
+    logp, entropy, norm = result("logp", (B, n)), result("entropy", (B,)), result("norm", (B, 2))
+    best = best_logp = None
+    if top != 0:
+        best, best_logp = result("top", (B, top), torch.int32), result("top_logp", (B, top))
     if workspace is None:
         workspace = torch.empty(label_logprobs_workspace(B, V, top, code), dtype=torch.uint8, device=dev)
-    _same_device(scores, labels, workspace, *r.values())
+    _same_device(scores, labels, workspace, logp, entropy, norm, best, best_logp)
     at, ld = _rows_at(scores, "scores")
     _launch(lib.xc_label_logprobs, "xc_label_logprobs", dev, at, ld, B, V, code, float(temperature),
-            _at(labels, torch.int32, "labels") if n else None, n, top, _at(r["logp"], torch.float32, "logp") if n else None,
-            _at(r["entropy"], torch.float32, "entropy"), _at(r["norm"], torch.float32, "norm"),
-            _at(r["top"], torch.int32, "top") if top else None, _at(r["top_logp"], torch.float32, "top_logp") if top else None,
+            _at(labels, torch.int32, "labels") if n else None, n, top, _at(logp, torch.float32, "logp") if n else None,
+            _at(entropy, torch.float32, "entropy"), _at(norm, torch.float32, "norm"),
+            _at(best, torch.int32, "top") if top else None, _at(best_logp, torch.float32, "top_logp") if top else None,
             _at(workspace, torch.uint8, "workspace"), workspace.numel())
-    return r
+    return {"logp": logp, "entropy": entropy, "norm": norm, "top": best, "top_logp": best_logp}
 
 
 def label_logprobs_grad(scores: torch.Tensor, labels: torch.Tensor, dlogp: torch.Tensor, norm: torch.Tensor, *,
