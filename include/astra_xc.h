@@ -325,7 +325,7 @@ int xc_scores_microscaled(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype 
  * A row without any label: m, log S and every logp are -infinity, its entropy is 0.  A row with a
  * score that is not a number, or +infinity: log S, entropy and logp are not numbers; a score that
  * is not a number is never among the top ones.
- * Sums are fp32, in an order that depends on (B, V, t) and on where a row lies relative to 16 bytes.
+ * Sums are fp32, in an order that depends on (B, V, k, t) and on where a row lies relative to 16 bytes.
  * Requires B >= 1, 1 <= V < 2^31, B*ld <= 2^44, 0 <= n <= XC_MAX_GIVEN, 0 <= k <= min(V, XC_MAX_TOP),
  * 1e-6 <= T <= 1e6.  labels and logp may be NULL if n = 0, top and top_logp if k = 0.  What is written
  * may overlap nothing else of the call (XC_EINVAL).

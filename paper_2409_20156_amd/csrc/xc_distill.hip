@@ -252,7 +252,9 @@ __global__ __launch_bounds__(kRowThreads)
 void distill_sums_kernel(const DistillArgs a) {
     constexpr int N = PiecedRow<T>::N, E = C * N, kMarks = kRowThreads * C / 4;
     __shared__ Sums sums[kRowWaves];
-    __shared__ uint32_t marks[2][kMarks + 1];                // a byte per piece; the edges.  A block's are set while the one before is summed
+    // A byte per piece; the edges.  Block n + 1's are set while block n is summed, block n's cleared behind the barrier that follows: of
+    // three, so that the next barrier lies between this and the block that has them next (of two, a fast wave's n + 2 would meet it).
+    __shared__ uint32_t marks[3][kMarks + 1];
     const int64_t b = blockIdx.x / static_cast<uint32_t>(a.segments), seg = blockIdx.x - b * a.segments;
     if (a.weight != nullptr && a.weight[b] == 0.0f) return;  // uniform
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
@@ -269,44 +271,46 @@ void distill_sums_kernel(const DistillArgs a) {
         if (static_cast<int>(threadIdx.x) < a.K) id = a.labels[b * a.K + threadIdx.x];
         if (!is_label(id, a.V)) id = -1;
         piece = id < row.head ? -1 : (id - row.head) / N;
-        for (int i = threadIdx.x; i <= kMarks; i += kRowThreads) marks[0][i] = marks[1][i] = 0;
+        for (int i = threadIdx.x; i <= kMarks; i += kRowThreads) marks[0][i] = marks[1][i] = marks[2][i] = 0;
         __syncthreads();
         if (id >= 0 && (piece < 0 || piece >= row.pieces))
             atomicOr(&marks[0][kMarks], 1u << (id < row.head ? id : static_cast<int>(id - row.pieces * N)));
     }
-    auto mark = [&](int n, bool on) __attribute__((always_inline)) {       // the thread's listed label, if it lies in block n
+    auto mark = [&](int n, uint32_t* of, bool on) __attribute__((always_inline)) {        // the thread's listed label, if it lies in block n
         const int64_t at = piece - (begin + static_cast<int64_t>(n) * (kRowThreads * C));
         if (id >= 0 && piece >= 0 && piece < end && at >= 0 && at < kRowThreads * C) {
-            uint32_t* w = &marks[n & 1][at >> 2];
+            uint32_t* w = of + (at >> 2);
             if (on) atomicOr(w, 1u << (static_cast<int>(at & 3) * 8 + static_cast<int>(id - row.first(piece))));
             else *w = 0;
         }
     };
     if (a.tail) {
-        mark(0, true);
+        mark(0, marks[0], true);
         __syncthreads();
         if (edge >= 0 && ((marks[0][kMarks] >> threadIdx.x) & 1u) != 0u) more = kNone;
     }
-    for (int n = 0; n < a.blocks; ++n) {
+    for (int n = 0, at = 0; n < a.blocks; ++n) {             // (at: n % 3)
         const int64_t first = begin + static_cast<int64_t>(n) * (kRowThreads * C);
+        const int next = at == 2 ? 0 : at + 1;
         float f[E];
         block.values(f);
         if (n + 1 < a.blocks) block.template load<true>(row, first + kRowThreads * C, end, kRowThreads);
         if (a.tail) {
 #pragma unroll
             for (int i = 0; i < C; ++i) {
-                const uint32_t m = reinterpret_cast<const unsigned char*>(marks[n & 1])[i * kRowThreads + threadIdx.x];
+                const uint32_t m = reinterpret_cast<const unsigned char*>(marks[at])[i * kRowThreads + threadIdx.x];
                 if (__ballot(m != 0u) == 0ull) continue;
 #pragma unroll
                 for (int e = 0; e < N; ++e) if ((m >> e) & 1u) f[i * N + e] = kNone;
             }
-            mark(n + 1, true);
+            mark(n + 1, marks[next], true);
         }
         run.template add<false>(f, largest_of<E>(f, 0), a.c);
         if (a.tail && n + 1 < a.blocks) {
             __syncthreads();                                 // (block n's marks have been read, those of n + 1 are set)
-            mark(n, false);
+            mark(n, marks[at], false);
         }
+        at = next;
     }
     run.add_one(more, a.c);
     const Sums s = block_sums<kRowWaves>(run.sums(a.c), a.c, sums);

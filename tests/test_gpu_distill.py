@@ -76,9 +76,36 @@ def _check(X, labels, teacher, weight, T=1.0, tail=False, out=None, given=None, 
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
 @pytest.mark.parametrize("B,V,K", [(1, 1, 1), (2, 2, 1), (3, 5, 5), (4, 8, 3), (5, 9, 2), (3, 17, 256), (33, 100, 7), (2, 4096, 16), (7, 4103, 64), (9, 8193, 33), (2, 50021, 128),
-                                   (1, 131072, 64), (600, 777, 4), (5, 3000, 256), (1, 300007, 20), (260, 16387, 8)])
+                                   (1, 131072, 64), (600, 777, 4), (5, 3000, 256), (1, 300007, 20), (260, 16387, 8), (520, 9001, 12),
+                                   (70, 40001, 20), (66, 70001, 33)])
 def test_matches_the_oracle(B, V, K, dtype, out, tail):
     _check(*_case(B + V + K, B, V, K, dtype, tail), tail=tail, out=out)
+
+
+@pytest.mark.parametrize("dtype,V", [(F32, 41000), (BF16, 82003)])
+def test_listed_labels_at_the_same_places_of_every_block(dtype, V):
+    """Rows that workgroups go through in blocks of 1024 pieces of 16 bytes: listed labels lie in the same pieces of every block, whose marks
+    share their memory.  Equal rows that begin at the same place of a piece (every 8th one does) have equal results, bit for bit,
+    whichever workgroups had them."""
+    import paper_2409_20156_amd as xc
+    B, rows, K = 520, 4, 120
+    n = 1024 * (4 if dtype == F32 else 8)
+    X, _, _, _ = _case(3, rows, V, 1, dtype, True)
+    places = torch.tensor([5, 6, 700, 2051, 2052, 2053, 3300, n - 9, n - 8, n - 1])
+    labels = torch.cat([places + i * n for i in range(V // n + 1)])
+    labels = labels[labels < V][:K].to(torch.int32)[None].repeat(rows, 1)
+    X.scatter_(1, labels.long(), 6.0)                      # they have most of the probability: one that is missed shows
+    teacher = X.double().log_softmax(-1).gather(1, labels.long()).float() - 0.4
+    many = lambda t: t.repeat(B // rows, 1).contiguous().to(DEV)
+    loss, none = xc.distill(many(X), many(labels), many(teacher), tail=True, grad=False)
+    got = _np(loss).reshape(-1, 8)
+    assert none is None and (got == got[0]).all()
+    want, _, parts = ao.distill(_np(X), labels.numpy(), teacher.double().numpy(), 1.0, True, None)
+    _, mean = _sizes(_np(X), 1.0)
+    D = U * (60 + 3 * mean)
+    first = np.abs(parts["p_r"] - parts["q_r"])
+    tol = D * first + D * D + 1e-6 * D + U * np.abs(want)
+    _close(got[0], np.tile(want, 2), np.tile(tol, 2))
 
 
 @pytest.mark.parametrize("tail", [False, True])

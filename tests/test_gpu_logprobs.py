@@ -79,7 +79,8 @@ def _check(X, labels, T=1.0, top=0, given=None):
 @pytest.mark.parametrize("B,V,n,top", [(1, 1, 1, 1), (1, 2, 0, 2), (3, 3, 2, 3), (2, 5, 1, 5), (5, 7, 3, 0), (4, 8, 2, 8), (4, 9, 2, 1), (3, 15, 1, 15), (3, 17, 1, 4),
                                        (33, 100, 7, 3), (2, 1000, 256, 128), (7, 1023, 1, 20), (7, 2049, 1, 20), (9, 4095, 2, 5), (2, 4096, 1, 128), (2, 4103, 1, 64),
                                        (6, 8192, 1, 10), (3, 8200, 1, 100), (2, 16384, 2, 128), (2, 20011, 3, 7), (2, 50021, 1, 20), (1, 131072, 1, 20),
-                                       (1, 262144 + 3, 1, 128), (300, 4001, 1, 16), (700, 2100, 2, 9), (1, 600011, 4, 128)])
+                                       (1, 262144 + 3, 1, 128), (300, 4001, 1, 16), (700, 2100, 2, 9), (1, 600011, 4, 128),
+                                       (1, 600011, 1, 3), (1, 1200003, 0, 1), (520, 30011, 1, 128)])
 def test_matches_the_oracle(B, V, n, top, dtype):
     _check(*_case(B * 7 + V, B, V, n, dtype), top=top)
 
