@@ -249,7 +249,7 @@ inline RowCut cut_rows(int64_t B, int64_t V, size_t element, int k = 0) {
     r.blocks = static_cast<int>((r.length + kRowThreads * r.each - 1) / (kRowThreads * r.each));
     return r;
 }
-constexpr int64_t kSoftmaxGrid = 1 << 24;        // workgroups of a launch at most
+constexpr int64_t kSoftmaxGrid = 1 << 21;        // workgroups of a launch at most (of 1024 threads at most: a launch of 2^32 threads is refused)
 
 inline float softmax_scale(float temperature) { return static_cast<float>(1.4426950408889634 / static_cast<double>(temperature)); }
 inline bool softmax_temperature(float t) { return t >= 1e-6f && t <= 1e6f; }

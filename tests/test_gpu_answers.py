@@ -146,3 +146,54 @@ def test_nothing_is_allocated_with_buffers():
     xc.distill(c.student, c.out["top"], c.out["top_logp"], tail=True, workspace=c.ws[2], out=(c.loss, c.dX))
     xc.label_logprobs_grad(c.student, c.out["top"], c.dlogp, c.back["norm"], out=c.dX2)
     assert torch.cuda.memory_stats()["allocation.all.allocated"] == before
+
+
+def _equal_bits(a, b):
+    assert torch.equal(a.view(torch.int32) if a.dtype == F32 else a, b.view(torch.int32) if b.dtype == F32 else b)
+
+
+def _rows_by_themselves(X, lo, n, k, K):
+    """What the calls on a soft-max give for the rows from lo on, in a call of their own: of 512 rows or more and
+    from a multiple of 8 on, so that they are cut and lie alike."""
+    import paper_2409_20156_amd as xc
+    B, V = X.shape
+    g = torch.Generator(device=DEV).manual_seed(5)
+    labels = torch.randint(-1, V, (B, K), generator=g, dtype=torch.int32, device=DEV)
+    teacher = torch.randn((B, K), generator=g, device=DEV)
+    given, few = labels[:, :n].contiguous(), lambda t: t[lo:].clone()
+    r, part = xc.label_logprobs(X, given, top=k), xc.label_logprobs(few(X), few(given), top=k)
+    for name in r:
+        if r[name] is not None:
+            _equal_bits(few(r[name]), part[name])
+    dlogp = torch.randn((B, n), generator=g, device=DEV)
+    _equal_bits(few(xc.label_logprobs_grad(X, given, dlogp, r["norm"])), xc.label_logprobs_grad(few(X), few(given), few(dlogp), part["norm"]))
+    del r, part, dlogp
+    loss, dX = xc.distill(X, labels, teacher)
+    want, dx = xc.distill(few(X), few(labels), few(teacher))
+    _equal_bits(few(loss), want)
+    _equal_bits(few(dX), dx)
+    assert torch.isfinite(want).all()
+
+
+@pytest.mark.parametrize("B,V,dtype,k", [(17000, 131072, BF16, 4), ((1 << 24) + 700, 8, F32, 3), ((1 << 21) + 704, 999, BF16, 0)])
+def test_scores_beyond_32_bits_and_more_rows_than_a_launch_takes(B, V, dtype, k):
+    _rows_by_themselves(torch.empty((B, V), dtype=dtype, device=DEV).normal_(), B - 600, 2, k, 6)
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("B,L,d", [(800, 5600000, 768), (2200, 2000000, 1152), (2, 5600000, 1032)])
+def test_4_bit_rows_and_scores_beyond_32_bits(B, L, d):
+    import paper_2409_20156_amd as xc
+    W = torch.empty((L, d), dtype=BF16, device=DEV).normal_()
+    Z = torch.empty((B, d), dtype=BF16, device=DEV).normal_()
+    Q, s = xc.microscale_rows(W)
+    Q1, s1 = xc.microscale_rows(W[-2000:].clone())
+    _equal_bits(Q[-2000:], Q1)
+    _equal_bits(s[-2000:], s1)
+    del W
+    out = xc.scores_microscaled(Z, Q, s, dtype=BF16)
+    lo = max(B - 20, 0)
+    _equal_bits(out[:, -2000:].contiguous(), xc.scores_microscaled(Z, Q1, s1, dtype=BF16))
+    _equal_bits(out[lo:], xc.scores_microscaled(Z[lo:].clone(), Q, s, dtype=BF16))
+    del out
+    torch.cuda.empty_cache()
