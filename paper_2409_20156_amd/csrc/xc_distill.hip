@@ -119,7 +119,6 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t b, L
     for (int h = 0; h < kGroups; ++h) {
         if (h >= groups) continue;
         const int n = a.K - h * kWave < kWave ? a.K - h * kWave : kWave;
-#pragma unroll 8
         for (int j = 0; j < n; ++j) {
             const int32_t id = __builtin_amdgcn_readlane(ids[h], j);
             again[h] |= __ballot(ids[h] == id) & (~1ull << j);
@@ -358,7 +357,7 @@ void distill_terms_kernel(const DistillArgs a) {
 
 // The gradient of a chunk of a row, then that of the listed labels in it (their scores are read before anything is stored: dX may be X).
 // INLINE: every workgroup makes the row's terms for itself from the segments' sums, while its chunk is on its way, and the first one the
-// loss: a launch less, where few rows leave the device idle anyway (16 x 131072 bf16 24 us with it).  Not in place: the list's scores lie
+// loss: a launch less, where few rows leave the device idle anyway (kInlineGrid).  Not in place: the list's scores lie
 // in other workgroups' chunks.
 constexpr int kDistillThreads = 256, kDistillEach = 4, kDistillPieces = kDistillThreads * kDistillEach;
 template <typename T, typename TO, bool INLINE>
@@ -544,22 +543,28 @@ static size_t distill_bytes(int64_t B, int64_t V, xc_dtype t) {
     return static_cast<size_t>(B) * (sizeof(RowTerms) + static_cast<size_t>(cut_rows(B, V, t == XC_F32 ? 4 : 2).segments) * sizeof(float4));
 }
 
+// Up to as many workgroups make the row's terms themselves (K = 64, a tail; with a launch for the terms and without: 16 x 131072
+// bf16, 256 workgroups, 19.4 us and 15.5; 60 x 65536, 480, 22.8 and 18.7; 64 x 100000 fp32, 1600, 29.3 and 32.8).
 constexpr unsigned kInlineGrid = 1024;
-// Whether a row is one workgroup's, which holds it (pieces of a thread; 0: it is not).
-static int distill_whole(int64_t B, int64_t V, size_t element) {
+// Whether a row is one workgroup's, which holds it (0: it is not): read once.  As few waves as hold it with 4 pieces to a thread, or 16 where
+// there are more rows than compute units: two rows at a time on one (16 waves with 4 and 4 with 16: 300 x 32000 bf16 28.1 us and 21.8, 400 x
+// 20000 26.0 and 18.7, 2048 x 32000 117 and 64; 257 x 32000 20.4 and 20.8).  Long rows only where they keep the device busy: in two or three
+// launches and held, 16 x 131072 bf16 15.5 us and 19.9, 64 x 131072 20.8 and 25.0, 80 x 131072 30.9 and 25.2, 1024 x 131072 152 and 131; the
+// shorter rows: 16 x 32768 14.2 and 12.3.
+struct Held { int waves, pieces; };
+static Held distill_whole(int64_t B, int64_t V, size_t element) {
     const int64_t pieces = V / static_cast<int64_t>(16 / element);
-    if (pieces <= 4 * kWave * 4) return 4;                   // 4 waves with 4
-    if (B < 64) return pieces <= 16 * kWave * 4 ? 16 : 0;
-    if (B >= 512 && pieces <= 4 * kWave * 16) return 17;     // 4 waves with 16
-    if (pieces <= 16 * kWave * 4) return 16;                 // 16 waves with 4
-    if (pieces <= 8 * kWave * 16) return 32;                 // 8 waves with 16
-    return pieces <= 16 * kWave * 16 ? 64 : 0;               // 16 waves with 16
+    if (pieces <= 4 * kWave * 4) return {4, 4};
+    if (pieces <= 16 * kWave * 4) return B > 256 ? Held{4, 16} : Held{16, 4};
+    if (B < 72) return {0, 0};
+    if (pieces <= 8 * kWave * 16) return {8, 16};
+    return pieces <= 16 * kWave * 16 ? Held{16, 16} : Held{0, 0};
 }
 
 template <typename T, typename TO>
 static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_t st) {
-    const int whole = all.dX != nullptr ? distill_whole(all.B, all.V, sizeof(T)) : 0;
-    if (whole != 0) {
+    const Held held = all.dX != nullptr ? distill_whole(all.B, all.V, sizeof(T)) : Held{0, 0};
+    if (held.waves != 0) {
         for (int64_t b0 = 0; b0 < all.B; b0 += kSoftmaxGrid) {
             DistillArgs a = all;
             a.B = all.B - b0 < kSoftmaxGrid ? all.B - b0 : kSoftmaxGrid;
@@ -570,10 +575,10 @@ static void launch_distill(const DistillArgs& all, const RowCut& cut, hipStream_
             if (all.weight != nullptr) a.weight += b0;
             a.loss += b0;
             const unsigned grid = static_cast<unsigned>(a.B);
-            if (whole == 4) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 4><<<grid, 4 * kWave, 0, st>>>(a)));
-            else if (whole == 16) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 4><<<grid, 16 * kWave, 0, st>>>(a)));
-            else if (whole == 17) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 16><<<grid, 4 * kWave, 0, st>>>(a)));
-            else if (whole == 32) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 8, 16><<<grid, 8 * kWave, 0, st>>>(a)));
+            if (held.waves == 4 && held.pieces == 4) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 4><<<grid, 4 * kWave, 0, st>>>(a)));
+            else if (held.waves == 4) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 4, 16><<<grid, 4 * kWave, 0, st>>>(a)));
+            else if (held.waves == 8) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 8, 16><<<grid, 8 * kWave, 0, st>>>(a)));
+            else if (held.pieces == 4) XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 4><<<grid, 16 * kWave, 0, st>>>(a)));
             else XC_LAUNCH(K_DISTILL_GRAD, st, (distill_row_kernel<T, TO, 16, 16><<<grid, 16 * kWave, 0, st>>>(a)));
         }
         return;

@@ -209,22 +209,23 @@ __device__ __forceinline__ const void* mx_uniform(const void* p) {
         static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<uint32_t>(a)))));
 }
 
-// ---- few queries: 16 MQ of them stay in LDS (rows of up to 64 KU bytes), the labels pass, 64 to a wave at a time and two units of each to a
+// ---- up to 16 queries: they stay in LDS (rows of up to 64 KU bytes), the labels pass, 64 to a wave at a time and two units of each to a
 // step, through a ring of R steps in LDS that the wave fills and empties by itself.  Eight neighbouring lanes bring 128 bytes of a row, so
 // that a load meets eight lines; straight into registers, where neighbouring lanes have different rows, it meets 64, and so do a row's
 // scales: 1 x 131072 x 768 14.5 us, 1 x 670000 x 768 68.  Lane l has labels 4 (l % 16) .. + 3 of the 64, so that it stores neighbouring
 // scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
 // Bound: one read of Q.
+constexpr int kMicroFew = 16;                            // queries at most
 constexpr int kFewSlot = 64 * 128 + 2 * 64 * 4;          // a step of 64 labels, their scales
 constexpr int kFewLoads = 8 + 2;
 template <int N> __device__ __forceinline__ void few_wait() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
 __device__ __forceinline__ void lds_dma4_sbase(const void* sbase /* wave-uniform */, uint32_t voff, uint32_t lds_addr /* wave-uniform */) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" :: "v"(voff), "s"(sbase), "s"(lds_addr) : "memory");
 }
-template <typename TO, typename TZ, int MQ, int KU, int W, int R>
+template <typename TO, typename TZ, int KU, int W, int R>
 __global__ __launch_bounds__(W * kWave)
-void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
-    constexpr int kRows = 16 * MQ, kUpad = (KU + 3) / 4 * 4;
+void scores_micro_few_kernel(const MicroArgs a) {
+    constexpr int kRows = kMicroFew, kUpad = (KU + 3) / 4 * 4;
     __shared__ __align__(1024) unsigned char ring[W][R][kFewSlot];
     __shared__ __align__(1024) unsigned char codes[kRows * KU * 64];       // 128 bytes of every row, the next 128, ..; chunks of 16 swizzled
     __shared__ __align__(16) unsigned char scales[kRows * 4 * kUpad];
@@ -266,7 +267,7 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
 
     // the queries; rows past the last one are zeros
     if constexpr (!std::is_void<TZ>::value) {
-        const int rows = a.B - q0 < kRows ? static_cast<int>(a.B - q0) : kRows, all = rows * a.units;
+        const int rows = static_cast<int>(a.B), all = rows * a.units;
         if (rows < kRows) {
             for (int i = threadIdx.x; i < kRows * KU * 4; i += W * kWave)
                 if ((i >> 3) % kRows >= rows) *reinterpret_cast<uint4*>(codes + i * 16) = make_uint4(0, 0, 0, 0);
@@ -279,7 +280,7 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
 #pragma unroll
             for (int k = 0; k < U; ++k) {
                 const int i = i0 + k * W * 4, row = i / a.units, u = i - row * a.units;
-                if (i < all) eight<TZ>(a.Z + (q0 + row) * a.d * static_cast<int64_t>(sizeof(TZ) == 4 ? 4 : 2), u * kMxRow + sub * 8, a.d, f[k]);
+                if (i < all) eight<TZ>(a.Z + row * a.d * static_cast<int64_t>(sizeof(TZ) == 4 ? 4 : 2), u * kMxRow + sub * 8, a.d, f[k]);
             }
 #pragma unroll
             for (int k = 0; k < U; ++k) {
@@ -295,22 +296,20 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
         for (int i = threadIdx.x; i < kRows * chunks; i += W * kWave) {
             const int row = i / chunks, c = i - row * chunks;
             *reinterpret_cast<uint4*>(codes + (c >> 3) * (kRows * 128) + row * 128 + (((c & 7) ^ mx_swizzle(row)) * 16)) =
-                *reinterpret_cast<const uint4*>(a.P + (q0 + row) * a.ppitch + c * 16);
+                *reinterpret_cast<const uint4*>(a.P + row * a.ppitch + c * 16);
         }
         for (int i = threadIdx.x; i < kRows * a.upad; i += W * kWave) {    // words of 4 units
             const int row = i / a.upad, c = i - row * a.upad, b = c / (a.upad / 4), k = c - b * (a.upad / 4);
             *reinterpret_cast<uint32_t*>(scales + row * (4 * kUpad) + b * kUpad + k * 4) =
-                *reinterpret_cast<const uint32_t*>(a.pscale + (q0 + row) * 4 * a.upad + b * a.upad + k * 4);
+                *reinterpret_cast<const uint32_t*>(a.pscale + row * 4 * a.upad + b * a.upad + k * 4);
         }
     }
     __syncthreads();
     const int frag = r * 128 + ((quarter ^ mx_swizzle(r)) * 16);
-    mx_f32x4 acc[MQ][4];
+    mx_f32x4 acc[4];
     auto clear = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int x = 0; x < MQ; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) acc[x][y] = mx_f32x4{0, 0, 0, 0};
+        for (int y = 0; y < 4; ++y) acc[y] = mx_f32x4{0, 0, 0, 0};
     };
     clear();
     int step = 0, slot = 0;
@@ -330,13 +329,10 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
                 w[y] = *reinterpret_cast<const mx_i32x4*>(from + (r * 4 + y) * 128 + (((h * 4 + quarter) ^ (r & 7)) * 16));
                 ws[y] = from[64 * 128 + h * 256 + (r * 4 + y) * 4 + quarter];
             }
+            const mx_i32x4 z = *reinterpret_cast<const mx_i32x4*>(codes + (u >> 1) * (kRows * 128) + (frag ^ ((u & 1) * 64)));
+            const int zs = scales[r * (4 * kUpad) + quarter * kUpad + u];
 #pragma unroll
-            for (int x = 0; x < MQ; ++x) {                   // 16 queries, 64 bytes of each
-                const mx_i32x4 z = *reinterpret_cast<const mx_i32x4*>(codes + (u >> 1) * (kRows * 128) + x * 16 * 128 + (frag ^ ((u & 1) * 64)));
-                const int zs = scales[(x * 16 + r) * (4 * kUpad) + quarter * kUpad + u];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) acc[x][y] = mx_product<0>(z, w[y], acc[x][y], zs, ws[y]);
-            }
+            for (int y = 0; y < 4; ++y) acc[y] = mx_product<0>(z, w[y], acc[y], zs, ws[y]);
         }
         if (n + R < total) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");             // (the slot has been read)
@@ -348,14 +344,12 @@ void scores_micro_few_kernel(const MicroArgs a, int64_t q0) {
             const int64_t l = g * 64 + r * 4, have = a.L - l;
             const bool whole = g * 64 + 64 <= a.L;           // uniform
 #pragma unroll
-            for (int x = 0; x < MQ; ++x)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int64_t q = q0 + x * 16 + quarter * 4 + i;
-                    if (q >= a.B) continue;
-                    const float v[4] = {acc[x][0][i], acc[x][1][i], acc[x][2][i], acc[x][3][i]};
-                    put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
-                }
+            for (int i = 0; i < 4; ++i) {
+                const int64_t q = quarter * 4 + i;
+                if (q >= a.B) continue;
+                const float v[4] = {acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+                put_labels(static_cast<TO*>(a.out) + q * a.L + l, v, whole, have);
+            }
             clear();
             g += g_step;
         }
@@ -710,13 +704,12 @@ static MicroSpace micro_space(int64_t B, int d) {
 constexpr int64_t kMxCachedBytes = 256ll << 20;
 constexpr int kMicroFewUnits = 8, kMicroFewLong = 32, kMicroHeldUnits = 8;
 
-template <typename TO, typename TZ, int MQ, int KU, int W, int R>
+template <typename TO, typename TZ, int KU, int W, int R>
 static void launch_few(const MicroArgs& a, hipStream_t st) {
-    constexpr int kLds = W * R * kFewSlot + 16 * MQ * (KU * 64 + (KU + 3) / 4 * 16), kPerCu = 160 * 1024 / (kLds + 1024);
+    constexpr int kLds = W * R * kFewSlot + kMicroFew * (KU * 64 + (KU + 3) / 4 * 16), kPerCu = 160 * 1024 / (kLds + 1024);
     static_assert(kPerCu >= 1, "");
     const int64_t groups = (a.L + 63) / 64, per = ((groups + kXcds - 1) / kXcds + W - 1) / W, most = kCusPerXcd * kPerCu;
-    for (int64_t q0 = 0; q0 < a.B; q0 += 16 * MQ)
-        scores_micro_few_kernel<TO, TZ, MQ, KU, W, R><<<static_cast<unsigned>(kXcds * (per < most ? per : most)), W * kWave, 0, st>>>(a, q0);
+    scores_micro_few_kernel<TO, TZ, KU, W, R><<<static_cast<unsigned>(kXcds * (per < most ? per : most)), W * kWave, 0, st>>>(a);
 }
 template <typename TO, int NK>
 static void launch_micro_held(const MicroArgs& a, hipStream_t st) {
@@ -748,27 +741,34 @@ static bool small_tiles(const MicroArgs& a) {
     auto rounds = [&](int64_t side, int64_t at_once) { return ((a.B + side - 1) / side * ((a.L + side - 1) / side) + at_once - 1) / at_once; };
     return rounds(MicroTile<2, 4, 8>::BM, kMineGrid * MicroTile<2, 4, 8>::kPerCu) * 5 > rounds(MicroTile<2, 2, 4>::BM, kMineGrid * MicroTile<2, 2, 4>::kPerCu) * 3;
 }
+// Labels in registers: from four stages to a compute unit on, for more than 256 queries (a tile's labels cost a workgroup as much as several
+// stages) and tiles for all XCDs.  Held against in tiles, d = 768: 64 x 670000 92 us and 82, 256 x 64000 19.9 and 17.6, 2000 x 8000 18.5 and
+// 18.1, 2000 x 16000 25.0 and 26.0, 400 x 131072 43.5 and 49.9, 10000 x 2000 35 and 28, 10000 x 4000 38 and 46, 10000 x 64000 300 and 460.
+static bool hold_labels(const MicroArgs& a) {
+    const int64_t tiles = (a.L + kMicroHeldLabels - 1) / kMicroHeldLabels, stages = (a.B + MicroHeld<2>::QS - 1) / MicroHeld<2>::QS;
+    return a.units <= kMicroHeldUnits && a.B > 256 && tiles >= kXcds && tiles * stages >= 4 * kMineGrid;
+}
 constexpr int64_t kMicroInline = 128;                    // units of queries: two rounds of a workgroup's loads (16 x 131072 x 4096, 512 of
                                                          // them: 81 us, in a launch of their own 64; 4 x 2487 x 3280, 104: 14.7 against 18.8 with one round)
 
 template <typename TO>
 static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& space, hipStream_t st) {
     a.Z = static_cast<const unsigned char*>(Z);
-    if (a.B <= 16 && a.units <= kMicroFewLong && a.B * a.units <= kMicroInline) {      // every workgroup brings the queries to 4 bits for itself: one launch
+    if (a.B <= kMicroFew && a.units <= kMicroFewLong && a.B * a.units <= kMicroInline) {     // every workgroup brings the queries to 4 bits for itself: one launch
         auto go = [&]() {
             if (a.units <= kMicroFewUnits) {
-                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewUnits, 4, 2>(a, st);
-                else launch_few<TO, bf16_t, 1, kMicroFewUnits, 4, 2>(a, st);
+                if (t == XC_F32) launch_few<TO, float, kMicroFewUnits, 4, 2>(a, st);
+                else launch_few<TO, bf16_t, kMicroFewUnits, 4, 2>(a, st);
             } else {
-                if (t == XC_F32) launch_few<TO, float, 1, kMicroFewLong, 4, 3>(a, st);
-                else launch_few<TO, bf16_t, 1, kMicroFewLong, 4, 3>(a, st);
+                if (t == XC_F32) launch_few<TO, float, kMicroFewLong, 4, 3>(a, st);
+                else launch_few<TO, bf16_t, kMicroFewLong, 4, 3>(a, st);
             }
         };
         XC_LAUNCH(K_SCORES_MICRO, st, go());
         XC_HIP_CHECK(hipGetLastError());
         return XC_OK;
     }
-    const bool held = a.B > 64 && a.units <= kMicroHeldUnits, few = a.units <= kMicroFewUnits ? a.B <= 64 : a.B <= 16 && a.units <= kMicroFewLong;
+    const bool few = a.B <= kMicroFew && a.units <= kMicroFewLong, held = !few && hold_labels(a);
     uint8_t *P = const_cast<uint8_t*>(a.P), *pscale = const_cast<uint8_t*>(a.pscale);
     const int rc = held || few ? launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroQueries{P, pscale, space.units, space.pitch, space.upad}, space.rows, space.pitch / 64, st)
                                : launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroRows{P, pscale, space.units}, a.B, space.units, st);
@@ -782,9 +782,7 @@ static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& s
                 default: launch_micro_held<TO, 8>(a, st); break;
             }
         } else if (few) {
-            if (a.units > kMicroFewUnits) launch_few<TO, void, 1, kMicroFewLong, 4, 3>(a, st);
-            else if (a.B <= 32) launch_few<TO, void, 2, kMicroFewUnits, 4, 3>(a, st);
-            else launch_few<TO, void, 4, kMicroFewUnits, 4, 3>(a, st);
+            launch_few<TO, void, kMicroFewLong, 4, 3>(a, st);          // (shorter rows of as many queries went the way above)
         } else if (small_tiles(a)) {
             launch_micro_tile<TO, 2, 2, 4>(a, st);
         } else {

@@ -77,7 +77,7 @@ def _check(X, labels, teacher, weight, T=1.0, tail=False, out=None, given=None, 
 @pytest.mark.parametrize("dtype,out", [(F32, F32), (BF16, BF16), (BF16, F32), (F32, BF16)])
 @pytest.mark.parametrize("B,V,K", [(1, 1, 1), (2, 2, 1), (3, 5, 5), (4, 8, 3), (5, 9, 2), (3, 17, 256), (33, 100, 7), (2, 4096, 16), (7, 4103, 64), (9, 8193, 33), (2, 50021, 128),
                                    (1, 131072, 64), (600, 777, 4), (5, 3000, 256), (1, 300007, 20), (260, 16387, 8), (520, 9001, 12),
-                                   (70, 40001, 20), (66, 70001, 33)])
+                                   (70, 40001, 20), (66, 70001, 33), (75, 40001, 20), (73, 70001, 33), (300, 8200, 5)])
 def test_matches_the_oracle(B, V, K, dtype, out, tail):
     _check(*_case(B + V + K, B, V, K, dtype, tail), tail=tail, out=out)
 

@@ -142,9 +142,11 @@ def test_scores_do_not_depend_on_the_batch_or_the_range():
         assert torch.equal(xc.scores_microscaled(Z, Q, s, dtype=BF16), whole.bfloat16())
 
 
-@pytest.mark.parametrize("B,L,d", [(520, 33001, 1096), (2500, 16385, 1160), (2049, 16384, 1400), (90, 70003, 1288)])
+@pytest.mark.parametrize("B,L,d", [(520, 33001, 1096), (2500, 16385, 1160), (2049, 16384, 1400), (90, 70003, 1288),
+                                   (4100, 8001, 128), (4097, 8192, 72), (2050, 16000, 256), (4100, 8100, 384), (2112, 16385, 640), (300, 140001, 512), (257, 131072, 768),
+                                   (4100, 8001, 1000), (1000, 33000, 1024), (400, 270000, 136)])
 def test_workgroups_that_take_several_tiles(B, L, d):
-    """More tiles of long rows than there are workgroups: every tile's scores are those of the rows by themselves, 16 of them at a time."""
+    """More tiles than there are workgroups, and labels held in registers: every tile's scores are those of the rows by themselves, 16 of them at a time."""
     import paper_2409_20156_amd as xc
     Z, W = _matrix(B, B, d, BF16).to(DEV), _matrix(L, L, d, BF16).to(DEV)
     Q, s = xc.microscale_rows(W)
