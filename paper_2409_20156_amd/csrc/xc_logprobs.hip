@@ -94,14 +94,21 @@ __device__ __forceinline__ uint32_t reached_by(int n, int k, V value) {
     return lo;
 }
 
-// How many of n keys are better than this one (the keys behind them, up to a multiple of four, are ~0).
+// How many of n keys are better than this one (the keys behind them, up to a multiple of four, are ~0); of LANES neighbouring lanes with the
+// same key each counts its share of them.
+template <int LANES = 1>
 __device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
+    static_assert(LANES == 1 || LANES == 4, "");
     int rank = 0;
 #pragma unroll 2
-    for (int j = 0; j < n; j += 4) {
+    for (int j = LANES == 1 ? 0 : (lane_id() & (LANES - 1)) * 4; j < n; j += 4 * LANES) {
         uint64_t k[4];
         __builtin_memcpy(k, __builtin_assume_aligned(keys + j, 16), 32);
         rank += (k[0] < key ? 1 : 0) + (k[1] < key ? 1 : 0) + (k[2] < key ? 1 : 0) + (k[3] < key ? 1 : 0);
+    }
+    if constexpr (LANES == 4) {
+        rank += __builtin_amdgcn_update_dpp(0, rank, 0xB1, 0xf, 0xf, false);           // quad_perm 1 0 3 2
+        rank += __builtin_amdgcn_update_dpp(0, rank, 0x4E, 0xf, 0xf, false);           // quad_perm 2 3 0 1
     }
     return rank;
 }
@@ -320,10 +327,11 @@ void logprobs_kernel(const LogprobArgs a) {
     }
 }
 
-// The segments of a row joined, by a workgroup per row.  The best labels, of up to kJoinAtOnce segments at a time and the best of those
+// The segments of a row joined, by a workgroup per row, four lanes to a key that is ranked (67 rows of 15 segments, 128 labels: a thread to
+// a key 17.3 us).  The best labels, of up to kJoinAtOnce segments at a time and the best of those
 // before them: of the first r of each segment (2 k labels or a few more in all) the k-th best is found by ranking; whatever is worse than
 // that is left out, and the few others are ranked.
-constexpr int kJoinWaves = 4, kJoinAtOnce = 128;
+constexpr int kJoinWaves = 16, kJoinAtOnce = 128;
 constexpr int kJoinFirst = 2 * XC_MAX_TOP + kJoinAtOnce;     // labels of the first ranking at most
 template <typename T>
 __global__ __launch_bounds__(kJoinWaves * kWave)
@@ -365,8 +373,10 @@ void logprobs_join_kernel(const LogprobArgs a) {
         }
         __syncthreads();
         // (labels that are not there have the same key: where they reach the k-th place, `bound` stays what it is, theirs)
-        for (int i = threadIdx.x; i < first; i += kThreads)
-            if (keys[i] != kKeySentinel && rank_of(keys[i], keys, first) == a.k - 1) bound = keys[i];
+        for (int i = threadIdx.x >> 2; i < first; i += kThreads / 4) {
+            const uint64_t key = keys[i];
+            if (rank_of<4>(key, keys, first) == a.k - 1 && key != kKeySentinel) bound = key;
+        }
         __syncthreads();
         const uint64_t limit = bound;
         for (int i = threadIdx.x; i < have; i += kThreads) keys[i] = best[i];
@@ -378,9 +388,9 @@ void logprobs_join_kernel(const LogprobArgs a) {
         const int n = found;
         end_keys(keys, n);
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += kThreads) {
+        for (int i = threadIdx.x >> 2; i < n; i += kThreads / 4) {
             const uint64_t key = keys[i];
-            const int rank = rank_of(key, keys, n);
+            const int rank = rank_of<4>(key, keys, n);
             if (rank < a.k) best[rank] = key;
         }
         have = n < a.k ? n : a.k;
