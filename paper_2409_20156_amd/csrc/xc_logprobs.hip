@@ -169,6 +169,8 @@ __device__ __forceinline__ void best_of_block(const PiecedRow<T>& row, int64_t f
 // stretches.  In the end the few that are left are ranked by counting.
 // A piece with such a label is noted in a list of its wave, 64 of them are looked at together: most blocks have a few, and a wave would
 // spend as much on these as on 64.
+// Bound: 1024 x 131072 bf16 without top labels 44 to 50 us, one read at 5.4 to 6.1 TB/s; 2048 rows with 64 of them 118 us, 4.6 TB/s: vector
+// instructions are under way for 0.7 to 0.8 of the time (the exponential, the sums, the largest of every piece against the threshold).
 template <typename T, int C>
 __global__ __launch_bounds__(kRowThreads, 4)
 void logprobs_kernel(const LogprobArgs a) {
@@ -413,6 +415,7 @@ struct LogprobGradArgs {
 };
 constexpr int kGradThreads = 256, kGradEach = 4, kGradPieces = kGradThreads * kGradEach;       // pieces of a workgroup
 
+// Bound: memory.  1024 x 131072 bf16 84 to 86 us, 6.3 TB/s read and written.
 // A chunk of a row per workgroup, element by element; then the given labels that lie in the chunk, once each, whose sums of dlogp are
 // formed in the order of the list.  (Their scores are read before anything is stored: dX may be X.)
 template <typename T, typename TO>

@@ -212,8 +212,8 @@ __device__ __forceinline__ const void* mx_uniform(const void* p) {
 // ---- up to 16 queries: they stay in LDS (rows of up to 64 KU bytes), the labels pass, 64 to a wave at a time and two units of each to a
 // step, through a ring of R steps in LDS that the wave fills and empties by itself.  Eight neighbouring lanes bring 128 bytes of a row, so
 // that a load meets eight lines; straight into registers, where neighbouring lanes have different rows, it meets 64, and so do a row's
-// scales: 1 x 131072 x 768 14.5 us, 1 x 670000 x 768 68.  Lane l has labels 4 (l % 16) .. + 3 of the 64, so that it stores neighbouring
-// scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
+// scales: 1 x 131072 x 768 14.5 us, 1 x 670000 x 768 68, against 10.2 and 51 (5.3 TB/s).  Lane l has labels 4 (l % 16) .. + 3 of the 64, so
+// that it stores neighbouring scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
 // Bound: one read of Q.
 constexpr int kMicroFew = 16;                            // queries at most
 constexpr int kFewSlot = 64 * 128 + 2 * 64 * 4;          // a step of 64 labels, their scales
@@ -359,6 +359,8 @@ void scores_micro_few_kernel(const MicroArgs a) {
 // ---- many queries, rows of up to 512 bytes (1024 elements): the labels stay where they are.  A wave holds 64 labels as operands in registers
 // (NK units) and 512 labels of a workgroup meet the queries that stream through LDS, 64 at a time; a wave's scores are stored 16 queries at
 // a time, while the other wave of its SIMD multiplies.
+// Bound: stores and products beside each other, at the clock that the power limit leaves.  4096 x 131072 x 768 to bf16 235 to 250 us (1.07 GB
+// stored, 157 us of a fill; matrix pipe busy 47 % of the time); with a sixth of the products 208, without the stores 163.
 template <int NK_>
 struct MicroHeld {
     static constexpr int NK = NK_, QS = 64, kUpad = NK <= 4 ? 4 : 8, kStage = QS * NK * 64, kScales = QS * 4 * kUpad;
@@ -556,7 +558,9 @@ void scores_micro_held_kernel(const MicroArgs a, int tiles, int stages) {
 // workgroup takes one tile after the other, the first stage of the next one under way while the last is multiplied and the scores are
 // stored.  Rows of labels lie in the order of the products' blocks (block y, column j: label 4 j + y of 64), so that a lane stores
 // neighbouring scores.  Consecutive workgroups of an XCD take the query tiles of one label tile.
-// Bound: what brings the operands out of LDS (96 bytes a cycle of 128 with 128 x 64 to a wave), and the stores.
+// Bound: products and stores one after the other, since what a tile's second stage waits for is queued behind the stores before it.  1440 x
+// 164990 to bf16: 281 us for rows of 1152 elements, 639 of 4096, which is 3.9 PFLOP/s for what lies between them (96 of the 128 bytes a cycle
+// of LDS go to operands) and 140 us for the scores.
 template <int WQ, int WL, int MQ>
 struct MicroTile {
     static constexpr int kWaves = WQ * WL, BM = 16 * MQ * WQ, BN = 64 * WL, kRows = BM + BN, R = 2;

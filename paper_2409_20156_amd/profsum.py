@@ -37,6 +37,10 @@ KERNELS = {"mine_tile_kernel": "mine_tile", "mine_rows_kernel": "mine_tile", "mi
            "bucket_sort_kernel": "bucket_sort",
            "heads_count_kernel": "heads_count", "heads_write_kernel": "heads_write",
            "update_kernel": "update", "quantize_kernel": "quantize", "scores_kernel": "scores", "scores_held_kernel": "scores",
+           "logprobs_kernel": "logprobs", "logprobs_join_kernel": "logprobs_join", "logprobs_grad_kernel": "logprobs_grad",
+           "distill_row_kernel": "distill_grad", "distill_sums_kernel": "distill_sums", "distill_terms_kernel": "distill_terms",
+           "distill_grad_kernel": "distill_grad", "microscale_kernel": "microscale", "scores_micro_few_kernel": "scores_micro",
+           "scores_micro_held_kernel": "scores_micro", "scores_micro_tile_kernel": "scores_micro",
            "verify_one_kernel": "verify", "verify_sums_kernel": "verify_sums", "verify_draw_kernel": "verify", "dropout_kernel": "dropout",
            "copy_probe_kernel": "copy_probe", "mfma_probe_kernel": "mfma_probe"}
 
