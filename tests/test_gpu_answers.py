@@ -197,3 +197,44 @@ def test_4_bit_rows_and_scores_beyond_32_bits(B, L, d):
     _equal_bits(out[lo:], xc.scores_microscaled(Z[lo:].clone(), Q, s, dtype=BF16))
     del out
     torch.cuda.empty_cache()
+
+
+def test_which_kernels_a_call_launches():
+    """By the names of the event timing: one launch where a workgroup holds a row or brings the queries to 4 bits itself, more of them elsewhere."""
+    import paper_2409_20156_amd as xc
+    from paper_2409_20156_amd import binding
+
+    def kernels(call):
+        call()                                             # (outputs and workspaces that torch allocates)
+        torch.cuda.synchronize()
+        binding.profile_reset()
+        binding.profile_enable(True)
+        try:
+            call()
+        finally:
+            binding.profile_enable(False)
+        prof = binding.profile_collect()
+        binding.profile_reset()
+        return {name: n for name, (_, n) in prof.items() if n}
+
+    X = {(B, V): torch.randn((B, V), device=DEV).to(BF16) for B, V in ((2, 4096), (16, 131072), (300, 32000), (70, 131072))}
+    labels = {key: torch.zeros((key[0], 3), dtype=torch.int32, device=DEV) for key in X}
+    teacher = {key: torch.zeros((key[0], 3), device=DEV) for key in X}
+    for key, want in (((2, 4096), {"logprobs": 1}), ((16, 131072), {"logprobs": 1, "logprobs_join": 1}), ((300, 32000), {"logprobs": 1, "logprobs_join": 1})):
+        assert kernels(lambda: xc.label_logprobs(X[key], labels[key], top=2)) == want, key
+    norm = xc.label_logprobs(X[2, 4096], labels[2, 4096])["norm"]
+    assert kernels(lambda: xc.label_logprobs_grad(X[2, 4096], labels[2, 4096], teacher[2, 4096], norm)) == {"logprobs_grad": 1}
+    split = {"distill_sums": 1, "distill_terms": 1, "distill_grad": 1}
+    for key, grad, place, want in (((2, 4096), True, False, {"distill_grad": 1}), ((300, 32000), True, True, {"distill_grad": 1}),
+                                   ((16, 131072), True, False, {"distill_sums": 1, "distill_grad": 1}), ((16, 131072), True, True, split),
+                                   ((70, 131072), True, False, split), ((2, 4096), False, False, {"distill_sums": 1, "distill_terms": 1})):
+        x, out = X[key], None
+        if place:
+            x = x.clone()
+            out = (torch.empty(key[0], device=DEV), x)
+        assert kernels(lambda: xc.distill(x, labels[key], teacher[key], grad=grad, out=out)) == want, (key, grad, place)
+    for B, L, d, n in ((1, 100, 64, 1), (16, 100, 1024, 1), (17, 100, 64, 2), (4, 100, 4096, 1), (5, 100, 4096, 2), (2, 100, 4104, 2), (300, 2000, 768, 2)):
+        W, Z = torch.randn((L, d), device=DEV), torch.randn((B, d), device=DEV)
+        Q, s = xc.microscale_rows(W)
+        assert kernels(lambda: xc.scores_microscaled(Z, Q, s)) == ({"scores_micro": 1} if n == 1 else {"microscale": 1, "scores_micro": 1}), (B, L, d)
+        assert kernels(lambda: xc.microscale_rows(W)) == {"microscale": 1}

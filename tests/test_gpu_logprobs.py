@@ -246,7 +246,7 @@ def test_the_dense_soft_max_loss():
     x64 = X.double().requires_grad_()
     loss = torch.nn.functional.cross_entropy(x64, y[:, 0].long())
     loss.backward()
-    assert abs(float(-r["logp"].double().mean()) - float(loss)) < 1e-6
+    assert abs(float(-r["logp"].double().mean()) - loss.item()) < 1e-6
     assert (got.cpu().double() - x64.grad).abs().max() < 1e-6 / 16
 
 
