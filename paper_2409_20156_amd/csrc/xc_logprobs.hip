@@ -56,24 +56,29 @@ __device__ __forceinline__ uint64_t wave_min_u64(uint64_t v) { return ~wave_max_
 
 constexpr uint32_t kLowest = 0x00800000u;        // ordered image of the lowest number above -inf
 
-// Of n values (ordered images of scores; value(i) reads one): one that at least k of them reach, if as many lie above -inf, and that few
-// others do; found by halving the range, by one wave.  Equal values can make these many.
-template <typename V>
+// Of n values, 64 G at most (ordered images of scores; value(i) reads one): one that at least k of them reach, if as many lie above -inf, and
+// that few others do; found by halving the range, by one wave, which holds them (read from LDS every time: 1024 x 131072 bf16 with 128 labels
+// 73 us against 67).  Equal values can make these many.
+template <int G, typename V>
 __device__ __forceinline__ uint32_t reached_by(int n, int k, V value) {
-    uint32_t lo = ~0u, hi = 0u;
-    for (int i = lane_id(); i < n; i += kWave) {
-        const uint32_t o = value(i);
-        lo = o < lo ? o : lo;
-        hi = o > hi ? o : hi;
+    uint32_t lo = ~0u, hi = 0u, o[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        o[g] = 0u;
+        if (g * kWave >= n) continue;                        // uniform
+        const int i = g * kWave + lane_id();
+        if (i < n) {
+            o[g] = value(i);
+            lo = o[g] < lo ? o[g] : lo;
+            hi = o[g] > hi ? o[g] : hi;
+        }
     }
     lo = ~wave_max_u32(~lo);
     hi = wave_max_u32(hi) + 1u;
     auto count = [&](uint32_t t) __attribute__((always_inline)) {
         int c = 0;
-        for (int i0 = 0; i0 < n; i0 += kWave) {
-            const int i = i0 + lane_id();
-            c += __popcll(__ballot(i < n && value(i < n ? i : 0) >= t));
-        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) if (g * kWave < n) c += __popcll(__ballot(o[g] >= t));           // (t is never 0)
         return c;
     };
     if (lo < kLowest) lo = kLowest;
@@ -169,7 +174,7 @@ __device__ __forceinline__ void best_of_block(const PiecedRow<T>& row, int64_t f
 // stretches (behind 1, 2, 4, 8, ..: 4000 x 32000 bf16 with 64 labels 90.9 us against 86.7).  In the end the few that are left are ranked by counting.
 // A piece with such a label is noted in a list of its wave, 64 of them are looked at together: most blocks have a few, and a wave would
 // spend as much on these as on 64.
-// Bound: 1024 x 131072 bf16 without top labels 44 to 50 us, one read at 5.4 to 6.1 TB/s; 2048 rows with 64 of them 118 us, 4.6 TB/s: vector
+// Bound: 1024 x 131072 bf16 without top labels 44 to 50 us, one read at 5.4 to 6.1 TB/s; 2048 rows with 64 of them 113 us, 4.8 TB/s: vector
 // instructions are under way for 0.7 to 0.8 of the time (the exponential, the sums, the largest of every piece against the threshold).
 template <typename T, int C>
 __global__ __launch_bounds__(kRowThreads, 4)
@@ -204,7 +209,8 @@ void logprobs_kernel(const LogprobArgs a) {
         __syncthreads();                                     // (`kept` and `reach` have been read)
         if (threadIdx.x < kWave) {
             const uint32_t* words = reinterpret_cast<const uint32_t*>(keys);
-            const uint32_t r = reached_by(have, a.k, [&](int i) __attribute__((always_inline)) { return ~words[2 * i + 1]; });
+            auto value = [&](int i) __attribute__((always_inline)) { return ~words[2 * i + 1]; };
+            const uint32_t r = have <= 4 * kWave ? reached_by<4>(have, a.k, value) : reached_by<kTopKeys / kWave>(have, a.k, value);
             if (threadIdx.x == 0) {
                 reach = r > reach ? r : reach;
                 kept = 0;
@@ -276,7 +282,7 @@ void logprobs_kernel(const LogprobArgs a) {
             largest[threadIdx.x] = float_to_ordered(fmaxf(most, more) + 0.0f);
             __syncthreads();
             if (threadIdx.x < kWave) {
-                const uint32_t r = reached_by(kRowThreads, a.k, [&](int i) __attribute__((always_inline)) { return largest[i]; });
+                const uint32_t r = reached_by<kRowThreads / kWave>(kRowThreads, a.k, [&](int i) __attribute__((always_inline)) { return largest[i]; });
                 if (threadIdx.x == 0) reach = r;
             }
             __syncthreads();
