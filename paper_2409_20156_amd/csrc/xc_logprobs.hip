@@ -44,15 +44,20 @@ __device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t b, int r
     a.top_logp[b * a.k + rank] = there ? logp_of(key_score(key), z, a.T) : kNone;
 }
 
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) {
-        const uint32_t t = __shfl_xor(v, off, kWave);
-        v = t > v ? t : v;
-    }
-    return v;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t larger_of_lanes(uint32_t x) {
+    const uint32_t t = static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, ROWS, 0xf, false));
+    return t > x ? t : x;
 }
-__device__ __forceinline__ uint64_t wave_min_u64(uint64_t v) { return ~wave_max_u64(~v); }
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+    v = larger_of_lanes<0x111, 0xf>(v);                      // row_shr 1, 2, 4, 8
+    v = larger_of_lanes<0x112, 0xf>(v);
+    v = larger_of_lanes<0x114, 0xf>(v);
+    v = larger_of_lanes<0x118, 0xf>(v);
+    v = larger_of_lanes<0x142, 0xa>(v);                      // row_bcast 15, 31
+    v = larger_of_lanes<0x143, 0xc>(v);
+    return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), kWave - 1));
+}
 
 constexpr uint32_t kLowest = 0x00800000u;        // ordered image of the lowest number above -inf
 
