@@ -358,11 +358,12 @@ int xc_label_logprobs_grad(const void* X /* [B*ld] */, int64_t ld, int64_t B, in
  *   loss[b] = w_b T^2 (sum_k q_k (log q_k - log p_k) + q_r (log q_r - log p_r)),
  *   dX      = its derivative: w_b T (Q p_v - q_v) for a listed label, w_b T (Q p_r - q_r) p_v / p_r for any
  *             other one, Q = sum_k q_k + q_r.
- * Terms with q = 0 are 0.  A label that occurs several times in a list has the sum of its q.  weight is
- * [B] or NULL (all 1); a row of weight 0 counts for nothing, whatever it holds: loss and gradient 0; so does a row
- * without a label in its list, or (tail = 0) with teacher values of -infinity alone.  A row of scores without any
- * label has loss infinity where q > 0, and p counts as 0 in its gradient.  Where scores or teacher values are not
- * numbers, the loss is not a number.  Sums over a row are fp32, what is formed from them 64 bits.
+ * Terms with q = 0 are 0.  A label that occurs several times in a list is one label with the sum of its q, in the
+ * loss as well as in the gradient.  weight is [B] or NULL (all 1); a row of weight 0 counts for nothing, whatever it
+ * holds: loss and gradient 0; so does a row without a label in its list, or (tail = 0) with teacher values of -infinity
+ * alone.  A row of scores without any label has loss infinity where q > 0, and p counts as 0 in its gradient.  Where
+ * scores or teacher values are not numbers, the loss is not a number.  Sums over a row are fp32, what is formed from
+ * them 64 bits.
  * dX (or NULL: the loss alone) has rows ldd elements apart and type out_t; it may be X if types and row distances
  * are the same.  Otherwise what is written may overlap nothing else of the call (XC_EINVAL).
  * Requires B, V, ld, T as above, 1 <= K <= XC_MAX_TEACHER.

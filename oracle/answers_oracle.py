@@ -148,7 +148,9 @@ def distill(X, labels, teacher, T=1.0, tail=False, weight=None):
             target = np.zeros(V)
             np.add.at(target, ids, q)
             lq = t if tail else t - t.max() - np.log(np.exp(t - t.max()).sum())
-            value = sum(qk * (l - lp[v]) for qk, l, v in zip(q, lq, ids) if qk != 0)
+            # (a label that is listed several times has the sum of its probabilities)
+            merged = {v: (target[v], np.logaddexp.reduce(lq[ids == v])) for v in ids.tolist()}
+            value = sum(qv * (l - lp[v]) for v, (qv, l) in merged.items() if qv != 0)
             p_r = q_r = 0.0
             if tail:
                 rest = X[b][~listed]

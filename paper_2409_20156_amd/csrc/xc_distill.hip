@@ -79,7 +79,7 @@ __device__ __forceinline__ Elsewhere listed_elsewhere(const int32_t* list, int K
 // once, quotients of sums stand where differences of their logarithms would (200 x 131072 fp32: 11.8 us with a logarithm, an exponential
 // after the other and a loop over the list for each place).
 struct Teacher {
-    double sum, weighted;                // of the list: sum of q = exp(t - t0), of q (t - t0)
+    double sum, weighted;                // of the list: sum of q = exp(t - t0), of q log q over its labels, q of all places of a label together
     float t0, x_max;
     bool any;
 };
@@ -139,6 +139,7 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t b, L
             list.places[g * kWave + lane_id()].once = once;
             twice |= !once;
         }
+    const bool dup = __ballot(twice) != 0ull;
     // (one exponential in the code for all places: a kernel that runs once per row waits for its own instructions as well)
 #pragma unroll 1
     for (int k = lane_id(); k < a.K; k += kWave) {
@@ -146,21 +147,21 @@ __device__ __forceinline__ Teacher teacher_of(const DistillArgs& a, int64_t b, L
         const double d = static_cast<double>(list.places[k].t) - static_cast<double>(r.t0), q = exp(d);
         list.places[k].q = q;
         r.sum += q;
-        if (!(q == 0.0)) r.weighted += q * d;
+        if (!dup && !(q == 0.0)) r.weighted += q * d;
     }
     r.sum = wave_sum(r.sum);
-    r.weighted = wave_sum(r.weighted);
     const double scale = a.tail ? 1.0 : 1.0 / r.sum;
-    const bool dup = __ballot(twice) != 0ull;
 #pragma unroll 1
     for (int k = lane_id(); k < a.K; k += kWave) {
         double q = list.places[k].q;
         if (dup && list.places[k].once) {
             const int32_t id = list.labels[k];
             for (int j = k + 1; j < a.K; ++j) if (list.labels[j] == id) q += list.places[j].q;
+            if (!(q == 0.0)) r.weighted += q * log(q);
         }
         list.places[k].q_all = static_cast<float>(q * scale);
     }
+    r.weighted = wave_sum(r.weighted);
     return r;
 }
 // 2^n of the size of x (or 1), by which factors are kept from being rounded in an exponent.

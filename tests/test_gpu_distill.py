@@ -188,3 +188,36 @@ def test_in_place_and_rows_further_apart(B, V, ld, dtype, tail):
     wide = torch.full((B + 2, ld + 3), 9.0, dtype=F32, device=DEV)
     _check(X, labels, teacher, weight, tail=tail, out=F32, target=wide[:B, :V])
     assert (wide[:, V:] == 9).all() and (wide[B:] == 9).all()
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,V,K", [(6, 50, 5), (4, 4096, 256), (300, 9001, 70), (5, 70001, 130), (70, 131072, 66), (80, 40003, 64)])
+def test_labels_listed_several_times(B, V, K, dtype, tail):
+    """A label's probability is the sum over its places, in the loss as well as in the gradient: rows that a workgroup holds, rows in two
+    launches, in three (in place), the loss alone; repeats next to each other and 64 places and more apart."""
+    g = torch.Generator().manual_seed(B + K)
+    X = (2.5 * torch.randn((B, V), generator=g)).to(dtype)
+    pool = torch.randperm(V, generator=g)[: max(2, K // 3)]
+    labels = pool[torch.randint(0, len(pool), (B, K), generator=g)].to(torch.int32)
+    labels[0] = labels[0, 0]
+    labels[1, ::2] = labels[1, 0]
+    labels[2, -1] = labels[2, 0]
+    labels[3, torch.rand(K, generator=g) < 0.4] = -1
+    share = torch.rand((B, K), generator=g) + 0.01
+    teacher = (0.9 * share / share.sum(1, keepdim=True)).log()           # a tenth is left for the others
+    if not tail:
+        teacher += 2.0
+    weight = torch.rand(B, generator=g) + 0.1
+    _check(X, labels, teacher, weight, tail=tail)
+    place = X.to(DEV)
+    _check(X, labels, teacher, weight, tail=tail, given=place, target=place)
+
+
+def test_a_label_that_is_listed_twice_and_has_all_of_both_distributions():
+    import paper_2409_20156_amd as xc
+    X = torch.full((1, 50), -80.0, device=DEV)
+    X[0, 3] = 20.0
+    loss, dX = xc.distill(X, torch.tensor([[3, 3]], dtype=torch.int32, device=DEV), torch.zeros((1, 2), device=DEV))
+    # (log S is off by 60 u: all of the sum is one exponential)
+    assert abs(loss.item()) <= 60 * U and dX.abs().max().item() <= 40 * U

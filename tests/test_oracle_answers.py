@@ -94,3 +94,21 @@ def test_scales():
     for m, e in ((1.0, -2), (7.9, 0), (8.0, 1), (0.49, -4), (2.0 ** -126, -127), (2.0 ** -140, -127), (2.0 ** 127, 125)):
         assert ao.scale_byte(m) == e + 127
     assert ao.scale_byte(0.0) == 0 and ao.scale_byte(math.inf) == 255
+
+
+@pytest.mark.parametrize("T", [1.0, 2.0])
+@pytest.mark.parametrize("tail", [False, True])
+def test_a_label_listed_several_times_is_one_label(tail, T):
+    """Loss and gradient are those of the list in which every label stands once, with the sum of its probabilities."""
+    rng, X = _scores(9, 4, 12)
+    labels = np.array([[3, 3, 3, 3, 3], [0, 7, 0, 7, 11], [5, -1, 5, 12, 2], [1, 2, 3, 4, 1]])
+    q = rng.dirichlet(np.ones(6), size=4)[:, :5]
+    once, merged = np.full((4, 5), -1), np.zeros((4, 5))
+    for b in range(4):
+        for j, v in enumerate(dict.fromkeys(v for v in labels[b].tolist() if 0 <= v < 12)):
+            once[b, j], merged[b, j] = v, np.log(q[b][labels[b] == v].sum())
+    a, b = ao.distill(X, labels, np.log(q), T, tail), ao.distill(X, once, merged, T, tail)
+    assert np.abs(a[0] - b[0]).max() < 1e-13 and np.abs(a[1] - b[1]).max() < 1e-13
+    if not tail:                                           # the student has nothing but the label: no divergence
+        X[0], X[0, 3] = -np.inf, 1.0
+        assert abs(ao.distill(X, labels, np.log(q), T)[0][0]) < 1e-13
