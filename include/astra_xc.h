@@ -11,7 +11,7 @@
  *   - Every data pointer is a DEVICE pointer owned by the caller.  The library
  *     allocates nothing; temporary memory is a caller-provided workspace whose
  *     size is asked for first (xc_*_workspace).  Workspaces and all arrays must
- *     be 16-byte aligned.
+ *     be 16-byte aligned, unless a call says otherwise.
  *   - Work is enqueued on the HIP stream passed as `stream` (a hipStream_t cast
  *     to void*, NULL = the default stream).  No call synchronises; results,
  *     including scalars, appear in device memory in stream order.
@@ -291,7 +291,7 @@ int xc_scores_quantized(const void* Z /* [B*d] */, int64_t B, int d, xc_dtype t,
  * gets zeros and scale 255, which makes every score with its row not a number.
  * ids, m, count as in xc_quantize_rows.  Requires 1 <= N < 2^31, m >= 0, d*sizeof(element) a
  * multiple of 16, d <= XC_MAX_D_QUANTIZED; Q and scale may overlap neither each other nor an
- * input (XC_EINVAL).
+ * input (XC_EINVAL).  scale has to be aligned to 4 bytes only: any range of rows may be written.
  * ------------------------------------------------------------------------- */
 int xc_microscale_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
                        const int32_t* ids /* [m] or NULL */, int64_t m, const int32_t* count /* [1] or NULL */,
@@ -303,8 +303,9 @@ int xc_microscale_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
  *   out[i*L + l] = sum over blocks of 2^(s_i + s_l - 254) * (sum over the block of p_i q_l),
  * sums in fp32 in an order that depends on d alone, rounded to out_t at the end: a score does not
  * depend on how many queries or labels are scored with it, bit for bit.  Q and scale are what
- * xc_microscale_rows gives for the classifier (or for a contiguous range of its rows).  The
- * workspace holds the 4-bit rows of Z; it is written before it is read.
+ * xc_microscale_rows gives for the classifier (or a contiguous range of its rows, from any row on:
+ * scale has to be aligned to 4 bytes only).  The workspace holds the 4-bit rows of Z; it is written
+ * before it is read.
  * Requires B >= 1, 1 <= L < 2^31, B*L <= 2^40, d as above; out and the workspace may
  * overlap neither each other nor an input (XC_EINVAL).
  * ------------------------------------------------------------------------- */

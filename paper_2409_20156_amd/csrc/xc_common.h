@@ -46,6 +46,7 @@ void profile_mark(int kernel_id, hipStream_t st, bool begin);
     } while (0)
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
 // Arrays of a call by address and size: those it writes may overlap neither each other nor what it reads.
 struct Span {

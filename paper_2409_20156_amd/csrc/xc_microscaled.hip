@@ -691,6 +691,7 @@ void scores_micro_tile_kernel(const MicroArgs a, uint32_t tiles_m, uint32_t tile
 // ---------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------
+// (a row has 4 bytes of scales to a unit, read and written as a word: `scale` of a range of rows is aligned to as much, whichever its first row)
 static bool micro_d(int d, xc_dtype t) { return d >= 1 && d <= XC_MAX_D_QUANTIZED && (static_cast<int64_t>(d) * (t == XC_F32 ? 4 : 2)) % 16 == 0; }
 
 // The queries in the workspace: rows padded to whole pairs of units, their number to whole tiles of 64.
@@ -806,7 +807,7 @@ extern "C" int xc_microscale_rows(const void* X, int64_t N, int d, xc_dtype t, c
     if (t != XC_F32 && t != XC_BF16) return XC_EDTYPE;
     if (N < 1 || N > 0x7fffffffLL || !micro_d(d, t) || m < 0) return XC_ESHAPE;
     if (!X || !Q || !scale || (count && !ids)) return XC_EINVAL;
-    if (!aligned16(X) || !aligned16(ids) || !aligned16(count) || !aligned16(Q) || !aligned16(scale)) return XC_EINVAL;
+    if (!aligned16(X) || !aligned16(ids) || !aligned16(count) || !aligned16(Q) || !aligned4(scale)) return XC_EINVAL;
     const unsigned __int128 n = N;
     if (overlap({Span(Q, n * (mx_pitch(d) / 2)), Span(scale, n * (mx_pitch(d) / 32))},
                 {Span(X, n * d * (t == XC_F32 ? 4 : 2)), Span(ids, static_cast<unsigned __int128>(m) * 4), Span(count, 4)}))
@@ -830,7 +831,7 @@ extern "C" int xc_scores_microscaled(const void* Z, int64_t B, int d, xc_dtype t
     if ((t != XC_F32 && t != XC_BF16) || (out_t != XC_F32 && out_t != XC_BF16)) return XC_EDTYPE;
     if (B < 1 || B > 0x7fffffffLL || L < 1 || L > 0x7fffffffLL || !micro_d(d, t) || static_cast<unsigned __int128>(B) * L > (1ull << 40)) return XC_ESHAPE;
     if (!Z || !Q || !scale || !out || !ws) return XC_EINVAL;
-    if (!aligned16(Z) || !aligned16(Q) || !aligned16(scale) || !aligned16(out) || !aligned16(ws)) return XC_EINVAL;
+    if (!aligned16(Z) || !aligned16(Q) || !aligned4(scale) || !aligned16(out) || !aligned16(ws)) return XC_EINVAL;
     const MicroSpace space = micro_space(B, d);
     if (ws_bytes < space.bytes) return XC_EWORKSPACE;
     const unsigned __int128 b = B, l = L;

@@ -190,3 +190,15 @@ def test_binding_refuses_before_it_calls():
         else:
             with pytest.raises(ValueError):
                 binding._rows_at(one_, "X")
+
+
+def test_scales_of_a_range_of_rows(lib):  # noqa: F811
+    """A row of up to 128 elements has 4 bytes of scales: those of a range of rows begin at any multiple of 4."""
+    far = [(1 << 40) + (i << 20) for i in range(6)]
+    rc, need = _size(lib.xc_scores_microscaled_workspace, 100, 72)
+    assert rc == 0
+    for by in range(16):
+        # (a workspace that is too small, and an empty list, are found behind the addresses: nothing is launched)
+        scores = lib.xc_scores_microscaled(far[0], 100, 72, 1, far[1], far[2] + by, 1000, 0, far[3], far[4], need - 1, None)
+        rows = lib.xc_microscale_rows(far[0], 10, 64, 1, far[1], 0, None, far[2], far[3] + by, None)
+        assert (scores, rows) == ((EWORKSPACE, 0) if by % 4 == 0 else (EINVAL, EINVAL)), by

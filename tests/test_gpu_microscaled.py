@@ -189,3 +189,22 @@ def test_outputs_end_where_they_should():
             assert (q[0] == 77).all() and (q[-1] == 77).all() and (s[:16] == 77).all() and (s[16 + L * pitch // 32:] == 77).all()
             assert (buf[:32] == -7).all() and (buf[32 + B * L:] == -7).all()
             assert torch.equal(out, xc.scores_microscaled(Z, q[1:-1].clone(), sv.clone(), dtype=dtype))
+
+
+@pytest.mark.parametrize("d", [72, 128, 256, 768, 1280, 4200])
+def test_ranges_of_rows_as_they_lie(d):
+    """Rows from any row on, without a copy: their scales begin at any multiple of 4 bytes.  Few queries, many, and labels held in registers."""
+    import paper_2409_20156_amd as xc
+    W = _matrix(d, 8400, d, BF16).to(DEV)
+    Q, s = xc.microscale_rows(W)
+    pitch = xc.microscaled_pitch(d)
+    for B in (3, 100, 4200 if d <= 1024 else 300):
+        Z = _matrix(B, B, d, BF16).to(DEV)
+        whole = xc.scores_microscaled(Z, Q, s, dtype=BF16)
+        for lo, hi in ((1, 8400), (2, 8399), (3, 4200), (5, 6), (7, 80)):
+            assert torch.equal(xc.scores_microscaled(Z, Q[lo:hi], s[lo:hi], dtype=BF16), whole[:, lo:hi]), (B, lo, hi)
+    for lo, hi in ((1, 8400), (3, 50), (6, 7)):
+        q2, s2 = torch.full((8400, pitch // 2), 77, dtype=torch.uint8, device=DEV), torch.full((8400, pitch // 32), 77, dtype=torch.uint8, device=DEV)
+        xc.microscale_rows(W[lo:hi], out=(q2[lo:hi], s2[lo:hi]))
+        assert torch.equal(q2[lo:hi], Q[lo:hi]) and torch.equal(s2[lo:hi], s[lo:hi])
+        assert (q2[:lo] == 77).all() and (q2[hi:] == 77).all() and (s2[:lo] == 77).all() and (s2[hi:] == 77).all()
