@@ -268,8 +268,9 @@ int xc_quantize_rows(const void* X /* [N*d] */, int64_t N, int d, xc_dtype t,
  *   out[i*L + l] = (<p_i, q_l> * a_i) * scale[l],
  * <p, q> exact in 32-bit integers, then rounded to fp32, multiplied in fp32 and
  * rounded to out_t at the end.  Q and scale are what xc_quantize_rows gives for the
- * classifier (or for a contiguous range of its rows).  The workspace holds the
- * integers of Z; it is written before it is read.
+ * classifier (or for a contiguous range of its rows, from a multiple of 4 on: scale is
+ * aligned to 16 bytes as all arrays are).  The workspace holds the integers of Z; it is
+ * written before it is read.
  * A score does not depend on how many queries or labels are scored with it, bit for bit.
  * Requires B >= 1, 1 <= L < 2^31, B*L <= 2^40, d as above; out and the workspace may
  * overlap neither each other nor an input (XC_EINVAL).
