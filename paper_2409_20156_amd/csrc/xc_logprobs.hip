@@ -134,41 +134,117 @@ __device__ __forceinline__ void end_keys(uint64_t* keys, int n) {
     if (threadIdx.x < 3) keys[n + threadIdx.x] = kKeySentinel;
 }
 
-// Of a block's elements (read again, so that this takes few registers from what always runs) the k best, by halving the range of their keys, to
-// `keys`; k of them at least score `least` or more.  Where a threshold lets through more labels than a workgroup holds, that is where many
-// scores are equal.
+// Of a stretch of blocks in which more labels score `least` or more than a workgroup holds (`room` or more of them): the k best, or up to `room`
+// that reach a score which k of them reach; to `keys`, kept[0] of them.  That is where many scores are equal, or grow along the row.  The stretch
+// is read again a few times, so that this takes few registers from what always runs.  `least`, or a score that k of the threads' largest ones
+// reach, is mostly the answer, or more than k labels share it: of equal labels the first ones are taken in their order, by counting.  Else the
+// range above it is halved, 32 times at most.  (2048 x 131072 bf16 with 64 top labels: 112 to 116 us for normal scores, 128 to 141 for rows of one
+// value, of three, or masked with the type's lowest value but for three labels, where halving keys of score and label and looking at every
+// stretch took 18 ms; 507 for rows that grow from end to end.)  `range`, `counts` and `largest` [kRowThreads] are free again after the caller's next barrier.
 template <typename T>
-__device__ __forceinline__ void best_of_block(const PiecedRow<T>& row, int64_t first, int64_t end, int64_t edge, int k, uint32_t least, int* counts, uint64_t* keys,
-                                              int* kept) {
+__device__ __forceinline__ void best_of_stretch(const PiecedRow<T>& row, int first, int end, int edge, int k, int room, uint32_t least, uint32_t* largest,
+                                                uint32_t (&range)[2], int2 (&counts)[2][kRowWaves], uint64_t* keys, int* kept) {
     constexpr int N = PiecedRow<T>::N;
-    uint64_t lo = 0, hi = (static_cast<uint64_t>(~least) << 32) | 0xffffffffu;            // fewer than k keys up to lo, k at least up to hi
-    for (int turn = 1;; turn ^= 1) {
-        const bool done = hi - lo <= 1;
-        const uint64_t mid = done ? hi : lo + (hi - lo) / 2;
-        int n = 0;
+    const int wave = threadIdx.x >> 6;
+    uint32_t lo = least, hi = 0u, mid = least;               // k labels or more reach lo, fewer reach hi (0: not known yet)
+    int turn = 0, want = 0;                                  // (one buffer of the counts is read while the other is written)
+    bool done = false;
+    if (threadIdx.x == 0) *kept = 0;
+    for (;;) {
+        const float t = ordered_to_float(mid), next = ordered_to_float(mid + 1u);            // (behind +infinity: not a number, which nothing reaches)
+        float most = kNone;
+        int n = 0, above = 0, taken = 0;
+        // the row's edges before its pieces, the pieces, the edges behind them
 #pragma unroll 1
-        for (int64_t at = first + threadIdx.x - kRowThreads; at < end; at += kRowThreads) {        // (before the pieces: the edge)
-            const bool edges = at < first;
-            if (edges && edge < 0) continue;
-            const T* p = row.p + (edges ? edge : row.first(at));
-#pragma unroll 1
-            for (int e = 0; e < (edges ? 1 : N); ++e) {
-                const float x = Elem<T>::get(p + e);
-                const uint64_t key = x == x ? make_key(x + 0.0f, static_cast<int32_t>(p + e - row.p)) : kKeySentinel;
-                if (key > mid) continue;
-                ++n;
-                if (done) keys[atomicAdd(kept, 1)] = key;
+        for (int at0 = first - kRowThreads;; at0 += kRowThreads) {
+            const int at = at0 + static_cast<int>(threadIdx.x);
+            const bool inside = at0 >= first && at0 < end;   // uniform
+            int id = edge;
+            uint4 v = Elem<T>::none();
+            float x0 = kNone;
+            if (inside) {
+                id = static_cast<int>(row.first(at));
+                if (at < end) v = row.template load<false>(at);
+                x0 = Elem<T>::value(v, 0);
+            } else if (edge >= 0 && (at0 < first) == (edge < row.head)) {
+                x0 = Elem<T>::get(row.p + edge);
             }
-        }
-        if (done) return;                                    // uniform
+            uint32_t which = x0 >= t ? 1u : 0u, over = x0 >= next ? 1u : 0u;
+            most = fmaxf(most, x0);
 #pragma unroll
-        for (int off = kWave / 2; off > 0; off >>= 1) n += __shfl_xor(n, off, kWave);
-        if (threadIdx.x == 0) counts[turn] = 0;
+            for (int e = 1; e < N; ++e) {
+                const float x = Elem<T>::value(v, e);
+                which |= x >= t ? 1u << e : 0u;
+                over |= x >= next ? 1u << e : 0u;
+                most = fmaxf(most, x);
+            }
+            n += __popc(which);
+            above += __popc(over);
+            if (done) {                                      // uniform, as all that follows but the labels themselves
+                int at_tie = want;                           // of the thread's labels that score t, the first one's place among all
+                if (taken < want) {
+                    const int own = __popc(which & ~over), upto = wave_incl_scan(own);
+                    turn ^= 1;
+                    if (lane_id() == kWave - 1) counts[turn][wave].x = upto;
+                    __syncthreads();
+                    at_tie = taken + upto - own;
+#pragma unroll
+                    for (int w = 0; w < kRowWaves; ++w) {
+                        const int c = counts[turn][w].x;
+                        if (w < wave) at_tie += c;
+                        taken += c;
+                    }
+                }
+                if (want == 0) which = over;
+#pragma unroll 1
+                for (; which != 0u; which &= which - 1u) {
+                    const int e = __ffs(static_cast<int>(which)) - 1;
+                    const float x = Elem<T>::get(row.p + id + e);
+                    if (x >= next || at_tie++ < want) keys[atomicAdd(kept, 1)] = make_key(x + 0.0f, id + e);
+                }
+            }
+            if (at0 >= end) break;
+        }
+        if (done) return;
+        turn ^= 1;
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1) {
+            n += __shfl_xor(n, off, kWave);
+            above += __shfl_xor(above, off, kWave);
+        }
+        if (lane_id() == 0) counts[turn][wave] = make_int2(n, above);
+        if (hi == 0u) largest[threadIdx.x] = float_to_ordered(most + 0.0f);
         __syncthreads();
-        if (lane_id() == 0) atomicAdd(&counts[turn], n);
-        __syncthreads();
-        if (counts[turn] >= k) hi = mid;
-        else lo = mid;
+        n = above = 0;
+#pragma unroll
+        for (int w = 0; w < kRowWaves; ++w) {
+            n += counts[turn][w].x;
+            above += counts[turn][w].y;
+        }
+        if (n >= k && (above < k || n <= room)) {
+            done = true;
+            want = n <= room ? 0 : k - above;                // of the labels that score t, the first ones
+            if (n <= room) --mid;                            // (all that reach t: those above the number before it)
+        } else if (hi == 0u) {
+            if (threadIdx.x < kWave) {
+                uint32_t top = 0u;
+#pragma unroll
+                for (int g = 0; g < kRowWaves; ++g) top = largest[g * kWave + lane_id()] > top ? largest[g * kWave + lane_id()] : top;
+                top = wave_max_u32(top);
+                const uint32_t r = reached_by<kRowWaves>(kRowThreads, k, [&](int i) __attribute__((always_inline)) { return largest[i]; });
+                if (threadIdx.x == 0) {
+                    range[0] = r > least ? r : least + 1u;
+                    range[1] = top + 1u;
+                }
+            }
+            __syncthreads();
+            mid = lo = range[0];
+            hi = range[1];
+        } else {
+            if (n >= k) lo = mid + 1u;
+            else hi = mid;
+            mid = lo + (hi - lo) / 2u;
+        }
     }
 }
 
@@ -181,16 +257,18 @@ __device__ __forceinline__ void best_of_block(const PiecedRow<T>& row, int64_t f
 // spend as much on these as on 64.
 // Bound: 1024 x 131072 bf16 without top labels 44 to 50 us, one read at 5.4 to 6.1 TB/s; 2048 rows with 64 of them 113 us, 4.8 TB/s: vector
 // instructions are under way for 0.7 to 0.8 of the time (the exponential, the sums, the largest of every piece against the threshold).
+// (C <= 2: five waves to a SIMD, which what runs for crowded stretches alone would take a register too many for.)
 template <typename T, int C>
-__global__ __launch_bounds__(kRowThreads, 4)
+__global__ __launch_bounds__(kRowThreads, C <= 2 ? 5 : 4)
 void logprobs_kernel(const LogprobArgs a) {
     constexpr int N = PiecedRow<T>::N, E = C * N;
     __shared__ Sums sums[kRowWaves];
     __shared__ uint32_t largest[kRowThreads];
     __shared__ __align__(16) uint64_t lists[2][kTopKeys + 4];
     __shared__ int noted[kRowWaves][kWave + kWave * C];      // pieces, counted from the segment's first
-    __shared__ uint32_t reach;
-    __shared__ int found, counts[2], kept;
+    __shared__ uint32_t reach, range[2];
+    __shared__ int2 counts[2][kRowWaves];
+    __shared__ int found, kept;
     const int64_t b = blockIdx.x / static_cast<uint32_t>(a.segments), seg = blockIdx.x - b * a.segments;
     const PiecedRow<T> row(static_cast<const T*>(a.X) + b * a.ld, a.V);
     const int64_t begin = seg * a.length, end = begin + a.length < row.pieces ? begin + a.length : row.pieces;
@@ -211,19 +289,20 @@ void logprobs_kernel(const LogprobArgs a) {
     int have = 0;                                            // keys from the blocks before
     // the threshold among the keys, and what reaches it, in the other list; by the whole workgroup
     auto thin = [&]() __attribute__((always_inline)) {
-        __syncthreads();                                     // (`kept` and `reach` have been read)
+        __syncthreads();                                     // (`kept` and `range` have been read)
         if (threadIdx.x < kWave) {
             const uint32_t* words = reinterpret_cast<const uint32_t*>(keys);
             auto value = [&](int i) __attribute__((always_inline)) { return ~words[2 * i + 1]; };
             const uint32_t r = have <= 4 * kWave ? reached_by<4>(have, a.k, value) : reached_by<kTopKeys / kWave>(have, a.k, value);
             if (threadIdx.x == 0) {
-                reach = r > reach ? r : reach;
+                range[0] = r;                                // (may be below `reach`, see the end of a stretch)
+                if (r > reach) reach = r;
                 kept = 0;
             }
         }
         __syncthreads();
         uint64_t* other = keys == lists[0] ? lists[1] : lists[0];
-        const uint32_t r = reach;
+        const uint32_t r = range[0];
         for (int i = threadIdx.x; i < have; i += kRowThreads)
             if (~static_cast<uint32_t>(keys[i] >> 32) >= r) other[atomicAdd(&kept, 1)] = keys[i];
         __syncthreads();
@@ -310,19 +389,27 @@ void logprobs_kernel(const LogprobArgs a) {
         if (!ends) continue;
         __syncthreads();
         const int now = found;
-        if (__builtin_expect(have + now > kTopKeys, 0)) {    // uniform, as all of these
-            if (threadIdx.x == 0) kept = 0;
-            __syncthreads();
-            best_of_block<T>(row, since, stop, n == 0 ? edge : -1, a.k, reach, counts, keys + have, &kept);
+        const bool crowded = have + now > kTopKeys;          // uniform, as all of these
+        if (__builtin_expect(crowded, 0)) {
+            best_of_stretch<T>(row, static_cast<int>(since), static_cast<int>(stop), n == 0 ? static_cast<int>(edge) : -1, a.k, kTopKeys - have, reach,
+                               largest, range, counts, keys + have, &kept);
             __syncthreads();
             have += kept;
         } else {
             have += now;
         }
         if (have > a.k + a.k / 2 + 8) thin();
-        if (last || have > kTopKeys / 2) cut();
+        if (last || crowded || have > kTopKeys / 2) cut();
         __syncthreads();                                     // (everyone has read `found`)
-        if (threadIdx.x == 0) found = 0;
+        if (threadIdx.x == 0) {
+            found = 0;
+            // What scores as the k-th best label does and lies behind it is worse: where scores are equal, no label of the blocks to come is
+            // looked at again.  (The elements behind the row's last piece were looked at with the first block.)
+            if (crowded && have == a.k) {
+                const uint32_t o = ~static_cast<uint32_t>(keys[have - 1] >> 32) + (key_id(keys[have - 1]) < row.first(row.pieces) ? 1u : 0u);
+                if (o > reach) reach = o;
+            }
+        }
         __syncthreads();
         least = ordered_to_float(reach);
         since = stop;

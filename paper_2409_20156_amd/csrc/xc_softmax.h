@@ -18,12 +18,17 @@ template <> struct Elem<float> {
     static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
     static __device__ __forceinline__ uint4 none() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
     static __device__ __forceinline__ void values(const uint4& v, float (&f)[4]) { __builtin_memcpy(f, &v, 16); }
+    static __device__ __forceinline__ float value(const uint4& v, int e) { return __uint_as_float(e == 0 ? v.x : e == 1 ? v.y : e == 2 ? v.z : v.w); }
 };
 template <> struct Elem<bf16_t> {
     static __device__ __forceinline__ float get(const bf16_t* p) { return bf16_bits_to_float(p->bits); }
     static __device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = static_cast<uint16_t>(float_to_bf16_bits(v)); }
     static __device__ __forceinline__ uint4 none() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     static __device__ __forceinline__ void values(const uint4& v, float (&f)[8]) { unpack8(v, f); }
+    static __device__ __forceinline__ float value(const uint4& v, int e) {
+        const uint32_t two = e < 2 ? v.x : e < 4 ? v.y : e < 6 ? v.z : v.w;
+        return __uint_as_float((e & 1) != 0 ? two & 0xffff0000u : two << 16);
+    }
 };
 
 // N neighbouring elements at an address that may be any (nearest, ties to even)
