@@ -2,6 +2,7 @@
 // 32 neighbouring elements of a row share a scale 2^(byte - 127); an element is a sign, two bits of exponent and one of mantissa: 0, 0.5, 1,
 // 1.5, 2, 3, 4 or 6.  The largest magnitude of a block decides the scale: the power of two that brings it into [4, 8).  What lies beyond 6
 // then is 6 (the format's published conversion, so that rows laid out elsewhere mean the same here).
+#include "xc_microscaled_choice.h"
 #include "xc_mine.h"
 
 namespace xc {
@@ -215,7 +216,6 @@ __device__ __forceinline__ const void* mx_uniform(const void* p) {
 // scales: 1 x 131072 x 768 14.5 us, 1 x 670000 x 768 68, against 10.2 and 51 (5.3 TB/s).  Lane l has labels 4 (l % 16) .. + 3 of the 64, so
 // that it stores neighbouring scores.  TZ: what the queries are brought to 4 bits from by every workgroup for itself (void: they are in the workspace).
 // Bound: one read of Q.
-constexpr int kMicroFew = 16;                            // queries at most
 constexpr int kFewSlot = 64 * 128 + 2 * 64 * 4;          // a step of 64 labels, their scales
 constexpr int kFewLoads = 8 + 2;
 template <int N> __device__ __forceinline__ void few_wait() { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(N) : "memory"); }
@@ -225,7 +225,7 @@ __device__ __forceinline__ void lds_dma4_sbase(const void* sbase /* wave-uniform
 template <typename TO, typename TZ, int KU, int W, int R>
 __global__ __launch_bounds__(W * kWave)
 void scores_micro_few_kernel(const MicroArgs a) {
-    constexpr int kRows = kMicroFew, kUpad = (KU + 3) / 4 * 4;
+    constexpr int kRows = kMicroFewQueries, kUpad = (KU + 3) / 4 * 4;
     __shared__ __align__(1024) unsigned char ring[W][R][kFewSlot];
     __shared__ __align__(1024) unsigned char codes[kRows * KU * 64];       // 128 bytes of every row, the next 128, ..; chunks of 16 swizzled
     __shared__ __align__(16) unsigned char scales[kRows * 4 * kUpad];
@@ -363,14 +363,13 @@ void scores_micro_few_kernel(const MicroArgs a) {
 // stored, 157 us of a fill; matrix pipe busy 47 % of the time); with a sixth of the products 208, without the stores 163.
 template <int NK_>
 struct MicroHeld {
-    static constexpr int NK = NK_, QS = 64, kUpad = NK <= 4 ? 4 : 8, kStage = QS * NK * 64, kScales = QS * 4 * kUpad;
+    static constexpr int NK = NK_, QS = kMicroHeldQueries, kUpad = NK <= 4 ? 4 : 8, kStage = QS * NK * 64, kScales = QS * 4 * kUpad;
     static constexpr int kTurn = 2048;                                                       // of a wave, to turn its labels in
     static constexpr int kFit = (160 * 1024 - 8 * kTurn - 1024) / (kStage + kScales), R = kFit < 6 ? kFit : 6;        // stages in LDS
     static constexpr int kLoads = kStage / 1024 / 8, kStores = QS / 4;                      // of a wave and stage
     static constexpr int kLds = R * (kStage + kScales) + 8 * kTurn;
     static_assert(kLoads * 8 * 1024 == kStage && R >= 3 && (kLoads + kStores) * (R - 3) < 64, "whole loads, and a count that the wait can hold");
 };
-constexpr int kMicroHeldLabels = 512;
 constexpr int kMicroPieces = 4;                          // of the tiles behind the last whole round, to a workgroup
 
 template <typename TO, int NK>
@@ -707,11 +706,10 @@ static MicroSpace micro_space(int64_t B, int d) {
 }
 
 constexpr int64_t kMxCachedBytes = 256ll << 20;
-constexpr int kMicroFewUnits = 8, kMicroFewLong = 32, kMicroHeldUnits = 8;
 
 template <typename TO, typename TZ, int KU, int W, int R>
 static void launch_few(const MicroArgs& a, hipStream_t st) {
-    constexpr int kLds = W * R * kFewSlot + kMicroFew * (KU * 64 + (KU + 3) / 4 * 16), kPerCu = 160 * 1024 / (kLds + 1024);
+    constexpr int kLds = W * R * kFewSlot + kMicroFewQueries * (KU * 64 + (KU + 3) / 4 * 16), kPerCu = 160 * 1024 / (kLds + 1024);
     static_assert(kPerCu >= 1, "");
     const int64_t groups = (a.L + 63) / 64, per = ((groups + kXcds - 1) / kXcds + W - 1) / W, most = kCusPerXcd * kPerCu;
     scores_micro_few_kernel<TO, TZ, KU, W, R><<<static_cast<unsigned>(kXcds * (per < most ? per : most)), W * kWave, 0, st>>>(a);
@@ -739,56 +737,46 @@ static void launch_micro_tile(const MicroArgs& a, hipStream_t st) {
     }
 }
 
-// Tiles of 128 x 128, two workgroups of them to a compute unit, or of 256 x 256: whichever's rounds take less, a round of large ones
-// 5/3 of the others' (d = 2048, small against large: 2000 x 2000 18.3 us against 27.8, 300 x 50021 40.9 against 44.3, 2000 x 6000 29.0
-// against 28.2, 4096 x 4096 35.3 against 29.5; 4096 x 131072 x 4096 1817 against 1346).
-static bool small_tiles(const MicroArgs& a) {
-    auto rounds = [&](int64_t side, int64_t at_once) { return ((a.B + side - 1) / side * ((a.L + side - 1) / side) + at_once - 1) / at_once; };
-    return rounds(MicroTile<2, 4, 8>::BM, kMineGrid * MicroTile<2, 4, 8>::kPerCu) * 5 > rounds(MicroTile<2, 2, 4>::BM, kMineGrid * MicroTile<2, 2, 4>::kPerCu) * 3;
-}
-// Labels in registers: from four stages to a compute unit on, for more than 256 queries (a tile's labels cost a workgroup as much as several
-// stages) and tiles for all XCDs.  Held against in tiles, d = 768: 64 x 670000 92 us and 82, 256 x 64000 19.9 and 17.6, 2000 x 8000 18.5 and
-// 18.1, 2000 x 16000 25.0 and 26.0, 400 x 131072 43.5 and 49.9, 10000 x 2000 35 and 28, 10000 x 4000 38 and 46, 10000 x 64000 300 and 460.
-static bool hold_labels(const MicroArgs& a) {
-    const int64_t tiles = (a.L + kMicroHeldLabels - 1) / kMicroHeldLabels, stages = (a.B + MicroHeld<2>::QS - 1) / MicroHeld<2>::QS;
-    return a.units <= kMicroHeldUnits && a.B > 256 && tiles >= kXcds && tiles * stages >= 4 * kMineGrid;
-}
-constexpr int64_t kMicroInline = 128;                    // units of queries: two rounds of a workgroup's loads (16 x 131072 x 4096, 512 of
-                                                         // them: 81 us, in a launch of their own 64; 4 x 2487 x 3280, 104: 14.7 against 18.8 with one round)
+typedef MicroTile<2, 2, 4> SmallTile;
+typedef MicroTile<2, 4, 8> LargeTile;
+static_assert(kMicroCus == kMineGrid && kMicroXcds == kXcds && SmallTile::BM == kMicroSmallSide && SmallTile::BN == kMicroSmallSide &&
+              SmallTile::kPerCu == kMicroSmallPerCu && LargeTile::BM == kMicroLargeSide && LargeTile::BN == kMicroLargeSide &&
+              LargeTile::kPerCu == kMicroLargePerCu, "what the choice counts with");
 
 template <typename TO>
 static int run_micro(MicroArgs a, const void* Z, xc_dtype t, const MicroSpace& space, hipStream_t st) {
     a.Z = static_cast<const unsigned char*>(Z);
-    if (a.B <= kMicroFew && a.units <= kMicroFewLong && a.B * a.units <= kMicroInline) {     // every workgroup brings the queries to 4 bits for itself: one launch
+    const MicroKernel kernel = choose_micro(a.B, a.L, a.units);
+    if (kernel == kMicroOnline) {                            // one launch
         auto go = [&]() {
-            if (a.units <= kMicroFewUnits) {
-                if (t == XC_F32) launch_few<TO, float, kMicroFewUnits, 4, 2>(a, st);
-                else launch_few<TO, bf16_t, kMicroFewUnits, 4, 2>(a, st);
+            if (a.units <= kMicroShortUnits) {
+                if (t == XC_F32) launch_few<TO, float, kMicroShortUnits, 4, 2>(a, st);
+                else launch_few<TO, bf16_t, kMicroShortUnits, 4, 2>(a, st);
             } else {
-                if (t == XC_F32) launch_few<TO, float, kMicroFewLong, 4, 3>(a, st);
-                else launch_few<TO, bf16_t, kMicroFewLong, 4, 3>(a, st);
+                if (t == XC_F32) launch_few<TO, float, kMicroFewUnits, 4, 3>(a, st);
+                else launch_few<TO, bf16_t, kMicroFewUnits, 4, 3>(a, st);
             }
         };
         XC_LAUNCH(K_SCORES_MICRO, st, go());
         XC_HIP_CHECK(hipGetLastError());
         return XC_OK;
     }
-    const bool few = a.B <= kMicroFew && a.units <= kMicroFewLong, held = !few && hold_labels(a);
     uint8_t *P = const_cast<uint8_t*>(a.P), *pscale = const_cast<uint8_t*>(a.pscale);
-    const int rc = held || few ? launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroQueries{P, pscale, space.units, space.pitch, space.upad}, space.rows, space.pitch / 64, st)
-                               : launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroRows{P, pscale, space.units}, a.B, space.units, st);
+    const bool padded = kernel == kMicroHeld || kernel == kMicroFew;
+    const int rc = padded ? launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroQueries{P, pscale, space.units, space.pitch, space.upad}, space.rows, space.pitch / 64, st)
+                          : launch_microscale(Z, a.B, a.d, t, nullptr, 0, nullptr, MicroRows{P, pscale, space.units}, a.B, space.units, st);
     if (rc != XC_OK) return rc;
     auto go = [&]() {
-        if (held) {
+        if (kernel == kMicroHeld) {
             switch (space.pitch / 128) {
                 case 1: launch_micro_held<TO, 2>(a, st); break;
                 case 2: launch_micro_held<TO, 4>(a, st); break;
                 case 3: launch_micro_held<TO, 6>(a, st); break;
                 default: launch_micro_held<TO, 8>(a, st); break;
             }
-        } else if (few) {
-            launch_few<TO, void, kMicroFewLong, 4, 3>(a, st);          // (shorter rows of as many queries went the way above)
-        } else if (small_tiles(a)) {
+        } else if (kernel == kMicroFew) {
+            launch_few<TO, void, kMicroFewUnits, 4, 3>(a, st);         // (shorter rows of as many queries went the way above)
+        } else if (kernel == kMicroSmall) {
             launch_micro_tile<TO, 2, 2, 4>(a, st);
         } else {
             launch_micro_tile<TO, 2, 4, 8>(a, st);
