@@ -465,7 +465,7 @@ def scores_microscaled_workspace(B: int, d: int) -> int:
 def scores_microscaled(Z: torch.Tensor, Q: torch.Tensor, scale: torch.Tensor, *, dtype: torch.dtype = torch.float32,
                        workspace: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """[B, L] scores of all labels: the rows of Z [B, d] in 4 bits times the rows of Q, block by block with the scales of both
-    (Q and scale from `microscale_rows` of the classifier).  fp32 or bf16, by `out` or `dtype`."""
+    (Q and scale from `microscale_rows` of the classifier, or any range of their rows).  fp32 or bf16, by `out` or `dtype`."""
     lib = load_library()
     code = _dtype_code(Z)
     if Z.dim() != 2 or Q.dim() != 2 or Q.shape[1] * 2 != microscaled_pitch(Z.shape[1]):
@@ -589,7 +589,8 @@ def distill(scores: torch.Tensor, labels: torch.Tensor, teacher: torch.Tensor, *
             weight: torch.Tensor | None = None, grad: bool = True, dtype: torch.dtype | None = None,
             workspace: torch.Tensor | None = None, out: tuple | None = None):
     """(loss fp32 [B], gradient for the scores [B, V] or None): weight * temperature^2 * the divergence of the soft-max of scores /
-    temperature from a teacher's distribution, of which labels int32 [B, K] (padding is ignored) and teacher fp32 [B, K] are given.
+    temperature from a teacher's distribution, of which labels int32 [B, K] (padding is ignored, a label that is listed several times
+    has the sum of its probabilities) and teacher fp32 [B, K] are given.
 
     teacher holds logits that are already divided by the temperature (for example `mine_negatives`' scores), whose soft-max over the
     list is taken; with tail log probabilities (for example `label_logprobs`' top_logp), and the labels that are not listed are one

@@ -246,7 +246,8 @@ __device__ __forceinline__ float listed_gradient(const DistillArgs& a, const Row
     return r.factor * fmaf(r.mass, p, -q);
 }
 
-// Bound: one read.  Sums of a segment.  With a tail the listed labels of a block are marked, a bit each, before its elements are looked at.
+// Bound: one read.  The loss alone, by this and the next kernel, 64 labels and a tail: 1024 x 131072 bf16 53 us (5.0 TB/s), fp32 89 (6.0), 2048 x
+// 131072 bf16 100 (5.3), 2048 x 32000 bf16 38 (3.5: one block to a workgroup).  Sums of a segment.  With a tail the listed labels of a block are marked, a bit each, before its elements are looked at.
 template <typename T, int C>
 __global__ __launch_bounds__(kRowThreads)
 void distill_sums_kernel(const DistillArgs a) {

@@ -88,6 +88,7 @@ struct MicroQueries {
 
 // 16 lanes bring 128 elements of a row, U of these at a time.  Rows from N on (of the queries' padding) and units behind a row are zeros.
 // Bound: memory.  670000 x 768 bf16: 240 us, 5.4 TB/s, what a copy reaches here; one at a time 252, four 237, with the non-temporal hint 240.
+// Listed rows of as many: 100000 42.7 us (4.6 TB/s), 20000 10.1, 1000 7.7 (the caller's).
 template <typename T, typename TO, int U>
 __global__ __launch_bounds__(256)
 void microscale_kernel(const unsigned char* __restrict__ X, int64_t N, int d, const int32_t* __restrict__ ids, int64_t m, const int32_t* __restrict__ count,
@@ -192,8 +193,7 @@ __device__ __forceinline__ void put_one(bf16_t* p, float v) {
     const __bf16 h = static_cast<__bf16>(v);
     __builtin_memcpy(p, &h, 2);
 }
-// (`whole` is the same for a wave: where lanes decided each for themselves, the compiler, ROCm 7.2's, let the last of fewer than four
-// scores take the fourth one's register in all lanes)
+// (`whole` is the same for a wave: the stores one by one are left out where all labels of the wave are there)
 template <typename TO> __device__ __forceinline__ void put_labels(TO* p, const float (&v)[4], bool whole, int64_t have) {
     if (whole) {
         put_four(p, v, false);
@@ -359,8 +359,10 @@ void scores_micro_few_kernel(const MicroArgs a) {
 // ---- many queries, rows of up to 512 bytes (1024 elements): the labels stay where they are.  A wave holds 64 labels as operands in registers
 // (NK units) and 512 labels of a workgroup meet the queries that stream through LDS, 64 at a time; a wave's scores are stored 16 queries at
 // a time, while the other wave of its SIMD multiplies.
-// Bound: stores and products beside each other, at the clock that the power limit leaves.  4096 x 131072 x 768 to bf16 235 to 250 us (1.07 GB
-// stored, 157 us of a fill; matrix pipe busy 47 % of the time); with a sixth of the products 208, without the stores 163.
+// Bound: stores and products that overlap in part.  4096 x 131072 x 768 to bf16 235 to 262 us (1.07 GB stored, 157 us of a fill; matrix pipe
+// busy 47 % of the time); without the stores 163, with a sixth of the products 208: the stores as they are made here take more than a fill does,
+// and the eight waves load, store and meet at a barrier in every stage, so that both waves of a SIMD tend to be in the same phase.  To fp32 400
+// (2.15 GB, 316 us of a fill).
 template <int NK_>
 struct MicroHeld {
     static constexpr int NK = NK_, QS = kMicroHeldQueries, kUpad = NK <= 4 ? 4 : 8, kStage = QS * NK * 64, kScales = QS * 4 * kUpad;

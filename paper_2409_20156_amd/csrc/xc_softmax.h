@@ -234,9 +234,10 @@ constexpr int kRowWaves = 4, kRowThreads = kRowWaves * kWave;
 constexpr int small_block(size_t element) { return element == 4 ? 2 : 1; }        // pieces to a thread: 8 elements,
 constexpr int large_block(size_t) { return 4; }                                  // 16 (fp32), 32
 struct RowCut { int each, blocks; int64_t segments, length /* pieces of a segment */; };
-// Segments: as many as give every compute unit several workgroups, of 4096 elements at least (8 x 131072 fp32 with 20 top labels 13.8 us,
-// of 2048 15.1), and no more than the kernel that joins their top labels takes at a time (1 x 262144 bf16, 128 labels: 16 segments 25 us;
-// 128 of them, joined in rounds by a thread to a key, 102 where 16 took 30).
+// Segments: as many as give every compute unit several workgroups, of about 4096 elements at least (8 x 131072 fp32 with 20 top labels 13.8 us,
+// of 2048 15.1; their number is rounded up, so that just beyond a multiple they are shorter: 4100 elements are two of 2052), and no more than the
+// kernel that joins them has room for all top labels of (1 x 262144 bf16, 128 labels: 16 segments 25 us; 128 of them, joined in rounds by
+// a thread to a key, 102 where 16 took 30).  It takes 128 segments at a time: with fewer than 16 top labels there may be more, in rounds.
 constexpr int kJoinKeys = 2048;
 inline RowCut cut_rows(int64_t B, int64_t V, size_t element, int k = 0) {
     const int64_t pieces = V / static_cast<int64_t>(16 / element);
